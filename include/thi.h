@@ -213,6 +213,97 @@ int thi_decode_attention(const void* q, const void* k_cache, const void* v_cache
                          void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * ---- A paged key/value cache in 4 bits -------------------------------------------------------------------
+ *
+ * What it holds.  A page holds THI_KV4_PAGE positions of all cache heads of one layer: thi_kv4_page_bytes(Hkv, D) = 68 * D bytes per
+ * head (4.25 bits a value), D = 64 or 128.  A value is an e2m1 code -- 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign bit, two to a byte, the lower
+ * column in the low bits -- times 2^(byte - 127), one scale byte for 32 neighbouring columns of a position (the OCP MX format's e2m1 with
+ * e8m0 scales).  The scale of a block is the smallest 2^e with max|x| <= 7 * 2^e (half a step past 6), e in [-23, 13], so that every
+ * stored value is an fp16 number; a code is the nearest, ties to the even one, at most 6 (magnitudes past 57344 become 49152).
+ * A block with an infinity or a NaN is stored as NaN (byte 255).  Per head, in this order:
+ *   key codes     32 D bytes  [position][column / 2]
+ *   key scales     2 D        [column / 32][position % 16][position / 16]
+ *   value codes   32 D        [column / 32][position % 16 / 4][column % 32 / 2][position / 16][position % 4]
+ *   value scales   2 D        [column / 32][position % 16 / 4][position / 16][position % 4]
+ * `pages` is [num_pages][Hkv][68 D], 16-byte aligned; num_pages * 64 must fit an int32 (THI_ERR_SHAPE).  Byte offsets are 64-bit.
+ *
+ * Who has which page.  page_table [B][max_pages] int32: entry j of row b is the page of that request's positions 64 j .. 64 j + 63;
+ * an entry outside [0, num_pages) is no page: its positions hold nothing and are not attended to (-1 by convention; what
+ * an engine does to drop old positions).  seq_lens [B] int32, taken as 0 if negative and as 64 * max_pages if larger.  All of it is
+ * device memory, 4-byte aligned, and not checked on the host; whatever stands there, no access leaves the buffers.
+ */
+#define THI_KV4_PAGE 64
+size_t thi_kv4_page_bytes(int Hkv, int D);
+
+/*
+ * From a QKV projection's rows to the cache: RMSNorm of each head's query and key, rotary embedding, and the store in 4 bits.
+ *
+ *   n(x)_c = gamma_c x_c / sqrt( (1/D) sum x^2 + eps )  (n(x) = x where the gamma is NULL)
+ *   y(x)   = n(x) with its pairs (2i, 2i+1) turned by positions[t] * theta[i]  (as thi_rmsnorm_qkv_rope; theta NULL: not turned)
+ *   q_out[t,h,:] = y(query h of row t);  the cache at slots[t] = (y(key), value), as described above
+ *
+ * qkv [T][ld] fp16, each row the Hq queries, Hkv keys, Hkv values of D columns (what thi_rmsnorm_qkv writes); ld >= (Hq + 2 Hkv) D, a
+ * multiple of 8.  q_gamma, k_gamma [D] fp16 or NULL; positions [T] int32 and theta [D/2] fp32 (may both be NULL); slots [T] int32 = page *
+ * THI_KV4_PAGE + position in it; a slot outside the pool is not stored (padding rows: -1).  q_out [T,Hq,D] fp16.  No two tokens of a call may
+ * have the same slot.  Norm, angle and rotation are computed in 64 bits and rounded once, to fp16 or to a code.  No workspace.
+ */
+int thi_qk_norm_rope_kv4(const void* qkv, int ld, const void* q_gamma, const void* k_gamma, float eps, const int* positions, const float* theta,
+                         const int* slots, void* q_out, void* pages, int T, int Hq, int Hkv, int D, int num_pages, void* hip_stream);
+
+/*
+ * What the cache holds at slots [T], as fp16 (exact): k_out, v_out [T,Hkv,D], either may be NULL; zeros for a slot outside the pool.
+ */
+int thi_kv4_read(const void* pages, const int* slots, void* k_out, void* v_out, int T, int Hkv, int D, int num_pages, void* hip_stream);
+
+/*
+ * Attention of each request's new tokens over its pages (Eq. 6 per head, grouped-query as thi_decode_attention):
+ *
+ *   out[t,h,:] = sum_j p_j v_j,  p = softmax_j(scale * q[t,h,:] . k_j)  over the positions j <= seq_lens[b] - n_b + i that have a page
+ *
+ * for row t = q_offsets[b] + i, i < n_b = q_offsets[b+1] - q_offsets[b]: the new tokens are the request's last n_b positions, already in the
+ * cache, and see what stands before them and themselves.  A row that sees no position (an empty request, more rows than positions) is zero.
+ * q, out [T,Hq,D] fp16; q_offsets [B+1] int32 device memory, not decreasing, or NULL: one token per request, T = B.  max_q is the
+ * largest n_b (from the host, it sizes the launch; rows of a request past it are not written).  Scores, statistics and sums are fp32; a weight reaches the
+ * matrix cores as fp16 (two summands up to 16 rows of a cache head, one beyond).  Workspace: thi_kv4_attention_workspace_bytes(), 256-byte aligned, no
+ * preparation needed.  Reproducible bit for bit.
+ */
+size_t thi_kv4_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages);
+int thi_kv4_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, void* out,
+                      int B, int T, int Hq, int Hkv, int D, int max_q, int num_pages, int max_pages,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rows of a page table become other rows: forked (samples, beams), dropped, and given pages for their next tokens, in one pass on the
+ * device.  A page is free where its count of references is 0.  The counts and tables given are read, the *_out ones written (other
+ * buffers; THI_ERR_SHAPE if the same), so that launches in flight may still read the old table.  Row i of the new table, i < rows_out,
+ * continues row p = parents[i] of the old one (outside [0, rows_in): it starts empty), with its length:
+ *   - whole pages are shared;
+ *   - the partly filled page, and pages held beyond the length: the lowest row that continues p takes them over if nobody else
+ *     has them (count 1); other rows get a fresh page, the partly filled one's contents copied in every layer;
+ *   - then fresh pages for headroom[i] >= 0 more positions (headroom NULL: none); pages held beyond that are given up; entries behind are -1.
+ * Fresh pages are the lowest free ones of refs_in, in the order of rows and entries; where none is left the entry is -1 and the positions are
+ * lost.  refs_out = refs_in - occurrences in the old table + occurrences in the new one: pages of rows nobody continues are freed, references held
+ * elsewhere (a prefix kept for later requests) stay.  info (may be NULL) [2]: fresh pages taken, fresh pages missing.
+ *
+ * refs_* [num_pages], table_in [rows_in][max_pages], table_out [rows_out][max_pages], lens_in [rows_in], lens_out, parents, headroom [rows_out],
+ * all int32.  pages: layer l's pool begins at pages + l * layer_bytes, page_bytes each (multiples of 16; any cache's pages, not this one's only).
+ * Workspace: thi_kv4_pages_workspace_bytes(), 256-byte aligned, no preparation needed.
+ */
+size_t thi_kv4_pages_workspace_bytes(int rows_out, int rows_in, int max_pages, int num_pages);
+int thi_kv4_fork(const int* refs_in, const int* table_in, const int* lens_in, const int* parents, const int* headroom,
+                 int* refs_out, int* table_out, int* lens_out, int* info, void* pages, size_t page_bytes, int layers, size_t layer_bytes,
+                 int rows_in, int rows_out, int num_pages, int max_pages, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Compaction: the L pages with references move into pages 0 .. L-1, so that the pool's tail can be given back.  The live pages behind L
+ * go, in the order of their numbers, into the free ones in front of it, in theirs; the others stay.  table_out and refs_out name the new places
+ * (an entry without a live page becomes -1); the old places keep their contents.  info (may be NULL) [2]: L, pages moved.  Workspace:
+ * thi_kv4_pages_workspace_bytes(rows, rows, ...); everything else as thi_kv4_fork.
+ */
+int thi_kv4_compact(const int* refs_in, const int* table_in, int* refs_out, int* table_out, int* info, void* pages, size_t page_bytes,
+                    int layers, size_t layer_bytes, int rows, int num_pages, int max_pages, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Bytes of workspace the given operator needs for the given shape
  * (op = thi_op; (M, N, K) for the first two operators, (M, H, I) for the MLP).
  * Pure host arithmetic: touches no device.  Returns 0 for invalid arguments.

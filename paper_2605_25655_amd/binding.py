@@ -13,6 +13,7 @@ import os
 THI_OK = 0
 THI_ERR_WORKSPACE = 4
 THI_ERR_TIMEOUT = 6
+THI_KV4_PAGE = 64
 THI_OP_RMSNORM_QKV, THI_OP_LINEAR, THI_OP_SWIGLU_MLP = 0, 1, 2
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -24,6 +25,8 @@ _probe_lib = None
 EXPORTED_SYMBOLS = (
     "thi_rmsnorm_qkv", "thi_rmsnorm_qkv_rope", "thi_linear", "thi_linear_static", "thi_swiglu_mlp", "thi_swiglu_gate_up",
     "thi_linear_residual", "thi_rmsnorm_swiglu_mlp", "thi_decode_attention", "thi_attention_workspace_bytes",
+    "thi_kv4_page_bytes", "thi_qk_norm_rope_kv4", "thi_kv4_read", "thi_kv4_attention_workspace_bytes", "thi_kv4_attention",
+    "thi_kv4_pages_workspace_bytes", "thi_kv4_fork", "thi_kv4_compact",
     "thi_workspace_bytes",
     "thi_workspace_init", "thi_workspace_status", "thi_debug_handover", "thi_status_string", "thi_version", "thi_set_kernel_family", "thi_set_rowblock_split", "thi_set_mlp_fusion", "thi_query_kernel_family",
 )
@@ -75,6 +78,22 @@ def load_library():
     lib.thi_decode_attention.restype = ci
     lib.thi_attention_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
     lib.thi_attention_workspace_bytes.restype = sz
+    lib.thi_kv4_page_bytes.argtypes = [ci, ci]
+    lib.thi_kv4_page_bytes.restype = sz
+    lib.thi_qk_norm_rope_kv4.argtypes = [vp, ci, vp, vp, cf, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp]
+    lib.thi_qk_norm_rope_kv4.restype = ci
+    lib.thi_kv4_read.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, vp]
+    lib.thi_kv4_read.restype = ci
+    lib.thi_kv4_attention_workspace_bytes.argtypes = [ci] * 7
+    lib.thi_kv4_attention_workspace_bytes.restype = sz
+    lib.thi_kv4_attention.argtypes = [vp, vp, vp, vp, vp, cf, vp, ci, ci, ci, ci, ci, ci, ci, ci, vp, sz, vp]
+    lib.thi_kv4_attention.restype = ci
+    lib.thi_kv4_pages_workspace_bytes.argtypes = [ci] * 4
+    lib.thi_kv4_pages_workspace_bytes.restype = sz
+    lib.thi_kv4_fork.argtypes = [vp] * 10 + [sz, ci, sz, ci, ci, ci, ci, vp, sz, vp]
+    lib.thi_kv4_fork.restype = ci
+    lib.thi_kv4_compact.argtypes = [vp] * 6 + [sz, ci, sz, ci, ci, ci, vp, sz, vp]
+    lib.thi_kv4_compact.restype = ci
     lib.thi_workspace_bytes.argtypes = [ci, ci, ci, ci]
     lib.thi_workspace_bytes.restype = sz
     lib.thi_workspace_init.argtypes = [vp, sz, vp]
@@ -293,6 +312,89 @@ def thi_decode_attention(q, k_cache, v_cache, seq_lens, scale, out, workspace, s
                                              _ptr(out), B, Hq, Hkv, D, S_max, wp, wb, _stream(stream))
     if check and rc != THI_OK:
         raise ThiError(rc, "thi_decode_attention")
+    return rc
+
+
+def thi_kv4_page_bytes(Hkv: int, D: int) -> int:
+    """Bytes of one page (THI_KV4_PAGE positions of Hkv heads of D) of the 4-bit cache; 0 for heads it does not hold."""
+    return int(load_library().thi_kv4_page_bytes(int(Hkv), int(D)))
+
+
+def thi_qk_norm_rope_kv4(qkv, q_gamma, k_gamma, eps: float, positions, theta, slots, q_out, pages, stream=None, check: bool = True) -> int:
+    """q_out = rotated, normalised queries of qkv's rows; their keys and values into the 4-bit cache at `slots`.
+
+    qkv [T, >= (Hq+2Hkv)*D] fp16 (rows may be strided); q_gamma, k_gamma [D] fp16 or None; positions [T] int32 and theta [D/2] fp32, or both None;
+    slots [T] int32; q_out [T,Hq,D] fp16; pages [num_pages,Hkv,68*D] uint8."""
+    T, Hq, D = q_out.shape
+    rc = load_library().thi_qk_norm_rope_kv4(_ptr(qkv), qkv.stride(0), _ptr(q_gamma), _ptr(k_gamma), eps, _ptr(positions), _ptr(theta),
+                                             _ptr(slots), _ptr(q_out), _ptr(pages), T, Hq, pages.shape[1], D, pages.shape[0], _stream(stream))
+    if check and rc != THI_OK:
+        raise ThiError(rc, "thi_qk_norm_rope_kv4")
+    return rc
+
+
+def thi_kv4_read(pages, slots, k_out, v_out, stream=None, check: bool = True) -> int:
+    """k_out, v_out [T,Hkv,D] fp16 (either may be None) = what the 4-bit cache holds at slots [T]."""
+    T, Hkv, D = (k_out if k_out is not None else v_out).shape
+    rc = load_library().thi_kv4_read(_ptr(pages), _ptr(slots), _ptr(k_out), _ptr(v_out), T, Hkv, D, pages.shape[0], _stream(stream))
+    if check and rc != THI_OK:
+        raise ThiError(rc, "thi_kv4_read")
+    return rc
+
+
+def thi_kv4_attention_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, max_q: int, max_pages: int) -> int:
+    return int(load_library().thi_kv4_attention_workspace_bytes(int(B), int(T), int(Hq), int(Hkv), int(D), int(max_q), int(max_pages)))
+
+
+def thi_kv4_attention(q, pages, page_table, seq_lens, q_offsets, scale, out, max_q: int, workspace, stream=None, check: bool = True) -> int:
+    """out[T,Hq,D] = softmax(scale q k^T) v per head of each request's new tokens over its pages of the 4-bit cache.
+
+    q, out [T,Hq,D] fp16; pages [num_pages,Hkv,68*D] uint8; page_table [B,max_pages], seq_lens [B] int32; q_offsets [B+1] int32 (the rows of
+    request b) or None (one row each); max_q: the most rows of a request."""
+    T, Hq, D = q.shape
+    B, max_pages = page_table.shape
+    wp, wb = _ws(workspace)
+    rc = load_library().thi_kv4_attention(_ptr(q), _ptr(pages), _ptr(page_table), _ptr(seq_lens), _ptr(q_offsets), scale, _ptr(out),
+                                          B, T, Hq, pages.shape[1], D, max_q, pages.shape[0], max_pages, wp, wb, _stream(stream))
+    if check and rc != THI_OK:
+        raise ThiError(rc, "thi_kv4_attention")
+    return rc
+
+
+def thi_kv4_pages_workspace_bytes(rows_out: int, rows_in: int, max_pages: int, num_pages: int) -> int:
+    return int(load_library().thi_kv4_pages_workspace_bytes(int(rows_out), int(rows_in), int(max_pages), int(num_pages)))
+
+
+def _pool(pages):
+    """pages [layers, num_pages, ...] (a layer's pool contiguous): (bytes of a page, layers, bytes from layer to layer)."""
+    size = pages.element_size()
+    return pages.stride(1) * size, pages.shape[0], pages.stride(0) * size
+
+
+def thi_kv4_fork(refs_in, table_in, lens_in, parents, headroom, refs_out, table_out, lens_out, info, pages, workspace, stream=None,
+                 check: bool = True) -> int:
+    """Rows of table_in become rows of table_out: row i continues parents[i], with pages for headroom[i] more positions.
+
+    int32: refs_* [num_pages], table_in [rows_in,max_pages], table_out [rows_out,max_pages], lens_in [rows_in], lens_out, parents, headroom
+    (or None) [rows_out], info [2] (or None); pages [layers,num_pages,...]."""
+    page_bytes, layers, layer_bytes = _pool(pages)
+    wp, wb = _ws(workspace)
+    rc = load_library().thi_kv4_fork(_ptr(refs_in), _ptr(table_in), _ptr(lens_in), _ptr(parents), _ptr(headroom), _ptr(refs_out), _ptr(table_out),
+                                     _ptr(lens_out), _ptr(info), _ptr(pages), page_bytes, layers, layer_bytes, table_in.shape[0],
+                                     table_out.shape[0], refs_in.shape[0], table_in.shape[1], wp, wb, _stream(stream))
+    if check and rc != THI_OK:
+        raise ThiError(rc, "thi_kv4_fork")
+    return rc
+
+
+def thi_kv4_compact(refs_in, table_in, refs_out, table_out, info, pages, workspace, stream=None, check: bool = True) -> int:
+    """The pages with references move to the front of the pool; table_out [rows,max_pages] and refs_out name the new places."""
+    page_bytes, layers, layer_bytes = _pool(pages)
+    wp, wb = _ws(workspace)
+    rc = load_library().thi_kv4_compact(_ptr(refs_in), _ptr(table_in), _ptr(refs_out), _ptr(table_out), _ptr(info), _ptr(pages), page_bytes, layers,
+                                        layer_bytes, table_in.shape[0], refs_in.shape[0], table_in.shape[1], wp, wb, _stream(stream))
+    if check and rc != THI_OK:
+        raise ThiError(rc, "thi_kv4_compact")
     return rc
 
 

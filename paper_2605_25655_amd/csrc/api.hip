@@ -21,20 +21,6 @@ std::atomic<unsigned> g_spin_limit{SK_SPIN_LIMIT};   // polls of a hand-over fla
 std::atomic<int> g_withhold_flags{0};      // test hook: contributors never raise their flags
 std::atomic<int> g_mlp_fusion{0};          // opt-in: the decode MLP as one launch where the fused kernel serves the shape
 
-int device_cu_count()
-{
-    // once-initialised, per-device cache of the CU count (the only state the library keeps)
-    static std::atomic<int> cache[64];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-    int v = cache[dev].load(std::memory_order_relaxed);
-    if (v > 0) return v;
-    int cus = 0;
-    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) cus = 256;
-    cache[dev].store(cus, std::memory_order_relaxed);
-    return cus;
-}
-
 inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

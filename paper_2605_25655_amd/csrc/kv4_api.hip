@@ -1,0 +1,143 @@
+// C-ABI entry points of the 4-bit cache's operators: argument validation and launches.  Declarations and contract: include/thi.h.
+#include "../../include/thi.h"
+#include "kv4.h"
+
+namespace {
+
+using namespace thi;
+
+inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+bool heads_ok(int Hq, int Hkv, int D) { return Hq >= 1 && Hkv >= 1 && Hq <= 65535 && Hkv <= 65535 && Hq % Hkv == 0 && (D == 64 || D == 128); }
+
+// slots are int32: the pool's last position has to have one
+bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff / KV4_PAGE; }
+
+int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
+
+}  // namespace
+
+extern "C" {
+
+size_t thi_kv4_page_bytes(int Hkv, int D)
+{
+    return heads_ok(Hkv, Hkv, D) ? (size_t)Hkv * kv4_head_bytes(D) : 0;
+}
+
+int thi_qk_norm_rope_kv4(const void* qkv, int ld, const void* q_gamma, const void* k_gamma, float eps, const int* positions, const float* theta,
+                         const int* slots, void* q_out, void* pages, int T, int Hq, int Hkv, int D, int num_pages, void* hip_stream)
+{
+    if (!qkv || !slots || !q_out || !pages || (theta && !positions)) return THI_ERR_NULL;
+    if (T < 1 || !heads_ok(Hq, Hkv, D) || !pool_ok(num_pages)) return THI_ERR_SHAPE;
+    if ((ld & 7) || ld < (long)(Hq + 2 * Hkv) * D) return THI_ERR_SHAPE;
+    if (misaligned(qkv, 16) || misaligned(q_gamma, 16) || misaligned(k_gamma, 16) || misaligned(q_out, 16) || misaligned(pages, 16) ||
+        misaligned(positions, 4) || misaligned(theta, 4) || misaligned(slots, 4))
+        return THI_ERR_ALIGN;
+    (void)hipGetLastError();      // an error another user of the runtime left behind is not ours to report
+    Kv4AppendArgs a{};
+    a.qkv = (const uint16_t*)qkv;
+    a.q_gamma = (const uint16_t*)q_gamma;
+    a.k_gamma = (const uint16_t*)k_gamma;
+    a.positions = positions;
+    a.theta = theta;
+    a.slots = slots;
+    a.q_out = (uint16_t*)q_out;
+    a.pages = (unsigned char*)pages;
+    a.eps = eps;
+    a.T = T; a.ld = ld; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.num_pages = num_pages;
+    return finish(launch_kv4_append(a, device_cu_count(), (hipStream_t)hip_stream));
+}
+
+int thi_kv4_read(const void* pages, const int* slots, void* k_out, void* v_out, int T, int Hkv, int D, int num_pages, void* hip_stream)
+{
+    if (!pages || !slots || (!k_out && !v_out)) return THI_ERR_NULL;
+    if (T < 1 || !heads_ok(Hkv, Hkv, D) || !pool_ok(num_pages)) return THI_ERR_SHAPE;
+    if (misaligned(pages, 16) || misaligned(slots, 4) || misaligned(k_out, 16) || misaligned(v_out, 16)) return THI_ERR_ALIGN;
+    (void)hipGetLastError();
+    Kv4ReadArgs a{(const unsigned char*)pages, slots, (uint16_t*)k_out, (uint16_t*)v_out, T, Hkv, D, num_pages};
+    return finish(launch_kv4_read(a, (hipStream_t)hip_stream));
+}
+
+size_t thi_kv4_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages)
+{
+    if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_pages < 1 || max_pages > 0x7fffffff / KV4_PAGE) return 0;
+    return 256;
+}
+
+int thi_kv4_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, void* out,
+                      int B, int T, int Hq, int Hkv, int D, int max_q, int num_pages, int max_pages,
+                      void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!q || !pages || !page_table || !seq_lens || !out || !workspace) return THI_ERR_NULL;
+    const size_t need = thi_kv4_attention_workspace_bytes(B, T, Hq, Hkv, D, max_q, max_pages);
+    if (!need || !pool_ok(num_pages) || (!q_offsets && (T != B || max_q != 1))) return THI_ERR_SHAPE;
+    if (misaligned(q, 16) || misaligned(pages, 16) || misaligned(out, 16) || misaligned(page_table, 4) || misaligned(seq_lens, 4) ||
+        misaligned(q_offsets, 4) || misaligned(workspace, 256))
+        return THI_ERR_ALIGN;
+    if (workspace_bytes < need) return THI_ERR_WORKSPACE;
+    (void)hipGetLastError();
+    Kv4AttnArgs a{};
+    a.q = (const uint16_t*)q;
+    a.pages = (const unsigned char*)pages;
+    a.page_table = page_table;
+    a.seq_lens = seq_lens;
+    a.q_offsets = q_offsets;
+    a.out = (uint16_t*)out;
+    a.scale2 = scale * 1.44269504088896340736f;
+    a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.num_pages = num_pages; a.max_pages = max_pages;
+    return finish(launch_kv4_attention(a, (hipStream_t)hip_stream));
+}
+
+size_t thi_kv4_pages_workspace_bytes(int rows_out, int rows_in, int max_pages, int num_pages)
+{
+    if (rows_in < 1 || rows_out < 1 || max_pages < 1 || max_pages > 0x7fffffff / KV4_PAGE || !pool_ok(num_pages)) return 0;
+    return (pages_workspace_words(rows_in, rows_out, num_pages) * 4 + 255) / 256 * 256;
+}
+
+static int check_pages(const void* pages, size_t page_bytes, int layers, size_t layer_bytes, int num_pages)
+{
+    if (!page_bytes || (page_bytes & 15) || layers < 1 || layers > 65533 || (layer_bytes & 15)) return THI_ERR_SHAPE;
+    if (page_bytes > ((size_t)1 << 62) / (size_t)num_pages || (layers > 1 && layer_bytes < page_bytes * (size_t)num_pages)) return THI_ERR_SHAPE;
+    return misaligned(pages, 16) ? THI_ERR_ALIGN : THI_OK;
+}
+
+int thi_kv4_fork(const int* refs_in, const int* table_in, const int* lens_in, const int* parents, const int* headroom,
+                 int* refs_out, int* table_out, int* lens_out, int* info, void* pages, size_t page_bytes, int layers, size_t layer_bytes,
+                 int rows_in, int rows_out, int num_pages, int max_pages, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!refs_in || !table_in || !lens_in || !parents || !refs_out || !table_out || !lens_out || !pages || !workspace) return THI_ERR_NULL;
+    const size_t need = thi_kv4_pages_workspace_bytes(rows_out, rows_in, max_pages, num_pages);
+    if (!need || refs_out == refs_in || table_out == table_in || lens_out == lens_in) return THI_ERR_SHAPE;
+    const int rc = check_pages(pages, page_bytes, layers, layer_bytes, num_pages);
+    if (rc != THI_OK) return rc;
+    const void* const words[] = {refs_in, table_in, lens_in, parents, headroom, refs_out, table_out, lens_out, info};
+    for (const void* p : words)
+        if (misaligned(p, 4)) return THI_ERR_ALIGN;
+    if (misaligned(workspace, 256)) return THI_ERR_ALIGN;
+    if (workspace_bytes < need) return THI_ERR_WORKSPACE;
+    (void)hipGetLastError();
+    const PagesArgs a{refs_in, table_in, lens_in, parents, headroom, refs_out, table_out, lens_out, info, (char*)pages, page_bytes, layer_bytes,
+                      rows_in, rows_out, layers, num_pages, max_pages, (int*)workspace};
+    return finish(launch_kv4_fork(a, device_cu_count(), (hipStream_t)hip_stream));
+}
+
+int thi_kv4_compact(const int* refs_in, const int* table_in, int* refs_out, int* table_out, int* info, void* pages, size_t page_bytes,
+                    int layers, size_t layer_bytes, int rows, int num_pages, int max_pages, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!refs_in || !table_in || !refs_out || !table_out || !pages || !workspace) return THI_ERR_NULL;
+    const size_t need = thi_kv4_pages_workspace_bytes(rows, rows, max_pages, num_pages);
+    if (!need || refs_out == refs_in || table_out == table_in) return THI_ERR_SHAPE;
+    const int rc = check_pages(pages, page_bytes, layers, layer_bytes, num_pages);
+    if (rc != THI_OK) return rc;
+    const void* const words[] = {refs_in, table_in, refs_out, table_out, info};
+    for (const void* p : words)
+        if (misaligned(p, 4)) return THI_ERR_ALIGN;
+    if (misaligned(workspace, 256)) return THI_ERR_ALIGN;
+    if (workspace_bytes < need) return THI_ERR_WORKSPACE;
+    (void)hipGetLastError();
+    const PagesArgs a{refs_in, table_in, nullptr, nullptr, nullptr, refs_out, table_out, nullptr, info, (char*)pages, page_bytes, layer_bytes,
+                      rows, rows, layers, num_pages, max_pages, (int*)workspace};
+    return finish(launch_kv4_compact(a, device_cu_count(), (hipStream_t)hip_stream));
+}
+
+}  // extern "C"

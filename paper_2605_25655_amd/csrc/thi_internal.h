@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <atomic>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -260,5 +261,19 @@ __device__ __forceinline__ uint16_t to_half_bits(float v) {
 }
 
 hipError_t launch_fill_words(void* ptr, size_t bytes, uint32_t value, hipStream_t stream);
+
+inline int device_cu_count()
+{
+    // once-initialised, per-device cache of the CU count (with the scratch array's address the only state the library keeps)
+    static std::atomic<int> cache[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+    int v = cache[dev].load(std::memory_order_relaxed);
+    if (v > 0) return v;
+    int cus = 0;
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) cus = 256;
+    cache[dev].store(cus, std::memory_order_relaxed);
+    return cus;
+}
 
 }  // namespace thi
