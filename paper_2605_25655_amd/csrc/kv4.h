@@ -54,7 +54,14 @@ struct Kv4AttnArgs {
     uint16_t* out;                   // [T,Hq,D]
     float scale2;                    // softmax scale times log2(e)
     int B, T, Hq, Hkv, D, max_q, num_pages, max_pages;
+    // how the rows are dealt (kv4_plan)
+    float* part;                     // [T*Hq][KV4_MAX_SPLIT][D + 2]: a chunk's unnormalised output, maximum, sum
+    bool split_rows;                 // 16 rows of a cache head at a time, cut along the positions
+    int tiles;                       // tiles of 16 rows
+    int nsplit, min_chunk;           // chunks per request at most, pages per chunk at least
 };
+constexpr int KV4_MAX_SPLIT = 64;
+void kv4_plan(Kv4AttnArgs& a, int num_cus);
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, hipStream_t stream);
 
 struct PagesArgs {

@@ -17,6 +17,20 @@ int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 
 }  // namespace
 
+// Few rows: 16 of a cache head at a time, the requests cut so that the chip is full: three workgroups for each of the two places per compute unit.
+void thi::kv4_plan(Kv4AttnArgs& a, int num_cus)
+{
+    const int group = a.Hq / a.Hkv;
+    a.tiles = (int)(((long)a.max_q * group + 15) / 16);
+    a.split_rows = (long)a.max_q * group <= 64;
+    const long items = (long)a.B * a.Hkv * a.tiles;
+    long n = (6L * num_cus + items - 1) / items;
+    n = n > KV4_MAX_SPLIT ? KV4_MAX_SPLIT : n;
+    a.min_chunk = 4;
+    const long most = (a.max_pages + a.min_chunk - 1) / a.min_chunk;
+    a.nsplit = (int)(n > most ? most : n);
+}
+
 extern "C" {
 
 size_t thi_kv4_page_bytes(int Hkv, int D)
@@ -61,7 +75,10 @@ int thi_kv4_read(const void* pages, const int* slots, void* k_out, void* v_out, 
 size_t thi_kv4_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages)
 {
     if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_pages < 1 || max_pages > 0x7fffffff / KV4_PAGE) return 0;
-    return 256;
+    Kv4AttnArgs a{};
+    a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.max_pages = max_pages;
+    kv4_plan(a, device_cu_count());
+    return a.split_rows && a.nsplit > 1 ? ((size_t)T * Hq * KV4_MAX_SPLIT * (D + 2) * 4 + 255) / 256 * 256 : 256;
 }
 
 int thi_kv4_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, void* out,
@@ -85,6 +102,8 @@ int thi_kv4_attention(const void* q, const void* pages, const int* page_table, c
     a.out = (uint16_t*)out;
     a.scale2 = scale * 1.44269504088896340736f;
     a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.num_pages = num_pages; a.max_pages = max_pages;
+    kv4_plan(a, device_cu_count());
+    a.part = (float*)workspace;
     return finish(launch_kv4_attention(a, (hipStream_t)hip_stream));
 }
 
