@@ -23,10 +23,11 @@ void thi::kv4_plan(Kv4AttnArgs& a, int num_cus)
     const int group = a.Hq / a.Hkv;
     a.tiles = (int)(((long)a.max_q * group + 15) / 16);
     a.split_rows = (long)a.max_q * group <= 64;
-    const long items = (long)a.B * a.Hkv * a.tiles;
-    long n = (6L * num_cus + items - 1) / items;
+    const long items = (long)a.B * a.Hkv * (a.split_rows ? a.tiles : (a.tiles + 15) / 16);
+    long n = ((a.split_rows ? 6L : 2L) * num_cus + items - 1) / items;
     n = n > KV4_MAX_SPLIT ? KV4_MAX_SPLIT : n;
-    a.min_chunk = 4;
+    a.min_chunk = a.split_rows ? 4 : 16;
+    if (!a.split_rows && items >= num_cus) n = 1;
     const long most = (a.max_pages + a.min_chunk - 1) / a.min_chunk;
     a.nsplit = (int)(n > most ? most : n);
 }
@@ -78,7 +79,7 @@ size_t thi_kv4_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, i
     Kv4AttnArgs a{};
     a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.max_pages = max_pages;
     kv4_plan(a, device_cu_count());
-    return a.split_rows && a.nsplit > 1 ? ((size_t)T * Hq * KV4_MAX_SPLIT * (D + 2) * 4 + 255) / 256 * 256 : 256;
+    return a.nsplit > 1 ? ((size_t)T * Hq * a.nsplit * (D + 2) * 4 + 255) / 256 * 256 : 256;
 }
 
 int thi_kv4_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, void* out,
@@ -101,6 +102,7 @@ int thi_kv4_attention(const void* q, const void* pages, const int* page_table, c
     a.q_offsets = q_offsets;
     a.out = (uint16_t*)out;
     a.scale2 = scale * 1.44269504088896340736f;
+    if (a.scale2 == 0.f) a.scale2 = 1e-30f;      // (all weights equal either way; a masked score of -inf stays what it is)
     a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.num_pages = num_pages; a.max_pages = max_pages;
     kv4_plan(a, device_cu_count());
     a.part = (float*)workspace;

@@ -2,6 +2,8 @@
 // positions 0 .. length - n + i whose page exists.
 #include "kv4.h"
 
+#include <mutex>
+
 namespace thi {
 
 namespace {
@@ -26,58 +28,6 @@ __device__ __forceinline__ Request find_request(const Kv4AttnArgs& a, int b)
     r.len = r.len < 0 ? 0 : r.len > most ? (int)most : r.len;
     return r;
 }
-
-// One wave per row and head; a lane takes a position of a page for the scores, then columns of the output.
-template <int D>
-__global__ __launch_bounds__(64) void kv4_attn_simple(Kv4AttnArgs a)
-{
-    __shared__ float s_q[D], s_p[64];
-    const int h = blockIdx.x % a.Hq, i = blockIdx.x / a.Hq, b = blockIdx.y, lane = threadIdx.x;
-    const Request rq = find_request(a, b);
-    if (i >= rq.n) return;
-    const size_t row = ((size_t)(rq.first + i) * a.Hq + h) * D;
-    for (int d = lane; d < D; d += 64) s_q[d] = half_bits_to_float(a.q[row + d]) * a.scale2;
-    __syncthreads();
-    const int last = rq.len - rq.n + i, g = h / (a.Hq / a.Hkv);
-    float m = -__builtin_inff(), l = 0.f, o[D / 64] = {};
-    for (int pg = 0; pg * KV4_PAGE <= last; ++pg) {
-        const int page = a.page_table[(size_t)b * a.max_pages + pg];
-        if (page < 0 || page >= a.num_pages) continue;
-        const unsigned char* const base = a.pages + ((size_t)page * a.Hkv + g) * kv4_head_bytes(D);
-        const bool live = pg * KV4_PAGE + lane <= last;
-        float t = 0.f;
-        for (int blk = 0; blk < D / 32; ++blk) {
-            const float s = __builtin_bit_cast(float, (unsigned)base[kv4_key_scales(D) + kv4_key_scale_at(lane, blk)] << 23);
-            for (int e = 0; e < 16; ++e) {
-                const half2v x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4((unsigned)base[lane * (D / 2) + blk * 16 + e], s, 0);
-                t += (float)x[0] * s_q[blk * 32 + 2 * e] + (float)x[1] * s_q[blk * 32 + 2 * e + 1];
-            }
-        }
-        t = live ? t : -__builtin_inff();
-        float mx = t;
-        for (int sh = 1; sh < 64; sh <<= 1) mx = __builtin_fmaxf(mx, __shfl_xor(mx, sh));
-        const float mn = __builtin_fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.f : mn;
-        const float corr = __builtin_amdgcn_exp2f(m - ms), p = __builtin_amdgcn_exp2f(t - ms);
-        m = mn;
-        l = l * corr + p;
-        s_p[lane] = p;
-        __syncthreads();
-        for (int c = 0; c < D / 64; ++c) {
-            const int d = lane + 64 * c;
-            float acc = o[c] * corr;
-            for (int pos = 0; pos < KV4_PAGE && pg * KV4_PAGE + pos <= last; ++pos) {
-                const float s = __builtin_bit_cast(float, (unsigned)base[kv4_value_scales(D) + kv4_value_scale_at(pos, d / 32)] << 23);
-                const half2v x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4((unsigned)base[kv4_values(D) + kv4_value_at(pos, d / 2)], s, 0);
-                acc += s_p[pos] * (float)x[d & 1];
-            }
-            o[c] = acc;
-        }
-        __syncthreads();
-    }
-    for (int sh = 1; sh < 64; sh <<= 1) l += __shfl_xor(l, sh);
-    for (int c = 0; c < D / 64; ++c) a.out[row + lane + 64 * c] = l == 0.f && m == -__builtin_inff() ? 0 : to_half_bits(o[c] / l);
-}
-
 
 // ---- one token per request, or a few: 16 rows of a cache head at a time, cut along the positions --------------------
 //
@@ -379,7 +329,7 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
         const size_t row = row_of_column(c);
         if (whole) a.out[row * D + d] = lf == 0.f ? 0 : to_half_bits(of / lf);
         else {
-            float* const po = a.part + (row * KV4_MAX_SPLIT + chunk) * (D + 2);
+            float* const po = a.part + (row * a.nsplit + chunk) * (D + 2);
             po[d] = of;
             if (d == 0) { po[D] = mn; po[D + 1] = lf; }
         }
@@ -397,7 +347,7 @@ __global__ __launch_bounds__(D) void kv4_attn_combine(Kv4AttnArgs a)
     if (pages <= size) return;                  // one chunk: the first pass has written this output
     const int live = (pages + size - 1) / size;
     const size_t row = (size_t)(rq.first + i) * a.Hq + h;
-    const float* const first = a.part + row * KV4_MAX_SPLIT * (D + 2);
+    const float* const first = a.part + row * a.nsplit * (D + 2);
     const float mine = lane < live ? first[(size_t)lane * (D + 2) + D] : -__builtin_inff();
     float top = mine;
 #pragma unroll
@@ -422,15 +372,328 @@ hipError_t launch_decode(const Kv4AttnArgs& a, hipStream_t stream)
     return hipGetLastError();
 }
 
+
+// ---- many rows of a cache head: prompts and chunks of them ----------------------------------------------------------
+//
+// A workgroup takes KP_WAVES * 16 * CT rows of one cache head and walks the pages that any of them sees.  Its waves bring a page in once
+// between them, convert it to fp16 and leave it in LDS in the order in which the matrix operands are read (a lane's 16 bytes behind
+// its neighbour's: no bank conflicts, no address arithmetic); two such buffers, and the codes of the page behind in registers.  Products and
+// the lanes' order of positions are the few-rows kernel's; a wave holds CT tiles of 16 rows, each operand read from LDS feeds CT products.
+// Bound by the matrix cores and the vector ALU together (an exponential costs a wave 16 cycles, 16 of them and some 50 plain instructions against 32 products of
+// 16 cycles per page and tile).
+//
+// A weight is one fp16 number here (off by as much as the result is by its own rounding), 2^11 p of a maximum that may lag by 2^4 (so that weights down to 2^-25 are normal numbers):
+// the sums are rescaled only when some row's maximum has grown by more than that.
+constexpr float KP_WEIGHT_LOG2 = 11.0f, KP_LAG = 4.0f;
+
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");      // (loads into registers stay in flight)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <int D, int CT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void kv4_attn_prompt(Kv4AttnArgs a)
+{
+    constexpr int NB = D / 32, KS = D / 32, ROWS = WAVES * 16 * CT;
+    constexpr int K_UNITS = 4 * KS * 64, V_UNITS = 4 * NB * 64, BUF = K_UNITS + V_UNITS;      // 16-byte units
+    extern __shared__ uintx4 kp_smem[];
+    __shared__ int s_nan[2][NB];                 // of a buffer that not every row sees whole: a block's first position that is not a number
+
+    const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = a.Hq / a.Hkv;
+    const int b = blockIdx.y, chunk = blockIdx.z;
+    const Request rq = find_request(a, b);
+    const int all_rows = rq.n * group;
+    // the cache head varies fastest: workgroups are dealt to the XCDs in turn, and those of a head share what they read; the last rows, which see the
+    // most, come first
+    const int g = blockIdx.x % a.Hkv, tiles = (all_rows + ROWS - 1) / ROWS, tile = tiles - 1 - (int)(blockIdx.x / a.Hkv);
+    if (tile < 0) return;
+    const int r0 = tile * ROWS, rows = all_rows - r0 < ROWS ? all_rows - r0 : ROWS;
+    const int pages = (rq.len + KV4_PAGE - 1) / KV4_PAGE, size = chunk_pages(a, pages);
+    if (chunk > 0 && chunk * size >= pages) return;
+    const bool whole = pages <= size;
+    const int before = rq.len - rq.n;            // positions in front of the new tokens (negative: the first rows see nothing)
+    const int tile_sees = before + (r0 + rows - 1) / group + 1;                  // by its last row
+    const int tile_all = before + r0 / group + 1;                                // by every row
+    int c0 = chunk * size, c1 = c0 + size < pages ? c0 + size : pages;
+    const int last = (tile_sees + KV4_PAGE - 1) / KV4_PAGE;
+    c1 = c1 < last ? c1 : last;
+
+    const int w0 = r0 + wv * 16 * CT;            // this wave's first row
+    auto row_index = [&](int ct) { const int r = w0 + ct * 16 + lo; return r < all_rows ? r : all_rows - 1; };
+    const bool flip = a.scale2 < 0.f;
+    const float scale2 = __builtin_fabsf(a.scale2);
+    half8 qf[CT][KS];
+    int seen[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const int r = row_index(ct), token = r / group;
+        seen[ct] = before + token + 1;
+        const uint16_t* const qrow = a.q + ((size_t)(rq.first + token) * a.Hq + (size_t)g * group + r % group) * D + hi * (D / 4);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            uintx4 x = ld_cached(qrow + s * 8);
+            if (flip) x ^= 0x80008000u;
+            qf[ct][s] = __builtin_bit_cast(half8, x);
+        }
+    }
+    const int wave_all = before + (w0 < all_rows ? w0 : all_rows - 1) / group + 1;
+    const int wave_last = w0 + 16 * CT - 1 < all_rows ? w0 + 16 * CT - 1 : all_rows - 1;
+    const int wave_sees = w0 < all_rows ? before + wave_last / group + 1 : -0x7fffffff;      // (no rows: nothing)
+
+    float m[CT], l[CT];
+    floatx4 o[CT][2 * NB];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        m[ct] = -__builtin_inff();
+        l[ct] = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2 * NB; ++t) o[ct][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    int entries = -1;
+    const int* const table = a.page_table + (size_t)b * a.max_pages;
+    auto page_at = [&](int it) {                 // page c0 + it, asked for in order
+        if ((it & 63) == 0) {
+            const int j = c0 + it + lane;
+            entries = j < c1 ? table[j] : -1;
+        }
+        const int e = __builtin_amdgcn_readlane(entries, it & 63);
+        return e >= 0 && e < a.num_pages ? e : -1;
+    };
+    // A wave's share of a page: KU tiles of 16 positions of the keys and VU blocks of 32 columns of the values.
+    constexpr int KU = WAVES >= 8 ? 1 : 4 / WAVES, VU = WAVES >= 8 ? 1 : (NB + WAVES - 1) / WAVES;
+    const int k_first = WAVES >= 8 ? wv : wv * KU, v_first = WAVES >= 8 ? wv - 4 : wv * VU;
+    typedef __typeof__(typename PageRegsOf<D>::type{}.k[0]) KPiece;
+    KPiece rk[KU];
+    unsigned rks = 0;
+    uintx4 rv[VU], rvs[VU];
+    auto issue = [&](int page) __attribute__((always_inline)) {
+        if (page < 0) return;
+        const unsigned char* const base = a.pages + ((size_t)page * a.Hkv + g) * kv4_head_bytes(D);
+        if (k_first < 4) {
+#pragma unroll
+            for (int u = 0; u < KU; ++u) rk[u] = *reinterpret_cast<const KPiece*>(base + (k_first + u) * 8 * D + lo * (D / 2) + hi * (D / 8));
+            rks = *reinterpret_cast<const unsigned*>(base + kv4_key_scales(D) + ((D == 128 ? hi : hi >> 1) * 16 + lo) * 4);
+        }
+#pragma unroll
+        for (int u = 0; u < VU; ++u)
+            if (v_first + u >= 0 && v_first + u < NB) {
+                rv[u] = *reinterpret_cast<const uintx4*>(base + kv4_values(D) + (v_first + u) * 1024 + lane * 16);
+                rvs[u] = *reinterpret_cast<const uintx4*>(base + kv4_value_scales(D) + (v_first + u) * 64 + hi * 16);
+            }
+    };
+    auto convert = [&](int it, int buf) __attribute__((always_inline)) {
+        uintx4* const kb = kp_smem + buf * BUF;
+        uintx4* const vb = kb + K_UNITS;
+        const int base = (c0 + it) * KV4_PAGE;
+        if (k_first < 4) {
+#pragma unroll
+            for (int u = 0; u < KU; ++u) {
+                const float s = __builtin_bit_cast(float, (rks >> (8 * (k_first + u)) & 255u) << 23);
+#pragma unroll
+                for (int k = 0; k < KS; ++k) kb[((k_first + u) * KS + k) * 64 + lane] = __builtin_bit_cast(uintx4, row_values(rk[u][k], s));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < VU; ++u) {
+            const int t = v_first + u;
+            if (t < 0 || t >= NB) continue;
+            if (base + KV4_PAGE > tile_all) {    // some row does not see all of it: as in the few-rows kernel
+                int first = 0x7fffffff;
+#pragma unroll
+                for (int i = 15; i >= 0; --i) {
+                    const int pos = base + 16 * (i >> 2) + 4 * hi + (i & 3);
+                    const bool dead = pos >= rq.len, odd = (rvs[u][i >> 2] >> (8 * (i & 3)) & 255u) == 255u;
+                    if (odd && !dead) first = pos;
+                    if (odd || dead) rvs[u][i >> 2] &= ~(255u << (8 * (i & 3)));
+                }
+#pragma unroll
+                for (int sh = 16; sh < 64; sh <<= 1) {
+                    const int other = __shfl_xor(first, sh);
+                    first = other < first ? other : first;
+                }
+                if (lane == 0) s_nan[buf][t] = first;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uintx4 e, d;
+#pragma unroll
+                for (int i2 = 0; i2 < 2; ++i2) {
+                    const unsigned c = rv[u][2 * k + i2], w = rvs[u][2 * k + i2];
+                    const unsigned y0 = pair_of<0>(c, scale_of(w, 0)), y1 = pair_of<1>(c, scale_of(w, 1)), y2 = pair_of<2>(c, scale_of(w, 2)), y3 = pair_of<3>(c, scale_of(w, 3));
+                    e[2 * i2] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
+                    e[2 * i2 + 1] = __builtin_amdgcn_perm(y3, y2, 0x05040100u);
+                    d[2 * i2] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
+                    d[2 * i2 + 1] = __builtin_amdgcn_perm(y3, y2, 0x07060302u);
+                }
+                vb[(t * 4 + k) * 64 + lane] = e;
+                vb[(t * 4 + 2 + k) * 64 + lane] = d;
+            }
+        }
+    };
+
+    const int n_it = c1 - c0;
+    int page = n_it > 0 ? page_at(0) : -1, next = -1;
+    issue(page);
+    if (page >= 0) convert(0, 0);
+    next = 1 < n_it ? page_at(1) : -1;
+    issue(next);
+    lds_barrier();
+    for (int it = 0; it < n_it; ++it) {
+        const int buf = it & 1, base = (c0 + it) * KV4_PAGE;
+        const bool active = page >= 0 && base < wave_sees;
+        const uintx4* const kb = kp_smem + buf * BUF;
+        const uintx4* const vb = kb + K_UNITS;
+        floatx4 acc[CT][4];
+        if (active) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) acc[ct][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const half8 kf = __builtin_bit_cast(half8, kb[(i * KS + k) * 64 + lane]);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) acc[ct][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[ct][k], acc[ct][i], 0, 0, 0);
+                }
+            }
+        }
+        if (next >= 0) convert(it + 1, buf ^ 1);
+        const int behind = it + 2 < n_it ? page_at(it + 2) : -1;
+        issue(behind);
+        if (active) {
+            const bool masked = base + KV4_PAGE > wave_all;
+            half8 pw[CT][2];
+            float top[CT];
+            if (masked) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (base + 16 * (i >> 2) + 4 * hi + (i & 3) >= seen[ct]) acc[ct][i >> 2][i & 3] = -__builtin_inff();
+            }
+            bool grown = false;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                float mb = acc[ct][0][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) mb = __builtin_fmaxf(mb, acc[ct][i >> 2][i & 3]);
+                top[ct] = max_over_hi(mb) * scale2;
+                grown = grown || top[ct] - m[ct] > KP_LAG;
+            }
+            if (__builtin_amdgcn_ballot_w64(grown) != 0ull) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    const float mn = __builtin_fmaxf(m[ct], top[ct]);
+                    const float corr = __builtin_amdgcn_exp2f(m[ct] - (mn == -__builtin_inff() ? 0.f : mn));
+                    m[ct] = mn;
+                    l[ct] *= corr;
+#pragma unroll
+                    for (int t = 0; t < 2 * NB; ++t) o[ct][t] *= corr;
+                }
+            }
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const float off = KP_WEIGHT_LOG2 - (m[ct] == -__builtin_inff() ? 0.f : m[ct]);
+                float sum = 0.f;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float w[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        w[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[ct][2 * k + (r >> 2)][r & 3], scale2, off));
+                        sum += w[r];
+                    }
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) pw[ct][k][r] = (_Float16)w[r];
+                }
+                l[ct] += sum;
+            }
+#pragma unroll
+            for (int t = 0; t < NB; ++t)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const half8 ev = __builtin_bit_cast(half8, vb[(t * 4 + k) * 64 + lane]), od = __builtin_bit_cast(half8, vb[(t * 4 + 2 + k) * 64 + lane]);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        o[ct][2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ev, pw[ct][k], o[ct][2 * t], 0, 0, 0);
+                        o[ct][2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(od, pw[ct][k], o[ct][2 * t + 1], 0, 0, 0);
+                    }
+                }
+            if (base + KV4_PAGE > tile_all) {
+#pragma unroll
+                for (int t = 0; t < NB; ++t) {
+                    const int first = s_nan[buf][t];
+                    if (first != 0x7fffffff) {
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct)
+                            if (first < seen[ct]) o[ct][2 * t] = o[ct][2 * t + 1] = floatx4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+                    }
+                }
+            }
+        }
+        lds_barrier();
+        page = next;
+        next = behind;
+    }
+
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const int r = w0 + ct * 16 + lo;
+        const float lf = sum_over_hi(l[ct]);
+        if (r >= all_rows) continue;
+        const size_t row = (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group;
+        if (whole) {
+            const float inv = lf == 0.f ? 0.f : 1.0f / lf;
+#pragma unroll
+            for (int t = 0; t < NB; ++t) {
+                half8 y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    y[2 * i] = (_Float16)(o[ct][2 * t][i] * inv);
+                    y[2 * i + 1] = (_Float16)(o[ct][2 * t + 1][i] * inv);
+                }
+                *reinterpret_cast<uintx4*>(a.out + row * D + 32 * t + 8 * hi) = __builtin_bit_cast(uintx4, y);
+            }
+        } else {
+            float* const po = a.part + (row * a.nsplit + chunk) * (D + 2);
+#pragma unroll
+            for (int t = 0; t < NB; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    po[32 * t + 8 * hi + 2 * i] = o[ct][2 * t][i];
+                    po[32 * t + 8 * hi + 2 * i + 1] = o[ct][2 * t + 1][i];
+                }
+            if (hi == 0) { po[D] = m[ct]; po[D + 1] = lf; }
+        }
+    }
+}
+
+template <int D, int CT, int WAVES>
+hipError_t launch_prompt(const Kv4AttnArgs& a, hipStream_t stream)
+{
+    constexpr int LDS = 2 * (4 * (D / 32) + 4 * (D / 32)) * 64 * 16;
+    static std::once_flag attr_once;
+    std::call_once(attr_once, [] {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_attn_prompt<D, CT, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    });
+    const long rows = (long)a.max_q * (a.Hq / a.Hkv), per = WAVES * 16 * CT;
+    const dim3 grid((unsigned)((rows + per - 1) / per * a.Hkv), (unsigned)a.B, (unsigned)a.nsplit);
+    hipLaunchKernelGGL((kv4_attn_prompt<D, CT, WAVES>), grid, dim3(64 * WAVES), LDS, stream, a);
+    if (a.nsplit > 1) hipLaunchKernelGGL((kv4_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(D), 0, stream, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, hipStream_t stream)
 {
     if (a.split_rows) return a.D == 128 ? launch_decode<128>(a, stream) : launch_decode<64>(a, stream);
-    const dim3 grid((unsigned)a.max_q * (unsigned)a.Hq, (unsigned)a.B);
-    if (a.D == 128) hipLaunchKernelGGL((kv4_attn_simple<128>), grid, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL((kv4_attn_simple<64>), grid, dim3(64), 0, stream, a);
-    return hipGetLastError();
+    return a.D == 128 ? launch_prompt<128, 2, 8>(a, stream) : launch_prompt<64, 2, 8>(a, stream);
 }
 
 }  // namespace thi
