@@ -3,6 +3,7 @@
 #include "kv4.h"
 
 #include <mutex>
+#include <type_traits>
 
 namespace thi {
 
@@ -41,11 +42,12 @@ __device__ __forceinline__ Request find_request(const Kv4AttnArgs& a, int b)
 //               lane's 16 bytes are these positions of two neighbouring columns (even and odd columns are tiles of their own).
 // So nothing but the rows' maxima crosses lanes.  Weights are multiplied as two fp16 summands of 2^15 p (2^-22 of a weight off at most down to 2^-17, where
 // one alone is off by 2^-11 and as much as the result's own rounding).
-struct PageRegs128 { uintx4 k[4]; unsigned ks; uintx4 v[4], vs[4]; };
 typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
-struct PageRegs64 { uintx2 k[4]; unsigned ks; uintx4 v[2], vs[2]; };
-template <int D> struct PageRegsOf { typedef PageRegs128 type; };
-template <> struct PageRegsOf<64> { typedef PageRegs64 type; };
+template <int D> struct PageRegs {
+    uintx4 k[4];
+    unsigned ks;
+    uintx4 v[D / 32], vs[D / 32];
+};
 
 constexpr int KD_THREADS = 256, KD_WAVES = 4;
 constexpr float KD_WEIGHT_LOG2 = 15.0f;          // weights are held as 2^15 p
@@ -56,10 +58,101 @@ __device__ __forceinline__ float scale_of(unsigned w, int i)
     return __builtin_bit_cast(float, i == 0 ? w << 23 : i == 1 ? w << 15 : i == 2 ? w << 7 : w >> 1);
 }
 template <int I> __device__ __forceinline__ unsigned pair_of(unsigned codes, float s) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, s, I)); }
-__device__ __forceinline__ half8 row_values(unsigned codes, float s)
+
+// Scores of 16 positions x 16 rows, in powers of two.
+//
+// The keys' codes are a matrix operand as they stand (v_mfma_scale_f32_16x16x128_f8f6f4: a lane's 16 bytes are one block of 32, the scales of the
+// four tiles of a page one dword).  The queries, times the softmax scale and log2 e, are the other: each block of 32 as the sum of four e2m3
+// numbers with scales of their own, 2^-4 apart.  Each takes four bits more; what is left is 2^-18 of the block's largest at most.  The instruction runs
+// at four times fp16's rate, so the four products cost what fp16's would; nothing has to be converted, nor, where the keys come from LDS, read in
+// four times the bytes.  With D = 64 two of the four blocks are empty (the lanes hi >= 2: zeros on the queries' side).
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef float floatx32 __attribute__((ext_vector_type(32)));
+typedef unsigned uintx6 __attribute__((ext_vector_type(6)));
+
+struct Queries {
+    intx8 f[4];
+    unsigned scales;
+};
+
+template <int D> __device__ __forceinline__ void take_queries(const uint16_t* row, int hi, float scale2, Queries& q)
 {
-    const uintx4 o = {pair_of<0>(codes, s), pair_of<1>(codes, s), pair_of<2>(codes, s), pair_of<3>(codes, s)};
-    return __builtin_bit_cast(half8, o);
+    const bool any = hi < D / 32;
+    const uint16_t* const from = row + (any ? hi : 0) * 32;
+    floatx32 rest;
+    unsigned high = 0, low = 0;                  // the largest magnitudes' bits of the odd and even columns, in the upper half
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const uintx4 x = ld_cached(from + s * 8);
+        const half8 h = __builtin_bit_cast(half8, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rest[8 * s + e] = any ? (float)h[e] * scale2 : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned u = x[e] & 0x7fff0000u, v = (x[e] << 16) & 0x7fff0000u;
+            high = u > high ? u : high;
+            low = v > low ? v : low;
+        }
+    }
+    const unsigned top16 = any ? (high > low ? high : low) >> 16 : 0u;
+    const unsigned top = __builtin_bit_cast(unsigned, half_bits_to_float((uint16_t)top16) * __builtin_fabsf(scale2));
+    // the smallest 2^e that keeps the largest within 7.5; the summands' scales go down to e - 12
+    int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x700000u ? 1 : 0);
+    e = e < 13 ? 13 : e;
+    q.scales = 0;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const float scale = __builtin_bit_cast(float, (unsigned)(e - 4 * s) << 23);
+        floatx16 even, odd;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            even[k] = rest[2 * k];
+            odd[k] = rest[2 * k + 1];
+        }
+        const uintx6 codes = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
+        rest -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(codes, scale);
+        // The conversion writes its six registers while it still reads the scale, and the compiler does not know: a scale that is needed no more
+        // may be given one of the six (the last summand was wrong that way).  It is needed until here.
+        asm volatile("" : : "v"(scale), "v"(codes));
+#pragma unroll
+        for (int k = 0; k < 6; ++k) q.f[s][k] = (int)codes[k];
+        q.f[s][6] = q.f[s][7] = 0;
+        q.scales |= (unsigned)(e - 4 * s) << (8 * s);
+    }
+    if (top16 >= 0x7c00u || top >= 0x7f800000u) q.scales = 0xffffffffu;      // infinities and NaN: the row is not a number
+}
+// where the lane's share of a page's keys lies; its scales, but for the lanes whose queries are empty, which must not meet a NaN
+template <int D> __device__ __forceinline__ int key_offset(int lo, int hi) { return lo * (D / 2) + (hi & (D / 32 - 1)) * 16; }
+template <int D> __device__ __forceinline__ int key_scale_offset(int lo, int hi) { return kv4_key_scales(D) + ((hi & (D / 32 - 1)) * 16 + lo) * 4; }
+template <int D> __device__ __forceinline__ unsigned lane_scales(unsigned scales, int hi) { return D == 128 || hi < D / 32 ? scales : 0x7f7f7f7fu; }
+
+// One of the four products of a tile (the smallest summand first).  A product that waits for the one in front of it takes twice as long: they go over
+// several tiles before the next step.
+template <int TILE, int STEP> __device__ __forceinline__ floatx4 score_step(uintx4 keys, unsigned scales, const Queries& q, floatx4 acc)
+{
+    const intx8 k = {(int)keys[0], (int)keys[1], (int)keys[2], (int)keys[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.f[3 - STEP], acc, 4, 2, TILE, (int)scales, 3 - STEP, (int)q.scales);
+}
+// Scores of a page's four tiles of 16 positions with CT tiles of rows, plus `from` of the lane's row.
+template <int CT> __device__ __forceinline__ void score_page(const uintx4 (&keys)[4], unsigned scales, const Queries (&q)[CT], const floatx4 (&from)[CT], floatx4 (&acc)[CT][4])
+{
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[ct][i] = from[ct];
+    auto step = [&](auto s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            acc[ct][0] = score_step<0, decltype(s)::value>(keys[0], scales, q[ct], acc[ct][0]);
+            acc[ct][1] = score_step<1, decltype(s)::value>(keys[1], scales, q[ct], acc[ct][1]);
+            acc[ct][2] = score_step<2, decltype(s)::value>(keys[2], scales, q[ct], acc[ct][2]);
+            acc[ct][3] = score_step<3, decltype(s)::value>(keys[3], scales, q[ct], acc[ct][3]);
+        }
+    };
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 3>{});
 }
 
 // over the lanes of the same lo (the four hi)
@@ -102,8 +195,8 @@ __device__ __forceinline__ half8 join(half4 a, half4 b) { return half8{a[0], a[1
 template <int D, bool MULTI>
 __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
 {
-    constexpr int NB = D / 32, KS = D / 32;      // blocks of a row; matrix steps of a score
-    typedef typename PageRegsOf<D>::type Regs;
+    constexpr int NB = D / 32;                   // blocks of a row
+    typedef PageRegs<D> Regs;
     __shared__ float s_o[KD_WAVES][16][D + 4];
     __shared__ float s_m[KD_WAVES][16], s_l[KD_WAVES][16];
 
@@ -125,12 +218,8 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
         return (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group;
     };
     const int col = lo < rows ? lo : rows - 1;
-    half8 qf[KS];
-    {
-        const uint16_t* const qrow = a.q + row_of_column(col) * D + hi * (D / 4);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(half8, ld_cached(qrow + s * 8));
-    }
+    Queries queries[1];
+    take_queries<D>(a.q + row_of_column(col) * D, hi, a.scale2, queries[0]);
     // positions this lane's row sees, and what every row of the tile sees
     const int seen = rq.len - rq.n + (MULTI ? (r0 + col) / group : 0) + 1;
     const int all_see = rq.len - rq.n + (MULTI ? r0 / group : 0) + 1;
@@ -147,6 +236,8 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
         if ((it & 63) == 0) {
             const int j = c0 + wv + (it + lane) * KD_WAVES;
             entries = j < c1 ? table[j] : -1;
+            // waited for here, and not in every iteration behind whatever else is in flight
+            asm volatile("" : "+v"(entries));
         }
         const int e = __builtin_amdgcn_readlane(entries, it & 63);
         return e >= 0 && e < a.num_pages ? e : -1;
@@ -155,11 +246,8 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
         if (page < 0) return;
         const unsigned char* const base = a.pages + ((size_t)page * a.Hkv + g) * kv4_head_bytes(D);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            typedef __typeof__(x.k[0]) K;
-            x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const K*>(base + i * 8 * D + lo * (D / 2) + hi * (D / 8)));
-        }
-        x.ks = *reinterpret_cast<const unsigned*>(base + kv4_key_scales(D) + ((D == 128 ? hi : hi >> 1) * 16 + lo) * 4);
+        for (int i = 0; i < 4; ++i) x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(base + i * 8 * D + key_offset<D>(lo, hi)));
+        x.ks = *reinterpret_cast<const unsigned*>(base + key_scale_offset<D>(lo, hi));
 #pragma unroll
         for (int t = 0; t < NB; ++t) {
             x.v[t] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(base + kv4_values(D) + t * 1024 + lane * 16));
@@ -202,15 +290,11 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
         const int base = (c0 + wv + it * KD_WAVES) * KV4_PAGE;
         const bool masked = base + KV4_PAGE > all_see;
         float t[16];
+        floatx4 scores[1][4];
+        const floatx4 zero[1] = {floatx4{0.f, 0.f, 0.f, 0.f}};
+        score_page<1>(x.k, lane_scales<D>(x.ks, hi), queries, zero, scores);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float s = scale_of(x.ks, i);
-            floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < KS; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(row_values(x.k[i][k], s), qf[k], acc, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) t[4 * i + r] = acc[r] * a.scale2;
-        }
+        for (int i = 0; i < 16; ++i) t[i] = scores[0][i >> 2][i & 3];
         if (masked) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) t[i] = base + 16 * (i >> 2) + 4 * hi + (i & 3) < seen ? t[i] : -__builtin_inff();
@@ -384,6 +468,8 @@ hipError_t launch_decode(const Kv4AttnArgs& a, hipStream_t stream)
 //
 // A weight is one fp16 number here (off by as much as the result is by its own rounding), 2^11 p of a maximum that may lag by 2^4 (so that weights down to 2^-25 are normal numbers):
 // the sums are rescaled only when some row's maximum has grown by more than that.
+constexpr int KP_WAVES = 8, KP_AHEAD = 2;
+template <int D> constexpr int KP_BUF = 4096 + 256 + 128 * D;      // a page in LDS: key codes, key scales, values in fp16
 constexpr float KP_WEIGHT_LOG2 = 11.0f, KP_LAG = 4.0f;
 
 __device__ __forceinline__ void lds_barrier()
@@ -393,13 +479,14 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int D, int CT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void kv4_attn_prompt(Kv4AttnArgs a)
+template <int D, int CT>
+__global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
 {
-    constexpr int NB = D / 32, KS = D / 32, ROWS = WAVES * 16 * CT;
-    constexpr int K_UNITS = 4 * KS * 64, V_UNITS = 4 * NB * 64, BUF = K_UNITS + V_UNITS;      // 16-byte units
+    constexpr int NB = D / 32, ROWS = KP_WAVES * 16 * CT;
+    constexpr int BUF = KP_BUF<D>, V_AT = 4096 + 256;       // bytes of a buffer: key codes and scales as loaded (a lane's behind each other), values in fp16
     extern __shared__ uintx4 kp_smem[];
-    __shared__ int s_nan[2][NB];                 // of a buffer that not every row sees whole: a block's first position that is not a number
+    __shared__ int s_nan[2][NB][2];              // of a buffer that not every row sees whole: the first position that is not a number in half a block
+    char* const smem = reinterpret_cast<char*>(kp_smem);
 
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -424,32 +511,28 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void kv4_attn_prompt(Kv4Attn
 
     const int w0 = r0 + wv * 16 * CT;            // this wave's first row
     auto row_index = [&](int ct) { const int r = w0 + ct * 16 + lo; return r < all_rows ? r : all_rows - 1; };
-    const bool flip = a.scale2 < 0.f;
-    const float scale2 = __builtin_fabsf(a.scale2);
-    half8 qf[CT][KS];
+    Queries queries[CT];
     int seen[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         const int r = row_index(ct), token = r / group;
         seen[ct] = before + token + 1;
-        const uint16_t* const qrow = a.q + ((size_t)(rq.first + token) * a.Hq + (size_t)g * group + r % group) * D + hi * (D / 4);
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            uintx4 x = ld_cached(qrow + s * 8);
-            if (flip) x ^= 0x80008000u;
-            qf[ct][s] = __builtin_bit_cast(half8, x);
-        }
+        take_queries<D>(a.q + ((size_t)(rq.first + token) * a.Hq + (size_t)g * group + r % group) * D, hi, a.scale2, queries[ct]);
     }
     const int wave_all = before + (w0 < all_rows ? w0 : all_rows - 1) / group + 1;
     const int wave_last = w0 + 16 * CT - 1 < all_rows ? w0 + 16 * CT - 1 : all_rows - 1;
     const int wave_sees = w0 < all_rows ? before + wave_last / group + 1 : -0x7fffffff;      // (no rows: nothing)
 
-    float m[CT], l[CT];
-    floatx4 o[CT][2 * NB];
+    // m: the maximum that a row's weights refer to; from: what its scores start from (KP_WEIGHT_LOG2 - m, so that a weight is 2^score); l: the
+    // weights' sums, as a product with ones (every element is the lane's row's)
+    float m[CT];
+    floatx4 from[CT], l[CT], o[CT][2 * NB];
+    bool fresh = true;                           // some row has no maximum yet
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         m[ct] = -__builtin_inff();
-        l[ct] = 0.f;
+        from[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
+        l[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < 2 * NB; ++t) o[ct][t] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
@@ -460,191 +543,246 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void kv4_attn_prompt(Kv4Attn
         if ((it & 63) == 0) {
             const int j = c0 + it + lane;
             entries = j < c1 ? table[j] : -1;
+            // waited for here, and not in every iteration behind whatever else is in flight
+            asm volatile("" : "+v"(entries));
         }
         const int e = __builtin_amdgcn_readlane(entries, it & 63);
         return e >= 0 && e < a.num_pages ? e : -1;
     };
-    // A wave's share of a page: KU tiles of 16 positions of the keys and VU blocks of 32 columns of the values.
-    constexpr int KU = WAVES >= 8 ? 1 : 4 / WAVES, VU = WAVES >= 8 ? 1 : (NB + WAVES - 1) / WAVES;
-    const int k_first = WAVES >= 8 ? wv : wv * KU, v_first = WAVES >= 8 ? wv - 4 : wv * VU;
-    typedef __typeof__(typename PageRegsOf<D>::type{}.k[0]) KPiece;
-    KPiece rk[KU];
-    unsigned rks = 0;
-    uintx4 rv[VU], rvs[VU];
-    auto issue = [&](int page) __attribute__((always_inline)) {
-        if (page < 0) return;
-        const unsigned char* const base = a.pages + ((size_t)page * a.Hkv + g) * kv4_head_bytes(D);
-        if (k_first < 4) {
-#pragma unroll
-            for (int u = 0; u < KU; ++u) rk[u] = *reinterpret_cast<const KPiece*>(base + (k_first + u) * 8 * D + lo * (D / 2) + hi * (D / 8));
-            rks = *reinterpret_cast<const unsigned*>(base + kv4_key_scales(D) + ((D == 128 ? hi : hi >> 1) * 16 + lo) * 4);
-        }
-#pragma unroll
-        for (int u = 0; u < VU; ++u)
-            if (v_first + u >= 0 && v_first + u < NB) {
-                rv[u] = *reinterpret_cast<const uintx4*>(base + kv4_values(D) + (v_first + u) * 1024 + lane * 16);
-                rvs[u] = *reinterpret_cast<const uintx4*>(base + kv4_value_scales(D) + (v_first + u) * 64 + hi * 16);
-            }
+    // What a wave brings in of a page: half a tile of 16 positions of the keys, as it is, and half a block of 32 columns of the values, converted (D = 64: a
+    // quarter, by every other wave).  Loads are unconditional (a page that is not there: page 0), so that nothing waits for them but what uses them.
+    const int k_tile = wv >> 1, k_half = wv & 1, block = wv & (NB - 1), half = (wv >> 2) & 1;
+    const bool brings_values = D == 128 || (wv & 2) == 0;
+    uintx2 raw_k, raw_v, raw_vs;
+    unsigned raw_ks;
+    const unsigned char* const heads = a.pages + (size_t)g * kv4_head_bytes(D);
+    const size_t page_bytes = (size_t)a.Hkv * kv4_head_bytes(D);
+    const unsigned k_off = k_tile * 8 * D + key_offset<D>(lo, hi) + k_half * 8, ks_off = key_scale_offset<D>(lo, hi);
+    const unsigned v_off = kv4_values(D) + block * 1024 + lane * 16 + half * 8, vs_off = kv4_value_scales(D) + block * 64 + hi * 16 + half * 8;
+    auto head = [&](int page) { return heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_bytes; };
+    auto issue_keys = [&](int page) __attribute__((always_inline)) {
+        raw_k = *reinterpret_cast<const uintx2*>(head(page) + k_off);
+        raw_ks = *reinterpret_cast<const unsigned*>(head(page) + ks_off);
     };
-    auto convert = [&](int it, int buf) __attribute__((always_inline)) {
-        uintx4* const kb = kp_smem + buf * BUF;
-        uintx4* const vb = kb + K_UNITS;
-        const int base = (c0 + it) * KV4_PAGE;
-        if (k_first < 4) {
+    auto issue_values = [&](int page) __attribute__((always_inline)) {
+        raw_v = *reinterpret_cast<const uintx2*>(head(page) + v_off);
+        raw_vs = *reinterpret_cast<const uintx2*>(head(page) + vs_off);
+    };
+    auto put_keys = [&](int it) __attribute__((always_inline)) {
+        char* const buf = smem + (it & 1) * BUF;
+        *reinterpret_cast<uintx2*>(buf + (k_tile * 64 + lane) * 16 + k_half * 8) = raw_k;
+        if (wv == 0) reinterpret_cast<unsigned*>(buf + 4096)[lane] = lane_scales<D>(raw_ks, hi);
+    };
+    auto put_values = [&](int it, bool there) __attribute__((always_inline)) {
+        if (!brings_values) return;
+        const int buf = it & 1, base = (c0 + it) * KV4_PAGE;
+        uintx2 vs = raw_vs;
+        if (base + KV4_PAGE > tile_all || !there) {      // some row does not see all of it: as in the few-rows kernel
+            int first = 0x7fffffff;
 #pragma unroll
-            for (int u = 0; u < KU; ++u) {
-                const float s = __builtin_bit_cast(float, (rks >> (8 * (k_first + u)) & 255u) << 23);
+            for (int i = 7; i >= 0; --i) {
+                const int pos = base + 32 * half + 16 * (i >> 2) + 4 * hi + (i & 3);
+                const bool dead = pos >= rq.len || !there, odd = (vs[i >> 2] >> (8 * (i & 3)) & 255u) == 255u;
+                if (odd && !dead) first = pos;
+                if (odd || dead) vs[i >> 2] &= ~(255u << (8 * (i & 3)));
+            }
 #pragma unroll
-                for (int k = 0; k < KS; ++k) kb[((k_first + u) * KS + k) * 64 + lane] = __builtin_bit_cast(uintx4, row_values(rk[u][k], s));
+            for (int sh = 16; sh < 64; sh <<= 1) {
+                const int other = __shfl_xor(first, sh);
+                first = other < first ? other : first;
+            }
+            if (lane == 0) s_nan[buf][block][half] = first;
+        }
+        uintx4 e, d;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const unsigned c = raw_v[i], w = vs[i];
+            const unsigned y0 = pair_of<0>(c, scale_of(w, 0)), y1 = pair_of<1>(c, scale_of(w, 1)), y2 = pair_of<2>(c, scale_of(w, 2)), y3 = pair_of<3>(c, scale_of(w, 3));
+            e[2 * i] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
+            e[2 * i + 1] = __builtin_amdgcn_perm(y3, y2, 0x05040100u);
+            d[2 * i] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
+            d[2 * i + 1] = __builtin_amdgcn_perm(y3, y2, 0x07060302u);
+        }
+        uintx4* const vb = reinterpret_cast<uintx4*>(smem + buf * BUF + V_AT);
+        vb[(block * 4 + half) * 64 + lane] = e;
+        vb[(block * 4 + 2 + half) * 64 + lane] = d;
+    };
+
+    half8 pw[CT][2];
+    const half8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+    struct Keys {
+        uintx4 k[4];
+        unsigned scales;
+    };
+    auto fetch_keys = [&](int it, Keys& keys) __attribute__((always_inline)) {
+        const char* const buf = smem + (it & 1) * BUF;
+        keys.scales = reinterpret_cast<const unsigned*>(buf + 4096)[lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keys.k[i] = reinterpret_cast<const uintx4*>(buf)[i * 64 + lane];
+    };
+    // Weights times values of iteration `it`, whose weights are in pw.  The operands of two blocks of columns are asked for ahead, in this order, or the
+    // compiler would ask for each where it is needed and wait; the next page's keys behind them.
+    auto weigh = [&](int it, Keys& keys) __attribute__((always_inline)) {
+        const int buf = it & 1, base = (c0 + it) * KV4_PAGE;
+        const uintx4* const vb = reinterpret_cast<const uintx4*>(smem + buf * BUF + V_AT) + lane;
+        half8 f[KP_AHEAD + 1][4];
+        auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[t % (KP_AHEAD + 1)][i] = __builtin_bit_cast(half8, vb[(t * 4 + i) * 64]);
+        };
+#pragma unroll
+        for (int t = 0; t < KP_AHEAD && t < NB; ++t) fetch(t);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[ct][k], l[ct], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < NB; ++t) {
+            if (t + KP_AHEAD < NB) fetch(t + KP_AHEAD);
+            else if (t + KP_AHEAD == NB) fetch_keys(it + 1, keys);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    o[ct][2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t % (KP_AHEAD + 1)][k], pw[ct][k], o[ct][2 * t], 0, 0, 0);
+                    o[ct][2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t % (KP_AHEAD + 1)][2 + k], pw[ct][k], o[ct][2 * t + 1], 0, 0, 0);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (base + KV4_PAGE > tile_all) {
+#pragma unroll
+            for (int t = 0; t < NB; ++t) {
+                const int u = s_nan[buf][t][0], v = s_nan[buf][t][1], first = u < v ? u : v;
+                if (first != 0x7fffffff) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+                        if (first < seen[ct]) o[ct][2 * t] = o[ct][2 * t + 1] = floatx4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+                }
             }
         }
+    };
+    auto soften = [&](int it, bool there, floatx4 (&acc)[CT][4]) __attribute__((always_inline)) {
+        const int base = there ? (c0 + it) * KV4_PAGE : 0x7fffff00;      // (nothing of a page that is not there is seen)
+        if (base + KV4_PAGE > wave_all) {
 #pragma unroll
-        for (int u = 0; u < VU; ++u) {
-            const int t = v_first + u;
-            if (t < 0 || t >= NB) continue;
-            if (base + KV4_PAGE > tile_all) {    // some row does not see all of it: as in the few-rows kernel
-                int first = 0x7fffffff;
+            for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int i = 15; i >= 0; --i) {
-                    const int pos = base + 16 * (i >> 2) + 4 * hi + (i & 3);
-                    const bool dead = pos >= rq.len, odd = (rvs[u][i >> 2] >> (8 * (i & 3)) & 255u) == 255u;
-                    if (odd && !dead) first = pos;
-                    if (odd || dead) rvs[u][i >> 2] &= ~(255u << (8 * (i & 3)));
-                }
+                for (int i = 0; i < 16; ++i)
+                    if (base + 16 * (i >> 2) + 4 * hi + (i & 3) >= seen[ct]) acc[ct][i >> 2][i & 3] = -__builtin_inff();
+        }
+        auto weights = [&](int ct) __attribute__((always_inline)) {
 #pragma unroll
-                for (int sh = 16; sh < 64; sh <<= 1) {
-                    const int other = __shfl_xor(first, sh);
-                    first = other < first ? other : first;
-                }
-                if (lane == 0) s_nan[buf][t] = first;
-            }
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                uintx4 e, d;
+                for (int r = 0; r < 8; ++r) pw[ct][k][r] = (_Float16)__builtin_amdgcn_exp2f(acc[ct][2 * k + (r >> 2)][r & 3]);
+        };
 #pragma unroll
-                for (int i2 = 0; i2 < 2; ++i2) {
-                    const unsigned c = rv[u][2 * k + i2], w = rvs[u][2 * k + i2];
-                    const unsigned y0 = pair_of<0>(c, scale_of(w, 0)), y1 = pair_of<1>(c, scale_of(w, 1)), y2 = pair_of<2>(c, scale_of(w, 2)), y3 = pair_of<3>(c, scale_of(w, 3));
-                    e[2 * i2] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
-                    e[2 * i2 + 1] = __builtin_amdgcn_perm(y3, y2, 0x05040100u);
-                    d[2 * i2] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
-                    d[2 * i2 + 1] = __builtin_amdgcn_perm(y3, y2, 0x07060302u);
-                }
-                vb[(t * 4 + k) * 64 + lane] = e;
-                vb[(t * 4 + 2 + k) * 64 + lane] = d;
-            }
+        for (int ct = 0; ct < CT; ++ct) weights(ct);
+        // Is a weight past 2^(KP_WEIGHT_LOG2 + KP_LAG) = 2^15?  Its fp16 exponent is 30 or 31 then, and 0x0800 more carries into the sign.  No maximum crosses
+        // lanes unless one is.
+        bool grown[CT], any = fresh;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            half2v top = {0, 0};
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int r = 0; r < 8; r += 2) top = __builtin_elementwise_maximum(top, half2v{pw[ct][k][r], pw[ct][k][r + 1]});
+            grown[ct] = fresh || __builtin_amdgcn_ballot_w64(((__builtin_bit_cast(unsigned, top) + 0x08000800u) & 0x80008000u) != 0) != 0ull;
+            any = any || grown[ct];
+        }
+        if (!any) return;
+        fresh = false;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            if (!grown[ct]) continue;
+            float mb = acc[ct][0][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mb = __builtin_fmaxf(mb, acc[ct][i >> 2][i & 3]);
+            const float mn = __builtin_fmaxf(m[ct], max_over_hi(mb) - from[ct][0]);
+            const bool none = mn == -__builtin_inff();
+            const float corr = __builtin_amdgcn_exp2f(m[ct] - (none ? 0.f : mn)), start = none ? 0.f : KP_WEIGHT_LOG2 - mn, more = start - from[ct][0];
+            fresh = fresh || __builtin_amdgcn_ballot_w64(none) != 0ull;
+            m[ct] = mn;
+            from[ct] = floatx4{start, start, start, start};
+            l[ct] *= corr;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[ct][i] += more;
+#pragma unroll
+            for (int t = 0; t < 2 * NB; ++t) o[ct][t] *= corr;
+            weights(ct);
         }
     };
 
-    const int n_it = c1 - c0;
-    int page = n_it > 0 ? page_at(0) : -1, next = -1;
-    issue(page);
-    if (page >= 0) convert(0, 0);
-    next = 1 < n_it ? page_at(1) : -1;
-    issue(next);
+    // The two halves of the waves (one of each on every SIMD) take turns: while one multiplies, the other has its exponentials and brings things into LDS.
+    // In slot 2 p the first half multiplies (the weights of page p - 1 with their values, then the scores of page p), in slot 2 p + 1 the second half.  In slot
+    // 2 p + 1 the first half, in slot 2 p the second half puts its part of the values of page p and of the keys of page p + 1: before slot 2 p + 2
+    // all of that is there, and what it replaces, two pages before, was read in slot 2 p - 1 for the last time.
+    const int n_it = c1 - c0 > 0 ? c1 - c0 : 0, shift = wv < 4 ? 0 : 1;
+    const int sees = wave_sees - c0 * KV4_PAGE, n_wave = wave_sees <= c0 * KV4_PAGE ? 0 : (sees + KV4_PAGE - 1) / KV4_PAGE < n_it ? (sees + KV4_PAGE - 1) / KV4_PAGE : n_it;
+    int page[4];                                 // of iterations it .. it + 3
+#pragma unroll
+    for (int i = 0; i < 4; ++i) page[i] = i < n_it ? page_at(i) : -1;
+    issue_keys(page[0]);
+    issue_values(page[0]);
+    put_keys(0);
+    issue_keys(page[1]);
     lds_barrier();
-    for (int it = 0; it < n_it; ++it) {
-        const int buf = it & 1, base = (c0 + it) * KV4_PAGE;
-        const bool active = page >= 0 && base < wave_sees;
-        const uintx4* const kb = kp_smem + buf * BUF;
-        const uintx4* const vb = kb + K_UNITS;
-        floatx4 acc[CT][4];
-        if (active) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) acc[ct][i] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const half8 kf = __builtin_bit_cast(half8, kb[(i * KS + k) * 64 + lane]);
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) acc[ct][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[ct][k], acc[ct][i], 0, 0, 0);
-                }
-            }
-        }
-        if (next >= 0) convert(it + 1, buf ^ 1);
-        const int behind = it + 2 < n_it ? page_at(it + 2) : -1;
-        issue(behind);
-        if (active) {
-            const bool masked = base + KV4_PAGE > wave_all;
-            half8 pw[CT][2];
-            float top[CT];
-            if (masked) {
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (base + 16 * (i >> 2) + 4 * hi + (i & 3) >= seen[ct]) acc[ct][i >> 2][i & 3] = -__builtin_inff();
-            }
-            bool grown = false;
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                float mb = acc[ct][0][0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) mb = __builtin_fmaxf(mb, acc[ct][i >> 2][i & 3]);
-                top[ct] = max_over_hi(mb) * scale2;
-                grown = grown || top[ct] - m[ct] > KP_LAG;
-            }
-            if (__builtin_amdgcn_ballot_w64(grown) != 0ull) {
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    const float mn = __builtin_fmaxf(m[ct], top[ct]);
-                    const float corr = __builtin_amdgcn_exp2f(m[ct] - (mn == -__builtin_inff() ? 0.f : mn));
-                    m[ct] = mn;
-                    l[ct] *= corr;
-#pragma unroll
-                    for (int t = 0; t < 2 * NB; ++t) o[ct][t] *= corr;
-                }
-            }
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const float off = KP_WEIGHT_LOG2 - (m[ct] == -__builtin_inff() ? 0.f : m[ct]);
-                float sum = 0.f;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float w[8];
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        w[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[ct][2 * k + (r >> 2)][r & 3], scale2, off));
-                        sum += w[r];
-                    }
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) pw[ct][k][r] = (_Float16)w[r];
-                }
-                l[ct] += sum;
-            }
-#pragma unroll
-            for (int t = 0; t < NB; ++t)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const half8 ev = __builtin_bit_cast(half8, vb[(t * 4 + k) * 64 + lane]), od = __builtin_bit_cast(half8, vb[(t * 4 + 2 + k) * 64 + lane]);
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        o[ct][2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ev, pw[ct][k], o[ct][2 * t], 0, 0, 0);
-                        o[ct][2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(od, pw[ct][k], o[ct][2 * t + 1], 0, 0, 0);
-                    }
-                }
-            if (base + KV4_PAGE > tile_all) {
-#pragma unroll
-                for (int t = 0; t < NB; ++t) {
-                    const int first = s_nan[buf][t];
-                    if (first != 0x7fffffff) {
-#pragma unroll
-                        for (int ct = 0; ct < CT; ++ct)
-                            if (first < seen[ct]) o[ct][2 * t] = o[ct][2 * t + 1] = floatx4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-                    }
-                }
-            }
-        }
+    if (shift) {
+        put_values(0, page[0] >= 0);
+        put_keys(1);
+        issue_values(page[1]);
+        issue_keys(page[2]);
         lds_barrier();
-        page = next;
-        next = behind;
     }
+    floatx4 acc[CT][4];
+    Keys keys;
+    auto pin = [&]() __attribute__((always_inline)) {      // (products may be moved past a barrier, which concerns memory only; here they are what the turns are about)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[ct][i]));
+    };
+    if (n_wave > 0) {
+        fetch_keys(0, keys);
+        score_page<CT>(keys.k, keys.scales, queries, from, acc);
+        pin();
+    }
+    lds_barrier();
+    // what comes in behind the exponentials of iteration `it`
+    auto bring = [&](int it) __attribute__((always_inline)) {
+        const int j = it + shift;
+        if (j < n_it) put_values(j, (shift ? page[1] : page[0]) >= 0);
+        if (j + 1 < n_it) put_keys(j + 1);
+        issue_values(shift ? page[2] : page[1]);
+        issue_keys(shift ? page[3] : page[2]);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) page[i] = page[i + 1];
+        page[3] = it + 4 < n_it ? page_at(it + 4) : -1;
+        lds_barrier();
+    };
+    for (int it = 0; it < n_wave; ++it) {
+        soften(it, page[0] >= 0, acc);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) asm volatile("" : "+v"(pw[ct][0]), "+v"(pw[ct][1]));
+        bring(it);
+        weigh(it, keys);
+        score_page<CT>(keys.k, keys.scales, queries, from, acc);      // (behind the last page: of whatever is there, for nobody)
+        pin();
+        lds_barrier();
+    }
+    for (int it = n_wave; it < n_it; ++it) {
+        bring(it);
+        lds_barrier();
+    }
+    if (!shift) lds_barrier();
 
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         const int r = w0 + ct * 16 + lo;
-        const float lf = sum_over_hi(l[ct]);
+        const float lf = l[ct][0];               // (summed by the matrix product over all lanes)
         if (r >= all_rows) continue;
         const size_t row = (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group;
         if (whole) {
@@ -673,17 +811,17 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 4) void kv4_attn_prompt(Kv4Attn
     }
 }
 
-template <int D, int CT, int WAVES>
+template <int D, int CT>
 hipError_t launch_prompt(const Kv4AttnArgs& a, hipStream_t stream)
 {
-    constexpr int LDS = 2 * (4 * (D / 32) + 4 * (D / 32)) * 64 * 16;
+    constexpr int LDS = 2 * KP_BUF<D>;
     static std::once_flag attr_once;
     std::call_once(attr_once, [] {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_attn_prompt<D, CT, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_attn_prompt<D, CT>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     });
-    const long rows = (long)a.max_q * (a.Hq / a.Hkv), per = WAVES * 16 * CT;
+    const long rows = (long)a.max_q * (a.Hq / a.Hkv), per = KP_WAVES * 16 * CT;
     const dim3 grid((unsigned)((rows + per - 1) / per * a.Hkv), (unsigned)a.B, (unsigned)a.nsplit);
-    hipLaunchKernelGGL((kv4_attn_prompt<D, CT, WAVES>), grid, dim3(64 * WAVES), LDS, stream, a);
+    hipLaunchKernelGGL((kv4_attn_prompt<D, CT>), grid, dim3(64 * KP_WAVES), LDS, stream, a);
     if (a.nsplit > 1) hipLaunchKernelGGL((kv4_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(D), 0, stream, a);
     return hipGetLastError();
 }
@@ -693,7 +831,7 @@ hipError_t launch_prompt(const Kv4AttnArgs& a, hipStream_t stream)
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, hipStream_t stream)
 {
     if (a.split_rows) return a.D == 128 ? launch_decode<128>(a, stream) : launch_decode<64>(a, stream);
-    return a.D == 128 ? launch_prompt<128, 2, 8>(a, stream) : launch_prompt<64, 2, 8>(a, stream);
+    return a.D == 128 ? launch_prompt<128, 2>(a, stream) : launch_prompt<64, 2>(a, stream);
 }
 
 }  // namespace thi
