@@ -466,11 +466,12 @@ hipError_t launch_decode(const Kv4AttnArgs& a, hipStream_t stream)
 // Bound by the matrix cores and the vector ALU together (an exponential costs a wave 16 cycles, 16 of them and some 50 plain instructions against 32 products of
 // 16 cycles per page and tile).
 //
-// A weight is one fp16 number here (off by as much as the result is by its own rounding), 2^11 p of a maximum that may lag by 2^4 (so that weights down to 2^-25 are normal numbers):
-// the sums are rescaled only when some row's maximum has grown by more than that.
+// A weight is one fp16 number here (off by as much as the result is by its own rounding): 2^9 p of a maximum that may lag by 2^6, so that weights down
+// to 2^-23 are normal numbers.  The sums are rescaled when some row's maximum has grown by more, which costs as much as the rest of a page's vector work, and all
+// waves wait for the one: with 2^11 and a lag of 2^4 that was most iterations.
 constexpr int KP_WAVES = 8, KP_AHEAD = 2;
 template <int D> constexpr int KP_BUF = 4096 + 256 + 128 * D;      // a page in LDS: key codes, key scales, values in fp16
-constexpr float KP_WEIGHT_LOG2 = 11.0f, KP_LAG = 4.0f;
+constexpr float KP_WEIGHT_LOG2 = 9.0f;          // 2^15 less KP_WEIGHT_LOG2: what a maximum may lag by
 
 __device__ __forceinline__ void lds_barrier()
 {
@@ -485,7 +486,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
     constexpr int NB = D / 32, ROWS = KP_WAVES * 16 * CT;
     constexpr int BUF = KP_BUF<D>, V_AT = 4096 + 256;       // bytes of a buffer: key codes and scales as loaded (a lane's behind each other), values in fp16
     extern __shared__ uintx4 kp_smem[];
-    __shared__ int s_nan[2][NB][2];              // of a buffer that not every row sees whole: the first position that is not a number in half a block
+    __shared__ int s_nan[4][NB][2];              // of a page that not every row sees whole: the first position that is not a number in half a block
     char* const smem = reinterpret_cast<char*>(kp_smem);
 
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
@@ -560,52 +561,66 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
     const unsigned k_off = k_tile * 8 * D + key_offset<D>(lo, hi) + k_half * 8, ks_off = key_scale_offset<D>(lo, hi);
     const unsigned v_off = kv4_values(D) + block * 1024 + lane * 16 + half * 8, vs_off = kv4_value_scales(D) + block * 64 + hi * 16 + half * 8;
     auto head = [&](int page) { return heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_bytes; };
+    // (an offset that the compiler may not add to the uniform part of the address outside the loop: that is an addition of 64 bits per load)
+    auto lane_part = [](unsigned off) __attribute__((always_inline)) { asm volatile("" : "+v"(off)); return off; };
     auto issue_keys = [&](int page) __attribute__((always_inline)) {
-        raw_k = *reinterpret_cast<const uintx2*>(head(page) + k_off);
-        raw_ks = *reinterpret_cast<const unsigned*>(head(page) + ks_off);
+        raw_k = *reinterpret_cast<const uintx2*>(head(page) + lane_part(k_off));
+        raw_ks = *reinterpret_cast<const unsigned*>(head(page) + lane_part(ks_off));
     };
     auto issue_values = [&](int page) __attribute__((always_inline)) {
-        raw_v = *reinterpret_cast<const uintx2*>(head(page) + v_off);
-        raw_vs = *reinterpret_cast<const uintx2*>(head(page) + vs_off);
+        raw_v = *reinterpret_cast<const uintx2*>(head(page) + lane_part(v_off));
+        raw_vs = *reinterpret_cast<const uintx2*>(head(page) + lane_part(vs_off));
     };
     auto put_keys = [&](int it) __attribute__((always_inline)) {
         char* const buf = smem + (it & 1) * BUF;
         *reinterpret_cast<uintx2*>(buf + (k_tile * 64 + lane) * 16 + k_half * 8) = raw_k;
-        if (wv == 0) reinterpret_cast<unsigned*>(buf + 4096)[lane] = lane_scales<D>(raw_ks, hi);
+        reinterpret_cast<unsigned*>(buf + 4096)[lane] = lane_scales<D>(raw_ks, hi);      // (the same by every wave)
     };
-    auto put_values = [&](int it, bool there) __attribute__((always_inline)) {
-        if (!brings_values) return;
-        const int buf = it & 1, base = (c0 + it) * KV4_PAGE;
-        uintx2 vs = raw_vs;
-        if (base + KV4_PAGE > tile_all || !there) {      // some row does not see all of it: as in the few-rows kernel
-            int first = 0x7fffffff;
+    // Values about to be put of which some row does not see everything: as in the few-rows kernel.
+    auto scrub = [&](int it, bool there) __attribute__((always_inline)) {
+        const int base = (c0 + it) * KV4_PAGE;
+        if (base + KV4_PAGE <= tile_all && there) return;
+        int first = 0x7fffffff;
 #pragma unroll
-            for (int i = 7; i >= 0; --i) {
-                const int pos = base + 32 * half + 16 * (i >> 2) + 4 * hi + (i & 3);
-                const bool dead = pos >= rq.len || !there, odd = (vs[i >> 2] >> (8 * (i & 3)) & 255u) == 255u;
-                if (odd && !dead) first = pos;
-                if (odd || dead) vs[i >> 2] &= ~(255u << (8 * (i & 3)));
-            }
-#pragma unroll
-            for (int sh = 16; sh < 64; sh <<= 1) {
-                const int other = __shfl_xor(first, sh);
-                first = other < first ? other : first;
-            }
-            if (lane == 0) s_nan[buf][block][half] = first;
+        for (int i = 7; i >= 0; --i) {
+            const int pos = base + 32 * half + 16 * (i >> 2) + 4 * hi + (i & 3);
+            const bool dead = pos >= rq.len || !there, odd = (raw_vs[i >> 2] >> (8 * (i & 3)) & 255u) == 255u;
+            if (odd && !dead) first = pos;
+            if (odd || dead) raw_vs[i >> 2] &= ~(255u << (8 * (i & 3)));
         }
-        uintx4 e, d;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const unsigned c = raw_v[i], w = vs[i];
-            const unsigned y0 = pair_of<0>(c, scale_of(w, 0)), y1 = pair_of<1>(c, scale_of(w, 1)), y2 = pair_of<2>(c, scale_of(w, 2)), y3 = pair_of<3>(c, scale_of(w, 3));
-            e[2 * i] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
-            e[2 * i + 1] = __builtin_amdgcn_perm(y3, y2, 0x05040100u);
-            d[2 * i] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
-            d[2 * i + 1] = __builtin_amdgcn_perm(y3, y2, 0x07060302u);
+        for (int sh = 16; sh < 64; sh <<= 1) {
+            const int other = __shfl_xor(first, sh);
+            first = other < first ? other : first;
         }
-        uintx4* const vb = reinterpret_cast<uintx4*>(smem + buf * BUF + V_AT);
-        vb[(block * 4 + half) * 64 + lane] = e;
-        vb[(block * 4 + 2 + half) * 64 + lane] = d;
+        if (brings_values && lane == 0) s_nan[it & 3][block][half] = first;
+    };
+    // The conversion in steps of two or three instructions, to stand between products: 0 .. 3 and 4 .. 7 the positions of a tile each, 8 the store.
+    struct Converted {
+        unsigned y[4];
+        uintx4 even, odd;
+    };
+    auto convert = [&](int step, int it, Converted& x) __attribute__((always_inline)) {
+        const int i = step >> 2;
+        if (step < 8) {
+            const unsigned c = raw_v[i], w = raw_vs[i];
+            if ((step & 3) == 0) x.y[0] = pair_of<0>(c, scale_of(w, 0));
+            if ((step & 3) == 1) {
+                x.y[1] = pair_of<1>(c, scale_of(w, 1));
+                x.even[2 * i] = __builtin_amdgcn_perm(x.y[1], x.y[0], 0x05040100u);
+                x.odd[2 * i] = __builtin_amdgcn_perm(x.y[1], x.y[0], 0x07060302u);
+            }
+            if ((step & 3) == 2) x.y[2] = pair_of<2>(c, scale_of(w, 2));
+            if ((step & 3) == 3) {
+                x.y[3] = pair_of<3>(c, scale_of(w, 3));
+                x.even[2 * i + 1] = __builtin_amdgcn_perm(x.y[3], x.y[2], 0x05040100u);
+                x.odd[2 * i + 1] = __builtin_amdgcn_perm(x.y[3], x.y[2], 0x07060302u);
+            }
+        } else if (step == 8 && brings_values) {
+            uintx4* const vb = reinterpret_cast<uintx4*>(smem + (it & 1) * BUF + V_AT);
+            vb[(block * 4 + half) * 64 + lane] = x.even;
+            vb[(block * 4 + 2 + half) * 64 + lane] = x.odd;
+        }
     };
 
     half8 pw[CT][2];
@@ -622,7 +637,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
     };
     // Weights times values of iteration `it`, whose weights are in pw.  The operands of two blocks of columns are asked for ahead, in this order, or the
     // compiler would ask for each where it is needed and wait; the next page's keys behind them.
-    auto weigh = [&](int it, Keys& keys) __attribute__((always_inline)) {
+    auto weigh = [&](int it, Keys& keys, auto between) __attribute__((always_inline)) {
         const int buf = it & 1, base = (c0 + it) * KV4_PAGE;
         const uintx4* const vb = reinterpret_cast<const uintx4*>(smem + buf * BUF + V_AT) + lane;
         half8 f[KP_AHEAD + 1][4];
@@ -634,27 +649,27 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
         for (int t = 0; t < KP_AHEAD && t < NB; ++t) fetch(t);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[ct][k], l[ct], 0, 0, 0);
-#pragma unroll
         for (int t = 0; t < NB; ++t) {
             if (t + KP_AHEAD < NB) fetch(t + KP_AHEAD);
             else if (t + KP_AHEAD == NB) fetch_keys(it + 1, keys);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 2; ++k) {
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
+                    if (t == 0) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[ct][k], l[ct], 0, 0, 0);
                     o[ct][2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t % (KP_AHEAD + 1)][k], pw[ct][k], o[ct][2 * t], 0, 0, 0);
                     o[ct][2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t % (KP_AHEAD + 1)][2 + k], pw[ct][k], o[ct][2 * t + 1], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    between((t * 2 + k) * CT + ct);      // vector work for the time that the products take
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-            __builtin_amdgcn_sched_barrier(0);
+            }
         }
         if (base + KV4_PAGE > tile_all) {
 #pragma unroll
             for (int t = 0; t < NB; ++t) {
-                const int u = s_nan[buf][t][0], v = s_nan[buf][t][1], first = u < v ? u : v;
+                const int u = s_nan[it & 3][t][0], v = s_nan[it & 3][t][1], first = u < v ? u : v;
                 if (first != 0x7fffffff) {
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
@@ -680,9 +695,10 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
         };
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) weights(ct);
-        // Is a weight past 2^(KP_WEIGHT_LOG2 + KP_LAG) = 2^15?  Its fp16 exponent is 30 or 31 then, and 0x0800 more carries into the sign.  No maximum crosses
+        // Is a weight past 2^15?  Its fp16 exponent is 30 or 31 then, and 0x0800 more carries into the sign.  No maximum crosses
         // lanes unless one is.
-        bool grown[CT], any = fresh;
+        const bool again = fresh || it == 1 || it == 3 || it == 7;       // (all waves together, while maxima still grow)
+        bool grown[CT], any = again;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             half2v top = {0, 0};
@@ -690,7 +706,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int r = 0; r < 8; r += 2) top = __builtin_elementwise_maximum(top, half2v{pw[ct][k][r], pw[ct][k][r + 1]});
-            grown[ct] = fresh || __builtin_amdgcn_ballot_w64(((__builtin_bit_cast(unsigned, top) + 0x08000800u) & 0x80008000u) != 0) != 0ull;
+            grown[ct] = again || __builtin_amdgcn_ballot_w64(((__builtin_bit_cast(unsigned, top) + 0x08000800u) & 0x80008000u) != 0) != 0ull;
             any = any || grown[ct];
         }
         if (!any) return;
@@ -698,10 +714,10 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             if (!grown[ct]) continue;
-            float mb = acc[ct][0][0];
+            float mb = acc[ct][0][0];            // (a NaN comes through; its row is not a number anyway)
 #pragma unroll
-            for (int i = 1; i < 16; ++i) mb = __builtin_fmaxf(mb, acc[ct][i >> 2][i & 3]);
-            const float mn = __builtin_fmaxf(m[ct], max_over_hi(mb) - from[ct][0]);
+            for (int i = 1; i < 16; ++i) mb = __builtin_elementwise_maximum(mb, acc[ct][i >> 2][i & 3]);
+            const float mn = __builtin_elementwise_maximum(m[ct], max_over_hi(mb) - from[ct][0]);
             const bool none = mn == -__builtin_inff();
             const float corr = __builtin_amdgcn_exp2f(m[ct] - (none ? 0.f : mn)), start = none ? 0.f : KP_WEIGHT_LOG2 - mn, more = start - from[ct][0];
             fresh = fresh || __builtin_amdgcn_ballot_w64(none) != 0ull;
@@ -716,11 +732,11 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
         }
     };
 
-    // The two halves of the waves (one of each on every SIMD) take turns: while one multiplies, the other has its exponentials and brings things into LDS.
-    // In slot 2 p the first half multiplies (the weights of page p - 1 with their values, then the scores of page p), in slot 2 p + 1 the second half.  In slot
-    // 2 p + 1 the first half, in slot 2 p the second half puts its part of the values of page p and of the keys of page p + 1: before slot 2 p + 2
-    // all of that is there, and what it replaces, two pages before, was read in slot 2 p - 1 for the last time.
-    const int n_it = c1 - c0 > 0 ? c1 - c0 : 0, shift = wv < 4 ? 0 : 1;
+    // The two halves of the waves (one of each on every SIMD) take turns: while one multiplies, the other has its exponentials.  In slot 2 p the first half
+    // multiplies (the weights of page p - 1 with their values, then the scores of page p), in slot 2 p + 1 the second half.  Between its products a wave puts
+    // its part of the values of page p and of the keys of page p + 1 into LDS: before slot 2 p + 2 all of that is there, and what it
+    // replaces, two pages before, was read in slot 2 p - 1 for the last time.
+    const int n_it = c1 - c0 > 0 ? c1 - c0 : 0;
     const int sees = wave_sees - c0 * KV4_PAGE, n_wave = wave_sees <= c0 * KV4_PAGE ? 0 : (sees + KV4_PAGE - 1) / KV4_PAGE < n_it ? (sees + KV4_PAGE - 1) / KV4_PAGE : n_it;
     int page[4];                                 // of iterations it .. it + 3
 #pragma unroll
@@ -730,13 +746,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
     put_keys(0);
     issue_keys(page[1]);
     lds_barrier();
-    if (shift) {
-        put_values(0, page[0] >= 0);
-        put_keys(1);
-        issue_values(page[1]);
-        issue_keys(page[2]);
-        lds_barrier();
-    }
+    if (wv >= 4) lds_barrier();
     floatx4 acc[CT][4];
     Keys keys;
     auto pin = [&]() __attribute__((always_inline)) {      // (products may be moved past a barrier, which concerns memory only; here they are what the turns are about)
@@ -745,39 +755,63 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
 #pragma unroll
             for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[ct][i]));
     };
+    // everything that comes in for iteration `it`, page[0] being its page (pages past the last one: of page 0, for nobody)
+    auto bring = [&](int it) __attribute__((always_inline)) {
+        Converted x;
+#pragma unroll
+        for (int i = 0; i < 9; ++i) convert(i, it, x);
+        put_keys(it + 1);
+        issue_values(page[1]);
+        issue_keys(page[2]);
+    };
+    auto advance = [&](int it) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) page[i] = page[i + 1];
+        page[3] = it + 4 < n_it ? page_at(it + 4) : -1;
+    };
     if (n_wave > 0) {
         fetch_keys(0, keys);
         score_page<CT>(keys.k, keys.scales, queries, from, acc);
         pin();
     }
+    scrub(0, page[0] >= 0);
+    bring(0);
     lds_barrier();
-    // what comes in behind the exponentials of iteration `it`
-    auto bring = [&](int it) __attribute__((always_inline)) {
-        const int j = it + shift;
-        if (j < n_it) put_values(j, (shift ? page[1] : page[0]) >= 0);
-        if (j + 1 < n_it) put_keys(j + 1);
-        issue_values(shift ? page[2] : page[1]);
-        issue_keys(shift ? page[3] : page[2]);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) page[i] = page[i + 1];
-        page[3] = it + 4 < n_it ? page_at(it + 4) : -1;
-        lds_barrier();
-    };
     for (int it = 0; it < n_wave; ++it) {
         soften(it, page[0] >= 0, acc);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) asm volatile("" : "+v"(pw[ct][0]), "+v"(pw[ct][1]));
-        bring(it);
-        weigh(it, keys);
+        advance(it);
+        scrub(it + 1, page[0] >= 0);
+        lds_barrier();
+        Converted x;
+        weigh(it, keys, [&](int step) __attribute__((always_inline)) {
+            constexpr int LAST = 4 * NB * CT / 2 - 1;                // of the steps (D = 64: seven, so two at a time)
+            if constexpr (LAST >= 13) {
+                convert(step, it + 1, x);
+                if (step == 9) put_keys(it + 2);
+                if (step == 11) issue_values(page[1]);
+                if (step == 13) issue_keys(page[2]);
+            } else {
+                convert(2 * step, it + 1, x);
+                convert(2 * step + 1, it + 1, x);
+                if (step == 5) put_keys(it + 2);
+                if (step == 6) issue_values(page[1]);
+                if (step == 7) issue_keys(page[2]);
+            }
+        });
         score_page<CT>(keys.k, keys.scales, queries, from, acc);      // (behind the last page: of whatever is there, for nobody)
         pin();
         lds_barrier();
     }
     for (int it = n_wave; it < n_it; ++it) {
-        bring(it);
+        advance(it);
+        scrub(it + 1, page[0] >= 0);
+        lds_barrier();
+        bring(it + 1);
         lds_barrier();
     }
-    if (!shift) lds_barrier();
+    if (wv < 4) lds_barrier();
 
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
