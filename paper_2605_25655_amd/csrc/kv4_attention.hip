@@ -75,15 +75,25 @@ struct Queries {
     unsigned scales;
 };
 
-template <int D> __device__ __forceinline__ void take_queries(const uint16_t* row, int hi, float scale2, Queries& q)
+struct QueryRow {
+    uintx4 x[4];
+};
+// the lane's block of a row as it stands
+template <int D> __device__ __forceinline__ QueryRow ask_queries(const uint16_t* row, int hi)
+{
+    QueryRow q;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) q.x[s] = ld_cached(row + (hi < D / 32 ? hi : 0) * 32 + s * 8);
+    return q;
+}
+template <int D> __device__ __forceinline__ void take_queries(const QueryRow& row, int hi, float scale2, Queries& q)
 {
     const bool any = hi < D / 32;
-    const uint16_t* const from = row + (any ? hi : 0) * 32;
     floatx32 rest;
     unsigned high = 0, low = 0;                  // the largest magnitudes' bits of the odd and even columns, in the upper half
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-        const uintx4 x = ld_cached(from + s * 8);
+        const uintx4 x = row.x[s];
         const half8 h = __builtin_bit_cast(half8, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) rest[8 * s + e] = any ? (float)h[e] * scale2 : 0.f;
@@ -193,10 +203,9 @@ __device__ __forceinline__ half8 join(half4 a, half4 b) { return half8{a[0], a[1
 
 // MULTI: the rows of a tile may be of several new tokens, which see different positions.
 template <int D, bool MULTI>
-__global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
+__global__ __launch_bounds__(KD_THREADS, MULTI ? 2 : 3) void kv4_attn_decode(Kv4AttnArgs a)
 {
     constexpr int NB = D / 32;                   // blocks of a row
-    typedef PageRegs<D> Regs;
     __shared__ float s_o[KD_WAVES][16][D + 4];
     __shared__ float s_m[KD_WAVES][16], s_l[KD_WAVES][16];
 
@@ -213,13 +222,50 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
     if (chunk > 0 && c0 >= pages) return;
     const bool whole = pages <= size;
 
+    const int n_it = (c1 - c0 - wv + KD_WAVES - 1) / KD_WAVES;      // this wave's pages: c0 + wv, c0 + wv + 4, ...
     auto row_of_column = [&](int c) {            // (token, head) row of q and out
         const int r = r0 + c;
         return (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group;
     };
     const int col = lo < rows ? lo : rows - 1;
+    const QueryRow query_row = ask_queries<D>(a.q + row_of_column(col) * D, hi);      // (in front of the page: it is waited for first)
+    int entries = -1;                            // of the 64 pages from iteration `it` & ~63 on, one per lane
+    const int* const table = a.page_table + (size_t)b * a.max_pages;
+    auto page_at = [&](int it) {                 // asked for in order
+        if ((it & 63) == 0) {
+            const int j = c0 + wv + (it + lane) * KD_WAVES;
+            entries = j < c1 ? table[j] : -1;
+            asm volatile("" : "+v"(entries));    // waited for here, and not in every iteration behind whatever else is in flight
+        }
+        const int e = __builtin_amdgcn_readlane(entries, it & 63);
+        return e >= 0 && e < a.num_pages ? e : -1;
+    };
+    // One page's registers: the next page's keys are asked for when the scores are made, the next page's values block by block as they are multiplied.
+    // Unconditionally (a page that is not there: page 0), so that nothing waits for a load but what uses it.
+    PageRegs<D> x;
+    const unsigned char* const heads = a.pages + (size_t)g * kv4_head_bytes(D);
+    const size_t page_bytes = (size_t)a.Hkv * kv4_head_bytes(D);
+    auto head = [&](int page) { return heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_bytes; };
+    auto lane_part = [](unsigned off) __attribute__((always_inline)) { asm volatile("" : "+v"(off)); return off; };
+    auto ask_keys = [&](int page) __attribute__((always_inline)) {
+        const unsigned char* const from = head(page);
+        const unsigned off = lane_part(key_offset<D>(lo, hi));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + off + i * 8 * D));
+        x.ks = *reinterpret_cast<const unsigned*>(from + lane_part(key_scale_offset<D>(lo, hi)));
+    };
+    auto ask_values = [&](int page, int t) __attribute__((always_inline)) {
+        const unsigned char* const from = head(page) + kv4_values(D);
+        x.vs[t] = *reinterpret_cast<const uintx4*>(from + 32 * D + t * 64 + lane_part(hi * 16));
+        x.v[t] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + t * 1024 + lane_part(lane * 16)));
+    };
+    int page = n_it > 0 ? page_at(0) : -1;
+    ask_keys(page);
+#pragma unroll
+    for (int t = 0; t < NB; ++t) ask_values(page, t);
+
     Queries queries[1];
-    take_queries<D>(a.q + row_of_column(col) * D, hi, a.scale2, queries[0]);
+    take_queries<D>(query_row, hi, a.scale2, queries[0]);
     // positions this lane's row sees, and what every row of the tile sees
     const int seen = rq.len - rq.n + (MULTI ? (r0 + col) / group : 0) + 1;
     const int all_see = rq.len - rq.n + (MULTI ? r0 / group : 0) + 1;
@@ -229,79 +275,61 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
 #pragma unroll
     for (int t = 0; t < 2 * NB; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    const int n_it = (c1 - c0 - wv + KD_WAVES - 1) / KD_WAVES;      // this wave's pages: c0 + wv, c0 + wv + 4, ...
-    int entries = -1;                            // of the 64 pages from iteration `it` & ~63 on, one per lane
-    const int* const table = a.page_table + (size_t)b * a.max_pages;
-    auto page_at = [&](int it) {
-        if ((it & 63) == 0) {
-            const int j = c0 + wv + (it + lane) * KD_WAVES;
-            entries = j < c1 ? table[j] : -1;
-            // waited for here, and not in every iteration behind whatever else is in flight
-            asm volatile("" : "+v"(entries));
-        }
-        const int e = __builtin_amdgcn_readlane(entries, it & 63);
-        return e >= 0 && e < a.num_pages ? e : -1;
-    };
-    auto issue = [&](int page, Regs& x) __attribute__((always_inline)) {
-        if (page < 0) return;
-        const unsigned char* const base = a.pages + ((size_t)page * a.Hkv + g) * kv4_head_bytes(D);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(base + i * 8 * D + key_offset<D>(lo, hi)));
-        x.ks = *reinterpret_cast<const unsigned*>(base + key_scale_offset<D>(lo, hi));
-#pragma unroll
-        for (int t = 0; t < NB; ++t) {
-            x.v[t] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(base + kv4_values(D) + t * 1024 + lane * 16));
-            x.vs[t] = *reinterpret_cast<const uintx4*>(base + kv4_value_scales(D) + t * 64 + hi * 16);
-        }
-    };
-    auto multiply = [&](const Regs& x, const uintx4 (&vs)[NB], const half8 (&pl)[2], const half8 (&ps)[2]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int t = 0; t < NB; ++t) {
-            half8 ev[2], od[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                uintx4 e, d;
-#pragma unroll
-                for (int i2 = 0; i2 < 2; ++i2) {
-                    const unsigned c = x.v[t][2 * k + i2], w = vs[t][2 * k + i2];
-                    const unsigned y0 = pair_of<0>(c, scale_of(w, 0)), y1 = pair_of<1>(c, scale_of(w, 1)), y2 = pair_of<2>(c, scale_of(w, 2)), y3 = pair_of<3>(c, scale_of(w, 3));
-                    e[2 * i2] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
-                    e[2 * i2 + 1] = __builtin_amdgcn_perm(y3, y2, 0x05040100u);
-                    d[2 * i2] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
-                    d[2 * i2 + 1] = __builtin_amdgcn_perm(y3, y2, 0x07060302u);
-                }
-                ev[k] = __builtin_bit_cast(half8, e);
-                od[k] = __builtin_bit_cast(half8, d);
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                o[2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ev[k], pl[k], o[2 * t], 0, 0, 0);
-                o[2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(od[k], pl[k], o[2 * t + 1], 0, 0, 0);
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                o[2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ev[k], ps[k], o[2 * t], 0, 0, 0);
-                o[2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(od[k], ps[k], o[2 * t + 1], 0, 0, 0);
-            }
-        }
-    };
-    auto compute = [&](int page, int it, Regs& x) __attribute__((always_inline)) {
-        if (page < 0) return;
-        const int base = (c0 + wv + it * KD_WAVES) * KV4_PAGE;
+    for (int it = 0; it < n_it; ++it) {
+        const int next = it + 1 < n_it ? page_at(it + 1) : -1;
+        const bool there = page >= 0;
+        const int base = there ? (c0 + wv + it * KD_WAVES) * KV4_PAGE : 0x7fffff00;      // (nothing of a page that is not there is seen)
         const bool masked = base + KV4_PAGE > all_see;
-        float t[16];
         floatx4 scores[1][4];
-        const floatx4 zero[1] = {floatx4{0.f, 0.f, 0.f, 0.f}};
-        score_page<1>(x.k, lane_scales<D>(x.ks, hi), queries, zero, scores);
+        {
+            const floatx4 zero[1] = {floatx4{0.f, 0.f, 0.f, 0.f}};
+            score_page<1>(x.k, lane_scales<D>(x.ks, hi), queries, zero, scores);
+        }
+        ask_keys(next);
+        float t[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) t[i] = scores[0][i >> 2][i & 3];
+        int first[NB];                               // the first position of a block that is not a number, where rows see different positions
+        bool told = false;
         if (masked) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) t[i] = base + 16 * (i >> 2) + 4 * hi + (i & 3) < seen ? t[i] : -__builtin_inff();
+            // Weights are zero where a row does not see a position, but 0 * NaN must not come through: scales of positions that no row sees become 0, and
+            // where rows see different ones a NaN's scale too; the rows that do see it are told afterwards.
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int live = there ? rq.len - (base + 16 * i + 4 * hi) : 0;      // of the four bytes
+                const unsigned keep = live >= 4 ? 0xffffffffu : live <= 0 ? 0u : (1u << (8 * live)) - 1u;
+#pragma unroll
+                for (int k = 0; k < NB; ++k) {
+                    x.vs[k][i] &= keep;
+                    const unsigned w = ~x.vs[k][i];                      // a byte of zero: a scale byte of 255
+                    odd = odd || ((w - 0x01010101u) & ~w & 0x80808080u) != 0;
+                }
+            }
+            if (MULTI && __builtin_amdgcn_ballot_w64(odd) != 0ull) {
+                told = true;
+#pragma unroll
+                for (int k = 0; k < NB; ++k) {
+                    first[k] = 0x7fffffff;
+#pragma unroll
+                    for (int i = 15; i >= 0; --i)
+                        if ((x.vs[k][i >> 2] >> (8 * (i & 3)) & 255u) == 255u) {
+                            first[k] = base + 16 * (i >> 2) + 4 * hi + (i & 3);
+                            x.vs[k][i >> 2] &= ~(255u << (8 * (i & 3)));
+                        }
+#pragma unroll
+                    for (int sh = 16; sh < 64; sh <<= 1) {
+                        const int other = __shfl_xor(first[k], sh);
+                        first[k] = other < first[k] ? other : first[k];
+                    }
+                }
+            }
         }
         float mb = t[0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) mb = __builtin_fmaxf(mb, t[i]);
+        for (int i = 1; i < 16; ++i) mb = __builtin_elementwise_maximum(mb, t[i]);
         const float mn = __builtin_fmaxf(m, max_over_hi(mb));
         const float ms = mn == -__builtin_inff() ? 0.f : mn;
         const float corr = __builtin_amdgcn_exp2f(m - ms);
@@ -329,62 +357,42 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv4_attn_decode(Kv4AttnArgs a)
 #pragma unroll
             for (int k = 0; k < 2 * NB; ++k) o[k] *= corr;
         }
-        if (!masked) {
-            multiply(x, x.vs, pl, ps);
-            return;
-        }
-        // Weights are zero where a row does not see a position, but 0 * NaN must not come through: scales of positions that no row sees become 0, and where
-        // rows see different ones a NaN's scale too; the rows that do see it are told afterwards.
-        uintx4 vs[NB];
-        bool odd = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int live = rq.len - (base + 16 * i + 4 * hi);          // of the four bytes
-            const unsigned keep = live >= 4 ? 0xffffffffu : live <= 0 ? 0u : (1u << (8 * live)) - 1u;
+        for (int b4 = 0; b4 < NB; ++b4) {
+            half8 ev[2], od[2];
 #pragma unroll
-            for (int k = 0; k < NB; ++k) {
-                vs[k][i] = x.vs[k][i] & keep;
-                const unsigned w = ~vs[k][i];                            // a byte of zero: a scale byte of 255
-                odd = odd || ((w - 0x01010101u) & ~w & 0x80808080u) != 0;
-            }
-        }
-        if (MULTI && __builtin_amdgcn_ballot_w64(odd) != 0ull) {
-            int first[NB];                                               // the first position of a block that is not a number
+            for (int k = 0; k < 2; ++k) {
+                uintx4 e, d;
 #pragma unroll
-            for (int k = 0; k < NB; ++k) {
-                first[k] = 0x7fffffff;
-#pragma unroll
-                for (int i = 15; i >= 0; --i)
-                    if ((vs[k][i >> 2] >> (8 * (i & 3)) & 255u) == 255u) {
-                        first[k] = base + 16 * (i >> 2) + 4 * hi + (i & 3);
-                        vs[k][i >> 2] &= ~(255u << (8 * (i & 3)));
-                    }
-            }
-            multiply(x, vs, pl, ps);
-#pragma unroll
-            for (int k = 0; k < NB; ++k) {
-#pragma unroll
-                for (int sh = 16; sh < 64; sh <<= 1) {
-                    const int other = __shfl_xor(first[k], sh);
-                    first[k] = other < first[k] ? other : first[k];
+                for (int i2 = 0; i2 < 2; ++i2) {
+                    const unsigned c = x.v[b4][2 * k + i2], w = x.vs[b4][2 * k + i2];
+                    const unsigned y0 = pair_of<0>(c, scale_of(w, 0)), y1 = pair_of<1>(c, scale_of(w, 1)), y2 = pair_of<2>(c, scale_of(w, 2)), y3 = pair_of<3>(c, scale_of(w, 3));
+                    e[2 * i2] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
+                    e[2 * i2 + 1] = __builtin_amdgcn_perm(y3, y2, 0x05040100u);
+                    d[2 * i2] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
+                    d[2 * i2 + 1] = __builtin_amdgcn_perm(y3, y2, 0x07060302u);
                 }
-                if (first[k] < seen) o[2 * k] = o[2 * k + 1] = floatx4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+                ev[k] = __builtin_bit_cast(half8, e);
+                od[k] = __builtin_bit_cast(half8, d);
             }
-            return;
+            ask_values(next, b4);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                o[2 * b4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ev[k], pl[k], o[2 * b4], 0, 0, 0);
+                o[2 * b4 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(od[k], pl[k], o[2 * b4 + 1], 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                o[2 * b4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ev[k], ps[k], o[2 * b4], 0, 0, 0);
+                o[2 * b4 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(od[k], ps[k], o[2 * b4 + 1], 0, 0, 0);
+            }
         }
-        multiply(x, vs, pl, ps);
-    };
-
-    Regs x0, x1;
-    int p0 = n_it > 0 ? page_at(0) : -1, p1;
-    issue(p0, x0);
-    for (int it = 0; it < n_it; it += 2) {
-        p1 = it + 1 < n_it ? page_at(it + 1) : -1;
-        issue(p1, x1);
-        compute(p0, it, x0);
-        p0 = it + 2 < n_it ? page_at(it + 2) : -1;
-        issue(p0, x0);
-        compute(p1, it + 1, x1);
+        if (MULTI && told) {
+#pragma unroll
+            for (int k = 0; k < NB; ++k)
+                if (first[k] < seen) o[2 * k] = o[2 * k + 1] = floatx4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+        }
+        page = next;
     }
 
     l = sum_over_hi(l);
@@ -518,7 +526,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
     for (int ct = 0; ct < CT; ++ct) {
         const int r = row_index(ct), token = r / group;
         seen[ct] = before + token + 1;
-        take_queries<D>(a.q + ((size_t)(rq.first + token) * a.Hq + (size_t)g * group + r % group) * D, hi, a.scale2, queries[ct]);
+        take_queries<D>(ask_queries<D>(a.q + ((size_t)(rq.first + token) * a.Hq + (size_t)g * group + r % group) * D, hi), hi, a.scale2, queries[ct]);
     }
     const int wave_all = before + (w0 < all_rows ? w0 : all_rows - 1) / group + 1;
     const int wave_last = w0 + 16 * CT - 1 < all_rows ? w0 + 16 * CT - 1 : all_rows - 1;
