@@ -17,18 +17,28 @@ int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 
 }  // namespace
 
-// Few rows: 16 of a cache head at a time, the requests cut so that the chip is full: three workgroups for each of the two places per compute unit.
+// Few rows of a cache head: 16 at a time, the requests cut until there are three workgroups for every compute unit (so many fit), but not below 8 pages a chunk, two
+// for each wave, and not at all up to 16 pages: a chunk more costs its start, its merge, and the second launch.  Measured with 1 / 2 / 3 / 4 chunks: 32 x 32 items of
+// up to 32 pages 39.4 / 42.9 / 46.0 / 48.8 us, 64 x 8 of 16 pages 15.8 / 29.1 / 30.1 / 31.4; with 8 / 16 / 24 / 32: 6 x 8 items of up to 126 pages 19.1 / 18.7 / 22.8 / 23.3,
+// 4 x 8 of 2047 87.4 / 87.3 / 89.1 / 89.5, 8 of 313 19.8 / 14.4 / 13.4 / 12.6 (48: 14.7); 2 x 8 of 15 pages with one chunk 6.9, with two 9.3.
+// Many rows: whole requests where the row tiles fill the chip, else chunks of 16 pages or more.
 void thi::kv4_plan(Kv4AttnArgs& a, int num_cus)
 {
     const int group = a.Hq / a.Hkv;
     a.tiles = (int)(((long)a.max_q * group + 15) / 16);
     a.split_rows = (long)a.max_q * group <= 64;
-    const long items = (long)a.B * a.Hkv * (a.split_rows ? a.tiles : (a.tiles + 15) / 16);
-    long n = ((a.split_rows ? 6L : 2L) * num_cus + items - 1) / items;
-    n = n > KV4_MAX_SPLIT ? KV4_MAX_SPLIT : n;
-    a.min_chunk = a.split_rows ? 4 : 16;
-    if (!a.split_rows && items >= num_cus) n = 1;
+    long n;
+    if (a.split_rows) {
+        const long items = (long)a.B * a.Hkv * a.tiles;
+        a.min_chunk = 8;
+        n = a.max_pages <= 16 ? 1 : 3L * num_cus / items;
+    } else {
+        const long items = (long)a.B * a.Hkv * ((a.tiles + 15) / 16);
+        a.min_chunk = 16;
+        n = items >= num_cus ? 1 : 2L * num_cus / items;
+    }
     const long most = (a.max_pages + a.min_chunk - 1) / a.min_chunk;
+    n = n < 1 ? 1 : n > KV4_MAX_SPLIT ? KV4_MAX_SPLIT : n;
     a.nsplit = (int)(n > most ? most : n);
 }
 

@@ -40,8 +40,8 @@ __device__ __forceinline__ Request find_request(const Kv4AttnArgs& a, int b)
 //   O^T = V^T P^T : a lane has the weights of positions 16 i + 4 hi + r of its row, which is the B operand of the next product as
 //               it stands if the product's inner index runs over the positions in that order; the page holds the values so that a
 //               lane's 16 bytes are these positions of two neighbouring columns (even and odd columns are tiles of their own).
-// So nothing but the rows' maxima crosses lanes.  Weights are multiplied as two fp16 summands of 2^15 p (2^-22 of a weight off at most down to 2^-17, where
-// one alone is off by 2^-11 and as much as the result's own rounding).
+// So nothing but the rows' maxima crosses lanes, and those only when a weight leaves fp16's range.  Weights are multiplied as two fp16 summands (2^-21 of a weight
+// off at most down to 2^-12 of the largest, 2^-33 of that below, where one alone is off by 2^-11 and as much as the result's own rounding).
 typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
 template <int D> struct PageRegs {
     uintx4 k[4];
@@ -50,7 +50,7 @@ template <int D> struct PageRegs {
 };
 
 constexpr int KD_THREADS = 256, KD_WAVES = 4;
-constexpr float KD_WEIGHT_LOG2 = 15.0f;          // weights are held as 2^15 p
+constexpr float WEIGHT_LOG2 = 9.0f;              // weights are held as 2^9 p of a maximum that may lag by 2^6 (fp16 ends at 2^16)
 
 // byte i of w as the exponent of a float; the conversions take nothing else of it
 __device__ __forceinline__ float scale_of(unsigned w, int i)
@@ -173,12 +173,13 @@ __device__ __forceinline__ float max_over_hi(float x)
     auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
     return __builtin_fmaxf(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
 }
-__device__ __forceinline__ float sum_over_hi(float x)
+// The uniform part of an address, which stays in scalar registers this way.
+#define GLOBAL __attribute__((address_space(1)))
+__device__ __forceinline__ const GLOBAL unsigned char* uniform(const unsigned char* p)
 {
-    auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-    x = __builtin_bit_cast(float, (unsigned)a[0]) + __builtin_bit_cast(float, (unsigned)a[1]);
-    auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-    return __builtin_bit_cast(float, (unsigned)b[0]) + __builtin_bit_cast(float, (unsigned)b[1]);
+    unsigned long long u = reinterpret_cast<unsigned long long>(p);
+    asm volatile("" : "+s"(u));
+    return reinterpret_cast<const GLOBAL unsigned char*>(u);
 }
 
 // Pages per chunk of a request with `pages` of them: a function of its own length and of how many workgroups the call has, so that a
@@ -189,13 +190,15 @@ __device__ __forceinline__ int chunk_pages(const Kv4AttnArgs& a, int pages)
     return size > a.min_chunk ? size : a.min_chunk;
 }
 
-// Two fp16 summands of four weights.
+// Two fp16 summands of four weights (the large one truncated, so that the small one is not negative).
 __device__ __forceinline__ void split_weights(const float (&w)[4], half4& large, half4& small)
 {
     const half2v h0 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[0], w[1])), h1 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[2], w[3]));
     large = half4{h0[0], h0[1], h1[0], h1[1]};
-    const half2v s0 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[0] - (float)h0[0], w[1] - (float)h0[1]));
-    const half2v s1 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[2] - (float)h1[0], w[3] - (float)h1[1]));
+    const half2v first = {(_Float16)-1.0f, (_Float16)0.0f}, second = {(_Float16)0.0f, (_Float16)-1.0f};
+    const float r[4] = {__builtin_amdgcn_fdot2(h0, first, w[0], false), __builtin_amdgcn_fdot2(h0, second, w[1], false), __builtin_amdgcn_fdot2(h1, first, w[2], false),
+                        __builtin_amdgcn_fdot2(h1, second, w[3], false)};      // w - large, without conversions
+    const half2v s0 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(r[0], r[1])), s1 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(r[2], r[3]));
     small = half4{s0[0], s0[1], s1[0], s1[1]};
 }
 
@@ -246,18 +249,17 @@ __global__ __launch_bounds__(KD_THREADS, MULTI ? 2 : 3) void kv4_attn_decode(Kv4
     const unsigned char* const heads = a.pages + (size_t)g * kv4_head_bytes(D);
     const size_t page_bytes = (size_t)a.Hkv * kv4_head_bytes(D);
     auto head = [&](int page) { return heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_bytes; };
-    auto lane_part = [](unsigned off) __attribute__((always_inline)) { asm volatile("" : "+v"(off)); return off; };
+    unsigned k_off = key_offset<D>(lo, hi), ks_off = key_scale_offset<D>(lo, hi) - kv4_key_scales(D), v_off = lane * 16, vs_off = hi * 16;
     auto ask_keys = [&](int page) __attribute__((always_inline)) {
-        const unsigned char* const from = head(page);
-        const unsigned off = lane_part(key_offset<D>(lo, hi));
+        const unsigned char* from = head(page);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + off + i * 8 * D));
-        x.ks = *reinterpret_cast<const unsigned*>(from + lane_part(key_scale_offset<D>(lo, hi)));
+        for (int i = 0; i < 4; ++i) x.k[i] = __builtin_nontemporal_load(reinterpret_cast<const GLOBAL uintx4*>(uniform(from) + k_off + i * 8 * D));
+        x.ks = *reinterpret_cast<const GLOBAL unsigned*>(uniform(from + kv4_key_scales(D)) + ks_off);
     };
     auto ask_values = [&](int page, int t) __attribute__((always_inline)) {
-        const unsigned char* const from = head(page) + kv4_values(D);
-        x.vs[t] = *reinterpret_cast<const uintx4*>(from + 32 * D + t * 64 + lane_part(hi * 16));
-        x.v[t] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + t * 1024 + lane_part(lane * 16)));
+        const unsigned char* const from = head(page);
+        x.vs[t] = *reinterpret_cast<const GLOBAL uintx4*>(uniform(from + kv4_value_scales(D) + t * 64) + vs_off);
+        x.v[t] = __builtin_nontemporal_load(reinterpret_cast<const GLOBAL uintx4*>(uniform(from + kv4_values(D) + t * 1024) + v_off));
     };
     int page = n_it > 0 ? page_at(0) : -1;
     ask_keys(page);
@@ -270,20 +272,26 @@ __global__ __launch_bounds__(KD_THREADS, MULTI ? 2 : 3) void kv4_attn_decode(Kv4
     const int seen = rq.len - rq.n + (MULTI ? (r0 + col) / group : 0) + 1;
     const int all_see = rq.len - rq.n + (MULTI ? r0 / group : 0) + 1;
 
-    float m = -__builtin_inff(), l = 0.f;
+    // m: the maximum that the row's weights refer to; start: what its scores start from (WEIGHT_LOG2 - m, so that a weight is 2^score); l: the weights'
+    // sum, as a product with ones (every element is the lane's row's)
+    float m = -__builtin_inff(), start = 0.f;
+    bool fresh = true;                           // some row has no maximum yet
+    floatx4 l = {0.f, 0.f, 0.f, 0.f};
+    const half8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
     floatx4 o[2 * NB];                           // O^T: column 32 t + 2 (4 hi + i) of the lane's row in o[2 t], its right neighbour in o[2 t + 1]
 #pragma unroll
     for (int t = 0; t < 2 * NB; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
     for (int it = 0; it < n_it; ++it) {
         const int next = it + 1 < n_it ? page_at(it + 1) : -1;
+        asm volatile("" : "+v"(k_off), "+v"(ks_off), "+v"(v_off), "+v"(vs_off));      // (not to be added to addresses in front of the loop, 64 bits wide)
         const bool there = page >= 0;
         const int base = there ? (c0 + wv + it * KD_WAVES) * KV4_PAGE : 0x7fffff00;      // (nothing of a page that is not there is seen)
         const bool masked = base + KV4_PAGE > all_see;
         floatx4 scores[1][4];
         {
-            const floatx4 zero[1] = {floatx4{0.f, 0.f, 0.f, 0.f}};
-            score_page<1>(x.k, lane_scales<D>(x.ks, hi), queries, zero, scores);
+            const floatx4 from[1] = {floatx4{start, start, start, start}};
+            score_page<1>(x.k, lane_scales<D>(x.ks, hi), queries, from, scores);
         }
         ask_keys(next);
         float t[16];
@@ -327,36 +335,50 @@ __global__ __launch_bounds__(KD_THREADS, MULTI ? 2 : 3) void kv4_attn_decode(Kv4
                 }
             }
         }
-        float mb = t[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mb = __builtin_elementwise_maximum(mb, t[i]);
-        const float mn = __builtin_fmaxf(m, max_over_hi(mb));
-        const float ms = mn == -__builtin_inff() ? 0.f : mn;
-        const float corr = __builtin_amdgcn_exp2f(m - ms);
-        float sum = 0.f;
         half8 pl[2], ps[2];
+        auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            half4 large[2], small[2];
+            for (int k = 0; k < 2; ++k) {
+                half4 large[2], small[2];
 #pragma unroll
-            for (int i2 = 0; i2 < 2; ++i2) {
-                float w[4];
+                for (int i2 = 0; i2 < 2; ++i2) {
+                    float w[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    w[r] = __builtin_amdgcn_exp2f(t[8 * k + 4 * i2 + r] - (ms - KD_WEIGHT_LOG2));
-                    sum += w[r];
+                    for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(t[8 * k + 4 * i2 + r]);
+                    split_weights(w, large[i2], small[i2]);
                 }
-                split_weights(w, large[i2], small[i2]);
+                pl[k] = join(large[0], large[1]);
+                ps[k] = join(small[0], small[1]);
             }
-            pl[k] = join(large[0], large[1]);
-            ps[k] = join(small[0], small[1]);
-        }
-        l = l * corr + sum;
-        m = mn;
-        if (__builtin_amdgcn_ballot_w64(corr != 1.0f) != 0ull) {
+        };
+        weights();
+        // Is a weight past 2^15?  Its fp16 exponent is 30 or 31 then, and 0x0800 more carries into the sign.  No maximum crosses lanes unless one is.
+        half2v top = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int r = 0; r < 8; r += 2) top = __builtin_elementwise_maximum(top, half2v{pl[k][r], pl[k][r + 1]});
+        if (fresh || __builtin_amdgcn_ballot_w64(((__builtin_bit_cast(unsigned, top) + 0x08000800u) & 0x80008000u) != 0) != 0ull) {
+            float mb = t[0];                         // (a NaN comes through; its row is not a number anyway)
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mb = __builtin_elementwise_maximum(mb, t[i]);
+            const float mn = __builtin_elementwise_maximum(m, max_over_hi(mb) - start);
+            const bool none = mn == -__builtin_inff();
+            const float corr = __builtin_amdgcn_exp2f(m - (none ? 0.f : mn)), now = none ? 0.f : WEIGHT_LOG2 - mn;
+            fresh = __builtin_amdgcn_ballot_w64(none) != 0ull;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) t[i] += now - start;
+            m = mn;
+            start = now;
+            l *= corr;
 #pragma unroll
             for (int k = 0; k < 2 * NB; ++k) o[k] *= corr;
+            weights();
         }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) l = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl[k], l, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) l = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ps[k], l, 0, 0, 0);
 #pragma unroll
         for (int b4 = 0; b4 < NB; ++b4) {
             half8 ev[2], od[2];
@@ -395,7 +417,6 @@ __global__ __launch_bounds__(KD_THREADS, MULTI ? 2 : 3) void kv4_attn_decode(Kv4
         page = next;
     }
 
-    l = sum_over_hi(l);
 #pragma unroll
     for (int t = 0; t < NB; ++t)
 #pragma unroll
@@ -403,7 +424,7 @@ __global__ __launch_bounds__(KD_THREADS, MULTI ? 2 : 3) void kv4_attn_decode(Kv4
             s_o[wv][lo][32 * t + 8 * hi + 2 * i] = o[2 * t][i];
             s_o[wv][lo][32 * t + 8 * hi + 2 * i + 1] = o[2 * t + 1][i];
         }
-    if (hi == 0) { s_m[wv][lo] = m; s_l[wv][lo] = l; }
+    if (hi == 0) { s_m[wv][lo] = m; s_l[wv][lo] = l[0]; }
     __syncthreads();
     for (int idx = tid; idx < rows * D; idx += KD_THREADS) {
         const int c = idx / D, d = idx % D;
@@ -428,11 +449,15 @@ __global__ __launch_bounds__(KD_THREADS, MULTI ? 2 : 3) void kv4_attn_decode(Kv4
     }
 }
 
-// The chunks' (sum, maximum, weight) triples of a row, in chunk order.
+// The chunks' (sum, maximum, weight) triples of a row.  Groups of D threads take every KC_GROUPS-th chunk each, eight loads in flight, and meet in LDS:
+// a fixed order.  (One thread per column over all chunks: 14.6 us with 48 of them, 256 rows.)
+constexpr int KC_THREADS = 512;
 template <int D>
-__global__ __launch_bounds__(D) void kv4_attn_combine(Kv4AttnArgs a)
+__global__ __launch_bounds__(KC_THREADS) void kv4_attn_combine(Kv4AttnArgs a)
 {
-    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, d = threadIdx.x, lane = threadIdx.x & 63;
+    constexpr int GROUPS = KC_THREADS / D;
+    __shared__ float s_o[GROUPS][D], s_w[KV4_MAX_SPLIT];
+    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, d = threadIdx.x % D, grp = threadIdx.x / D;
     const Request rq = find_request(a, b);
     if (i >= rq.n) return;
     const int pages = (rq.len + KV4_PAGE - 1) / KV4_PAGE, size = chunk_pages(a, pages);
@@ -440,18 +465,37 @@ __global__ __launch_bounds__(D) void kv4_attn_combine(Kv4AttnArgs a)
     const int live = (pages + size - 1) / size;
     const size_t row = (size_t)(rq.first + i) * a.Hq + h;
     const float* const first = a.part + row * a.nsplit * (D + 2);
-    const float mine = lane < live ? first[(size_t)lane * (D + 2) + D] : -__builtin_inff();
-    float top = mine;
+    const float m = lane < live ? first[(size_t)lane * (D + 2) + D] : -__builtin_inff();
+    const float w = lane < live ? first[(size_t)lane * (D + 2) + D + 1] : 0.f;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = grp + k * GROUPS < live ? first[(size_t)(grp + k * GROUPS) * (D + 2) + d] : 0.f;
+    float top = m;
 #pragma unroll
     for (int sh = 1; sh < 64; sh <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, sh));
-    const float ms = top == -__builtin_inff() ? 0.f : top;
-    float l = 0.f, o = 0.f;
-    for (int s = 0; s < live; ++s) {
-        const float c = __builtin_amdgcn_exp2f(first[(size_t)s * (D + 2) + D] - ms);
-        l += first[(size_t)s * (D + 2) + D + 1] * c;
-        o += first[(size_t)s * (D + 2) + d] * c;
+    const float c = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.f : top));
+    float l = w * c;
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) l += __shfl_xor(l, sh);
+    if (threadIdx.x < 64) s_w[lane] = c;
+    __syncthreads();
+    float o = 0.f;
+    for (int k0 = 0;;) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (grp + (k0 + k) * GROUPS < live) o += v[k] * s_w[grp + (k0 + k) * GROUPS];
+        k0 += 8;
+        if (k0 * GROUPS >= live) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = grp + (k0 + k) * GROUPS < live ? first[(size_t)(grp + (k0 + k) * GROUPS) * (D + 2) + d] : 0.f;
     }
-    a.out[row * D + d] = l == 0.f ? 0 : to_half_bits(o / l);
+    s_o[grp][d] = o;
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    float sum = s_o[0][d];
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) sum += s_o[k][d];
+    a.out[row * D + d] = l == 0.f ? 0 : to_half_bits(sum / l);
 }
 
 template <int D>
@@ -460,7 +504,7 @@ hipError_t launch_decode(const Kv4AttnArgs& a, hipStream_t stream)
     const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.B, (unsigned)a.nsplit);
     if (a.max_q > 1) hipLaunchKernelGGL((kv4_attn_decode<D, true>), grid, dim3(KD_THREADS), 0, stream, a);
     else hipLaunchKernelGGL((kv4_attn_decode<D, false>), grid, dim3(KD_THREADS), 0, stream, a);
-    if (a.nsplit > 1) hipLaunchKernelGGL((kv4_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(D), 0, stream, a);
+    if (a.nsplit > 1) hipLaunchKernelGGL((kv4_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -479,7 +523,6 @@ hipError_t launch_decode(const Kv4AttnArgs& a, hipStream_t stream)
 // waves wait for the one: with 2^11 and a lag of 2^4 that was most iterations.
 constexpr int KP_WAVES = 8, KP_AHEAD = 2;
 template <int D> constexpr int KP_BUF = 4096 + 256 + 128 * D;      // a page in LDS: key codes, key scales, values in fp16
-constexpr float KP_WEIGHT_LOG2 = 9.0f;          // 2^15 less KP_WEIGHT_LOG2: what a maximum may lag by
 
 __device__ __forceinline__ void lds_barrier()
 {
@@ -532,7 +575,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
     const int wave_last = w0 + 16 * CT - 1 < all_rows ? w0 + 16 * CT - 1 : all_rows - 1;
     const int wave_sees = w0 < all_rows ? before + wave_last / group + 1 : -0x7fffffff;      // (no rows: nothing)
 
-    // m: the maximum that a row's weights refer to; from: what its scores start from (KP_WEIGHT_LOG2 - m, so that a weight is 2^score); l: the
+    // m: the maximum that a row's weights refer to; from: what its scores start from (WEIGHT_LOG2 - m, so that a weight is 2^score); l: the
     // weights' sums, as a product with ones (every element is the lane's row's)
     float m[CT];
     floatx4 from[CT], l[CT], o[CT][2 * NB];
@@ -727,7 +770,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
             for (int i = 1; i < 16; ++i) mb = __builtin_elementwise_maximum(mb, acc[ct][i >> 2][i & 3]);
             const float mn = __builtin_elementwise_maximum(m[ct], max_over_hi(mb) - from[ct][0]);
             const bool none = mn == -__builtin_inff();
-            const float corr = __builtin_amdgcn_exp2f(m[ct] - (none ? 0.f : mn)), start = none ? 0.f : KP_WEIGHT_LOG2 - mn, more = start - from[ct][0];
+            const float corr = __builtin_amdgcn_exp2f(m[ct] - (none ? 0.f : mn)), start = none ? 0.f : WEIGHT_LOG2 - mn, more = start - from[ct][0];
             fresh = fresh || __builtin_amdgcn_ballot_w64(none) != 0ull;
             m[ct] = mn;
             from[ct] = floatx4{start, start, start, start};
@@ -864,7 +907,7 @@ hipError_t launch_prompt(const Kv4AttnArgs& a, hipStream_t stream)
     const long rows = (long)a.max_q * (a.Hq / a.Hkv), per = KP_WAVES * 16 * CT;
     const dim3 grid((unsigned)((rows + per - 1) / per * a.Hkv), (unsigned)a.B, (unsigned)a.nsplit);
     hipLaunchKernelGGL((kv4_attn_prompt<D, CT>), grid, dim3(64 * KP_WAVES), LDS, stream, a);
-    if (a.nsplit > 1) hipLaunchKernelGGL((kv4_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(D), 0, stream, a);
+    if (a.nsplit > 1) hipLaunchKernelGGL((kv4_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
