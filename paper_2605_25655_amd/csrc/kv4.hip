@@ -13,16 +13,32 @@ constexpr int KV4_THREADS = 256;
 constexpr int LANE_VALUES = 8;       // a lane's share of a head: 16 bytes
 
 // x rounded to 32 bits so that no border between codes or scales is met that x itself is not on: towards zero, the last bit set if
-// anything was dropped (|x| past the range: the largest finite value; not finite: not finite).
+// anything was dropped (past the range: the largest finite value; not finite: not finite).
 __device__ __forceinline__ float to_float_sticky(double x)
 {
-    const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
-    const unsigned hi = (unsigned)(b >> 32), lo = (unsigned)b, power = (hi >> 20) & 0x7ff;
-    unsigned f = ((hi & 0x7fffffffu) << 3 | lo >> 29) - (896u << 23);
-    f |= (lo & 0x1fffffffu) != 0 ? 1u : 0u;
-    if (power < 897) f = 0;
-    if (power > 1150) f = power == 2047 ? 0x7fc00000u : 0x7f7fffffu;
-    return __builtin_bit_cast(float, f | (hi & 0x80000000u));
+    const float f = (float)x;
+    const double back = (double)f;
+    unsigned b = __builtin_bit_cast(unsigned, f);
+    b -= __builtin_fabs(back) > __builtin_fabs(x) ? 1u : 0u;
+    b |= back != x ? 1u : 0u;
+    return __builtin_bit_cast(float, b);
+}
+
+// Rounded by way of 32 bits, by the conversion instructions: left to itself the compiler makes one conversion of the two, some 40 instructions a value.
+__device__ __forceinline__ _Float16 to_half(double x)
+{
+    float f = (float)x;
+    asm("" : "+v"(f));
+    return (_Float16)f;
+}
+
+// 1 / sqrt(x): the instruction's estimate and two steps of Newton's method (each squares the error: 2^-52 and better).
+__device__ __forceinline__ double inverse_sqrt(double x)
+{
+    double r = __builtin_amdgcn_rsq(x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = __builtin_fma(0.5 * r, __builtin_fma(-x * r, r, 1.0), r);
+    return r;
 }
 
 // The scale byte of a block whose largest magnitude has these bits: the smallest exponent e with max <= 7 2^e (7 is where the rounding to 6 would turn
@@ -60,79 +76,182 @@ __device__ __forceinline__ unsigned quantise(const float (&y)[LANE_VALUES], unsi
     return c;
 }
 
-template <int D>
+// Sine and cosine of x, to within 2^-52: x less the nearest multiple k of pi/2 (in two summands of 53 bits, each product fused), then the Taylor series up to
+// r^15 and r^16 (|r| <= pi/4: what is left out is below 5e-17).  Beyond 2^30, where k pi/2 would need more, the library's.
+__device__ __forceinline__ void sine_cosine(double x, double& sn, double& cs)
+{
+    if (!(__builtin_fabs(x) < 1073741824.0)) {
+        sincos(x, &sn, &cs);
+        return;
+    }
+    const double k = __builtin_rint(x * 0.63661977236758134308);
+    const double r = __builtin_fma(-k, 6.123233995736766036e-17, __builtin_fma(-k, 1.5707963267948965580, x)), z = r * r;
+    double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+    s = __builtin_fma(s, z, 1.0 / 6227020800.0);
+    s = __builtin_fma(s, z, -1.0 / 39916800.0);
+    s = __builtin_fma(s, z, 1.0 / 362880.0);
+    s = __builtin_fma(s, z, -1.0 / 5040.0);
+    s = __builtin_fma(s, z, 1.0 / 120.0);
+    s = __builtin_fma(s, z, -1.0 / 6.0);
+    s = __builtin_fma(s * z, r, r);
+    c = __builtin_fma(c, z, -1.0 / 87178291200.0);
+    c = __builtin_fma(c, z, 1.0 / 479001600.0);
+    c = __builtin_fma(c, z, -1.0 / 3628800.0);
+    c = __builtin_fma(c, z, 1.0 / 40320.0);
+    c = __builtin_fma(c, z, -1.0 / 720.0);
+    c = __builtin_fma(c, z, 1.0 / 24.0);
+    c = __builtin_fma(c, z, -0.5);
+    c = __builtin_fma(c, z, 1.0);
+    const int q = (int)k & 3;
+    const double u = q & 1 ? c : s, v = q & 1 ? s : c;
+    sn = q & 2 ? -u : u;
+    cs = (q + 1) & 2 ? -v : v;
+}
+
+// A workgroup takes TT tokens (1 or ROWS) and, of the heads, every (gridDim.y * ROWS / TT)-th group of ROWS / TT; a row of LPH lanes one head of one token at a time,
+// eight neighbouring values a lane, whose four angles it makes once.
+//
+// The values' codes lie in the page so that four neighbouring positions' bytes of a pair of columns are a dword (kv4.h); stored by
+// themselves, 4001 tokens of 40 heads made 10 million byte stores, and the call took 83 us.  With ROWS tokens a workgroup collects them in LDS
+// and stores dwords where a run of slots allows it.
+template <int D, int TT>
 __global__ __launch_bounds__(KV4_THREADS) void kv4_append(Kv4AppendArgs a)
 {
-    constexpr int LPH = D / LANE_VALUES, HEADS = KV4_THREADS / LPH;
-    __shared__ double s_turn[D / 2][2];
-    const int t = blockIdx.x, tid = threadIdx.x;
-    if (a.theta) {
-        if (tid < D / 2) {
-            double sn, cs;
-            sincos((double)a.positions[t] * (double)a.theta[tid], &sn, &cs);
-            s_turn[tid][0] = cs;
-            s_turn[tid][1] = sn;
-        }
-        __syncthreads();
-    }
-    const int part = tid % LPH;
-    const long slot = a.slots[t];
-    const bool stored = slot >= 0 && slot < (long)a.num_pages * KV4_PAGE;
+    constexpr int LPH = D / LANE_VALUES, ROWS = KV4_THREADS / LPH, HH = ROWS / TT;
+    __shared__ unsigned s_code[TT > 1 ? TT : 1][LPH];
+    __shared__ unsigned char s_byte[TT > 1 ? TT : 1][D / 32];
+    __shared__ long s_slot[TT];
+    const int tid = threadIdx.x, part = tid % LPH, row = tid / LPH, tt = row / HH;
+    const int t = blockIdx.x * TT + tt;
+    const bool token = t < a.T;
+    const long limit = (long)a.num_pages * KV4_PAGE;
+    const long slot = token ? a.slots[t] : -1;
+    const bool stored = slot >= 0 && slot < limit;
     const int pos = (int)(slot & (KV4_PAGE - 1));
-    const int H = a.Hq + 2 * a.Hkv;
-    for (int h = blockIdx.y * HEADS + tid / LPH; h < H; h += gridDim.y * HEADS) {
-        const uintx4 raw = *reinterpret_cast<const uintx4*>(a.qkv + (size_t)t * a.ld + (size_t)h * D + part * LANE_VALUES);
-        const half8 x = __builtin_bit_cast(half8, raw);
-        unsigned byte;
-        if (h >= a.Hq + a.Hkv) {                   // a value: stored as it is
-            float y[LANE_VALUES];
+    if (TT > 1 && part == 0) s_slot[tt] = stored ? slot : -1;
+    // the rows of the heads in front, two steps ahead of the arithmetic (without: 83 us for 4001 tokens of 120 heads)
+    const int H = a.Hq + 2 * a.Hkv, step = gridDim.y * HH;
+    const uint16_t* const from = a.qkv + (size_t)(token ? t : 0) * a.ld + part * LANE_VALUES;
+    auto ask = [&](int h0) {
+        const int h = h0 + row % HH;
+        return __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + (size_t)(h < H ? h : 0) * D));
+    };
+    uintx4 next = ask(blockIdx.y * HH), after = ask(blockIdx.y * HH + step);
+    double cs[LANE_VALUES / 2], sn[LANE_VALUES / 2];
+    if (a.theta) {
+        const double at = token ? (double)a.positions[t] : 0.0;
+        if (TT == 1) {                            // one token's angles, each once
+            __shared__ double s_turn[D / 2][2];
+            if (tid < D / 2) sine_cosine(at * (double)a.theta[tid], s_turn[tid][0], s_turn[tid][1]);
+            __syncthreads();
 #pragma unroll
-            for (int e = 0; e < LANE_VALUES; ++e) y[e] = (float)x[e];
-            const unsigned c = quantise(y, byte);
-            if (stored) {
-                unsigned char* const base = a.pages + ((size_t)(slot >> 6) * a.Hkv + (h - a.Hq - a.Hkv)) * kv4_head_bytes(D);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) base[kv4_values(D) + kv4_value_at(pos, part * 4 + e)] = (unsigned char)(c >> (8 * e));
-                if (part % 4 == 0) base[kv4_value_scales(D) + kv4_value_scale_at(pos, part / 4)] = (unsigned char)byte;
+            for (int e = 0; e < LANE_VALUES / 2; ++e) {
+                sn[e] = s_turn[part * 4 + e][0];
+                cs[e] = s_turn[part * 4 + e][1];
             }
-            continue;
+        } else {
+#pragma unroll
+            for (int e = 0; e < LANE_VALUES / 2; ++e) sine_cosine(at * (double)a.theta[part * 4 + e], sn[e], cs[e]);
         }
-        double y[LANE_VALUES];
-#pragma unroll
-        for (int e = 0; e < LANE_VALUES; ++e) y[e] = (double)(float)x[e];
-        const uint16_t* const gamma = h < a.Hq ? a.q_gamma : a.k_gamma;
-        if (gamma) {
-            double ss = 0.0;
-#pragma unroll
-            for (int e = 0; e < LANE_VALUES; ++e) ss += y[e] * y[e];
-#pragma unroll
-            for (int sh = 1; sh < LPH; sh <<= 1) ss += __shfl_xor(ss, sh);
-            const double r = 1.0 / sqrt(ss / D + (double)a.eps);
-            const half8 gm = __builtin_bit_cast(half8, *reinterpret_cast<const uintx4*>(gamma + part * LANE_VALUES));
-#pragma unroll
-            for (int e = 0; e < LANE_VALUES; ++e) y[e] *= r * (double)(float)gm[e];
-        }
-        if (a.theta) {
-#pragma unroll
-            for (int e = 0; e < LANE_VALUES; e += 2) {
-                const double cs = s_turn[part * 4 + e / 2][0], sn = s_turn[part * 4 + e / 2][1], u = y[e], v = y[e + 1];
-                y[e] = u * cs - v * sn;
-                y[e + 1] = v * cs + u * sn;
-            }
-        }
-        if (h < a.Hq) {
-            half8 o;
-#pragma unroll
-            for (int e = 0; e < LANE_VALUES; ++e) o[e] = (_Float16)(float)y[e];
-            *reinterpret_cast<uintx4*>(a.q_out + ((size_t)t * a.Hq + h) * D + part * LANE_VALUES) = __builtin_bit_cast(uintx4, o);
-            continue;
-        }
+    }
+    // TT > 1: this thread's four tokens when values are stored: a group that begins where a dword of the page does, counted round the TT tokens
+    int lead = 0, pair_of_part = 0;
+    bool run = false;
+    if (TT > 1) {
+        __syncthreads();
+        const int ahead = (int)(-s_slot[0] & 3);
+        lead = (ahead + (tid / LPH) % (TT / 4) * 4) % TT;
+        pair_of_part = tid / (LPH * (TT / 4));
+        const long s0 = s_slot[lead];
+        run = s0 >= 0 && (s0 & 3) == 0 && lead + 3 < TT;
+        for (int k = 1; k < 4 && run; ++k) run = s_slot[lead + k] == s0 + k;
+    }
+    for (int h0 = blockIdx.y * HH; h0 < H; h0 += step) {
+        const int h = h0 + row % HH;
+        const bool there = token && h < H;
+        const half8 x = __builtin_bit_cast(half8, next);
+        next = after;
+        after = ask(h0 + 2 * step);
         float f[LANE_VALUES];
+        if (h >= a.Hq + a.Hkv) {                   // a value: stored as it is
 #pragma unroll
-        for (int e = 0; e < LANE_VALUES; ++e) f[e] = to_float_sticky(y[e]);
+            for (int e = 0; e < LANE_VALUES; ++e) f[e] = (float)x[e];
+        } else {
+            double y[LANE_VALUES];
+#pragma unroll
+            for (int e = 0; e < LANE_VALUES; ++e) y[e] = (double)(float)x[e];
+            const uint16_t* const gamma = h < a.Hq ? a.q_gamma : a.k_gamma;
+            if (gamma) {
+                double ss = 0.0;
+#pragma unroll
+                for (int e = 0; e < LANE_VALUES; ++e) ss = __builtin_fma(y[e], y[e], ss);
+#pragma unroll
+                for (int sh = 1; sh < LPH; sh <<= 1) ss += __shfl_xor(ss, sh);
+                const double r = inverse_sqrt(ss * (1.0 / D) + (double)a.eps);
+                const half8 gm = __builtin_bit_cast(half8, *reinterpret_cast<const uintx4*>(gamma + part * LANE_VALUES));
+#pragma unroll
+                for (int e = 0; e < LANE_VALUES; ++e) y[e] *= r * (double)(float)gm[e];
+            }
+            if (a.theta) {
+#pragma unroll
+                for (int e = 0; e < LANE_VALUES; e += 2) {
+                    const double u = y[e], v = y[e + 1];
+                    y[e] = u * cs[e / 2] - v * sn[e / 2];
+                    y[e + 1] = v * cs[e / 2] + u * sn[e / 2];
+                }
+            }
+            if (h < a.Hq) {
+                half8 o;
+#pragma unroll
+                for (int e = 0; e < LANE_VALUES; ++e) o[e] = to_half(y[e]);
+                if (there) *reinterpret_cast<uintx4*>(a.q_out + ((size_t)t * a.Hq + h) * D + part * LANE_VALUES) = __builtin_bit_cast(uintx4, o);
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < LANE_VALUES; ++e) f[e] = to_float_sticky(y[e]);
+        }
+        unsigned byte;
         const unsigned c = quantise(f, byte);
-        if (stored) {
-            unsigned char* const base = a.pages + ((size_t)(slot >> 6) * a.Hkv + (h - a.Hq)) * kv4_head_bytes(D);
+        const bool value = h >= a.Hq + a.Hkv;
+        if (TT > 1 && value) {                     // (HH = 1: the same head for all rows)
+            s_code[tt][part] = c;
+            if (part % 4 == 0) s_byte[tt][part / 4] = (unsigned char)byte;
+            __syncthreads();
+            unsigned codes = 0, bytes = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                codes |= (s_code[(lead + k) % TT][part] >> (8 * pair_of_part) & 255u) << (8 * k);
+                bytes |= (unsigned)s_byte[(lead + k) % TT][part / 4] << (8 * k);
+            }
+            const int hv = h - a.Hq - a.Hkv;
+            auto head = [&](long s) { return a.pages + ((size_t)(s >> 6) * a.Hkv + hv) * kv4_head_bytes(D); };
+            const bool scales = pair_of_part == 0 && part % 4 == 0;
+            if (run) {
+                unsigned char* const base = head(s_slot[lead]);
+                const int p = (int)(s_slot[lead] & (KV4_PAGE - 1));
+                *reinterpret_cast<unsigned*>(base + kv4_values(D) + kv4_value_at(p, part * 4 + pair_of_part)) = codes;
+                if (scales) *reinterpret_cast<unsigned*>(base + kv4_value_scales(D) + kv4_value_scale_at(p, part / 4)) = bytes;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const long s = s_slot[(lead + k) % TT];
+                    if (s < 0) continue;
+                    unsigned char* const base = head(s);
+                    const int p = (int)(s & (KV4_PAGE - 1));
+                    base[kv4_values(D) + kv4_value_at(p, part * 4 + pair_of_part)] = (unsigned char)(codes >> (8 * k));
+                    if (scales) base[kv4_value_scales(D) + kv4_value_scale_at(p, part / 4)] = (unsigned char)(bytes >> (8 * k));
+                }
+            }
+            __syncthreads();                       // read before the next head's codes come
+            continue;
+        }
+        if (!there || !stored) continue;
+        unsigned char* const base = a.pages + ((size_t)(slot >> 6) * a.Hkv + (value ? h - a.Hq - a.Hkv : h - a.Hq)) * kv4_head_bytes(D);
+        if (value) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) base[kv4_values(D) + kv4_value_at(pos, part * 4 + e)] = (unsigned char)(c >> (8 * e));
+            if (part % 4 == 0) base[kv4_value_scales(D) + kv4_value_scale_at(pos, part / 4)] = (unsigned char)byte;
+        } else {
             *reinterpret_cast<unsigned*>(base + pos * (D / 2) + part * 4) = c;
             if (part % 4 == 0) base[kv4_key_scales(D) + kv4_key_scale_at(pos, part / 4)] = (unsigned char)byte;
         }
@@ -152,52 +271,110 @@ __device__ __forceinline__ uintx4 values_of(unsigned c, unsigned byte)
     return o;
 }
 
-template <int D>
+// TT tokens (1 or 4) of a head by LPH lanes.  Four neighbouring slots' value bytes are read as the dwords that hold them (one, or two where the run does not begin with
+// one); other slots byte by byte.
+template <int D, int TT>
 __global__ __launch_bounds__(KV4_THREADS) void kv4_read(Kv4ReadArgs a)
 {
     constexpr int LPH = D / LANE_VALUES;
-    const size_t item = ((size_t)blockIdx.x * KV4_THREADS + threadIdx.x) / LPH;      // (token, head)
+    const size_t item = ((size_t)blockIdx.x * KV4_THREADS + threadIdx.x) / LPH;      // (tokens, head)
     const int part = threadIdx.x % LPH;
-    if (item >= (size_t)a.T * a.Hkv) return;
-    const int t = (int)(item / a.Hkv), h = (int)(item % a.Hkv);
-    const long slot = a.slots[t];
-    const bool stored = slot >= 0 && slot < (long)a.num_pages * KV4_PAGE;
-    const int pos = (int)(slot & (KV4_PAGE - 1));
-    const unsigned char* const base = a.pages + ((size_t)(stored ? slot >> 6 : 0) * a.Hkv + h) * kv4_head_bytes(D);
+    const int t0 = (int)(item / a.Hkv) * TT, h = (int)(item % a.Hkv);
+    if (t0 >= a.T) return;
+    const long limit = (long)a.num_pages * KV4_PAGE;
+    long slot[TT];
+#pragma unroll
+    for (int k = 0; k < TT; ++k) {
+        slot[k] = t0 + k < a.T ? a.slots[t0 + k] : -1;
+        if (slot[k] >= limit) slot[k] = -1;
+    }
+    auto head = [&](long s) { return a.pages + ((size_t)(s >> 6) * a.Hkv + h) * kv4_head_bytes(D); };
+    auto out = [&](uint16_t* to, int k) { return reinterpret_cast<uintx4*>(to + ((size_t)(t0 + k) * a.Hkv + h) * D + part * LANE_VALUES); };
     const uintx4 none = {0u, 0u, 0u, 0u};
     if (a.k_out) {
-        const unsigned c = *reinterpret_cast<const unsigned*>(base + pos * (D / 2) + part * 4);
-        const uintx4 o = values_of(c, base[kv4_key_scales(D) + kv4_key_scale_at(pos, part / 4)]);
-        *reinterpret_cast<uintx4*>(a.k_out + item * D + part * LANE_VALUES) = stored ? o : none;
-    }
-    if (a.v_out) {
-        unsigned c = 0;
+        unsigned c[TT], e[TT];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c |= (unsigned)base[kv4_values(D) + kv4_value_at(pos, part * 4 + e)] << (8 * e);
-        const uintx4 o = values_of(c, base[kv4_value_scales(D) + kv4_value_scale_at(pos, part / 4)]);
-        *reinterpret_cast<uintx4*>(a.v_out + item * D + part * LANE_VALUES) = stored ? o : none;
+        for (int k = 0; k < TT; ++k) {
+            const long s = slot[k] < 0 ? 0 : slot[k];
+            const int pos = (int)(s & (KV4_PAGE - 1));
+            c[k] = *reinterpret_cast<const unsigned*>(head(s) + pos * (D / 2) + part * 4);
+            e[k] = head(s)[kv4_key_scales(D) + kv4_key_scale_at(pos, part / 4)];
+        }
+#pragma unroll
+        for (int k = 0; k < TT; ++k)
+            if (t0 + k < a.T) *out(a.k_out, k) = slot[k] < 0 ? none : values_of(c[k], e[k]);
+    }
+    if (!a.v_out) return;
+    // a token's four pairs and scale are bytes k of c[0 .. 3] and of e
+    unsigned c[4] = {0, 0, 0, 0}, e = 0;
+    bool run = TT == 4 && slot[0] >= 0;
+#pragma unroll
+    for (int k = 1; k < TT; ++k) run = run && slot[k] == slot[0] + k;
+    if (run) {
+        const long s0 = slot[0] & ~3l, s1 = (slot[0] + 3) & ~3l;
+        const unsigned char *b0 = head(s0) + kv4_values(D), *b1 = head(s1) + kv4_values(D);
+        const int p0 = (int)(s0 & (KV4_PAGE - 1)), p1 = (int)(s1 & (KV4_PAGE - 1));
+        const unsigned shift = (unsigned)(slot[0] & 3);
+        auto both = [&](int at0, int at1) { return __builtin_amdgcn_alignbyte(*reinterpret_cast<const unsigned*>(b1 + at1), *reinterpret_cast<const unsigned*>(b0 + at0), shift); };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = both(kv4_value_at(p0, part * 4 + i), kv4_value_at(p1, part * 4 + i));
+        e = both(32 * D + kv4_value_scale_at(p0, part / 4), 32 * D + kv4_value_scale_at(p1, part / 4));
+    } else {
+#pragma unroll
+        for (int k = 0; k < TT; ++k) {
+            const long s = slot[k] < 0 ? 0 : slot[k];
+            const int pos = (int)(s & (KV4_PAGE - 1));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] |= (unsigned)head(s)[kv4_values(D) + kv4_value_at(pos, part * 4 + i)] << (8 * k);
+            e |= (unsigned)head(s)[kv4_value_scales(D) + kv4_value_scale_at(pos, part / 4)] << (8 * k);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < TT; ++k) {
+        unsigned codes = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes |= (c[i] >> (8 * k) & 255u) << (8 * i);
+        if (t0 + k < a.T) *out(a.v_out, k) = slot[k] < 0 ? none : values_of(codes, e >> (8 * k) & 255u);
     }
 }
 
 }  // namespace
 
+template <int D>
+static void append(const Kv4AppendArgs& a, int num_cus, hipStream_t stream)
+{
+    constexpr int ROWS = KV4_THREADS / (D / LANE_VALUES);
+    const int H = a.Hq + 2 * a.Hkv;
+    if (a.T <= 4 * ROWS) {                        // few tokens, seldom neighbours in a page: the heads of one token in a workgroup, or several
+        hipLaunchKernelGGL((kv4_append<D, 1>), dim3((unsigned)a.T, (unsigned)((H + ROWS - 1) / ROWS)), dim3(KV4_THREADS), 0, stream, a);
+        return;
+    }
+    // one round of four workgroups a compute unit, while a workgroup has eight heads or more (its angles cost it as much as some heads)
+    const int windows = (a.T + ROWS - 1) / ROWS;
+    int split = windows > 4 * num_cus ? 1 : 4 * num_cus / windows;
+    split = split > (H + 7) / 8 ? (H + 7) / 8 : split;
+    hipLaunchKernelGGL((kv4_append<D, ROWS>), dim3((unsigned)windows, (unsigned)split), dim3(KV4_THREADS), 0, stream, a);
+}
+
 hipError_t launch_kv4_append(const Kv4AppendArgs& a, int num_cus, hipStream_t stream)
 {
-    const int heads = KV4_THREADS / (a.D / LANE_VALUES), groups = (a.Hq + 2 * a.Hkv + heads - 1) / heads;
-    // few tokens: the heads of a token in workgroups of their own; many: one workgroup a token, which makes the rotation's angles once
-    const int split = a.T >= 4 * num_cus ? 1 : groups;
-    const dim3 grid((unsigned)a.T, (unsigned)split);
-    if (a.D == 128) hipLaunchKernelGGL((kv4_append<128>), grid, dim3(KV4_THREADS), 0, stream, a);
-    else hipLaunchKernelGGL((kv4_append<64>), grid, dim3(KV4_THREADS), 0, stream, a);
+    if (a.D == 128) append<128>(a, num_cus, stream);
+    else append<64>(a, num_cus, stream);
     return hipGetLastError();
+}
+
+template <int D, int TT>
+static void read(const Kv4ReadArgs& a, hipStream_t stream)
+{
+    const size_t items = (size_t)((a.T + TT - 1) / TT) * a.Hkv, per = KV4_THREADS / (D / LANE_VALUES);
+    hipLaunchKernelGGL((kv4_read<D, TT>), dim3((unsigned)((items + per - 1) / per)), dim3(KV4_THREADS), 0, stream, a);
 }
 
 hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t stream)
 {
-    const size_t items = (size_t)a.T * a.Hkv, per = KV4_THREADS / (a.D / LANE_VALUES);
-    const dim3 grid((unsigned)((items + per - 1) / per));
-    if (a.D == 128) hipLaunchKernelGGL((kv4_read<128>), grid, dim3(KV4_THREADS), 0, stream, a);
-    else hipLaunchKernelGGL((kv4_read<64>), grid, dim3(KV4_THREADS), 0, stream, a);
+    const bool few = a.T <= 64;                   // seldom neighbours, and too few to give a thread four
+    if (a.D == 128) few ? read<128, 1>(a, stream) : read<128, 4>(a, stream);
+    else few ? read<64, 1>(a, stream) : read<64, 4>(a, stream);
     return hipGetLastError();
 }
 
