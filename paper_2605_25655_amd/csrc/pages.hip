@@ -3,35 +3,36 @@
 // taken in the order of their numbers, so results do not depend on the order in which workgroups run (the only atomics add
 // whole numbers).  Tables and counts are read from one set of arrays and written to another.
 //
-// Two launches each: one workgroup plans (which pages are free, which row gets which: prefix sums), then the chip writes the
-// tables and counts and copies pages.
+// Small pools and tables: one launch, in which every workgroup makes the whole plan for itself (a bit per page in LDS, prefix sums of the bits) and
+// then its share of the copies.  Large ones: one workgroup plans, a second launch writes tables and counts and copies.
 #include "kv4.h"
 
 namespace thi {
 
 namespace {
 
-constexpr int PLAN_THREADS = 1024, PLAN_PER = 8;          // counts per thread and step of the plan
+constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64, PLAN_PER = 8;          // counts per thread and step of the plan
 constexpr int APPLY_THREADS = 256;
 
 // Exclusive prefix sum over the workgroup; `total` to every thread.
-__device__ __forceinline__ int block_prefix(int v, int& total)
+template <class T>
+__device__ __forceinline__ T block_prefix(T v, T& total)
 {
-    __shared__ int s_wave[PLAN_THREADS / 64];
+    __shared__ T s_wave[PLAN_WAVES];
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    int x = v;
+    T x = v;
 #pragma unroll
     for (int sh = 1; sh < 64; sh <<= 1) {
-        const int y = __shfl_up(x, sh);
+        const T y = __shfl_up(x, sh);
         if (lane >= sh) x += y;
     }
     __syncthreads();                     // (the last call's sums have been read)
     if (lane == 63) s_wave[wv] = x;
     __syncthreads();
-    int before = 0, all = 0;
+    T before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < PLAN_THREADS / 64; ++w) {
-        const int s = s_wave[w];
+    for (int w = 0; w < PLAN_WAVES; ++w) {
+        const T s = s_wave[w];
         before += w < wv ? s : 0;
         all += s;
     }
@@ -46,24 +47,26 @@ __device__ __forceinline__ int clamp_len(const PagesArgs& a, int len)
 }
 __device__ __forceinline__ int pages_of(int len) { return (int)(((long)len + KV4_PAGE - 1) / KV4_PAGE); }
 
-// A row of the new table: its parent, positions, whole pages, pages in use, pages wanted.
+// A row of the new table: its parent, positions, whole pages, pages in use, entries that may be a page.
 struct Row {
-    int parent, len, full, used, want;
+    int parent, len, full, used, limit;
     bool first;            // the lowest row of this parent: takes over what only that parent has
 };
-__device__ __forceinline__ Row row_of(const PagesArgs& a, const int* first, int i)
+template <class First>      // the lowest row that continues a parent
+__device__ __forceinline__ Row row_of(const PagesArgs& a, int i, First first)
 {
     Row r{a.parents[i], 0, 0, 0, 0, false};
+    const int room = a.headroom ? a.headroom[i] : 0;
     if (r.parent < 0 || r.parent >= a.rows_in) r.parent = -1;
     else {
         r.len = clamp_len(a, a.lens_in[r.parent]);
-        r.first = __hip_atomic_load(first + r.parent, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i;
+        r.first = first(r.parent) == i;
     }
     r.full = r.len / KV4_PAGE;
     r.used = pages_of(r.len);
-    const int room = a.headroom ? a.headroom[i] : 0;
     const long want = ((long)r.len + (room > 0 ? room : 0) + KV4_PAGE - 1) / KV4_PAGE;
-    r.want = want < a.max_pages ? (int)want : a.max_pages;
+    const int most = want < a.max_pages ? (int)want : a.max_pages;
+    r.limit = most > r.used ? most : r.used;
     return r;
 }
 // What entry j >= full of a row becomes: the parent's page (kept), a fresh one (copied from the parent's where that is the partly filled
@@ -75,19 +78,61 @@ struct Entry {
 __device__ __forceinline__ Entry entry_of(const PagesArgs& a, const Row& r, int j)
 {
     Entry e{-1, false};
-    if (r.parent >= 0) {
+    if (j >= r.limit) return e;
+    if (r.parent >= 0 && (r.first || j < r.used)) {      // (what only the first row may take over concerns no other)
         e.src = a.table_in[(size_t)r.parent * a.max_pages + j];
         if (e.src < 0 || e.src >= a.num_pages) e.src = -1;
     }
-    if (j >= r.want && j >= r.used) { e.src = -1; return e; }
     const bool mine = e.src >= 0 && r.first && a.refs_in[e.src] == 1;
     e.fresh = !mine && (j >= r.used || e.src >= 0);
     return e;
 }
+__device__ __forceinline__ Row row_of_lane(const Row& r, int lane)
+{
+    return Row{__shfl(r.parent, lane), __shfl(r.len, lane), __shfl(r.full, lane), __shfl(r.used, lane), __shfl(r.limit, lane), __shfl((int)r.first, lane) != 0};
+}
+
+// The entries behind a row's whole pages, a row per lane: up to TAIL of them (the usual one or two) by the lane itself, all loads together; more
+// by the whole wave, 64 entries at a time.
+constexpr int TAIL = 4;
+struct Tail {
+    int src[TAIL];
+    unsigned fresh;        // bits
+};
+__device__ __forceinline__ int count_fresh(const PagesArgs& a, const Row& r, Tail& t)
+{
+    const int n = r.limit - r.full, lane = threadIdx.x & 63;
+    t.fresh = 0;
+    int count = 0;
+    if (n <= TAIL) {
+#pragma unroll
+        for (int k = 0; k < TAIL; ++k) {
+            const Entry e = entry_of(a, r, r.full + k);
+            t.src[k] = e.src;
+            t.fresh |= e.fresh ? 1u << k : 0u;
+        }
+        count = __builtin_popcount(t.fresh);
+    }
+    for (unsigned long long long_ones = __builtin_amdgcn_ballot_w64(n > TAIL); long_ones; long_ones &= long_ones - 1) {
+        const int of = __builtin_ctzll(long_ones);
+        const Row o = row_of_lane(r, of);
+        int total = 0;
+        for (int j = o.full; j < o.limit; j += 64) total += __builtin_popcountll(__builtin_amdgcn_ballot_w64(entry_of(a, o, j + lane).fresh));
+        if (lane == of) {
+            count = total;
+            t.src[0] = o.full < o.used ? a.table_in[(size_t)o.parent * a.max_pages + o.full] : -1;
+            t.fresh = o.full < o.used && entry_of(a, o, o.full).fresh ? 1u : 0u;
+        }
+    }
+    return count;
+}
+// Does the partly filled page need a copy?  (Of t.src[0], to the row's first fresh page.)
+__device__ __forceinline__ bool copies_page(const Row& r, const Tail& t) { return r.full < r.used && (t.fresh & 1u); }
 
 // workspace words: first[rows_in], rank[rows_out] (fresh pages of the rows before), free[num_pages], counts
 struct ForkWs {
     int *first, *rank, *free, *free_count;
+    __device__ __forceinline__ int operator()(int parent) const { return __hip_atomic_load(first + parent, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 };
 __device__ __forceinline__ ForkWs fork_ws(const PagesArgs& a)
 {
@@ -115,11 +160,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_plan(PagesArgs a)
     int carry = 0;
     for (int i0 = 0; i0 < a.rows_out; i0 += PLAN_THREADS) {
         const int i = i0 + tid;
-        int fresh = 0;
-        if (i < a.rows_out) {
-            const Row r = row_of(a, w.first, i);
-            for (int j = r.full; j < (r.want > r.used ? r.want : r.used); ++j) fresh += entry_of(a, r, j).fresh ? 1 : 0;
-        }
+        Row r{-1, 0, 0, 0, 0, false};
+        if (i < a.rows_out) r = row_of(a, i, w);
+        Tail t;
+        const int fresh = count_fresh(a, r, t);
         int total;
         const int before = block_prefix(fresh, total);
         if (i < a.rows_out) w.rank[i] = carry + before;
@@ -155,12 +199,20 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_plan(PagesArgs a)
     }
 }
 
-__device__ __forceinline__ void copy_page(const PagesArgs& a, int src, int dst, int layer, int part, int parts)
+// Bytes [at, end) of one layer's page src to page dst, `step` apart from one 16-byte load of a thread to its next (`at` the thread's first); eight loads in flight.
+__device__ __forceinline__ void copy_page(const PagesArgs& a, int src, int dst, int layer, size_t at, size_t end, size_t step)
 {
-    const uintx4* const from = reinterpret_cast<const uintx4*>(a.pages + layer * a.layer_bytes + (size_t)src * a.page_bytes);
-    uintx4* const to = reinterpret_cast<uintx4*>(a.pages + layer * a.layer_bytes + (size_t)dst * a.page_bytes);
-    const size_t n = a.page_bytes / 16;
-    for (size_t i = (size_t)part * APPLY_THREADS + threadIdx.x; i < n; i += (size_t)parts * APPLY_THREADS) to[i] = from[i];
+    const char* const from = a.pages + layer * a.layer_bytes + (size_t)src * a.page_bytes;
+    char* const to = a.pages + layer * a.layer_bytes + (size_t)dst * a.page_bytes;
+    for (; at < end; at += 8 * step) {
+        uintx4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (at + k * step < end) x[k] = *reinterpret_cast<const uintx4*>(from + at + k * step);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (at + k * step < end) *reinterpret_cast<uintx4*>(to + at + k * step) = x[k];
+    }
 }
 
 // Blocks (row, y): y = 0 writes a row of the new table and adds its references, y = 1 takes a row of the old table's away, y >= 2
@@ -178,12 +230,12 @@ __global__ __launch_bounds__(APPLY_THREADS) void fork_apply(PagesArgs a)
         return;
     }
     if (i >= a.rows_out) return;
-    const Row r = row_of(a, w.first, i);
+    const Row r = row_of(a, i, w);
     const int free_count = w.free_count[0], rank = w.rank[i];
     if (y >= 2) {
         if (r.full == r.used) return;
         const Entry e = entry_of(a, r, r.full);
-        if (e.fresh && rank < free_count) copy_page(a, e.src, w.free[rank], y - 2, 0, 1);
+        if (e.fresh && rank < free_count) copy_page(a, e.src, w.free[rank], y - 2, tid * 16, a.page_bytes, APPLY_THREADS * 16);
         return;
     }
     int* const out = a.table_out + (size_t)i * a.max_pages;
@@ -277,8 +329,245 @@ __global__ __launch_bounds__(APPLY_THREADS) void compact_apply(PagesArgs a)
     const long jobs = (long)w.count[1] * a.layers;
     for (long k = blockIdx.x; k < jobs; k += gridDim.x) {
         const int m = (int)(k / a.layers), layer = (int)(k % a.layers);
-        copy_page(a, w.mover[m], w.hole[m], layer, 0, 1);
+        copy_page(a, w.mover[m], w.hole[m], layer, threadIdx.x * 16, a.page_bytes, APPLY_THREADS * 16);
     }
+}
+
+// ---- one launch ---------------------------------------------------------------------------------------------------
+//
+// A bit per page of what `is` holds for, and the bits in front of each word: rank() and select() in a handful of LDS reads, so that no list is
+// written, no workspace read, and no workgroup waits for another.
+template <int WORDS> struct PageBits {
+    unsigned long long word[WORDS + 1];
+    int before[WORDS + 1];
+    __device__ __forceinline__ int rank(int p) const      // bits in front of p
+    {
+        return before[p >> 6] + __builtin_popcountll(word[p >> 6] & ((1ull << (p & 63)) - 1ull));
+    }
+    // The page of the k-th bit that is set (SET) or not; there has to be one.
+    template <bool SET> __device__ __forceinline__ int select(int k) const
+    {
+        int w = 0;
+#pragma unroll
+        for (int step = WORDS / 2; step; step >>= 1) {
+            const int front = SET ? before[w + step] : 64 * (w + step) - before[w + step];
+            if (front <= k) w += step;
+        }
+        unsigned long long m = SET ? word[w] : ~word[w];
+        int r = k - (SET ? before[w] : 64 * w - before[w]), p = 64 * w;
+#pragma unroll
+        for (int width = 32; width; width >>= 1) {
+            const int low = __builtin_popcountll(m & ((1ull << width) - 1ull));
+            if (r >= low) {
+                r -= low;
+                m >>= width;
+                p += width;
+            }
+        }
+        return p;
+    }
+};
+template <int WORDS, class Is>
+__device__ __forceinline__ void make_bits(const PagesArgs& a, PageBits<WORDS>& bits, Is is)
+{
+    static_assert((WORDS & (WORDS - 1)) == 0 && WORDS % 64 == 0, "");
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, words = (a.num_pages + 63) / 64;
+    for (int w0 = wv; w0 < WORDS; w0 += 8 * PLAN_WAVES) {
+        bool f[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int p = (w0 + k * PLAN_WAVES) * 64 + lane;
+            f[k] = p < a.num_pages && is(a.refs_in[p]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int w = w0 + k * PLAN_WAVES;
+            const unsigned long long m = __builtin_amdgcn_ballot_w64(f[k]);
+            if (lane == 0 && w < WORDS) bits.word[w] = w < words ? m : 0;
+        }
+    }
+    __syncthreads();
+    if (wv == 0) {
+        constexpr int PER = WORDS / 64;
+        int n[PER], sum = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            n[k] = __builtin_popcountll(bits.word[lane * PER + k]);
+            sum += n[k];
+        }
+        int x = sum;
+#pragma unroll
+        for (int sh = 1; sh < 64; sh <<= 1) {
+            const int y = __shfl_up(x, sh);
+            if (lane >= sh) x += y;
+        }
+        int at = x - sum;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            bits.before[lane * PER + k] = at;
+            at += n[k];
+        }
+        if (lane == 63) {
+            bits.before[WORDS] = at;
+            bits.word[WORDS] = 0;
+        }
+    }
+    __syncthreads();
+}
+
+// Copies of `jobs` pages in every layer, dealt to the waves in equal runs of SLICE bytes; places(k, src, dst) are those of the k-th.
+constexpr int SLICE = 1024;
+template <class Places>
+__device__ __forceinline__ void copy_share(const PagesArgs& a, int jobs, int block, int blocks, Places places)
+{
+    const int lane = threadIdx.x & 63;
+    const unsigned wave = (unsigned)block * PLAN_WAVES + (unsigned)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = (unsigned)blocks * PLAN_WAVES;
+    const size_t slices = (a.page_bytes + SLICE - 1) / SLICE, total = (size_t)jobs * a.layers * slices, per = total / waves, more = total % waves;
+    size_t s = wave * per + (wave < more ? wave : more);
+    const size_t s1 = s + per + (wave < more ? 1 : 0);
+    if (s >= s1) return;
+    const size_t job = s / slices;
+    size_t in = s % slices;
+    int k = (int)(job / (size_t)a.layers), layer = (int)(job % (size_t)a.layers), src, dst;
+    places(k, src, dst);
+    for (;;) {
+        const size_t n = s1 - s < slices - in ? s1 - s : slices - in, end = (in + n) * SLICE < a.page_bytes ? (in + n) * SLICE : a.page_bytes;
+        copy_page(a, src, dst, layer, in * SLICE + lane * 16, end, SLICE);
+        s += n;
+        in = 0;
+        if (s >= s1) return;
+        if (++layer == a.layers) {
+            layer = 0;
+            places(++k, src, dst);
+        }
+    }
+}
+
+constexpr int COMPACT_WORDS = 256, COMPACT_ENTRIES = 1 << 22;          // 16384 pages
+__global__ __launch_bounds__(PLAN_THREADS, 8) void compact_one(PagesArgs a)
+{
+    __shared__ PageBits<COMPACT_WORDS> live;
+    make_bits(a, live, [](int refs) { return refs > 0; });
+    const int L = live.before[COMPACT_WORDS], front = live.rank(L), moved = L - front;      // as many holes in front of L as live pages behind
+    const int tid = blockIdx.x * PLAN_THREADS + threadIdx.x, stride = gridDim.x * PLAN_THREADS;
+    auto is_live = [&](int p) { return (live.word[p >> 6] >> (p & 63) & 1ull) != 0; };
+    for (int i = tid; i < a.rows_in * a.max_pages; i += stride) {
+        const int e = a.table_in[i];
+        int to = -1;
+        if (e >= 0 && e < a.num_pages && is_live(e)) to = e < L ? e : live.select<false>(live.rank(e) - front);
+        a.table_out[i] = to;
+    }
+    for (int p = tid; p < a.num_pages; p += stride) {
+        int refs = 0;
+        if (p < L) refs = a.refs_in[is_live(p) ? p : live.select<true>(front + (p - live.rank(p)))];
+        a.refs_out[p] = refs;
+    }
+    if (tid == 0 && a.info) {
+        a.info[0] = L;
+        a.info[1] = moved;
+    }
+    copy_share(a, moved, blockIdx.x, gridDim.x, [&](int k, int& src, int& dst) {
+        src = __builtin_amdgcn_readfirstlane(live.select<true>(front + k));
+        dst = __builtin_amdgcn_readfirstlane(live.select<false>(k));
+    });
+}
+
+// The first workgroup writes tables, lengths and counts (which it sums in LDS), the others copy.
+constexpr int FORK_WORDS = 128, FORK_PAGES = FORK_WORDS * 64, FORK_ROWS = PLAN_THREADS, FORK_ENTRIES = 1 << 16;
+__global__ __launch_bounds__(PLAN_THREADS, 4) void fork_one(PagesArgs a)
+{
+    __shared__ PageBits<FORK_WORDS> free;
+    __shared__ int s_first[FORK_ROWS], s_copies;
+    __shared__ int s_src[FORK_ROWS], s_dst[FORK_ROWS];       // copies; of the first workgroup the rows' parents and whole pages
+    __shared__ int s_limit[FORK_ROWS], s_refs[FORK_PAGES];   // of the first workgroup
+    const int i = threadIdx.x;
+    const bool books = blockIdx.x == 0;
+    s_first[i] = 0x7fffffff;
+    if (i == 0) s_copies = 0;
+    if (books)
+        for (int p = i; p < a.num_pages; p += PLAN_THREADS) s_refs[p] = a.refs_in[p];
+    __syncthreads();
+    if (i < a.rows_out) {
+        const int p = a.parents[i];
+        if (p >= 0 && p < a.rows_in) atomicMin(&s_first[p], i);
+    }
+    make_bits(a, free, [](int refs) { return refs == 0; });      // (a barrier behind the minima)
+    Row r{-1, 0, 0, 0, 0, false};
+    if (i < a.rows_out) r = row_of(a, i, [&](int parent) { return s_first[parent]; });
+    Tail t;
+    const int fresh = count_fresh(a, r, t), free_count = free.before[FORK_WORDS];
+    const bool copies = copies_page(r, t);
+    // fresh pages and copies of the rows in front, in one sum; where pages run out they do for the rows behind as well
+    long long total;
+    const long long before = block_prefix((long long)fresh << 16 | (copies ? 1 : 0), total);
+    const int rank = (int)(before >> 16), wanted = (int)(total >> 16);
+    if (!books) {
+        if (copies && rank < free_count) {
+            const int k = (int)(before & 0xffff);
+            s_src[k] = t.src[0];
+            s_dst[k] = free.select<true>(rank);
+            atomicAdd(&s_copies, 1);
+        }
+        __syncthreads();
+        copy_share(a, s_copies, blockIdx.x - 1, gridDim.x - 1, [&](int k, int& src, int& dst) {
+            src = __builtin_amdgcn_readfirstlane(s_src[k]);
+            dst = __builtin_amdgcn_readfirstlane(s_dst[k]);
+        });
+        return;
+    }
+    s_src[i] = r.parent;
+    s_dst[i] = r.full;
+    s_limit[i] = r.limit;
+    __syncthreads();
+    for (int k = i; k < a.rows_in * a.max_pages; k += PLAN_THREADS) {
+        const int e = a.table_in[k];
+        if (e >= 0 && e < a.num_pages) atomicSub(&s_refs[e], 1);
+    }
+    for (int k = i; k < a.rows_out * a.max_pages; k += PLAN_THREADS) {
+        const int row = k / a.max_pages, j = k - row * a.max_pages;
+        if (j < s_dst[row]) {
+            int e = a.table_in[s_src[row] * a.max_pages + j];
+            if (e < 0 || e >= a.num_pages) e = -1;
+            a.table_out[k] = e;
+            if (e >= 0) atomicAdd(&s_refs[e], 1);
+        } else if (j >= s_limit[row]) a.table_out[k] = -1;
+    }
+    auto put = [&](int row, int j, const Entry& e, int k) {      // k: fresh pages in front
+        const int page = e.fresh ? (k < free_count ? free.select<true>(k) : -1) : e.src;
+        a.table_out[row * a.max_pages + j] = page;
+        if (page >= 0) atomicAdd(&s_refs[page], 1);
+    };
+    const int n = r.limit - r.full, lane = i & 63;
+    if (n <= TAIL) {
+#pragma unroll
+        for (int k = 0; k < TAIL; ++k)
+            if (k < n) put(i, r.full + k, Entry{t.src[k], (t.fresh >> k & 1u) != 0}, rank + __builtin_popcount(t.fresh & ((1u << k) - 1u)));
+    }
+    for (unsigned long long long_ones = __builtin_amdgcn_ballot_w64(n > TAIL); long_ones; long_ones &= long_ones - 1) {
+        const int of = __builtin_ctzll(long_ones), row = (i & ~63) + of;
+        const Row o = row_of_lane(r, of);
+        int at = __shfl(rank, of);
+        for (int j = o.full; j < o.limit; j += 64) {
+            const Entry e = entry_of(a, o, j + lane);
+            const unsigned long long mask = __builtin_amdgcn_ballot_w64(e.fresh);
+            if (j + lane < o.limit) put(row, j + lane, e, at + __builtin_popcountll(mask & ((1ull << lane) - 1ull)));
+            at += __builtin_popcountll(mask);
+        }
+    }
+    if (i < a.rows_out) a.lens_out[i] = r.len;
+    if (i == 0 && a.info) {
+        a.info[0] = wanted < free_count ? wanted : free_count;
+        a.info[1] = wanted < free_count ? 0 : wanted - free_count;
+    }
+    __syncthreads();
+    for (int p = i; p < a.num_pages; p += PLAN_THREADS) a.refs_out[p] = s_refs[p];
+}
+
+// Workgroups that copy: as many as fit, or as have a share of 64 KiB of the most that there can be to copy.
+unsigned copy_blocks(const PagesArgs& a, long pages, unsigned most)
+{
+    const double bytes = (double)pages * a.layers * (double)a.page_bytes;
+    return bytes >= 65536.0 * most ? most : (unsigned)(bytes / 65536.0) + 1u;
 }
 
 }  // namespace
@@ -291,7 +580,10 @@ size_t pages_workspace_words(int rows_in, int rows_out, int num_pages)
 
 hipError_t launch_kv4_fork(const PagesArgs& a, int num_cus, hipStream_t stream)
 {
-    (void)num_cus;
+    if (a.rows_in <= FORK_ROWS && a.rows_out <= FORK_ROWS && a.num_pages <= FORK_PAGES && ((long)a.rows_in + a.rows_out) * a.max_pages <= FORK_ENTRIES) {
+        hipLaunchKernelGGL(fork_one, dim3(1 + copy_blocks(a, a.rows_out, (unsigned)num_cus)), dim3(PLAN_THREADS), 0, stream, a);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(fork_plan, dim3(1), dim3(PLAN_THREADS), 0, stream, a);
     const dim3 grid((unsigned)(a.rows_in > a.rows_out ? a.rows_in : a.rows_out), (unsigned)(2 + a.layers));
     hipLaunchKernelGGL(fork_apply, grid, dim3(APPLY_THREADS), 0, stream, a);
@@ -300,6 +592,10 @@ hipError_t launch_kv4_fork(const PagesArgs& a, int num_cus, hipStream_t stream)
 
 hipError_t launch_kv4_compact(const PagesArgs& a, int num_cus, hipStream_t stream)
 {
+    if (a.num_pages <= 64 * COMPACT_WORDS && (long)a.rows_in * a.max_pages <= COMPACT_ENTRIES) {
+        hipLaunchKernelGGL(compact_one, dim3(copy_blocks(a, a.num_pages / 2 + 1, 2u * (unsigned)num_cus)), dim3(PLAN_THREADS), 0, stream, a);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(compact_plan, dim3(1), dim3(PLAN_THREADS), 0, stream, a);
     hipLaunchKernelGGL(compact_apply, dim3((unsigned)num_cus * 8), dim3(APPLY_THREADS), 0, stream, a);
     return hipGetLastError();

@@ -460,6 +460,31 @@ def test_compact_nothing_to_move(thi):
     check_compact(thi, c, "entries that are no page")
 
 
+@pytest.mark.parametrize("MP", [9, 70, 200])
+def test_fork_with_many_pages_behind_a_row(thi, MP):
+    """Headroom and pages held beyond the length by the hundred, next to rows without: taken over, given up, taken fresh, until none is left."""
+    c = page_case(40 + MP, 12, MP, 12 * MP + 40, 2 * PAGE, words=300)
+    used = set(c["table"][c["table"] >= 0].tolist())
+    spare = [p for p in range(len(c["refs"])) if c["refs"][p] == 0 and p not in used]
+    c["table"][3, 3:MP - 1] = spare[:MP - 4]                             # held far beyond the length, by row 3 alone
+    c["refs"][spare[:MP - 4]] = 1
+    check_fork(thi, c, [3, 3, 0, -1, 5, 5, 11, 1], [MP * PAGE, 0, 1, 65 * PAGE, 3, 64 * PAGE + 1, 0, 2 ** 31 - 1], "long tails")
+    check_fork(thi, c, list(range(12)) * 6, [MP * PAGE] * 72, "long tails, too few pages")
+
+
+@pytest.mark.parametrize("words", [4, 252, 256, 300, 4100])
+def test_page_sizes(thi, words):
+    """Pages of 16 bytes, of a slice of the copy more or less, of some slices and a rest."""
+    c = page_case(60, 30, 6, 260, 6 * PAGE, words=words, layers=3)
+    assert check_fork(thi, c, np.arange(90) // 3, np.ones(90, int), "page sizes")
+    assert check_compact(thi, c, "page sizes")
+
+
+def test_compact_large_pool(thi):
+    c = page_case(61, 200, 60, 20000, 60 * PAGE, words=4)
+    assert check_compact(thi, c, "large pool")
+
+
 # ---- streams and graphs -------------------------------------------------------------------------------------------
 
 
