@@ -52,16 +52,12 @@ struct Row {
     int parent, len, full, used, limit;
     bool first;            // the lowest row of this parent: takes over what only that parent has
 };
-template <class First>      // the lowest row that continues a parent
-__device__ __forceinline__ Row row_of(const PagesArgs& a, int i, First first)
+__device__ __forceinline__ Row row_of(const PagesArgs& a, int i)      // (but for `first`)
 {
     Row r{a.parents[i], 0, 0, 0, 0, false};
     const int room = a.headroom ? a.headroom[i] : 0;
     if (r.parent < 0 || r.parent >= a.rows_in) r.parent = -1;
-    else {
-        r.len = clamp_len(a, a.lens_in[r.parent]);
-        r.first = first(r.parent) == i;
-    }
+    else r.len = clamp_len(a, a.lens_in[r.parent]);
     r.full = r.len / KV4_PAGE;
     r.used = pages_of(r.len);
     const long want = ((long)r.len + (room > 0 ? room : 0) + KV4_PAGE - 1) / KV4_PAGE;
@@ -75,7 +71,8 @@ struct Entry {
     int src;               // the parent's page, -1: none
     bool fresh;
 };
-__device__ __forceinline__ Entry entry_of(const PagesArgs& a, const Row& r, int j)
+template <class Single>      // is a page's count 1?
+__device__ __forceinline__ Entry entry_of(const PagesArgs& a, const Row& r, int j, Single single)
 {
     Entry e{-1, false};
     if (j >= r.limit) return e;
@@ -83,7 +80,7 @@ __device__ __forceinline__ Entry entry_of(const PagesArgs& a, const Row& r, int 
         e.src = a.table_in[(size_t)r.parent * a.max_pages + j];
         if (e.src < 0 || e.src >= a.num_pages) e.src = -1;
     }
-    const bool mine = e.src >= 0 && r.first && a.refs_in[e.src] == 1;
+    const bool mine = e.src >= 0 && r.first && single(e.src);
     e.fresh = !mine && (j >= r.used || e.src >= 0);
     return e;
 }
@@ -99,7 +96,8 @@ struct Tail {
     int src[TAIL];
     unsigned fresh;        // bits
 };
-__device__ __forceinline__ int count_fresh(const PagesArgs& a, const Row& r, Tail& t)
+template <class Single>
+__device__ __forceinline__ int count_fresh(const PagesArgs& a, const Row& r, Tail& t, Single single)
 {
     const int n = r.limit - r.full, lane = threadIdx.x & 63;
     t.fresh = 0;
@@ -107,7 +105,7 @@ __device__ __forceinline__ int count_fresh(const PagesArgs& a, const Row& r, Tai
     if (n <= TAIL) {
 #pragma unroll
         for (int k = 0; k < TAIL; ++k) {
-            const Entry e = entry_of(a, r, r.full + k);
+            const Entry e = entry_of(a, r, r.full + k, single);
             t.src[k] = e.src;
             t.fresh |= e.fresh ? 1u << k : 0u;
         }
@@ -117,11 +115,11 @@ __device__ __forceinline__ int count_fresh(const PagesArgs& a, const Row& r, Tai
         const int of = __builtin_ctzll(long_ones);
         const Row o = row_of_lane(r, of);
         int total = 0;
-        for (int j = o.full; j < o.limit; j += 64) total += __builtin_popcountll(__builtin_amdgcn_ballot_w64(entry_of(a, o, j + lane).fresh));
+        for (int j = o.full; j < o.limit; j += 64) total += __builtin_popcountll(__builtin_amdgcn_ballot_w64(entry_of(a, o, j + lane, single).fresh));
         if (lane == of) {
             count = total;
             t.src[0] = o.full < o.used ? a.table_in[(size_t)o.parent * a.max_pages + o.full] : -1;
-            t.fresh = o.full < o.used && entry_of(a, o, o.full).fresh ? 1u : 0u;
+            t.fresh = o.full < o.used && entry_of(a, o, o.full, single).fresh ? 1u : 0u;
         }
     }
     return count;
@@ -132,7 +130,6 @@ __device__ __forceinline__ bool copies_page(const Row& r, const Tail& t) { retur
 // workspace words: first[rows_in], rank[rows_out] (fresh pages of the rows before), free[num_pages], counts
 struct ForkWs {
     int *first, *rank, *free, *free_count;
-    __device__ __forceinline__ int operator()(int parent) const { return __hip_atomic_load(first + parent, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 };
 __device__ __forceinline__ ForkWs fork_ws(const PagesArgs& a)
 {
@@ -143,6 +140,16 @@ __device__ __forceinline__ ForkWs fork_ws(const PagesArgs& a)
     w.free = w.rank + a.rows_out;
     return w;
 }
+__device__ __forceinline__ Row planned_row(const PagesArgs& a, const ForkWs& w, int i)
+{
+    Row r = row_of(a, i);
+    if (r.parent >= 0) r.first = __hip_atomic_load(w.first + r.parent, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i;
+    return r;
+}
+struct Counted {           // counts as they stand in memory
+    const int* refs;
+    __device__ __forceinline__ bool operator()(int page) const { return refs[page] == 1; }
+};
 
 __global__ __launch_bounds__(PLAN_THREADS) void fork_plan(PagesArgs a)
 {
@@ -161,9 +168,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_plan(PagesArgs a)
     for (int i0 = 0; i0 < a.rows_out; i0 += PLAN_THREADS) {
         const int i = i0 + tid;
         Row r{-1, 0, 0, 0, 0, false};
-        if (i < a.rows_out) r = row_of(a, i, w);
+        if (i < a.rows_out) r = planned_row(a, w, i);
         Tail t;
-        const int fresh = count_fresh(a, r, t);
+        const int fresh = count_fresh(a, r, t, Counted{a.refs_in});
         int total;
         const int before = block_prefix(fresh, total);
         if (i < a.rows_out) w.rank[i] = carry + before;
@@ -230,11 +237,11 @@ __global__ __launch_bounds__(APPLY_THREADS) void fork_apply(PagesArgs a)
         return;
     }
     if (i >= a.rows_out) return;
-    const Row r = row_of(a, i, w);
+    const Row r = planned_row(a, w, i);
     const int free_count = w.free_count[0], rank = w.rank[i];
     if (y >= 2) {
         if (r.full == r.used) return;
-        const Entry e = entry_of(a, r, r.full);
+        const Entry e = entry_of(a, r, r.full, Counted{a.refs_in});
         if (e.fresh && rank < free_count) copy_page(a, e.src, w.free[rank], y - 2, tid * 16, a.page_bytes, APPLY_THREADS * 16);
         return;
     }
@@ -250,7 +257,7 @@ __global__ __launch_bounds__(APPLY_THREADS) void fork_apply(PagesArgs a)
         for (int j0 = r.full; j0 < a.max_pages; j0 += 64) {
             const int j = j0 + tid;
             Entry e{-1, false};
-            if (j < a.max_pages) e = entry_of(a, r, j);
+            if (j < a.max_pages) e = entry_of(a, r, j, Counted{a.refs_in});
             const unsigned long long mask = __builtin_amdgcn_ballot_w64(e.fresh);
             const int k = at + __builtin_popcountll(mask & ((1ull << tid) - 1ull));
             at += __builtin_popcountll(mask);
@@ -367,25 +374,34 @@ template <int WORDS> struct PageBits {
         return p;
     }
 };
-template <int WORDS, class Is>
-__device__ __forceinline__ void make_bits(const PagesArgs& a, PageBits<WORDS>& bits, Is is)
+// The counts of all pages, 64 a word, every PLAN_WAVES-th word of them a wave's; -1 where there is no page.
+template <int WORDS> struct Counts {
+    int refs[WORDS / PLAN_WAVES];
+};
+template <int WORDS>
+__device__ __forceinline__ void ask_counts(const PagesArgs& a, Counts<WORDS>& c)
 {
     static_assert((WORDS & (WORDS - 1)) == 0 && WORDS % 64 == 0, "");
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, words = (a.num_pages + 63) / 64;
-    for (int w0 = wv; w0 < WORDS; w0 += 8 * PLAN_WAVES) {
-        bool f[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int p = (w0 + k * PLAN_WAVES) * 64 + lane;
-            f[k] = p < a.num_pages && is(a.refs_in[p]);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int w = w0 + k * PLAN_WAVES;
-            const unsigned long long m = __builtin_amdgcn_ballot_w64(f[k]);
-            if (lane == 0 && w < WORDS) bits.word[w] = w < words ? m : 0;
-        }
+    for (int k = 0; k < WORDS / PLAN_WAVES; ++k) {
+        const int p = k * PLAN_THREADS + (int)threadIdx.x;
+        c.refs[k] = p < a.num_pages ? a.refs_in[p] : -1;
     }
+}
+template <int WORDS, class Is>
+__device__ __forceinline__ void put_words(const Counts<WORDS>& c, unsigned long long* word, Is is)
+{
+#pragma unroll
+    for (int k = 0; k < WORDS / PLAN_WAVES; ++k) {
+        const unsigned long long m = __builtin_amdgcn_ballot_w64(is(c.refs[k]));
+        if ((threadIdx.x & 63) == 0) word[k * PLAN_WAVES + (threadIdx.x >> 6)] = m;
+    }
+}
+template <int WORDS, class Is>
+__device__ __forceinline__ void make_bits(const Counts<WORDS>& c, PageBits<WORDS>& bits, Is is)
+{
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    put_words(c, bits.word, is);
     __syncthreads();
     if (wv == 0) {
         constexpr int PER = WORDS / 64;
@@ -447,7 +463,9 @@ constexpr int COMPACT_WORDS = 256, COMPACT_ENTRIES = 1 << 22;          // 16384 
 __global__ __launch_bounds__(PLAN_THREADS, 8) void compact_one(PagesArgs a)
 {
     __shared__ PageBits<COMPACT_WORDS> live;
-    make_bits(a, live, [](int refs) { return refs > 0; });
+    Counts<COMPACT_WORDS> counts;
+    ask_counts(a, counts);
+    make_bits(counts, live, [](int refs) { return refs > 0; });
     const int L = live.before[COMPACT_WORDS], front = live.rank(L), moved = L - front;      // as many holes in front of L as live pages behind
     const int tid = blockIdx.x * PLAN_THREADS + threadIdx.x, stride = gridDim.x * PLAN_THREADS;
     auto is_live = [&](int p) { return (live.word[p >> 6] >> (p & 63) & 1ull) != 0; };
@@ -480,22 +498,27 @@ __global__ __launch_bounds__(PLAN_THREADS, 4) void fork_one(PagesArgs a)
     __shared__ int s_first[FORK_ROWS], s_copies;
     __shared__ int s_src[FORK_ROWS], s_dst[FORK_ROWS];       // copies; of the first workgroup the rows' parents and whole pages
     __shared__ int s_limit[FORK_ROWS], s_refs[FORK_PAGES];   // of the first workgroup
+    __shared__ unsigned long long s_single[FORK_WORDS];      // pages with a count of 1
     const int i = threadIdx.x;
     const bool books = blockIdx.x == 0;
+    Counts<FORK_WORDS> counts;
+    ask_counts(a, counts);
+    Row r{-1, 0, 0, 0, 0, false};
+    if (i < a.rows_out) r = row_of(a, i);
     s_first[i] = 0x7fffffff;
     if (i == 0) s_copies = 0;
-    if (books)
-        for (int p = i; p < a.num_pages; p += PLAN_THREADS) s_refs[p] = a.refs_in[p];
-    __syncthreads();
-    if (i < a.rows_out) {
-        const int p = a.parents[i];
-        if (p >= 0 && p < a.rows_in) atomicMin(&s_first[p], i);
+    if (books) {
+#pragma unroll
+        for (int k = 0; k < FORK_PAGES / PLAN_THREADS; ++k) s_refs[k * PLAN_THREADS + i] = counts.refs[k];
     }
-    make_bits(a, free, [](int refs) { return refs == 0; });      // (a barrier behind the minima)
-    Row r{-1, 0, 0, 0, 0, false};
-    if (i < a.rows_out) r = row_of(a, i, [&](int parent) { return s_first[parent]; });
+    __syncthreads();
+    if (r.parent >= 0) atomicMin(&s_first[r.parent], i);
+    put_words(counts, s_single, [](int refs) { return refs == 1; });
+    make_bits(counts, free, [](int refs) { return refs == 0; });      // (a barrier behind the minima)
+    if (r.parent >= 0) r.first = s_first[r.parent] == i;
+    auto single = [&](int page) { return (s_single[page >> 6] >> (page & 63) & 1ull) != 0; };
     Tail t;
-    const int fresh = count_fresh(a, r, t), free_count = free.before[FORK_WORDS];
+    const int fresh = count_fresh(a, r, t, single), free_count = free.before[FORK_WORDS];
     const bool copies = copies_page(r, t);
     // fresh pages and copies of the rows in front, in one sum; where pages run out they do for the rows behind as well
     long long total;
@@ -519,18 +542,32 @@ __global__ __launch_bounds__(PLAN_THREADS, 4) void fork_one(PagesArgs a)
     s_dst[i] = r.full;
     s_limit[i] = r.limit;
     __syncthreads();
-    for (int k = i; k < a.rows_in * a.max_pages; k += PLAN_THREADS) {
-        const int e = a.table_in[k];
-        if (e >= 0 && e < a.num_pages) atomicSub(&s_refs[e], 1);
+    constexpr int AHEAD = 8;                 // loads in flight
+    for (int k0 = i; k0 < a.rows_in * a.max_pages; k0 += AHEAD * PLAN_THREADS) {
+        int e[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) e[k] = k0 + k * PLAN_THREADS < a.rows_in * a.max_pages ? a.table_in[k0 + k * PLAN_THREADS] : -1;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (e[k] >= 0 && e[k] < a.num_pages) atomicSub(&s_refs[e[k]], 1);
     }
-    for (int k = i; k < a.rows_out * a.max_pages; k += PLAN_THREADS) {
-        const int row = k / a.max_pages, j = k - row * a.max_pages;
-        if (j < s_dst[row]) {
-            int e = a.table_in[s_src[row] * a.max_pages + j];
-            if (e < 0 || e >= a.num_pages) e = -1;
-            a.table_out[k] = e;
-            if (e >= 0) atomicAdd(&s_refs[e], 1);
-        } else if (j >= s_limit[row]) a.table_out[k] = -1;
+    for (int k0 = i; k0 < a.rows_out * a.max_pages; k0 += AHEAD * PLAN_THREADS) {
+        int e[AHEAD];
+        bool shared[AHEAD], none[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int at = k0 + k * PLAN_THREADS, row = at / a.max_pages, j = at - row * a.max_pages;
+            const bool in = row < a.rows_out;
+            shared[k] = in && j < s_dst[row];
+            none[k] = in && j >= s_limit[row];
+            e[k] = shared[k] ? a.table_in[s_src[row] * a.max_pages + j] : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (e[k] < 0 || e[k] >= a.num_pages) e[k] = -1;
+            if (shared[k] || none[k]) a.table_out[k0 + k * PLAN_THREADS] = e[k];
+            if (e[k] >= 0) atomicAdd(&s_refs[e[k]], 1);
+        }
     }
     auto put = [&](int row, int j, const Entry& e, int k) {      // k: fresh pages in front
         const int page = e.fresh ? (k < free_count ? free.select<true>(k) : -1) : e.src;
@@ -548,7 +585,7 @@ __global__ __launch_bounds__(PLAN_THREADS, 4) void fork_one(PagesArgs a)
         const Row o = row_of_lane(r, of);
         int at = __shfl(rank, of);
         for (int j = o.full; j < o.limit; j += 64) {
-            const Entry e = entry_of(a, o, j + lane);
+            const Entry e = entry_of(a, o, j + lane, single);
             const unsigned long long mask = __builtin_amdgcn_ballot_w64(e.fresh);
             if (j + lane < o.limit) put(row, j + lane, e, at + __builtin_popcountll(mask & ((1ull << lane) - 1ull)));
             at += __builtin_popcountll(mask);
