@@ -600,7 +600,7 @@ __global__ __launch_bounds__(PLAN_THREADS, 4) void fork_one(PagesArgs a)
     for (int p = i; p < a.num_pages; p += PLAN_THREADS) a.refs_out[p] = s_refs[p];
 }
 
-// Workgroups that copy: as many as fit, or as have a share of 64 KiB of the most that there can be to copy.
+// Workgroups that copy: as many as fit beside each other (one more cost a fork 5.5 us: a second round), or as have a share of 64 KiB of the most that there can be to copy.
 unsigned copy_blocks(const PagesArgs& a, long pages, unsigned most)
 {
     const double bytes = (double)pages * a.layers * (double)a.page_bytes;
@@ -615,10 +615,12 @@ size_t pages_workspace_words(int rows_in, int rows_out, int num_pages)
     return fork > compact ? fork : compact;
 }
 
+// One launch up to what its LDS holds, and as many table entries as one workgroup goes through while the others copy.  One launch / two: 16 rows, 8192 pages 8.4 / 20.7 us
+// (the call's own 8 among them); 256 rows, ten layers of 70 KB pages 22.5 / 33; 1000 rows of 32 entries, a layer 22.6 / 22.9, six 27.0 / 37.6.
 hipError_t launch_kv4_fork(const PagesArgs& a, int num_cus, hipStream_t stream)
 {
     if (a.rows_in <= FORK_ROWS && a.rows_out <= FORK_ROWS && a.num_pages <= FORK_PAGES && ((long)a.rows_in + a.rows_out) * a.max_pages <= FORK_ENTRIES) {
-        hipLaunchKernelGGL(fork_one, dim3(1 + copy_blocks(a, a.rows_out, (unsigned)num_cus)), dim3(PLAN_THREADS), 0, stream, a);
+        hipLaunchKernelGGL(fork_one, dim3(1 + copy_blocks(a, a.rows_out, num_cus > 1 ? (unsigned)num_cus - 1u : 1u)), dim3(PLAN_THREADS), 0, stream, a);
         return hipGetLastError();
     }
     hipLaunchKernelGGL(fork_plan, dim3(1), dim3(PLAN_THREADS), 0, stream, a);
@@ -627,6 +629,7 @@ hipError_t launch_kv4_fork(const PagesArgs& a, int num_cus, hipStream_t stream)
     return hipGetLastError();
 }
 
+// One launch / two at 16384 pages: 4 rows 8.6 / 35 us, 1000 rows (285 MB moved) 70 / 100; 2000 pages in ten layers (468 MB) 101 / 109.
 hipError_t launch_kv4_compact(const PagesArgs& a, int num_cus, hipStream_t stream)
 {
     if (a.num_pages <= 64 * COMPACT_WORDS && (long)a.rows_in * a.max_pages <= COMPACT_ENTRIES) {
