@@ -13,15 +13,13 @@ constexpr int KV4_THREADS = 256;
 constexpr int LANE_VALUES = 8;       // a lane's share of a head: 16 bytes
 
 // x rounded to 32 bits so that no border between codes or scales is met that x itself is not on: towards zero, the last bit set if
-// anything was dropped (past the range: the largest finite value; not finite: not finite).
+// anything was dropped (not finite: not finite).  Cut to 24 bits first, so that the conversion is exact; what lies below fp32's normal numbers is far below half the smallest code.
 __device__ __forceinline__ float to_float_sticky(double x)
 {
-    const float f = (float)x;
-    const double back = (double)f;
-    unsigned b = __builtin_bit_cast(unsigned, f);
-    b -= __builtin_fabs(back) > __builtin_fabs(x) ? 1u : 0u;
-    b |= back != x ? 1u : 0u;
-    return __builtin_bit_cast(float, b);
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+    const unsigned low = (unsigned)u, dropped = low & 0x1fffffffu;
+    const float f = (float)__builtin_bit_cast(double, (u & 0xffffffff00000000ull) | (low & 0xe0000000u));
+    return __builtin_bit_cast(float, __builtin_bit_cast(unsigned, f) | (dropped ? 1u : 0u));
 }
 
 // Rounded by way of 32 bits, by the conversion instructions: left to itself the compiler makes one conversion of the two, some 40 instructions a value.
@@ -122,21 +120,31 @@ __global__ __launch_bounds__(KV4_THREADS) void kv4_append(Kv4AppendArgs a)
     __shared__ unsigned char s_byte[TT > 1 ? TT : 1][D / 32];
     __shared__ long s_slot[TT];
     const int tid = threadIdx.x, part = tid % LPH, row = tid / LPH, tt = row / HH;
-    const int t = blockIdx.x * TT + tt;
+    // workgroups go round the eight XCDs: the four that follow each other on one take neighbouring tokens, whose bytes share lines of the page
+    int window = blockIdx.x;
+    if (TT > 1 && window < (int)(gridDim.x & ~31u)) window = (window & ~31) + (window & 7) * 4 + (window >> 3 & 3);
+    const int t = window * TT + tt;
     const bool token = t < a.T;
     const long limit = (long)a.num_pages * KV4_PAGE;
     const long slot = token ? a.slots[t] : -1;
     const bool stored = slot >= 0 && slot < limit;
     const int pos = (int)(slot & (KV4_PAGE - 1));
     if (TT > 1 && part == 0) s_slot[tt] = stored ? slot : -1;
-    // the rows of the heads in front, two steps ahead of the arithmetic (without: 83 us for 4001 tokens of 120 heads)
+    // the rows of the heads in front, four steps ahead of the arithmetic (4001 tokens of 120 heads: 83 us without, 52 with two or four; the waits are for all but the latest
+    // loads and stores, so that four let stores of the step before run on), and the gammas once
     const int H = a.Hq + 2 * a.Hkv, step = gridDim.y * HH;
     const uint16_t* const from = a.qkv + (size_t)(token ? t : 0) * a.ld + part * LANE_VALUES;
     auto ask = [&](int h0) {
         const int h = h0 + row % HH;
         return __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + (size_t)(h < H ? h : 0) * D));
     };
-    uintx4 next = ask(blockIdx.y * HH), after = ask(blockIdx.y * HH + step);
+    constexpr int AHEAD = 4;
+    uintx4 rows[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) rows[k] = ask(blockIdx.y * HH + k * step);
+    half8 gammas[2] = {};                          // the queries' and the keys'
+    if (a.q_gamma) gammas[0] = __builtin_bit_cast(half8, *reinterpret_cast<const uintx4*>(a.q_gamma + part * LANE_VALUES));
+    if (a.k_gamma) gammas[1] = __builtin_bit_cast(half8, *reinterpret_cast<const uintx4*>(a.k_gamma + part * LANE_VALUES));
     double cs[LANE_VALUES / 2], sn[LANE_VALUES / 2];
     if (a.theta) {
         const double at = token ? (double)a.positions[t] : 0.0;
@@ -169,9 +177,10 @@ __global__ __launch_bounds__(KV4_THREADS) void kv4_append(Kv4AppendArgs a)
     for (int h0 = blockIdx.y * HH; h0 < H; h0 += step) {
         const int h = h0 + row % HH;
         const bool there = token && h < H;
-        const half8 x = __builtin_bit_cast(half8, next);
-        next = after;
-        after = ask(h0 + 2 * step);
+        const half8 x = __builtin_bit_cast(half8, rows[0]);
+#pragma unroll
+        for (int k = 0; k + 1 < AHEAD; ++k) rows[k] = rows[k + 1];
+        rows[AHEAD - 1] = ask(h0 + AHEAD * step);
         float f[LANE_VALUES];
         if (h >= a.Hq + a.Hkv) {                   // a value: stored as it is
 #pragma unroll
@@ -180,15 +189,14 @@ __global__ __launch_bounds__(KV4_THREADS) void kv4_append(Kv4AppendArgs a)
             double y[LANE_VALUES];
 #pragma unroll
             for (int e = 0; e < LANE_VALUES; ++e) y[e] = (double)(float)x[e];
-            const uint16_t* const gamma = h < a.Hq ? a.q_gamma : a.k_gamma;
-            if (gamma) {
+            if (h < a.Hq ? a.q_gamma != nullptr : a.k_gamma != nullptr) {
                 double ss = 0.0;
 #pragma unroll
                 for (int e = 0; e < LANE_VALUES; ++e) ss = __builtin_fma(y[e], y[e], ss);
 #pragma unroll
                 for (int sh = 1; sh < LPH; sh <<= 1) ss += __shfl_xor(ss, sh);
                 const double r = inverse_sqrt(ss * (1.0 / D) + (double)a.eps);
-                const half8 gm = __builtin_bit_cast(half8, *reinterpret_cast<const uintx4*>(gamma + part * LANE_VALUES));
+                const half8 gm = h < a.Hq ? gammas[0] : gammas[1];
 #pragma unroll
                 for (int e = 0; e < LANE_VALUES; ++e) y[e] *= r * (double)(float)gm[e];
             }
