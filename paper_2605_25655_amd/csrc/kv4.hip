@@ -110,10 +110,10 @@ __device__ __forceinline__ void sine_cosine(double x, double& sn, double& cs)
 // eight neighbouring values a lane, whose four angles it makes once.
 //
 // The values' codes lie in the page so that four neighbouring positions' bytes of a pair of columns are a dword (kv4.h); stored by
-// themselves, 4001 tokens of 40 heads made 10 million byte stores, and the call took 83 us.  With ROWS tokens a workgroup collects them in LDS
-// and stores dwords where a run of slots allows it.
+// themselves, 4001 tokens of 40 heads made 10 million byte stores, and the call took 83 us.  With ROWS tokens a workgroup stores dwords: where all its rows are runs of
+// four that begin a dword, four rows exchange bytes within their wave; elsewhere it collects them in LDS, with two barriers a head, and stores dwords where a run allows it.
 template <int D, int TT>
-__global__ __launch_bounds__(KV4_THREADS) void kv4_append(Kv4AppendArgs a)
+__global__ __launch_bounds__(KV4_THREADS, 4) void kv4_append(Kv4AppendArgs a)
 {
     constexpr int LPH = D / LANE_VALUES, ROWS = KV4_THREADS / LPH, HH = ROWS / TT;
     __shared__ unsigned s_code[TT > 1 ? TT : 1][LPH];
@@ -123,22 +123,23 @@ __global__ __launch_bounds__(KV4_THREADS) void kv4_append(Kv4AppendArgs a)
     // workgroups go round the eight XCDs: the four that follow each other on one take neighbouring tokens, whose bytes share lines of the page
     int window = blockIdx.x;
     if (TT > 1 && window < (int)(gridDim.x & ~31u)) window = (window & ~31) + (window & 7) * 4 + (window >> 3 & 3);
-    const int t = window * TT + tt;
-    const bool token = t < a.T;
+    // (counted from a token whose dword of the page begins with it, if the first one's does, so that a run of slots is the same groups of four throughout)
+    const int t = window * TT + tt - (TT > 1 ? a.slots[0] & 3 : 0);
+    const bool token = t >= 0 && t < a.T;
     const long limit = (long)a.num_pages * KV4_PAGE;
     const long slot = token ? a.slots[t] : -1;
     const bool stored = slot >= 0 && slot < limit;
     const int pos = (int)(slot & (KV4_PAGE - 1));
     if (TT > 1 && part == 0) s_slot[tt] = stored ? slot : -1;
-    // the rows of the heads in front, four steps ahead of the arithmetic (4001 tokens of 120 heads: 83 us without, 52 with two or four; the waits are for all but the latest
-    // loads and stores, so that four let stores of the step before run on), and the gammas once
+    // the rows of the heads in front, three steps ahead of the arithmetic (4001 tokens of 120 heads: 83 us without, 52 with two or four; the waits are for all but the latest
+    // loads and stores, so that three let a store of the step before run on), and the gammas once
     const int H = a.Hq + 2 * a.Hkv, step = gridDim.y * HH;
     const uint16_t* const from = a.qkv + (size_t)(token ? t : 0) * a.ld + part * LANE_VALUES;
     auto ask = [&](int h0) {
         const int h = h0 + row % HH;
         return __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + (size_t)(h < H ? h : 0) * D));
     };
-    constexpr int AHEAD = 4;
+    constexpr int AHEAD = 3;
     uintx4 rows[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) rows[k] = ask(blockIdx.y * HH + k * step);
@@ -164,9 +165,11 @@ __global__ __launch_bounds__(KV4_THREADS) void kv4_append(Kv4AppendArgs a)
     }
     // TT > 1: this thread's four tokens when values are stored: a group that begins where a dword of the page does, counted round the TT tokens
     int lead = 0, pair_of_part = 0;
-    bool run = false;
+    bool run = false, whole = false;
     if (TT > 1) {
         __syncthreads();
+        const long s4 = s_slot[tt & ~3];
+        whole = __syncthreads_and(s4 >= 0 && (s4 & 3) == 0 && s_slot[tt] == s4 + (tt & 3)) != 0;      // every four rows are the four positions of a dword
         const int ahead = (int)(-s_slot[0] & 3);
         lead = (ahead + (tid / LPH) % (TT / 4) * 4) % TT;
         pair_of_part = tid / (LPH * (TT / 4));
@@ -221,6 +224,18 @@ __global__ __launch_bounds__(KV4_THREADS) void kv4_append(Kv4AppendArgs a)
         unsigned byte;
         const unsigned c = quantise(f, byte);
         const bool value = h >= a.Hq + a.Hkv;
+        if (TT > 1 && value && whole) {            // four rows lie in one wave: bytes change places between them
+            const int r = tt & 3;
+            unsigned char* const base = a.pages + ((size_t)(slot >> 6) * a.Hkv + (h - a.Hq - a.Hkv)) * kv4_head_bytes(D);
+            unsigned x = __builtin_amdgcn_perm((unsigned)__shfl_xor((int)c, 2 * LPH), c, r & 2 ? 0x03020706u : 0x05040100u);
+            x = __builtin_amdgcn_perm((unsigned)__shfl_xor((int)x, LPH), x, r & 1 ? 0x03070105u : 0x06020400u);
+            *reinterpret_cast<unsigned*>(base + kv4_values(D) + kv4_value_at(pos & ~3, part * 4 + r)) = x;      // the r-th pair of the four positions
+            unsigned e = byte << (8 * r);
+            e |= (unsigned)__shfl_xor((int)e, LPH);
+            e |= (unsigned)__shfl_xor((int)e, 2 * LPH);
+            if (r == 0 && part % 4 == 0) *reinterpret_cast<unsigned*>(base + kv4_value_scales(D) + kv4_value_scale_at(pos & ~3, part / 4)) = e;
+            continue;
+        }
         if (TT > 1 && value) {                     // (HH = 1: the same head for all rows)
             s_code[tt][part] = c;
             if (part % 4 == 0) s_byte[tt][part / 4] = (unsigned char)byte;
@@ -358,7 +373,7 @@ static void append(const Kv4AppendArgs& a, int num_cus, hipStream_t stream)
         return;
     }
     // one round of four workgroups a compute unit, while a workgroup has eight heads or more (its angles cost it as much as some heads)
-    const int windows = (a.T + ROWS - 1) / ROWS;
+    const int windows = (a.T + 3 + ROWS - 1) / ROWS;      // (up to three rows in front of the first token)
     int split = windows > 4 * num_cus ? 1 : 4 * num_cus / windows;
     split = split > (H + 7) / 8 ? (H + 7) / 8 : split;
     hipLaunchKernelGGL((kv4_append<D, ROWS>), dim3((unsigned)windows, (unsigned)split), dim3(KV4_THREADS), 0, stream, a);

@@ -125,6 +125,18 @@ def test_append_many_tokens(thi):
     check_append(thi, c, 1, 1, 64)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("first", [-1, 0, 2, 6 * PAGE])
+def test_append_first_slot_and_run(thi, D, first):
+    """Padding, or a slot of its own, in front of runs that begin a dword of the page, or do not; the last run ends inside one."""
+    T = 205
+    c = append_case(13 + first, T, 2, 1, D, 6)
+    c["slots"] = np.r_[first, 4 + np.arange(100), 130 + np.arange(T - 101)].astype(np.int32)
+    check_append(thi, c, 2, 1, D)
+    c["slots"] = (8 + np.arange(T)).astype(np.int32)
+    check_append(thi, c, 2, 1, D)
+
+
 def test_append_slots_outside_the_pool(thi):
     c = append_case(6, 12, 4, 2, 128, 3)
     c["slots"][[0, 3, 4, 11]] = [-1, 3 * PAGE, 2 ** 31 - 1, -2 ** 31]
