@@ -89,16 +89,16 @@ template <int D> __device__ __forceinline__ QueryRow ask_queries(const uint16_t*
 template <int D> __device__ __forceinline__ void take_queries(const QueryRow& row, int hi, float scale2, Queries& q)
 {
     const bool any = hi < D / 32;
-    floatx32 rest;
+    floatx16 even, odd;                          // columns of the block, then what the summands so far leave of them
     unsigned high = 0, low = 0;                  // the largest magnitudes' bits of the odd and even columns, in the upper half
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
         const uintx4 x = row.x[s];
         const half8 h = __builtin_bit_cast(half8, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rest[8 * s + e] = any ? (float)h[e] * scale2 : 0.f;
-#pragma unroll
         for (int e = 0; e < 4; ++e) {
+            even[4 * s + e] = any ? (float)h[2 * e] * scale2 : 0.f;
+            odd[4 * s + e] = any ? (float)h[2 * e + 1] * scale2 : 0.f;
             const unsigned u = x[e] & 0x7fff0000u, v = (x[e] << 16) & 0x7fff0000u;
             high = u > high ? u : high;
             low = v > low ? v : low;
@@ -113,17 +113,19 @@ template <int D> __device__ __forceinline__ void take_queries(const QueryRow& ro
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
         const float scale = __builtin_bit_cast(float, (unsigned)(e - 4 * s) << 23);
-        floatx16 even, odd;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            even[k] = rest[2 * k];
-            odd[k] = rest[2 * k + 1];
-        }
+        // The conversions write their registers while they still read, and the compiler does not know: an operand that is needed no more may be given
+        // some of the result's (a scale was, and the last summand was wrong that way).  Each is needed until behind its conversion.
         const uintx6 codes = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
-        rest -= __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(codes, scale);
-        // The conversion writes its six registers while it still reads the scale, and the compiler does not know: a scale that is needed no more
-        // may be given one of the six (the last summand was wrong that way).  It is needed until here.
-        asm volatile("" : : "v"(scale), "v"(codes));
+        asm volatile("" : "+v"(even), "+v"(odd) : "v"(scale), "v"(codes));
+        if (s < 3) {
+            const floatx32 part = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(codes, scale);
+            asm volatile("" : : "v"(scale), "v"(codes), "v"(part));
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                even[k] -= part[2 * k];
+                odd[k] -= part[2 * k + 1];
+            }
+        }
 #pragma unroll
         for (int k = 0; k < 6; ++k) q.f[s][k] = (int)codes[k];
         q.f[s][6] = q.f[s][7] = 0;
