@@ -11,22 +11,25 @@ namespace {
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 
-// What a request's rows are: [first, first + n) of q, on `len` positions.  Whatever the arrays hold stays within the buffers.
+// What a request's rows are: [first, first + n) of q, the last n of `len` positions.  Whatever the arrays hold stays within the buffers.
 struct Request {
     int first, n, len;
 };
 __device__ __forceinline__ Request find_request(const Kv4AttnArgs& a, int b)
 {
     Request r{b, 1, a.seq_lens[b]};
+    const long most = (long)a.max_pages * KV4_PAGE;
+    r.len = r.len < 0 ? 0 : r.len > most ? (int)most : r.len;
     if (a.q_offsets) {
         int o0 = a.q_offsets[b], o1 = a.q_offsets[b + 1];
         o0 = o0 < 0 ? 0 : o0 > a.T ? a.T : o0;
         o1 = o1 < o0 ? o0 : o1 > a.T ? a.T : o1;
         r.first = o0;
         r.n = o1 - o0 < a.max_q ? o1 - o0 : a.max_q;
+        // rows past max_q, which are not written, and the positions that only they see (fewer positions than that: the others see nothing, as with none)
+        const int left = o1 - o0 - r.n;
+        r.len = r.len > left ? r.len - left : 0;
     }
-    const long most = (long)a.max_pages * KV4_PAGE;
-    r.len = r.len < 0 ? 0 : r.len > most ? (int)most : r.len;
     return r;
 }
 
