@@ -30,13 +30,15 @@ __device__ __forceinline__ _Float16 to_half(double x)
     return (_Float16)f;
 }
 
-// 1 / sqrt(x): the instruction's estimate and two steps of Newton's method (each squares the error: 2^-52 and better).
+// 1 / sqrt(x): the instruction's estimate and two steps of Newton's method (each squares the error: 2^-52 and better).  Of an infinity (a head with one among its
+// values) it is 0, and a step would make infinity times 0 of it.
 __device__ __forceinline__ double inverse_sqrt(double x)
 {
-    double r = __builtin_amdgcn_rsq(x);
+    const double estimate = __builtin_amdgcn_rsq(x);
+    double r = estimate;
 #pragma unroll
     for (int i = 0; i < 2; ++i) r = __builtin_fma(0.5 * r, __builtin_fma(-x * r, r, 1.0), r);
-    return r;
+    return estimate == 0.0 ? 0.0 : r;
 }
 
 // The scale byte of a block whose largest magnitude has these bits: the smallest exponent e with max <= 7 2^e (7 is where the rounding to 6 would turn

@@ -1,0 +1,60 @@
+"""The 4-bit cache's store at its edges: infinities under the norm, special values in every way a value takes into a page, and the one rounding of a query."""
+import numpy as np
+import pytest
+
+from tests.gpu_common import say
+from tests.test_kv4_gpu import PAGE, append_case, check_append, dev, host, thi  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _special(T, Hkv, D, seed):
+    """Rows of zeros, fp16's smallest and largest numbers, the borders of scales and codes, infinities and NaN, each many times among ordinary rows."""
+    c = append_case(seed, T, 2, Hkv, D, -(-T // PAGE) + 3)
+    x = c["qkv"].reshape(T, 2 + 2 * Hkv, D)
+    for t in range(0, T, 2):
+        what = t // 2 % 9
+        if what == 0:
+            x[t] = 0
+        elif what == 1:
+            x[t] = np.float16(2.0 ** -24)
+        elif what == 2:
+            x[t], x[t, :, ::3] = np.float16(65504), np.float16(-40000)
+        elif what == 3:
+            x[t] = np.tile(np.float16([7, 0.25, -0.75, 1.25, 1.75, -2.5, 3.5, 5]), (len(x[t]), D // 8))
+        elif what == 4:
+            x[t] = np.tile(np.float16([7.004, 0.5, -1.5, 2.5, 3.5, -5, 7, 6]), (len(x[t]), D // 8))
+        elif what == 5:
+            x[t, :, 5] = np.inf
+        elif what == 6:
+            x[t, :, D - 26] = -np.inf
+        elif what == 7:
+            x[t, :, D - 1] = np.nan
+        else:
+            x[t] = np.tile(np.float16([6e-8, -1.2e-7, 4e-7, 3.6e-7, 8.4e-7, 0, -0.0, 1e-6]), (len(x[t]), D // 8))
+    return c
+
+
+def _slots(kind, T):
+    if kind == "aligned":
+        return 8 + np.arange(T)
+    if kind == "unaligned":
+        return 5 + np.arange(T)
+    s = 64 + np.arange(T)                                             # with padding rows in between
+    s[[T // 3, T // 3 + 1, T // 2]] = -1
+    return s
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind,T", [("aligned", 18), ("aligned", 150), ("unaligned", 150), ("padded", 150)])
+@pytest.mark.parametrize("norm,rope", [(True, True), (True, False), (False, False)])
+def test_special_values(thi, kind, T, D, norm, rope):  # noqa: F811
+    """One token a workgroup up to 128 (D = 64) or 64, then the exchange inside a wave, or LDS where the rows are no whole runs."""
+    c = _special(T, 2, D, T + D)
+    c["slots"] = _slots(kind, T).astype(np.int32)
+    if not norm:
+        c["q_gamma"] = c["k_gamma"] = None
+    if not rope:
+        c["theta"] = c["positions"] = None
+    with np.errstate(invalid="ignore"):
+        check_append(thi, c, 2, 2, D)
