@@ -58,3 +58,27 @@ def test_special_values(thi, kind, T, D, norm, rope):  # noqa: F811
         c["theta"] = c["positions"] = None
     with np.errstate(invalid="ignore"):
         check_append(thi, c, 2, 2, D)
+
+
+@pytest.mark.parametrize("T", [1, 150])
+@pytest.mark.parametrize("size,step", [(1.0, 2.0 ** -10), (2.0 ** -16, 2.0 ** -8)])
+def test_queries_are_rounded_once(thi, T, size, step):  # noqa: F811
+    """Rotated queries a little beside the middle between two fp16 numbers (also of those with fewer bits), on the side on which a rounding to 32 bits first (to the
+    middle, then to the even one) would end on the wrong one."""
+    import torch
+    D = 64
+    k = np.arange(D // 2)
+    middle = 1 + (2 * k + 1) * step / 2
+    beside = np.where(k % 2 == 0, 2.0 ** -25, -2.0 ** -25)
+    theta = (np.arcsin((middle + beside) / np.sqrt(2)) - np.pi / 4).astype(np.float32)
+    exact = np.cos(theta.astype(np.float64)) + np.sin(theta.astype(np.float64))
+    assert (np.abs(exact - middle) < 2.0 ** -24).all() and (np.abs(exact - middle) > 2.0 ** -30).all() and (np.sign(exact - middle) == np.sign(beside)).all()
+    want = (size * exact).astype(np.float16)
+    assert (want != (size * exact).astype(np.float32).astype(np.float16)).all()
+    qkv = np.tile(np.float16([size, -size]), (T, 3 * D // 2))
+    q_out = torch.empty(T, 1, D, dtype=torch.float16, device="cuda")
+    pages = torch.zeros(4, 1, 68 * D, dtype=torch.uint8, device="cuda")
+    say(f"[case] one rounding T={T} size={size}")
+    thi.thi_qk_norm_rope_kv4(dev(qkv), None, None, 1e-6, torch.ones(T, dtype=torch.int32, device="cuda"), dev(theta), torch.arange(T, dtype=torch.int32, device="cuda"), q_out, pages)
+    got = host(q_out)
+    assert (got[:, 0, 0::2] == want).all()
