@@ -55,7 +55,7 @@ struct Kv4AttnArgs {
     float scale2;                    // softmax scale times log2(e)
     int B, T, Hq, Hkv, D, max_q, num_pages, max_pages;
     // how the rows are dealt (kv4_plan)
-    float* part;                     // [T*Hq][nsplit][D + 2]: a chunk's unnormalised output, maximum, sum
+    float* part;                     // [B][max_q][Hq][nsplit][D + 2]: a chunk's unnormalised output, maximum, sum
     bool split_rows;                 // 16 rows of a cache head at a time, cut along the positions
     int tiles;                       // tiles of 16 rows
     int nsplit, min_chunk;           // chunks per request at most, pages per chunk at least

@@ -13,6 +13,25 @@ bool heads_ok(int Hq, int Hkv, int D) { return Hq >= 1 && Hkv >= 1 && Hq <= 6553
 // slots are int32: the pool's last position has to have one
 bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff / KV4_PAGE; }
 
+constexpr int FEW_ROWS = 64, FEW_CHUNK = 8, FEW_PER_CU = 3, MANY_CHUNK = 16, MANY_PER_CU = 2;      // kv4_plan
+
+// The most rows of partial results that a call of up to B requests, max_q rows and max_pages pages has.  Where kv4_plan cuts, the chunks are at most FEW_PER_CU (MANY_PER_CU)
+// workgroups of 16 (256) rows for every compute unit, so no batch has more rows than these hold; and no more than its own times the chunks of the longest table.
+size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
+{
+    auto at_most = [&](long q, int chunk, long held) {
+        const long chunks = (max_pages + chunk - 1) / chunk, own = (long)B * q * Hq;
+        const long rows = chunks < 2 ? 0 : own > held ? held : own * (chunks < KV4_MAX_SPLIT ? chunks : KV4_MAX_SPLIT);
+        return rows < held ? rows : held;
+    };
+    const int group = Hq / Hkv, q_few = FEW_ROWS / group < 1 ? 0 : FEW_ROWS / group;
+    const long few = max_pages <= 16 ? 0 : at_most(max_q < q_few ? max_q : q_few, FEW_CHUNK, 16L * FEW_PER_CU * num_cus);
+    const long many = (long)max_q * group <= FEW_ROWS ? 0 : at_most(max_q, MANY_CHUNK, 256L * MANY_PER_CU * num_cus);
+    return (size_t)(few > many ? few : many);
+}
+
+size_t bytes_of_rows(size_t rows, int D) { return rows ? (rows * (D + 2) * sizeof(float) + 255) / 256 * 256 : 256; }
+
 int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 
 }  // namespace
@@ -26,16 +45,16 @@ void thi::kv4_plan(Kv4AttnArgs& a, int num_cus)
 {
     const int group = a.Hq / a.Hkv;
     a.tiles = (int)(((long)a.max_q * group + 15) / 16);
-    a.split_rows = (long)a.max_q * group <= 64;
+    a.split_rows = (long)a.max_q * group <= FEW_ROWS;
     long n;
     if (a.split_rows) {
         const long items = (long)a.B * a.Hkv * a.tiles;
-        a.min_chunk = 8;
-        n = a.max_pages <= 16 ? 1 : 3L * num_cus / items;
+        a.min_chunk = FEW_CHUNK;
+        n = a.max_pages <= 16 ? 1 : (long)FEW_PER_CU * num_cus / items;
     } else {
         const long items = (long)a.B * a.Hkv * ((a.tiles + 15) / 16);
-        a.min_chunk = 16;
-        n = items >= num_cus ? 1 : 2L * num_cus / items;
+        a.min_chunk = MANY_CHUNK;
+        n = items >= num_cus ? 1 : (long)MANY_PER_CU * num_cus / items;
     }
     const long most = (a.max_pages + a.min_chunk - 1) / a.min_chunk;
     n = n < 1 ? 1 : n > KV4_MAX_SPLIT ? KV4_MAX_SPLIT : n;
@@ -86,10 +105,7 @@ int thi_kv4_read(const void* pages, const int* slots, void* k_out, void* v_out, 
 size_t thi_kv4_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages)
 {
     if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_pages < 1 || max_pages > 0x7fffffff / KV4_PAGE) return 0;
-    Kv4AttnArgs a{};
-    a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.max_pages = max_pages;
-    kv4_plan(a, device_cu_count());
-    return a.nsplit > 1 ? ((size_t)T * Hq * a.nsplit * (D + 2) * 4 + 255) / 256 * 256 : 256;
+    return bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D);
 }
 
 int thi_kv4_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, void* out,
@@ -97,14 +113,15 @@ int thi_kv4_attention(const void* q, const void* pages, const int* page_table, c
                       void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     if (!q || !pages || !page_table || !seq_lens || !out || !workspace) return THI_ERR_NULL;
-    const size_t need = thi_kv4_attention_workspace_bytes(B, T, Hq, Hkv, D, max_q, max_pages);
-    if (!need || !pool_ok(num_pages) || (!q_offsets && (T != B || max_q != 1))) return THI_ERR_SHAPE;
+    if (!thi_kv4_attention_workspace_bytes(B, T, Hq, Hkv, D, max_q, max_pages) || !pool_ok(num_pages) || (!q_offsets && (T != B || max_q != 1))) return THI_ERR_SHAPE;
     if (misaligned(q, 16) || misaligned(pages, 16) || misaligned(out, 16) || misaligned(page_table, 4) || misaligned(seq_lens, 4) ||
         misaligned(q_offsets, 4) || misaligned(workspace, 256))
         return THI_ERR_ALIGN;
-    if (workspace_bytes < need) return THI_ERR_WORKSPACE;
-    (void)hipGetLastError();
     Kv4AttnArgs a{};
+    a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.num_pages = num_pages; a.max_pages = max_pages;
+    kv4_plan(a, device_cu_count());
+    if (workspace_bytes < bytes_of_rows(a.nsplit > 1 ? (size_t)B * max_q * Hq * a.nsplit : 0, D)) return THI_ERR_WORKSPACE;
+    (void)hipGetLastError();
     a.q = (const uint16_t*)q;
     a.pages = (const unsigned char*)pages;
     a.page_table = page_table;
@@ -113,8 +130,6 @@ int thi_kv4_attention(const void* q, const void* pages, const int* page_table, c
     a.out = (uint16_t*)out;
     a.scale2 = scale * 1.44269504088896340736f;
     if (a.scale2 == 0.f) a.scale2 = 1e-30f;      // (all weights equal either way; a masked score of -inf stays what it is)
-    a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.num_pages = num_pages; a.max_pages = max_pages;
-    kv4_plan(a, device_cu_count());
     a.part = (float*)workspace;
     return finish(launch_kv4_attention(a, (hipStream_t)hip_stream));
 }

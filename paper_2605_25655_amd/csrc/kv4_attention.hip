@@ -195,6 +195,13 @@ __device__ __forceinline__ int chunk_pages(const Kv4AttnArgs& a, int pages)
     return size > a.min_chunk ? size : a.min_chunk;
 }
 
+// Where a request's r-th row of a cache head with `group` query heads lies among the partial results: by request and token, so that they
+// take what the largest request asks for and not what all tokens of the call do.
+__device__ __forceinline__ size_t part_row(const Kv4AttnArgs& a, int b, int r, int g, int group)
+{
+    return ((size_t)b * a.max_q + r / group) * a.Hq + (size_t)g * group + r % group;
+}
+
 // Two fp16 summands of four weights (the large one truncated, so that the small one is not negative).
 __device__ __forceinline__ void split_weights(const float (&w)[4], half4& large, half4& small)
 {
@@ -447,7 +454,7 @@ __global__ __launch_bounds__(KD_THREADS, MULTI ? 2 : 3) void kv4_attn_decode(Kv4
         const size_t row = row_of_column(c);
         if (whole) a.out[row * D + d] = lf == 0.f ? 0 : to_half_bits(of / lf);
         else {
-            float* const po = a.part + (row * a.nsplit + chunk) * (D + 2);
+            float* const po = a.part + (part_row(a, b, r0 + c, g, group) * a.nsplit + chunk) * (D + 2);
             po[d] = of;
             if (d == 0) { po[D] = mn; po[D + 1] = lf; }
         }
@@ -469,7 +476,7 @@ __global__ __launch_bounds__(KC_THREADS) void kv4_attn_combine(Kv4AttnArgs a)
     if (pages <= size) return;                  // one chunk: the first pass has written this output
     const int live = (pages + size - 1) / size;
     const size_t row = (size_t)(rq.first + i) * a.Hq + h;
-    const float* const first = a.part + row * a.nsplit * (D + 2);
+    const float* const first = a.part + part_row(a, b, i, h, 1) * a.nsplit * (D + 2);
     const float m = lane < live ? first[(size_t)lane * (D + 2) + D] : -__builtin_inff();
     const float w = lane < live ? first[(size_t)lane * (D + 2) + D + 1] : 0.f;
     float v[8];
@@ -888,7 +895,7 @@ __global__ __launch_bounds__(512, 2) void kv4_attn_prompt(Kv4AttnArgs a)
                 *reinterpret_cast<uintx4*>(a.out + row * D + 32 * t + 8 * hi) = __builtin_bit_cast(uintx4, y);
             }
         } else {
-            float* const po = a.part + (row * a.nsplit + chunk) * (D + 2);
+            float* const po = a.part + (part_row(a, b, r, g, group) * a.nsplit + chunk) * (D + 2);
 #pragma unroll
             for (int t = 0; t < NB; ++t)
 #pragma unroll
