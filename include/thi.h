@@ -264,7 +264,7 @@ int thi_kv4_read(const void* pages, const int* slots, void* k_out, void* v_out, 
  * cache, and see what stands before them and themselves.  A row that sees no position (an empty request, more rows than positions) is zero.
  * q, out [T,Hq,D] fp16; q_offsets [B+1] int32 device memory, not decreasing, or NULL: one token per request, T = B.  max_q is the
  * largest n_b (from the host, it sizes the launch; rows of a request past it are not written).  Scores, statistics and sums are fp32; a query's
- * block of 32 columns reaches the matrix cores to 2^-18 of its largest, a weight as fp16 (two summands up to 64 rows of a cache head, one beyond).  Workspace: thi_kv4_attention_workspace_bytes(), 256-byte aligned, no
+ * block of 32 columns reaches the matrix cores to 2^-16 / 3.75 (2^-17.9) of its largest, a weight as fp16 (two summands up to 64 rows of a cache head, one beyond).  Workspace: thi_kv4_attention_workspace_bytes(), 256-byte aligned, no
  * preparation needed; what that says for the largest B, T, max_q and max_pages does for every smaller call with these heads.  Reproducible bit for bit.
  */
 size_t thi_kv4_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages);

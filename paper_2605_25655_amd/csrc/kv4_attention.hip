@@ -66,9 +66,9 @@ template <int I> __device__ __forceinline__ unsigned pair_of(unsigned codes, flo
 //
 // The keys' codes are a matrix operand as they stand (v_mfma_scale_f32_16x16x128_f8f6f4: a lane's 16 bytes are one block of 32, the scales of the
 // four tiles of a page one dword).  The queries, times the softmax scale and log2 e, are the other: each block of 32 as the sum of four e2m3
-// numbers with scales of their own, 2^-4 apart.  Each takes four bits more; what is left is 2^-18 of the block's largest at most.  The instruction runs
-// at four times fp16's rate, so the four products cost what fp16's would; nothing has to be converted, nor, where the keys come from LDS, read in
-// four times the bytes.  With D = 64 two of the four blocks are empty (the lanes hi >= 2: zeros on the queries' side).
+// numbers with scales of their own, 2^-4 apart.  Each takes four bits more; what is left is 2^-16 of the first scale at most, and the block's largest is more than
+// 3.75 times that scale: 2^-17.9 of it.  The instruction runs at four times fp16's rate, so the four products cost what fp16's would; nothing has to be
+// converted, nor, where the keys come from LDS, read in four times the bytes.  With D = 64 two of the four blocks are empty (the lanes hi >= 2: zeros on the queries' side).
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef float floatx32 __attribute__((ext_vector_type(32)));
 typedef unsigned uintx6 __attribute__((ext_vector_type(6)));

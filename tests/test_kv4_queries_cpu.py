@@ -1,12 +1,63 @@
-"""What the compiler made of the conversions of queries in the 4-bit cache's attention."""
+"""The 4-bit cache's attention on the CPU: that the bounds of the GPU tests notice a summand less, and what the compiler made of the queries' conversions."""
 import os
 import re
 import shutil
 import subprocess
 
+import numpy as np
 import pytest
 
+from tests import kv4_bounds as bounds
+from tests.test_kv4_gpu import attention_case
+
 OBJDUMP = os.environ.get("LLVM_OBJDUMP", "/opt/rocm/llvm/bin/llvm-objdump")
+
+
+def _summands(x, n):
+    """x [..., D] as n e2m3 summands, 2^-4 apart, of scales by blocks of 32."""
+    rest = x.reshape(*x.shape[:-1], -1, 32)
+    big = np.abs(rest).max(-1, keepdims=True)
+    e = np.floor(np.log2(big)) - 2
+    e = np.where(big > 7.5 * 2.0 ** e, e + 1, e)
+    total = np.zeros_like(rest)
+    for s in range(n):
+        u = rest / 2.0 ** (e - 4 * s)
+        step = 2.0 ** np.maximum(np.floor(np.log2(np.maximum(np.abs(u), 1e-30))) - 3, -3)
+        part = np.clip(np.round(u / step) * step, -7.5, 7.5) * 2.0 ** (e - 4 * s)
+        total, rest = total + part, rest - part
+    return total.reshape(x.shape)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_bounds_notice_a_summand_less(D):
+    """The definition with queries of four summands stays inside the tolerance, with three it does not; with weights of two fp16 summands it does, with one not."""
+    for lens, new in (([2] * 40, [1] * 40), ([12] * 3, [12] * 3)):
+        c = bounds.far_queries(D, 4, 2, D, lens, new)
+        y, tol = bounds.attention(c, 0.125)
+        for n in (4, 3):
+            off = dict(c, q=_summands(c["q"].astype(np.float64), n))
+            ratio = (np.abs(bounds.attention(off, 0.125)[0] - y) / tol).max()
+            assert (ratio <= 1) == (n == 4), (n, ratio)
+    c, scale = bounds.whole_queries(attention_case(D + 1, 4, 2, D, [2, 3, 4, 5, 7, 9, 12, 16] * 3, [1] * 24))
+    assert np.array_equal(_summands(c["q"].astype(np.float64), 4), c["q"].astype(np.float64))
+    y, tol = bounds.attention(c, scale, query=0.0)
+
+    def fp16(p):
+        return (512 * p).astype(np.float16).astype(np.float64) / 512
+
+    for weights, fine in ((lambda p: fp16(p) + fp16(p - fp16(p)), True), (fp16, False)):
+        ratio = (np.abs(bounds.attention(c, scale, query=0.0, weights=weights)[0] - y) / tol).max()
+        assert (ratio <= 1) == fine, ratio
+
+
+def test_queries_left_is_within_the_bound():
+    """Four summands over all of a block's borders: what is left against 2^-16 / 3.75 of the largest, and that 2^-18 would be too little."""
+    rng = np.random.default_rng(5)
+    x = rng.uniform(-1, 1, (4000, 64)) * np.repeat(np.linspace(3.75, 7.5, 4000), 64).reshape(4000, 64)
+    x[:, ::32] = np.linspace(3.7501, 7.5, 4000)[:, None]
+    x = x.astype(np.float32).astype(np.float64)
+    left = np.abs(_summands(x, 4) - x).reshape(-1, 32).max(-1) / np.abs(x).reshape(-1, 32).max(-1)
+    assert 2.0 ** -18 < left.max() <= bounds.QUERY
 
 
 @pytest.mark.skipif(shutil.which(OBJDUMP) is None, reason="llvm-objdump not found")
