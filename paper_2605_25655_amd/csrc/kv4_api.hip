@@ -13,9 +13,9 @@ bool heads_ok(int Hq, int Hkv, int D) { return Hq >= 1 && Hkv >= 1 && Hq <= 6553
 // slots are int32: the pool's last position has to have one
 bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff / KV4_PAGE; }
 
-constexpr int FEW_ROWS = 64, FEW_CHUNK = 8, FEW_PER_CU = 3, MANY_CHUNK = 16, MANY_PER_CU = 2;      // kv4_plan
+constexpr int FEW_ROWS = 64, FEW_CHUNK = 8, ONE_PER_CU = 3, FEW_PER_CU = 2, MANY_CHUNK = 16, MANY_PER_CU = 1;      // kv4_plan
 
-// The most rows of partial results that a call of up to B requests, max_q rows and max_pages pages has.  Where kv4_plan cuts, the chunks are at most FEW_PER_CU (MANY_PER_CU)
+// The most rows of partial results that a call of up to B requests, max_q rows and max_pages pages has.  Where kv4_plan cuts, the chunks are at most ONE_PER_CU (MANY_PER_CU)
 // workgroups of 16 (256) rows for every compute unit, so no batch has more rows than these hold; and no more than its own times the chunks of the longest table.
 size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
 {
@@ -25,7 +25,7 @@ size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
         return rows < held ? rows : held;
     };
     const int group = Hq / Hkv, q_few = FEW_ROWS / group < 1 ? 0 : FEW_ROWS / group;
-    const long few = max_pages <= 16 ? 0 : at_most(max_q < q_few ? max_q : q_few, FEW_CHUNK, 16L * FEW_PER_CU * num_cus);
+    const long few = max_pages <= 16 ? 0 : at_most(max_q < q_few ? max_q : q_few, FEW_CHUNK, 16L * ONE_PER_CU * num_cus);
     const long many = (long)max_q * group <= FEW_ROWS ? 0 : at_most(max_q, MANY_CHUNK, 256L * MANY_PER_CU * num_cus);
     return (size_t)(few > many ? few : many);
 }
@@ -36,11 +36,21 @@ int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 
 }  // namespace
 
-// Few rows of a cache head: 16 at a time, the requests cut until there are three workgroups for every compute unit (so many fit), but not below 8 pages a chunk, two
-// for each wave, and not at all up to 16 pages: a chunk more costs its start, its merge, and the second launch.  Measured with 1 / 2 / 3 / 4 chunks: 32 x 32 items of
-// up to 32 pages 39.4 / 42.9 / 46.0 / 48.8 us, 64 x 8 of 16 pages 15.8 / 29.1 / 30.1 / 31.4; with 8 / 16 / 24 / 32: 6 x 8 items of up to 126 pages 19.1 / 18.7 / 22.8 / 23.3,
-// 4 x 8 of 2047 87.4 / 87.3 / 89.1 / 89.5, 8 of 313 19.8 / 14.4 / 13.4 / 12.6 (48: 14.7); 2 x 8 of 15 pages with one chunk 6.9, with two 9.3.
-// Many rows: whole requests where the row tiles fill the chip, else chunks of 16 pages or more.
+// Up to 64 rows of a cache head the few-rows kernel, beyond the prompt kernel.  The one / the other, 4 requests of 2000 positions, 64 query on 8 cache heads of 128:
+// 64 rows 21.5 / 37.9 us, 128 36.8 / 45.2, 192 43.5 / 58.4; one of 30000: 64 rows 34.2 / 37.2, 96 45.9 / 39.7; 16 requests of 2000, 32 on 32 heads: 32 rows 54.7 / 98.6, 64 109.9 / 105.2,
+// 96 163.6 / 109.8; 8 on 8 heads of 64, one of 30000: 64 rows 22.4 / 32.3, 128 34.2 / 35.9.
+//
+// Few rows: 16 at a time, the requests cut until there are as many workgroups for every compute unit as fit (three with one token a request; two with several, which for heads of 64 would
+// fit three times too), but not below 8 pages a chunk, two for each wave, and not at all up to 16 pages: a chunk more costs its start, its merge, and the second
+// launch.  Measured with 1 / 2 / 3 / 4 chunks: 32 x 32 items of up to 32 pages 39.4 / 42.9 / 46.0 / 48.8 us, 64 x 8 of 16 pages 15.8 / 29.1 / 30.1 / 31.4; with 8 / 16 / 24 / 32: 6 x 8 items of
+// up to 126 pages 19.1 / 18.7 / 22.8 / 23.3, 4 x 8 of 2047 87.4 / 87.3 / 89.1 / 89.5, 8 of 313 19.8 / 14.4 / 13.4 / 12.6 (48: 14.7); 2 x 8 of 15 pages with one chunk 6.9, with two 9.3.
+// Several tokens a request, for one / two / three workgroups a unit: 4 of up to 50000, 4 tokens, 40 on 40 heads 192 / 124 / 127 us; 6 of up to 12000, 3 tokens, 64 on 8 heads 35.6 / 29.3 / 34.7; 8 of 8000, 2
+// tokens 22.0 / 23.0 / 26.3; 4 of up to 50000, 4 tokens, 8 on 8 heads of 64 27.5 / 24.2 / 24.1, 32 of 2048 10.7 / 15.3 / 16.2.
+//
+// Many rows: whole requests where the row tiles fill the chip, else a workgroup, of which one fits, for every compute unit, and chunks of 16 pages or more.  For one / two / three: 700 tokens on 4096
+// positions, 64 on 8 heads 125 / 235 / 239 us, 32 on 32 125 / 141 / 141; 5 requests of 80 on up to 3000, 40 on 40 heads 71 / 107 / 98; 3 of 150 on up to 6000, 32 on 32 128 / 123 / 118; a prompt of 3000, 8 on 8 heads
+// of 64 110 / 98 / 98.  Chunks of 8 / 16 / 32 pages at least: 64 tokens on 8000 positions, 64 on 8 heads, one request 51 / 57 / 80 us, two 90 / 71 / 90; 128 tokens, 32 on 32 60 / 48 / 66;
+// 3 of 91 on 3388, 8 on 8 of 64 27 / 36 / 53.
 void thi::kv4_plan(Kv4AttnArgs& a, int num_cus)
 {
     const int group = a.Hq / a.Hkv;
@@ -50,7 +60,7 @@ void thi::kv4_plan(Kv4AttnArgs& a, int num_cus)
     if (a.split_rows) {
         const long items = (long)a.B * a.Hkv * a.tiles;
         a.min_chunk = FEW_CHUNK;
-        n = a.max_pages <= 16 ? 1 : (long)FEW_PER_CU * num_cus / items;
+        n = a.max_pages <= 16 ? 1 : (long)(a.max_q > 1 ? FEW_PER_CU : ONE_PER_CU) * num_cus / items;
     } else {
         const long items = (long)a.B * a.Hkv * ((a.tiles + 15) / 16);
         a.min_chunk = MANY_CHUNK;
