@@ -380,7 +380,11 @@ static void append(const Kv4AppendArgs& a, int num_cus, hipStream_t stream)
 {
     constexpr int ROWS = KV4_THREADS / (D / LANE_VALUES);
     const int H = a.Hq + 2 * a.Hkv;
-    if (a.T <= 4 * ROWS) {                        // few tokens, seldom neighbours in a page: the heads of one token in a workgroup, or several
+    // Rows of up to 8 MB: the heads of one token in a workgroup, or several, which have every compute unit busy at once; beyond, many tokens for a workgroup, whose angles are made
+    // once for its heads and whose values are stored as dwords.  One token / many, 64 + 8 + 8 heads of 128: 4 MB of scattered tokens 6.1 / 11.6 us, 8 MB 10.9 / 13.7, 16 MB 19.9 / 18.5, of one run
+    // 5.7 / 10.7, 10.0 / 12.4, 18.7 / 16.7; 40 + 40 + 40 scattered 8.8 / 14.0, 15.3 / 17.0, 26.3 / 26.0, one run 7.7 / 11.0, 12.9 / 12.2, 22.1 / 15.0; 8 + 8 + 8 of 64 scattered 8.6 / 13.7, 14.9 / 16.7,
+    // 27.7 / 25.2, one run 7.4 / 11.2, 12.3 / 11.4, 22.8 / 14.7.
+    if ((double)a.T * H * D * 2 <= 8.0e6) {
         hipLaunchKernelGGL((kv4_append<D, 1>), dim3((unsigned)a.T, (unsigned)((H + ROWS - 1) / ROWS)), dim3(KV4_THREADS), 0, stream, a);
         return;
     }
@@ -407,7 +411,9 @@ static void read(const Kv4ReadArgs& a, hipStream_t stream)
 
 hipError_t launch_kv4_read(const Kv4ReadArgs& a, hipStream_t stream)
 {
-    const bool few = a.T <= 64;                   // seldom neighbours, and too few to give a thread four
+    // Up to 4 MB of keys: a token for a thread, beyond four.  One / four, 32 heads of 128, scattered slots 1 MB 4.0 / 5.9 us, 4 MB 7.2 / 8.3, 8 MB 12.4 / 13.1, one run 3.6 / 4.9,
+    // 5.7 / 5.2, 8.8 / 7.5; 8 heads of 64, scattered 4 MB 7.4 / 8.3, 8 MB 13.1 / 13.6, one run 5.4 / 5.5, 8.7 / 7.6.
+    const bool few = (double)a.T * a.Hkv * a.D * 2 <= 4.0e6;
     if (a.D == 128) few ? read<128, 1>(a, stream) : read<128, 4>(a, stream);
     else few ? read<64, 1>(a, stream) : read<64, 4>(a, stream);
     return hipGetLastError();

@@ -1,4 +1,5 @@
-"""The 4-bit cache's store at its edges: infinities under the norm, special values in every way a value takes into a page, and the one rounding of a query."""
+"""The 4-bit cache's store and read-back at their edges: infinities under the norm, special values in every way a value takes into a page, the one rounding of a query, and calls of
+many tokens, which store and give what calls of few do."""
 import numpy as np
 import pytest
 
@@ -49,7 +50,6 @@ def _slots(kind, T):
 @pytest.mark.parametrize("kind,T", [("aligned", 18), ("aligned", 150), ("unaligned", 150), ("padded", 150)])
 @pytest.mark.parametrize("norm,rope", [(True, True), (True, False), (False, False)])
 def test_special_values(thi, kind, T, D, norm, rope):  # noqa: F811
-    """One token a workgroup up to 128 (D = 64) or 64, then the exchange inside a wave, or LDS where the rows are no whole runs."""
     c = _special(T, 2, D, T + D)
     c["slots"] = _slots(kind, T).astype(np.int32)
     if not norm:
@@ -58,6 +58,76 @@ def test_special_values(thi, kind, T, D, norm, rope):  # noqa: F811
         c["theta"] = c["positions"] = None
     with np.errstate(invalid="ignore"):
         check_append(thi, c, 2, 2, D)
+
+
+def _many_slots(kind, T, rng):
+    if kind == "scattered":
+        return rng.permutation(T + 2 * PAGE)[:T]
+    if kind == "prompts":                                             # runs of odd lengths that begin anywhere, one of them backwards, in pages of random order
+        page, slots = list(rng.permutation(T // PAGE + 40)), []
+        while len(slots) < T:
+            n, at = int(rng.integers(1, 200)), int(rng.integers(0, PAGE))
+            pages = [page.pop() for _ in range((at + n + PAGE - 1) // PAGE)]
+            run = [int(pages[(at + i) // PAGE]) * PAGE + (at + i) % PAGE for i in range(n)]
+            slots += run if n % 7 else run[::-1]
+            if len(page) < 5:
+                page = list(rng.permutation(T // PAGE + 40) + (T // PAGE + 40) * (1 + max(slots) // PAGE // (T // PAGE + 40)))
+        return np.array(slots[:T])
+    return _slots(kind, T)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind", ["aligned", "unaligned", "padded", "scattered", "prompts"])
+@pytest.mark.parametrize("norm", [True, False])
+def test_many_tokens_store_what_few_do(thi, kind, D, norm):  # noqa: F811
+    """One call of rows of more than 8 MB against calls of 61 tokens, bit for bit: four rows that exchange bytes inside a wave, LDS where they are no whole runs, special
+    values among them."""
+    import torch
+    Hq, Hkv, T = 10, 5, 1701 if D == 128 else 3303
+    rng = np.random.default_rng(D + len(kind))
+    c = _special(149, 9, D, 3)                                        # 20 heads a row
+    qkv = dev(np.tile(c["qkv"], (-(-T // 149), 1))[:T])
+    assert qkv.numel() * 2 > 8.2e6
+    slots = _many_slots(kind, T, rng)
+    P = int(slots.max()) // PAGE + 2
+    assert len(set(slots[slots >= 0].tolist())) == (slots >= 0).sum()
+    slots, positions, theta = dev(slots.astype(np.int32)), dev(rng.integers(0, 100000, T).astype(np.int32)), dev(c["theta"])
+    g = dev(c["q_gamma"]) if norm else None
+    say(f"[case] many tokens {kind} D={D} T={T} norm={norm}")
+    start = torch.randint(0, 256, (P, Hkv, 68 * D), dtype=torch.uint8, device="cuda")
+    got = []
+    for piece in (T, 61):
+        pages, q = start.clone(), torch.full((T, Hq, D), 7.0, dtype=torch.float16, device="cuda")
+        for a in range(0, T, piece):
+            e = min(a + piece, T)
+            thi.thi_qk_norm_rope_kv4(qkv[a:e], g, g, 1e-6, positions[a:e].clone(), theta, slots[a:e].clone(), q[a:e], pages)
+        got.append((pages, q))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1].view(torch.int16), got[1][1].view(torch.int16))
+    assert not torch.equal(got[0][0], start)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kind", ["aligned", "unaligned", "padded", "scattered", "prompts"])
+def test_many_tokens_read_what_few_do(thi, kind, D):  # noqa: F811
+    """One call of keys of more than 4 MB (four tokens a thread) against calls of 61 tokens, bit for bit."""
+    import torch
+    Hkv, T = 24, 811 if D == 128 else 1499
+    rng = np.random.default_rng(D + len(kind))
+    slots = _many_slots(kind, T, rng)
+    P = int(slots.max()) // PAGE + 1
+    slots[T // 2 + 40] = P * PAGE                                     # no page
+    pages = torch.randint(0, 256, (P, Hkv, 68 * D), dtype=torch.uint8, device="cuda")
+    assert T * Hkv * D * 2 > 4.1e6
+    say(f"[case] read {kind} D={D} T={T}")
+    slots, got = dev(slots.astype(np.int32)), []
+    for piece in (T, 61):
+        k, v = (torch.full((T, Hkv, D), 7.0, dtype=torch.float16, device="cuda") for _ in range(2))
+        for a in range(0, T, piece):
+            e = min(a + piece, T)
+            thi.thi_kv4_read(pages, slots[a:e].clone(), k[a:e], v[a:e])
+        got.append((k, v))
+    for x, y in zip(*got):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
 
 
 @pytest.mark.parametrize("T", [1, 150])
