@@ -107,7 +107,7 @@ __device__ __forceinline__ void sine_cosine(double x, double& sn, double& cs)
 // The values' codes lie in the page so that four neighbouring positions' bytes of a pair of columns are a dword (kv4.h); stored by
 // themselves, 4001 tokens of 40 heads made 10 million byte stores, and the call took 83 us.  With ROWS tokens a workgroup stores dwords: where all its rows are runs of
 // four that begin a dword, four rows exchange bytes within their wave; elsewhere it collects them in LDS, with two barriers a head, and stores dwords where a run allows it.
-// 4001 tokens of 40+40+40 heads (186 MB): 58 us through LDS, 49.6 within waves (3.8 TB/s).  Four workgroups a compute unit: at 130 registers three fitted, and the rest
+// 4001 tokens of 40+40+40 heads (186 MB): 58 us through LDS, 50 within waves (3.7 TB/s).  Four workgroups a compute unit: at 130 registers three fitted, and the rest
 // of the grid was a second round (with the read-back 93 us instead of 77).
 template <int D, int TT>
 __global__ __launch_bounds__(KV4_THREADS, 4) void kv4_append(Kv4AppendArgs a)

@@ -51,6 +51,9 @@ int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 // positions, 64 on 8 heads 125 / 235 / 239 us, 32 on 32 125 / 141 / 141; 5 requests of 80 on up to 3000, 40 on 40 heads 71 / 107 / 98; 3 of 150 on up to 6000, 32 on 32 128 / 123 / 118; a prompt of 3000, 8 on 8 heads
 // of 64 110 / 98 / 98.  Chunks of 8 / 16 / 32 pages at least: 64 tokens on 8000 positions, 64 on 8 heads, one request 51 / 57 / 80 us, two 90 / 71 / 90; 128 tokens, 32 on 32 60 / 48 / 66;
 // 3 of 91 on 3388, 8 on 8 of 64 27 / 36 / 53.
+//
+// Every request is dealt as one of max_q rows, for the host knows no others: single tokens with long contexts do better in a call of their own (a chunk of 512 tokens on 8000 positions with three of
+// them on 131000, 64 on 8 heads: 2414 us in one call, 309 in two).
 void thi::kv4_plan(Kv4AttnArgs& a, int num_cus)
 {
     const int group = a.Hq / a.Hkv;
@@ -64,7 +67,7 @@ void thi::kv4_plan(Kv4AttnArgs& a, int num_cus)
     } else {
         const long items = (long)a.B * a.Hkv * ((a.tiles + 15) / 16);
         a.min_chunk = MANY_CHUNK;
-        n = items >= num_cus ? 1 : (long)MANY_PER_CU * num_cus / items;
+        n = (long)MANY_PER_CU * num_cus / items;
     }
     const long most = (a.max_pages + a.min_chunk - 1) / a.min_chunk;
     n = n < 1 ? 1 : n > KV4_MAX_SPLIT ? KV4_MAX_SPLIT : n;

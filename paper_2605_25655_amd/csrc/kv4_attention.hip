@@ -527,10 +527,12 @@ hipError_t launch_decode(const Kv4AttnArgs& a, hipStream_t stream)
 // between them, convert it to fp16 and leave it in LDS in the order in which the matrix operands are read (a lane's 16 bytes behind
 // its neighbour's: no bank conflicts, no address arithmetic); two such buffers, and the codes of the page behind in registers.  Products and
 // the lanes' order of positions are the few-rows kernel's; a wave holds CT tiles of 16 rows, each operand read from LDS feeds CT products.
-// Bound by the matrix cores and the vector ALU together (an exponential costs a wave 16 cycles, 16 of them and some 50 plain instructions against 32 products of
-// 16 cycles per page and tile).
+// Bound by neither the matrix cores (busy 35 % of a prompt of 4096 tokens, 40 heads: some 223 us) nor the vector ALU (41 %; an exponential costs a wave 16 cycles, 16 of them and some 50 plain
+// instructions against 32 products of 16 cycles per page and tile): a page takes a SIMD some 5100 cycles, of which its two waves' products are 2180 and their vector work about as many, so that the
+// turns hardly overlap.  Causal tiles add an eighth (640 tiles of 4 to 64 pages end after 99 pages on the busiest unit, 87.5 on the mean one).  At heads of 128 six registers spill (28 bytes of scratch).
 //
-// A weight is one fp16 number here (off by as much as the result is by its own rounding): 2^9 p of a maximum that may lag by 2^6, so that weights down
+// A weight is one fp16 number here, as the sums that divide the result take it (error against 64 bits 2.4e-4 to 2.5e-4, of which the result's own rounding is 2.1e-4; a
+// second summand would take 36 products more to the 68 of a page and wave): 2^9 p of a maximum that may lag by 2^6, so that weights down
 // to 2^-23 are normal numbers.  The sums are rescaled when some row's maximum has grown by more, which costs as much as the rest of a page's vector work, and all
 // waves wait for the one: with 2^11 and a lag of 2^4 that was most iterations.
 constexpr int KP_WAVES = 8, KP_AHEAD = 2;
