@@ -304,6 +304,77 @@ int thi_kv4_compact(const int* refs_in, const int* table_in, int* refs_out, int*
                     int layers, size_t layer_bytes, int rows, int num_pages, int max_pages, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * ---- A paged key/value cache in fp16, and ways to bound it --------------------------------------------------
+ *
+ * What it holds.  A page holds THI_KV16_PAGE positions of all cache heads of one layer: thi_kv16_page_bytes(Hkv, D) = 256 D bytes per head, D = 64 or
+ * 128, the keys and then the values, fp16, in the order in which matrix operands take them:
+ *   keys     64 D values  [position / 16][column / 32][column % 32 / 8][position % 16][column % 8]
+ *   values   64 D values  [position / 32][column / 16][position % 16 / 4][column % 16][position % 32 / 16][position % 4]
+ * `pages` is [num_pages][Hkv][128 D], 16-byte aligned; num_pages * 64 must fit an int32 (THI_ERR_SHAPE).  Byte offsets are 64-bit.
+ *
+ * Who has which page: page_table and seq_lens as in the 4-bit cache (an entry outside [0, num_pages) is no page, and its positions are not attended to), up to 2^24
+ * pages a row (THI_ERR_SHAPE).  thi_kv4_fork and thi_kv4_compact serve these pages too.  Nothing in device memory is checked on the host; whatever stands there, no
+ * access leaves the buffers.  None of these calls allocates or waits, all can be captured into a graph, and no workspace needs preparation; calls that may run at the same time need
+ * workspaces of their own.
+ */
+#define THI_KV16_PAGE 64
+size_t thi_kv16_page_bytes(int Hkv, int D);
+
+/*
+ * thi_qk_norm_rope_kv4 with this cache: q_out = y(query), the cache at slots[t] = (y(key), value).  Arguments, slots and refusals are the same.  Norm and rotation in
+ * fp32, angles in 64 bits, one rounding to fp16; values are stored as they are.
+ */
+int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const void* k_gamma, float eps, const int* positions, const float* theta,
+                          const int* slots, void* q_out, void* pages, int T, int Hq, int Hkv, int D, int num_pages, void* hip_stream);
+
+/*
+ * Attention of each request's new tokens over its pages (Eq. 6 per head, grouped-query as thi_decode_attention):
+ *
+ *   out[t,h,:] = sum_j p_j v_j,  p = softmax_j(scale * q[t,h,:] . k_j)  over the positions j that have a page and that the token sees:
+ *   j <= P = seq_lens[b] - n_b + i  and, with window > 0,  (j > P - window  or  j < sinks)
+ *
+ * for row t = q_offsets[b] + i, i < n_b = q_offsets[b+1] - q_offsets[b]: the new tokens are the request's last n_b positions, already in the cache.  window 0: everything in
+ * front of a token (sinks mean nothing then); positions are places in the page table, so that behind an eviction the window counts what was kept.  Negative ones:
+ * THI_ERR_SHAPE.  A row that sees no position is zero.  What a row does not see does not matter to it, NaN and infinities among it; pages outside every window are not read.
+ * q, out [T,Hq,D] fp16; q_offsets [B+1] int32 device memory, not decreasing, or NULL: one token per request, T = B.  max_q <= 65535 is the largest n_b (from the
+ * host, it sizes the launch; rows of a request past it are not written, and it is as if their positions were not there).
+ *
+ * weights_out (or NULL) [B][Hkv][64 max_pages] fp32: what each position got of the attention, for thi_kv16_evict:
+ *   weights_out[b,g,j] = before + sum of p_j over the request's rows and the query heads of cache head g,  j < seq_lens[b]
+ * where before is weights_in[b,g,j] (the same shape, or the same buffer; NULL: 0) for the positions in front of the new tokens and 0 for theirs.  Entries from seq_lens[b] on
+ * are not written.
+ *
+ * Scores, statistics and sums are fp32, weights reach the matrix cores as fp16 (two summands up to 64 rows of a cache head, one beyond).  Workspace:
+ * thi_kv16_attention_workspace_bytes(), 256-byte aligned; what that says for the largest B, T, max_q and max_pages does for every smaller call with these heads
+ * (weights != 0: with weights_out).  Reproducible bit for bit.
+ */
+size_t thi_kv16_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages, int weights);
+int thi_kv16_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, int window, int sinks,
+                       void* out, const float* weights_in, float* weights_out, int B, int T, int Hq, int Hkv, int D, int max_q, int num_pages, int max_pages,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Requests that are longer than `budget` are brought back to it, in all layers at once.  Of such a row's positions that have a page, each cache head of each layer keeps
+ * min(budget, as many as there are): the first `sinks` and the last `recent` positions, and of the others those with the largest weights_in (of equal ones the
+ * lower position; a NaN is below everything).  They move, in their order, to positions 0 ..., in fresh pages: the lowest free ones of refs_in (count 0), in
+ * the order of rows and entries, enough for the kept positions and `headroom` more (at most max_pages); entries behind are -1.  From the first row on whose fresh pages are
+ * not there any more, rows stay as they are.  Rows within the budget stay as they are, too.
+ *
+ * The counts, tables, lengths and weights given are read, the *_out ones written (other buffers; THI_ERR_SHAPE if the same), and no page that anyone has is written, so
+ * that launches in flight may still read the old ones, and rows may share pages.  refs_out = refs_in - a moved row's entries in the old table + its fresh pages.
+ * weights_out: the kept positions' weights in their new places; entries from lens_out[b] on are not written.  info (may be NULL) [2]: rows moved, rows over the budget that
+ * stayed for want of pages.
+ *
+ * refs_* [num_pages], table_* [rows][max_pages], lens_* [rows] int32; weights_* [layers][rows][Hkv][64 max_pages] fp32; pages: layer l's pool begins at
+ * pages + l * layer_bytes (a multiple of 16).  1 <= budget, 0 <= sinks, recent, headroom, sinks + recent <= budget, layers * rows <= 65535 (THI_ERR_SHAPE).
+ * Workspace: thi_kv16_evict_workspace_bytes(), 256-byte aligned.
+ */
+size_t thi_kv16_evict_workspace_bytes(int layers, int rows, int Hkv, int max_pages, int num_pages);
+int thi_kv16_evict(const int* refs_in, const int* table_in, const int* lens_in, const float* weights_in, int budget, int sinks, int recent, int headroom,
+                   int* refs_out, int* table_out, int* lens_out, float* weights_out, int* info, void* pages, size_t layer_bytes, int layers, int rows,
+                   int Hkv, int D, int num_pages, int max_pages, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Bytes of workspace the given operator needs for the given shape
  * (op = thi_op; (M, N, K) for the first two operators, (M, H, I) for the MLP).
  * Pure host arithmetic: touches no device.  Returns 0 for invalid arguments.

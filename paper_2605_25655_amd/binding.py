@@ -14,6 +14,7 @@ THI_OK = 0
 THI_ERR_WORKSPACE = 4
 THI_ERR_TIMEOUT = 6
 THI_KV4_PAGE = 64
+THI_KV16_PAGE = 64
 THI_OP_RMSNORM_QKV, THI_OP_LINEAR, THI_OP_SWIGLU_MLP = 0, 1, 2
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -27,6 +28,8 @@ EXPORTED_SYMBOLS = (
     "thi_linear_residual", "thi_rmsnorm_swiglu_mlp", "thi_decode_attention", "thi_attention_workspace_bytes",
     "thi_kv4_page_bytes", "thi_qk_norm_rope_kv4", "thi_kv4_read", "thi_kv4_attention_workspace_bytes", "thi_kv4_attention",
     "thi_kv4_pages_workspace_bytes", "thi_kv4_fork", "thi_kv4_compact",
+    "thi_kv16_page_bytes", "thi_qk_norm_rope_kv16", "thi_kv16_attention_workspace_bytes", "thi_kv16_attention",
+    "thi_kv16_evict_workspace_bytes", "thi_kv16_evict",
     "thi_workspace_bytes",
     "thi_workspace_init", "thi_workspace_status", "thi_debug_handover", "thi_status_string", "thi_version", "thi_set_kernel_family", "thi_set_rowblock_split", "thi_set_mlp_fusion", "thi_query_kernel_family",
 )
@@ -94,6 +97,18 @@ def load_library():
     lib.thi_kv4_fork.restype = ci
     lib.thi_kv4_compact.argtypes = [vp] * 6 + [sz, ci, sz, ci, ci, ci, vp, sz, vp]
     lib.thi_kv4_compact.restype = ci
+    lib.thi_kv16_page_bytes.argtypes = [ci, ci]
+    lib.thi_kv16_page_bytes.restype = sz
+    lib.thi_qk_norm_rope_kv16.argtypes = [vp, ci, vp, vp, cf, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp]
+    lib.thi_qk_norm_rope_kv16.restype = ci
+    lib.thi_kv16_attention_workspace_bytes.argtypes = [ci] * 8
+    lib.thi_kv16_attention_workspace_bytes.restype = sz
+    lib.thi_kv16_attention.argtypes = [vp, vp, vp, vp, vp, cf, ci, ci, vp, vp, vp] + [ci] * 8 + [vp, sz, vp]
+    lib.thi_kv16_attention.restype = ci
+    lib.thi_kv16_evict_workspace_bytes.argtypes = [ci] * 5
+    lib.thi_kv16_evict_workspace_bytes.restype = sz
+    lib.thi_kv16_evict.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, sz] + [ci] * 6 + [vp, sz, vp]
+    lib.thi_kv16_evict.restype = ci
     lib.thi_workspace_bytes.argtypes = [ci, ci, ci, ci]
     lib.thi_workspace_bytes.restype = sz
     lib.thi_workspace_init.argtypes = [vp, sz, vp]
@@ -395,6 +410,66 @@ def thi_kv4_compact(refs_in, table_in, refs_out, table_out, info, pages, workspa
                                         layer_bytes, table_in.shape[0], refs_in.shape[0], table_in.shape[1], wp, wb, _stream(stream))
     if check and rc != THI_OK:
         raise ThiError(rc, "thi_kv4_compact")
+    return rc
+
+
+def thi_kv16_page_bytes(Hkv: int, D: int) -> int:
+    """Bytes of one page (THI_KV16_PAGE positions of Hkv heads of D) of the fp16 cache; 0 for heads it does not hold."""
+    return int(load_library().thi_kv16_page_bytes(int(Hkv), int(D)))
+
+
+def thi_qk_norm_rope_kv16(qkv, q_gamma, k_gamma, eps: float, positions, theta, slots, q_out, pages, stream=None, check: bool = True) -> int:
+    """q_out = rotated, normalised queries of qkv's rows; their keys and values into the fp16 cache at `slots`.
+
+    qkv [T, >= (Hq+2Hkv)*D] fp16 (rows may be strided); q_gamma, k_gamma [D] fp16 or None; positions [T] int32 and theta [D/2] fp32, or both None;
+    slots [T] int32; q_out [T,Hq,D] fp16; pages [num_pages,Hkv,128*D] fp16."""
+    T, Hq, D = q_out.shape
+    rc = load_library().thi_qk_norm_rope_kv16(_ptr(qkv), qkv.stride(0), _ptr(q_gamma), _ptr(k_gamma), eps, _ptr(positions), _ptr(theta),
+                                              _ptr(slots), _ptr(q_out), _ptr(pages), T, Hq, pages.shape[1], D, pages.shape[0], _stream(stream))
+    if check and rc != THI_OK:
+        raise ThiError(rc, "thi_qk_norm_rope_kv16")
+    return rc
+
+
+def thi_kv16_attention_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, max_q: int, max_pages: int, weights: bool = False) -> int:
+    return int(load_library().thi_kv16_attention_workspace_bytes(int(B), int(T), int(Hq), int(Hkv), int(D), int(max_q), int(max_pages), int(bool(weights))))
+
+
+def thi_kv16_attention(q, pages, page_table, seq_lens, q_offsets, scale, window: int, sinks: int, out, max_q: int, workspace, weights_in=None,
+                       weights_out=None, stream=None, check: bool = True) -> int:
+    """out[T,Hq,D] = softmax(scale q k^T) v per head of each request's new tokens over its pages of the fp16 cache.
+
+    q, out [T,Hq,D] fp16; pages [num_pages,Hkv,128*D] fp16; page_table [B,max_pages], seq_lens [B] int32; q_offsets [B+1] int32 (the rows of
+    request b) or None (one row each); max_q: the most rows of a request; window: how many positions up to its own a token sees, besides the first `sinks`
+    (0: all); weights_out [B,Hkv,64*max_pages] fp32 or None = weights_in (or None: 0) + what each position got of the attention."""
+    T, Hq, D = q.shape
+    B, max_pages = page_table.shape
+    wp, wb = _ws(workspace)
+    rc = load_library().thi_kv16_attention(_ptr(q), _ptr(pages), _ptr(page_table), _ptr(seq_lens), _ptr(q_offsets), scale, window, sinks, _ptr(out),
+                                           _ptr(weights_in), _ptr(weights_out), B, T, Hq, pages.shape[1], D, max_q, pages.shape[0], max_pages, wp, wb,
+                                           _stream(stream))
+    if check and rc != THI_OK:
+        raise ThiError(rc, "thi_kv16_attention")
+    return rc
+
+
+def thi_kv16_evict_workspace_bytes(layers: int, rows: int, Hkv: int, max_pages: int, num_pages: int) -> int:
+    return int(load_library().thi_kv16_evict_workspace_bytes(int(layers), int(rows), int(Hkv), int(max_pages), int(num_pages)))
+
+
+def thi_kv16_evict(refs_in, table_in, lens_in, weights_in, budget: int, sinks: int, recent: int, headroom: int, refs_out, table_out, lens_out, weights_out,
+                   info, pages, workspace, stream=None, check: bool = True) -> int:
+    """Rows longer than `budget` keep that many positions, each cache head of each layer its own: the first `sinks`, the last `recent`, the heaviest others.
+
+    int32: refs_* [num_pages], table_* [rows,max_pages], lens_* [rows], info [2] (or None); weights_* [layers,rows,Hkv,64*max_pages] fp32; pages
+    [layers,num_pages,Hkv,128*D] fp16 (a layer's pool contiguous)."""
+    layers, num_pages, Hkv, values = pages.shape
+    wp, wb = _ws(workspace)
+    rc = load_library().thi_kv16_evict(_ptr(refs_in), _ptr(table_in), _ptr(lens_in), _ptr(weights_in), budget, sinks, recent, headroom, _ptr(refs_out),
+                                       _ptr(table_out), _ptr(lens_out), _ptr(weights_out), _ptr(info), _ptr(pages), pages.stride(0) * pages.element_size(),
+                                       layers, table_in.shape[0], Hkv, values // 128, num_pages, table_in.shape[1], wp, wb, _stream(stream))
+    if check and rc != THI_OK:
+        raise ThiError(rc, "thi_kv16_evict")
     return rc
 
 

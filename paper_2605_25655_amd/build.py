@@ -16,7 +16,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libthi.so")
 PROBE_LIB = os.path.join(PKG, "libthi_probe.so")      # measurement probes: not part of the product library
 SOURCES = ["api.hip", "plan.hip", "skinny.hip", "rowslab.hip", "rowblock.hip", "attention.hip", "gemm.hip", "midgemm.hip",
-           "kv4_api.hip", "kv4.hip", "kv4_attention.hip", "pages.hip"]
+           "kv4_api.hip", "kv4.hip", "kv4_attention.hip", "pages.hip",
+           "kv16_api.hip", "kv16.hip", "kv16_attention.hip", "kv16_evict.hip"]
 PROBE_SOURCES = ["probes.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

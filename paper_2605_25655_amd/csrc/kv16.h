@@ -1,0 +1,72 @@
+// The paged key/value cache in fp16: page layout, argument blocks and launchers of kv16.hip, kv16_attention.hip and kv16_evict.hip.
+#pragma once
+
+#include "thi_internal.h"
+
+namespace thi {
+
+// A page holds KV16_PAGE positions of all cache heads of one layer, 128 D values per head: 64 D of keys, 64 D of values.  Their order is the one in which
+// the attention kernels' lanes take them (lane = 16 hi + lo of a 16x16x32 matrix operand, eight values a lane), so that every operand is 1 KB of contiguous memory:
+//   keys   : [tile of 16 positions][block of 32 columns][hi][lo = position % 16][column % 8]
+//   values : [half page][tile of 16 columns][hi][lo = column % 16][i][r] for position 32 half + 16 i + 4 hi + r: a lane's eight positions are those whose weights the
+//            scores' product leaves in the lanes of the same hi, so nothing crosses lanes between the two products.
+constexpr int KV16_PAGE = 64;
+constexpr int kv16_head_values(int D) { return 128 * D; }
+constexpr int kv16_values(int D) { return 64 * D; }
+__host__ __device__ constexpr int kv16_key_at(int pos, int part, int D) { return (pos >> 4) * 16 * D + part * 128 + (pos & 15) * 8; }      // columns 8 part ..
+__host__ __device__ constexpr int kv16_value_at(int pos, int col, int D)
+{
+    return 64 * D + (pos >> 5) * 32 * D + (col >> 4) * 512 + ((pos >> 2) & 3) * 128 + (col & 15) * 8 + ((pos >> 4) & 1) * 4 + (pos & 3);
+}
+
+struct Kv16AppendArgs {
+    const uint16_t* qkv;                 // [T, ld]
+    const uint16_t *q_gamma, *k_gamma;   // [D] or nullptr
+    const int* positions;                // [T], with theta
+    const float* theta;                  // [D/2] or nullptr: no rotation
+    const int* slots;                    // [T] page * KV16_PAGE + position in it; outside the pool: not stored
+    uint16_t* q_out;                     // [T,Hq,D]
+    uint16_t* pages;
+    float eps;
+    int T, ld, Hq, Hkv, D, num_pages;
+};
+hipError_t launch_kv16_append(const Kv16AppendArgs& a, int num_cus, hipStream_t stream);
+
+struct Kv16AttnArgs {
+    const uint16_t* q;               // [T,Hq,D]
+    const uint16_t* pages;
+    const int* page_table;           // [B,max_pages]
+    const int* seq_lens;             // [B]
+    const int* q_offsets;            // [B+1] or nullptr: one token per request
+    uint16_t* out;                   // [T,Hq,D]
+    const float* weights_in;         // [B,Hkv,64 max_pages] or nullptr: nothing so far
+    float* weights_out;              // the same shape, or nullptr: not asked for
+    float scale2;                    // softmax scale times log2(e)
+    int window, sinks;               // window 0: everything in front of a token
+    int B, T, Hq, Hkv, D, max_q, num_pages, max_pages;
+    // how the rows are dealt (kv16_plan)
+    float* part;                     // [B][max_q][Hq][nsplit][D + 2]: a chunk's unnormalised output, maximum, sum
+    float* stats;                    // [B][max_q][Hq][2]: a row's maximum and one over its sum, with weights_out
+    bool split_rows;                 // 16 rows of a cache head at a time, cut along the positions
+    int tiles;                       // tiles of 16 rows
+    int nsplit, min_chunk;           // chunks per request at most, pages per chunk at least
+};
+constexpr int KV16_MAX_SPLIT = 64;
+void kv16_plan(Kv16AttnArgs& a, int num_cus);
+hipError_t launch_kv16_attention(const Kv16AttnArgs& a, hipStream_t stream);
+
+struct Kv16EvictArgs {
+    const int *refs_in, *table_in, *lens_in;
+    const float* weights_in;         // [layers][rows][Hkv][64 max_pages]
+    int *refs_out, *table_out, *lens_out;
+    float* weights_out;
+    int* info;
+    uint16_t* pages;
+    size_t layer_values;             // from layer to layer
+    int budget, sinks, recent, headroom, layers, rows, Hkv, D, num_pages, max_pages;
+    int* ws;                         // kv16_evict_words()
+};
+size_t kv16_evict_words(int layers, int rows, int Hkv, int max_pages, int num_pages);
+hipError_t launch_kv16_evict(const Kv16EvictArgs& a, int num_cus, hipStream_t stream);
+
+}  // namespace thi

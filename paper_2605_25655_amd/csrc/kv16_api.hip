@@ -1,0 +1,149 @@
+// C-ABI entry points of the fp16 cache's operators: argument validation and launches.  Declarations and contract: include/thi.h.
+#include "../../include/thi.h"
+#include "kv16.h"
+
+namespace {
+
+using namespace thi;
+
+inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+
+bool heads_ok(int Hq, int Hkv, int D) { return Hq >= 1 && Hkv >= 1 && Hq <= 65535 && Hkv <= 65535 && Hq % Hkv == 0 && (D == 64 || D == 128); }
+
+// slots are int32: the pool's last position has to have one
+bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff / KV16_PAGE; }
+
+constexpr int MAX_PAGES = 1 << 24;      // of a row of the page table: positions stay below 2^30
+
+constexpr int FEW_CHUNK = 4, FEW_PER_CU = 2;      // kv16_plan
+
+size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
+
+// The most rows of partial results that a call of up to B requests, max_q rows and max_pages pages has.  Where kv16_plan cuts, the chunks are at most FEW_PER_CU
+// workgroups of 16 rows for every compute unit, so no batch has more rows than these hold; and no more than its own times the chunks of the longest table.
+size_t most_rows(int B, int Hq, int max_q, int max_pages, int num_cus)
+{
+    const long held = 16L * FEW_PER_CU * num_cus, chunks = (max_pages + FEW_CHUNK - 1) / FEW_CHUNK, own = (long)B * max_q * Hq;
+    const long rows = chunks < 2 ? 0 : own > held ? held : own * (chunks < KV16_MAX_SPLIT ? chunks : KV16_MAX_SPLIT);
+    return (size_t)(rows < held ? rows : held);
+}
+size_t bytes_of_rows(size_t rows, int D) { return rows ? round_up(rows * (D + 2) * sizeof(float)) : 256; }
+size_t bytes_of_stats(int B, int Hq, int max_q) { return round_up((size_t)B * max_q * Hq * 2 * sizeof(float)); }
+
+int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
+
+}  // namespace
+
+void thi::kv16_plan(Kv16AttnArgs& a, int num_cus)
+{
+    const int group = a.Hq / a.Hkv;
+    a.tiles = (int)(((long)a.max_q * group + 15) / 16);
+    a.split_rows = true;
+    const long items = (long)a.B * a.Hkv * a.tiles;
+    a.min_chunk = FEW_CHUNK;
+    long n = (long)FEW_PER_CU * num_cus / items;
+    const long most = (a.max_pages + a.min_chunk - 1) / a.min_chunk;
+    n = n < 1 ? 1 : n > KV16_MAX_SPLIT ? KV16_MAX_SPLIT : n;
+    a.nsplit = (int)(n > most ? most : n);
+}
+
+extern "C" {
+
+size_t thi_kv16_page_bytes(int Hkv, int D)
+{
+    return heads_ok(Hkv, Hkv, D) ? (size_t)Hkv * kv16_head_values(D) * 2 : 0;
+}
+
+int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const void* k_gamma, float eps, const int* positions, const float* theta,
+                          const int* slots, void* q_out, void* pages, int T, int Hq, int Hkv, int D, int num_pages, void* hip_stream)
+{
+    if (!qkv || !slots || !q_out || !pages || (theta && !positions)) return THI_ERR_NULL;
+    if (T < 1 || !heads_ok(Hq, Hkv, D) || !pool_ok(num_pages)) return THI_ERR_SHAPE;
+    if ((ld & 7) || ld < (long)(Hq + 2 * Hkv) * D) return THI_ERR_SHAPE;
+    if (misaligned(qkv, 16) || misaligned(q_gamma, 16) || misaligned(k_gamma, 16) || misaligned(q_out, 16) || misaligned(pages, 16) ||
+        misaligned(positions, 4) || misaligned(theta, 4) || misaligned(slots, 4))
+        return THI_ERR_ALIGN;
+    (void)hipGetLastError();      // an error another user of the runtime left behind is not ours to report
+    Kv16AppendArgs a{};
+    a.qkv = (const uint16_t*)qkv;
+    a.q_gamma = (const uint16_t*)q_gamma;
+    a.k_gamma = (const uint16_t*)k_gamma;
+    a.positions = positions;
+    a.theta = theta;
+    a.slots = slots;
+    a.q_out = (uint16_t*)q_out;
+    a.pages = (uint16_t*)pages;
+    a.eps = eps;
+    a.T = T; a.ld = ld; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.num_pages = num_pages;
+    return finish(launch_kv16_append(a, device_cu_count(), (hipStream_t)hip_stream));
+}
+
+size_t thi_kv16_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages, int weights)
+{
+    if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_q > 65535 || max_pages < 1 || max_pages > MAX_PAGES) return 0;
+    return bytes_of_rows(most_rows(B, Hq, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, max_q) : 0);
+}
+
+int thi_kv16_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, int window, int sinks,
+                       void* out, const float* weights_in, float* weights_out, int B, int T, int Hq, int Hkv, int D, int max_q, int num_pages, int max_pages,
+                       void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!q || !pages || !page_table || !seq_lens || !out || !workspace || (weights_in && !weights_out)) return THI_ERR_NULL;
+    if (!thi_kv16_attention_workspace_bytes(B, T, Hq, Hkv, D, max_q, max_pages, 0) || !pool_ok(num_pages) || (!q_offsets && (T != B || max_q != 1))) return THI_ERR_SHAPE;
+    if (window < 0 || sinks < 0) return THI_ERR_SHAPE;
+    if (misaligned(q, 16) || misaligned(pages, 16) || misaligned(out, 16) || misaligned(page_table, 4) || misaligned(seq_lens, 4) ||
+        misaligned(q_offsets, 4) || misaligned(weights_in, 4) || misaligned(weights_out, 4) || misaligned(workspace, 256))
+        return THI_ERR_ALIGN;
+    Kv16AttnArgs a{};
+    a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.num_pages = num_pages; a.max_pages = max_pages;
+    a.window = window;
+    a.sinks = window ? sinks : 0;
+    kv16_plan(a, device_cu_count());
+    const size_t stats = weights_out ? bytes_of_stats(B, Hq, max_q) : 0;
+    if (workspace_bytes < stats + bytes_of_rows(a.nsplit > 1 ? (size_t)B * max_q * Hq * a.nsplit : 0, D)) return THI_ERR_WORKSPACE;
+    (void)hipGetLastError();
+    a.q = (const uint16_t*)q;
+    a.pages = (const uint16_t*)pages;
+    a.page_table = page_table;
+    a.seq_lens = seq_lens;
+    a.q_offsets = q_offsets;
+    a.out = (uint16_t*)out;
+    a.weights_in = weights_in;
+    a.weights_out = weights_out;
+    a.scale2 = scale * 1.44269504088896340736f;
+    if (a.scale2 == 0.f) a.scale2 = 1e-30f;      // (all weights equal either way; a masked score of -inf stays what it is)
+    a.stats = weights_out ? (float*)workspace : nullptr;
+    a.part = (float*)((char*)workspace + stats);
+    return finish(launch_kv16_attention(a, (hipStream_t)hip_stream));
+}
+
+size_t thi_kv16_evict_workspace_bytes(int layers, int rows, int Hkv, int max_pages, int num_pages)
+{
+    if (layers < 1 || rows < 1 || layers > 65535 || rows > 65535 || (long)layers * rows > 65535 || !heads_ok(Hkv, Hkv, 64) || max_pages < 1 || max_pages > MAX_PAGES ||
+        !pool_ok(num_pages))
+        return 0;
+    return round_up(kv16_evict_words(layers, rows, Hkv, max_pages, num_pages) * 4);
+}
+
+int thi_kv16_evict(const int* refs_in, const int* table_in, const int* lens_in, const float* weights_in, int budget, int sinks, int recent, int headroom,
+                   int* refs_out, int* table_out, int* lens_out, float* weights_out, int* info, void* pages, size_t layer_bytes, int layers, int rows,
+                   int Hkv, int D, int num_pages, int max_pages, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!refs_in || !table_in || !lens_in || !weights_in || !refs_out || !table_out || !lens_out || !weights_out || !pages || !workspace) return THI_ERR_NULL;
+    const size_t need = thi_kv16_evict_workspace_bytes(layers, rows, Hkv, max_pages, num_pages);
+    if (!need || !heads_ok(Hkv, Hkv, D)) return THI_ERR_SHAPE;
+    if (budget < 1 || sinks < 0 || recent < 0 || headroom < 0 || (long)sinks + recent > budget) return THI_ERR_SHAPE;
+    if (refs_out == refs_in || table_out == table_in || lens_out == lens_in || weights_out == weights_in) return THI_ERR_SHAPE;
+    if ((layer_bytes & 15) || (layers > 1 && layer_bytes < thi_kv16_page_bytes(Hkv, D) * (size_t)num_pages)) return THI_ERR_SHAPE;
+    const void* const words[] = {refs_in, table_in, lens_in, weights_in, refs_out, table_out, lens_out, weights_out, info};
+    for (const void* p : words)
+        if (misaligned(p, 4)) return THI_ERR_ALIGN;
+    if (misaligned(pages, 16) || misaligned(workspace, 256)) return THI_ERR_ALIGN;
+    if (workspace_bytes < need) return THI_ERR_WORKSPACE;
+    (void)hipGetLastError();
+    const Kv16EvictArgs a{refs_in, table_in, lens_in, weights_in, refs_out, table_out, lens_out, weights_out, info, (uint16_t*)pages, layer_bytes / 2,
+                          budget, sinks, recent, headroom, layers, rows, Hkv, D, num_pages, max_pages, (int*)workspace};
+    return finish(launch_kv16_evict(a, device_cu_count(), (hipStream_t)hip_stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,490 @@
+// Attention over the paged fp16 cache.  out = softmax(scale q K^T) V per head, K and V in pages; row i of a request's n new tokens stands at position
+// length - n + i and sees the positions up to its own whose page exists: all of them, or with a window the last `window` and the first `sinks`.
+#include "kv16.h"
+
+#include <mutex>
+#include <type_traits>
+
+namespace thi {
+
+namespace {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+#define GLOBAL __attribute__((address_space(1)))
+
+// What a request's rows are -- [first, first + n) of q, the last n of `len` positions -- and which pages any of them sees: the `lead` first ones (sinks), then those from
+// `skip` pages further on.  Whatever the arrays hold stays within the buffers.
+struct Request {
+    int first, n, len;
+    int lead, skip, pages;           // the v-th page to look at, v < pages, is page v of the request, or v + skip from v = lead on
+};
+__device__ __forceinline__ Request find_request(const Kv16AttnArgs& a, int b)
+{
+    Request r{b, 1, a.seq_lens[b], 0, 0, 0};
+    const long most = (long)a.max_pages * KV16_PAGE;
+    r.len = r.len < 0 ? 0 : r.len > most ? (int)most : r.len;
+    if (a.q_offsets) {
+        int o0 = a.q_offsets[b], o1 = a.q_offsets[b + 1];
+        o0 = o0 < 0 ? 0 : o0 > a.T ? a.T : o0;
+        o1 = o1 < o0 ? o0 : o1 > a.T ? a.T : o1;
+        r.first = o0;
+        r.n = o1 - o0 < a.max_q ? o1 - o0 : a.max_q;
+        // rows past max_q, which are not written, and the positions that only they see (fewer positions than that: the others see nothing, as with none)
+        const int left = o1 - o0 - r.n;
+        r.len = r.len > left ? r.len - left : 0;
+    }
+    r.pages = (r.len + KV16_PAGE - 1) / KV16_PAGE;
+    if (a.window > 0) {
+        const int before = r.len - r.n + 1;                                   // positions up to the first row's own
+        const int from = before > a.window ? (before - a.window) / KV16_PAGE : 0;
+        const int sinks = a.sinks / KV16_PAGE + (a.sinks % KV16_PAGE != 0);
+        r.lead = sinks < from ? sinks : from;
+        r.skip = from - r.lead;
+        r.pages -= r.skip;
+    }
+    return r;
+}
+__device__ __forceinline__ int page_number(const Request& r, int v) { return v < r.lead ? v : v + r.skip; }
+
+// What a row sees: positions below `end`, from `from` on or below the sinks.
+struct Sight {
+    int from, end;
+};
+__device__ __forceinline__ Sight sight_of(const Kv16AttnArgs& a, const Request& rq, int token)
+{
+    const int end = rq.len - rq.n + token + 1;
+    return Sight{a.window > 0 && end > a.window ? end - a.window : 0, end};
+}
+__device__ __forceinline__ bool sees(const Sight& s, int sinks, int pos) { return pos < s.end && (pos >= s.from || pos < sinks); }
+
+// Pages per chunk of a request that looks at `pages` of them: a function of its own length and of how many workgroups the call has, so that a
+// request's chunk borders, and with them the bits of its result, do not depend on its neighbours.
+__device__ __forceinline__ int chunk_pages(const Kv16AttnArgs& a, int pages)
+{
+    const int size = (pages + a.nsplit - 1) / a.nsplit;
+    return size > a.min_chunk ? size : a.min_chunk;
+}
+
+// Where a request's r-th row of a cache head with `group` query heads lies among the partial results and statistics: by request and token, so that they
+// take what the largest request asks for and not what all tokens of the call do.
+__device__ __forceinline__ size_t part_row(const Kv16AttnArgs& a, int b, int r, int g, int group)
+{
+    return ((size_t)b * a.max_q + r / group) * a.Hq + (size_t)g * group + r % group;
+}
+
+// over the lanes of the same lo (the four hi)
+__device__ __forceinline__ float max_over_hi(float x)
+{
+    auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    x = __builtin_fmaxf(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    return __builtin_fmaxf(__builtin_bit_cast(float, (unsigned)b[0]), __builtin_bit_cast(float, (unsigned)b[1]));
+}
+__device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < __builtin_inff(); }
+
+// The sum of weights times values for one row, from the definition: only positions that it sees, each weight above zero.  For rows whose result is not finite in some
+// column: matrix products multiply a weight of zero with a value that the row does not see, and a NaN there must not come through; and a weight that underflows
+// turns an infinity into a NaN.  Called by all THREADS threads of a workgroup; thread d < D returns column d.
+template <int D, int THREADS>
+__device__ __forceinline__ float slow_row(const Kv16AttnArgs& a, const Request& rq, int b, int g, int head_row, int token, int v0, int v1, float m, float* s_w)
+{
+    const int tid = threadIdx.x;
+    const Sight sight = sight_of(a, rq, token);
+    const uint16_t* const q = a.q + (size_t)head_row * D;
+    const int* const table = a.page_table + (size_t)b * a.max_pages;
+    const float ms = m == -__builtin_inff() ? 0.f : m;
+    float sum = 0.f;
+    for (int v = v0; v < v1; ++v) {
+        const int number = page_number(rq, v), page = table[number];
+        if (page < 0 || page >= a.num_pages) continue;                        // (uniform)
+        const uint16_t* const head = a.pages + ((size_t)(unsigned)page * a.Hkv + g) * kv16_head_values(D);
+        __syncthreads();
+        if (tid < KV16_PAGE) {
+            float t = 0.f;
+            for (int part = 0; part < D / 8; ++part) {
+                const half8 k = __builtin_bit_cast(half8, ld_cached(head + kv16_key_at(tid, part, D))), x = __builtin_bit_cast(half8, ld_cached(q + part * 8));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) t = __builtin_fmaf((float)k[e], (float)x[e], t);
+            }
+            const float w = __builtin_amdgcn_exp2f(t * a.scale2 - ms);
+            s_w[tid] = !sees(sight, a.sinks, number * KV16_PAGE + tid) ? -1.f : w < 1e-37f && t * a.scale2 > -__builtin_inff() ? 1e-37f : w;
+        }
+        __syncthreads();
+        if (tid < D)
+            for (int p = 0; p < KV16_PAGE; ++p) {
+                const float w = s_w[p];
+                if (w != -1.f) sum += w * half_bits_to_float(head[kv16_value_at(p, tid, D)]);
+            }
+    }
+    __syncthreads();
+    return sum;
+}
+
+// ---- one token per request, or a few: 16 rows of a cache head at a time, cut along the positions --------------------
+//
+// A workgroup (4 waves) takes a chunk of the pages that one request looks at, for one cache head; a wave takes a page at a time, in halves of 32 positions, straight from
+// memory into registers, the next half in flight behind it.  Rows are (new token, query head of the group) pairs, 16 of them the columns of two matrix products
+// (v_mfma_f32_16x16x32_f16):
+//   S = K Q^T     : 16 positions x 16 rows;
+//   O^T = V^T P^T : a lane has the weights of positions 16 i + 4 hi + r of its row, which is the B operand as it stands, for the page holds the values in that order.
+// So nothing but the rows' maxima crosses lanes, and those only when a weight leaves fp16's range.  Weights are multiplied as two fp16 summands (2^-21 of a weight
+// off at most down to 2^-12 of the largest, 2^-33 of that below, where one alone is off by 2^-11 and as much as the result's own rounding).
+constexpr int KD_THREADS = 256, KD_WAVES = 4;
+constexpr float WEIGHT_LOG2 = 9.0f;              // weights are held as 2^9 p of a maximum that may lag by 2^6 (fp16 ends at 2^16)
+
+// Two fp16 summands of four weights (the large one truncated, so that the small one is not negative).
+__device__ __forceinline__ void split_weights(const float (&w)[4], half4& large, half4& small)
+{
+    const half2v h0 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[0], w[1])), h1 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w[2], w[3]));
+    large = half4{h0[0], h0[1], h1[0], h1[1]};
+    const half2v first = {(_Float16)-1.0f, (_Float16)0.0f}, second = {(_Float16)0.0f, (_Float16)-1.0f};
+    const float r[4] = {__builtin_amdgcn_fdot2(h0, first, w[0], false), __builtin_amdgcn_fdot2(h0, second, w[1], false), __builtin_amdgcn_fdot2(h1, first, w[2], false),
+                        __builtin_amdgcn_fdot2(h1, second, w[3], false)};      // w - large, without conversions
+    const half2v s0 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(r[0], r[1])), s1 = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(r[2], r[3]));
+    small = half4{s0[0], s0[1], s1[0], s1[1]};
+}
+__device__ __forceinline__ half8 join(half4 a, half4 b) { return half8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
+
+template <int D>
+__global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a)
+{
+    constexpr int NB = D / 32, NT = D / 16;      // blocks of a key, tiles of a value's columns
+    constexpr int HALF = 32;                     // positions of half a page
+    __shared__ float s_o[KD_WAVES][16][D + 4];
+    __shared__ float s_m[KD_WAVES][16], s_l[KD_WAVES][16], s_w[KV16_PAGE];
+    __shared__ unsigned s_odd;
+
+    const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = a.Hq / a.Hkv;
+    const int g = blockIdx.x / a.tiles, r0 = (blockIdx.x % a.tiles) * 16;      // first row of this tile: row r is token r / group, head r % group
+    const int b = blockIdx.y, chunk = blockIdx.z;
+    const Request rq = find_request(a, b);
+    const int rows = rq.n * group - r0 < 16 ? rq.n * group - r0 : 16;
+    if (rows <= 0) return;
+    const int size = chunk_pages(a, rq.pages);
+    const int c0 = chunk * size, c1 = c0 + size < rq.pages ? c0 + size : rq.pages;
+    if (chunk > 0 && c0 >= rq.pages) return;
+    const bool whole = rq.pages <= size;
+    if (tid == 0) s_odd = 0;
+
+    auto row_of_column = [&](int c) {            // (token, head) row of q and out
+        const int r = r0 + c;
+        return (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group;
+    };
+    const int col = lo < rows ? lo : rows - 1;
+    half8 queries[NB];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) queries[k] = __builtin_bit_cast(half8, ld_cached(a.q + row_of_column(col) * D + k * 32 + hi * 8));
+    const Sight mine = sight_of(a, rq, (r0 + col) / group);
+    const Sight low = sight_of(a, rq, r0 / group), high = sight_of(a, rq, (r0 + rows - 1) / group);      // of the tile's first and last row
+
+    // This wave's pages: c0 + wv, c0 + wv + 4, ...; an entry that is no page: -1.  Loads are unconditional (a page that is not there: page 0), so that nothing
+    // waits for a load but what uses it.
+    const int n_it = (c1 - c0 - wv + KD_WAVES - 1) / KD_WAVES;
+    int entries = -1;                            // of the 64 pages from iteration `it` & ~63 on, one per lane
+    const int* const table = a.page_table + (size_t)b * a.max_pages;
+    auto page_at = [&](int it) {                 // asked for in order
+        if ((it & 63) == 0) {
+            const int v = c0 + wv + (it + lane) * KD_WAVES;
+            entries = v < c1 ? table[page_number(rq, v)] : -1;
+            asm volatile("" : "+v"(entries));    // waited for here, and not in every iteration behind whatever else is in flight
+        }
+        const int e = __builtin_amdgcn_readlane(entries, it & 63);
+        return e >= 0 && e < a.num_pages ? e : -1;
+    };
+    const uint16_t* const heads = a.pages + (size_t)g * kv16_head_values(D);
+    const size_t page_values = (size_t)a.Hkv * kv16_head_values(D);
+    auto head = [&](int page) { return heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_values; };
+    uintx4 kx[2 * NB], vx[NT];                   // half a page: keys of two tiles of positions, values
+    auto ask_keys = [&](int page, int half) __attribute__((always_inline)) {
+        const uint16_t* const from = head(page) + half * HALF * D;
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i) kx[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + i * 512 + lane * 8));
+    };
+    auto ask_values = [&](int page, int half, int t) __attribute__((always_inline)) {
+        const uint16_t* const from = head(page) + kv16_values(D) + half * HALF * D;
+        vx[t] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + t * 512 + lane * 8));
+    };
+    int page = n_it > 0 ? page_at(0) : -1;
+    ask_keys(page, 0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) ask_values(page, 0, t);
+
+    // m: the maximum that the row's weights refer to; start: WEIGHT_LOG2 - m, so that a weight is 2^(score + start); l: the weights' sum, as a product with ones
+    // (every element is the lane's row's)
+    float m = -__builtin_inff(), start = 0.f;
+    bool fresh = true;                           // some row has no maximum yet
+    floatx4 l = {0.f, 0.f, 0.f, 0.f};
+    const half8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+    floatx4 o[NT];                               // O^T: column 16 t + 4 hi + i of the lane's row
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    for (int step = 0; step < 2 * n_it; ++step) {
+        const int half = step & 1, it = step >> 1, number = page_number(rq, c0 + wv + it * KD_WAVES);
+        const int next = !half ? page : it + 1 < n_it ? page_at(it + 1) : -1;
+        const bool there = page >= 0;
+        const int base = number * KV16_PAGE + half * HALF;
+        floatx4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kx[i * NB + k]), queries[k], s[i], 0, 0, 0);
+        ask_keys(next, half ^ 1);
+        float t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = __builtin_fmaf(s[i >> 2][i & 3], a.scale2, start);
+        if (!there || base + HALF > low.end || (base < high.from && base + HALF > a.sinks)) {      // some row does not see all of it
+            unsigned keep[4] = {0, 0, 0, 0};     // of the values' dwords: what any row of the tile sees
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int pos = base + 16 * (i >> 2) + 4 * hi + (i & 3);
+                if (!there || !sees(mine, a.sinks, pos)) t[i] = -__builtin_inff();
+                if (there && sees(Sight{low.from, high.end}, a.sinks, pos)) keep[i >> 1] |= 0xffffu << (16 * (i & 1));
+            }
+#pragma unroll
+            for (int k = 0; k < NT; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) vx[k][i] &= keep[i];
+        }
+        half8 pl, ps;
+        auto weights = [&]() __attribute__((always_inline)) {
+            half4 large[2], small[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float w[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(t[4 * i + r]);
+                split_weights(w, large[i], small[i]);
+            }
+            pl = join(large[0], large[1]);
+            ps = join(small[0], small[1]);
+        };
+        weights();
+        // Is a weight past 2^15?  Its fp16 exponent is 30 or 31 then, and 0x0800 more carries into the sign.  No maximum crosses lanes unless one is.
+        half2v top = {0, 0};
+#pragma unroll
+        for (int r = 0; r < 8; r += 2) top = __builtin_elementwise_maximum(top, half2v{pl[r], pl[r + 1]});
+        if (fresh || __builtin_amdgcn_ballot_w64(((__builtin_bit_cast(unsigned, top) + 0x08000800u) & 0x80008000u) != 0) != 0ull) {
+            float mb = t[0];                     // (a NaN comes through; its row is not a number anyway)
+#pragma unroll
+            for (int i = 1; i < 8; ++i) mb = __builtin_elementwise_maximum(mb, t[i]);
+            const float mn = __builtin_elementwise_maximum(m, max_over_hi(mb) - start);
+            const bool none = mn == -__builtin_inff();
+            const float corr = __builtin_amdgcn_exp2f(m - (none ? 0.f : mn)), now = none ? 0.f : WEIGHT_LOG2 - mn;
+            fresh = __builtin_amdgcn_ballot_w64(none) != 0ull;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = t[i] - start + now;
+            m = mn;
+            start = now;
+            l *= corr;
+#pragma unroll
+            for (int k = 0; k < NT; ++k) o[k] *= corr;
+            weights();
+        }
+        l = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pl, l, 0, 0, 0);
+        l = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, ps, l, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < NT; ++k) {
+            const half8 v = __builtin_bit_cast(half8, vx[k]);
+            o[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl, o[k], 0, 0, 0);
+            o[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ps, o[k], 0, 0, 0);
+            ask_values(next, half ^ 1, k);
+        }
+        page = next;
+    }
+
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<floatx4*>(&s_o[wv][lo][16 * t + 4 * hi]) = o[t];
+    if (hi == 0) { s_m[wv][lo] = m; s_l[wv][lo] = l[0]; }
+    __syncthreads();
+    auto finish = [&](int c, int d, float of, float lf, float mn) {
+        const size_t row = row_of_column(c), pr = part_row(a, b, r0 + c, g, group);
+        if (whole) {
+            a.out[row * D + d] = lf == 0.f ? 0 : to_half_bits(of / lf);
+            if (d == 0 && a.stats) {
+                a.stats[2 * pr] = mn == -__builtin_inff() ? 0.f : mn;
+                a.stats[2 * pr + 1] = lf == 0.f ? 0.f : 1.0f / lf;
+            }
+        } else {
+            float* const po = a.part + (pr * a.nsplit + chunk) * (D + 2);
+            po[d] = of;
+            if (d == 0) { po[D] = mn; po[D + 1] = lf; }
+        }
+    };
+    auto merge = [&](int c, float (&cw)[KD_WAVES], float& lf) {      // fixed order: waves 0..3
+        float mn = s_m[0][c];
+#pragma unroll
+        for (int w = 1; w < KD_WAVES; ++w) mn = __builtin_fmaxf(mn, s_m[w][c]);
+        const float ms = mn == -__builtin_inff() ? 0.f : mn;
+        lf = 0.f;
+#pragma unroll
+        for (int w = 0; w < KD_WAVES; ++w) {
+            cw[w] = __builtin_amdgcn_exp2f(s_m[w][c] - ms);
+            lf += s_l[w][c] * cw[w];
+        }
+        return mn;
+    };
+    for (int idx = tid; idx < rows * D; idx += KD_THREADS) {
+        const int c = idx / D, d = idx % D;
+        float cw[KD_WAVES], lf, of = 0.f;
+        const float mn = merge(c, cw, lf);
+#pragma unroll
+        for (int w = 0; w < KD_WAVES; ++w) of += s_o[w][c][d] * cw[w];
+        // (weights are 2^WEIGHT_LOG2 times what they stand for, all of them)
+        if (finite(of)) finish(c, d, of, lf, mn);
+        else atomicOr(&s_odd, 1u << c);
+    }
+    __syncthreads();
+    const unsigned odd = s_odd;
+    for (int c = 0; c < rows; ++c) {
+        if (!(odd >> c & 1)) continue;           // (uniform)
+        float cw[KD_WAVES], lf;
+        const float mn = merge(c, cw, lf);
+        const float of = slow_row<D, KD_THREADS>(a, rq, b, g, (int)row_of_column(c), (r0 + c) / group, c0, c1, mn, s_w) * 512.0f;
+        if (tid < D) finish(c, tid, of, lf, mn);
+    }
+}
+
+// The chunks' (sum, maximum, weight) triples of a row.  Groups of D threads take every GROUPS-th chunk each, eight loads in flight, and meet in LDS:
+// a fixed order.
+constexpr int KC_THREADS = 512;
+template <int D>
+__global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
+{
+    constexpr int GROUPS = KC_THREADS / D;
+    __shared__ float s_o[GROUPS][D], s_w[KV16_MAX_SPLIT];
+    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, d = threadIdx.x % D, grp = threadIdx.x / D;
+    const Request rq = find_request(a, b);
+    if (i >= rq.n) return;
+    const int size = chunk_pages(a, rq.pages);
+    if (rq.pages <= size) return;               // one chunk: the first pass has written this output
+    const int live = (rq.pages + size - 1) / size;
+    const size_t row = (size_t)(rq.first + i) * a.Hq + h, pr = part_row(a, b, i, h, 1);
+    const float* const first = a.part + pr * a.nsplit * (D + 2);
+    const float m = lane < live ? first[(size_t)lane * (D + 2) + D] : -__builtin_inff();
+    const float w = lane < live ? first[(size_t)lane * (D + 2) + D + 1] : 0.f;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = grp + k * GROUPS < live ? first[(size_t)(grp + k * GROUPS) * (D + 2) + d] : 0.f;
+    float top = m;
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, sh));
+    const float c = __builtin_amdgcn_exp2f(m - (top == -__builtin_inff() ? 0.f : top));
+    float l = w * c;
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) l += __shfl_xor(l, sh);
+    if (threadIdx.x < 64) s_w[lane] = __builtin_fmaxf(c, 1e-37f);      // (an infinity in a chunk whose weights underflow stays one)
+    __syncthreads();
+    float o = 0.f;
+    for (int k0 = 0;;) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (grp + (k0 + k) * GROUPS < live) o += v[k] * s_w[grp + (k0 + k) * GROUPS];
+        k0 += 8;
+        if (k0 * GROUPS >= live) break;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = grp + (k0 + k) * GROUPS < live ? first[(size_t)(grp + (k0 + k) * GROUPS) * (D + 2) + d] : 0.f;
+    }
+    s_o[grp][d] = o;
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    float sum = s_o[0][d];
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) sum += s_o[k][d];
+    a.out[row * D + d] = l == 0.f ? 0 : to_half_bits(sum / l);
+    if (d == 0 && a.stats) {
+        a.stats[2 * pr] = top == -__builtin_inff() ? 0.f : top;
+        a.stats[2 * pr + 1] = l == 0.f ? 0.f : 1.0f / l;
+    }
+}
+
+// ---- what each position got of the rows' attention -------------------------------------------------------------------
+//
+// A wave takes a page of a cache head: its keys stay in registers (the A operand), the rows that see any of it come by, 16 at a time, with the maxima and sums that the
+// attention left behind.  Weights are made again, in fp32, and added up per lane (a lane keeps one row of each 16), then over the lanes: a fixed order.
+constexpr int KW_THREADS = 256;
+template <int D>
+__global__ __launch_bounds__(KW_THREADS) void kv16_attn_weights(Kv16AttnArgs a)
+{
+    constexpr int NB = D / 32;
+    const int lane = threadIdx.x & 63, lo = lane & 15, hi = lane >> 4;
+    const int number = blockIdx.x * (KW_THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y, b = blockIdx.z;
+    const Request rq = find_request(a, b);
+    const int p0 = number * KV16_PAGE;
+    if (number >= a.max_pages || p0 >= rq.len) return;
+    const int group = a.Hq / a.Hkv, before = rq.len - rq.n;
+    const int page = a.page_table[(size_t)b * a.max_pages + number];
+    float sum[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+    // the tokens that see any of it: from the one at its first position on, to the last that has its last position in the window
+    int first = p0 > before ? p0 - before : 0, last = rq.n;
+    if (a.window > 0 && p0 >= a.sinks) {
+        const long most = (long)p0 + KV16_PAGE - 1 + a.window - before;      // token i sees from before + i + 1 - window on
+        last = most < last ? (most < 0 ? 0 : (int)most) : last;
+    }
+    if (page >= 0 && page < a.num_pages && first < last) {
+        const uint16_t* const head = a.pages + ((size_t)(unsigned)page * a.Hkv + g) * kv16_head_values(D);
+        half8 keys[4][NB];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < NB; ++k) keys[i][k] = __builtin_bit_cast(half8, ld_cached(head + (i * NB + k) * 512 + lane * 8));
+        for (int r0 = first * group; r0 < last * group; r0 += 16) {
+            const int r = r0 + lo < last * group ? r0 + lo : last * group - 1;
+            const uint16_t* const q = a.q + ((size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group) * D + hi * 8;
+            const float* const stats = a.stats + 2 * part_row(a, b, r, g, group);
+            const float m = stats[0], inv = r0 + lo < last * group ? stats[1] : 0.f;
+            const Sight mine = sight_of(a, rq, r / group);
+            floatx4 s[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NB; ++k) {
+                const half8 x = __builtin_bit_cast(half8, ld_cached(q + k * 32));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys[i][k], x, s[i], 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int pos = p0 + 16 * (i >> 2) + 4 * hi + (i & 3);
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][i & 3], a.scale2, -m)) * 512.0f * inv;
+                sum[i] += inv != 0.f && sees(mine, a.sinks, pos) ? w : 0.f;
+            }
+        }
+#pragma unroll
+        for (int sh = 1; sh < 16; sh <<= 1)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[i] += __shfl_xor(sum[i], sh);
+    }
+    // lane (lo, hi) writes tile lo / 4's position 4 hi + lo % 4
+    float mine = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mine = i == lo ? sum[i] : mine;
+    const int pos = p0 + 16 * (lo >> 2) + 4 * hi + (lo & 3);
+    if (pos >= rq.len) return;
+    const size_t at = ((size_t)b * a.Hkv + g) * a.max_pages * KV16_PAGE + pos;
+    a.weights_out[at] = (a.weights_in && pos < before ? a.weights_in[at] : 0.f) + mine;
+}
+
+template <int D>
+hipError_t launch(const Kv16AttnArgs& a, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.B, (unsigned)a.nsplit);
+    hipLaunchKernelGGL((kv16_attn_decode<D>), grid, dim3(KD_THREADS), 0, stream, a);
+    if (a.nsplit > 1) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
+    if (a.weights_out)
+        hipLaunchKernelGGL((kv16_attn_weights<D>), dim3((unsigned)((a.max_pages + 3) / 4), (unsigned)a.Hkv, (unsigned)a.B), dim3(KW_THREADS), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv16_attention(const Kv16AttnArgs& a, hipStream_t stream)
+{
+    return a.D == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+}
+
+}  // namespace thi
