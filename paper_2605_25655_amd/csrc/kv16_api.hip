@@ -15,19 +15,25 @@ bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff /
 
 constexpr int MAX_PAGES = 1 << 24;      // of a row of the page table: positions stay below 2^30
 
-constexpr int FEW_CHUNK = 4, FEW_PER_CU = 2;      // kv16_plan
+constexpr int FEW_ROWS = 64, FEW_CHUNK = 4, FEW_PER_CU = 2, MANY_CHUNK = 8, MANY_PER_CU = 1;      // kv16_plan
 
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
-// The most rows of partial results that a call of up to B requests, max_q rows and max_pages pages has.  Where kv16_plan cuts, the chunks are at most FEW_PER_CU
-// workgroups of 16 rows for every compute unit, so no batch has more rows than these hold; and no more than its own times the chunks of the longest table.
-size_t most_rows(int B, int Hq, int max_q, int max_pages, int num_cus)
+// The most rows of partial results that a call of up to B requests, max_q rows and max_pages pages has.  Where kv16_plan cuts, the chunks are at most FEW_PER_CU (MANY_PER_CU)
+// workgroups of 16 (256) rows for every compute unit, so no batch has more rows than these hold; and no more than its own times the chunks of the longest table.
+size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
 {
-    const long held = 16L * FEW_PER_CU * num_cus, chunks = (max_pages + FEW_CHUNK - 1) / FEW_CHUNK, own = (long)B * max_q * Hq;
-    const long rows = chunks < 2 ? 0 : own > held ? held : own * (chunks < KV16_MAX_SPLIT ? chunks : KV16_MAX_SPLIT);
-    return (size_t)(rows < held ? rows : held);
+    auto at_most = [&](long q, int chunk, long held) {
+        const long chunks = (max_pages + chunk - 1) / chunk, own = (long)B * q * Hq;
+        const long rows = chunks < 2 ? 0 : own > held ? held : own * (chunks < KV16_MAX_SPLIT ? chunks : KV16_MAX_SPLIT);
+        return rows < held ? rows : held;
+    };
+    const int group = Hq / Hkv, q_few = FEW_ROWS / group;
+    const long few = at_most(max_q < q_few ? max_q : q_few, FEW_CHUNK, 16L * FEW_PER_CU * num_cus);
+    const long many = (long)max_q * group <= FEW_ROWS ? 0 : at_most(max_q, MANY_CHUNK, 256L * MANY_PER_CU * num_cus);
+    return (size_t)(few > many ? few : many);
 }
-size_t bytes_of_rows(size_t rows, int D) { return rows ? round_up(rows * (D + 2) * sizeof(float)) : 256; }
+size_t bytes_of_rows(size_t rows, int D) { return rows ? round_up(rows * kv16_part(D) * sizeof(float)) : 256; }
 size_t bytes_of_stats(int B, int Hq, int max_q) { return round_up((size_t)B * max_q * Hq * 2 * sizeof(float)); }
 
 int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
@@ -37,11 +43,12 @@ int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 void thi::kv16_plan(Kv16AttnArgs& a, int num_cus)
 {
     const int group = a.Hq / a.Hkv;
-    a.tiles = (int)(((long)a.max_q * group + 15) / 16);
-    a.split_rows = true;
+    a.split_rows = (long)a.max_q * group <= FEW_ROWS;
+    const int rows = a.split_rows ? 16 : 256;
+    a.tiles = (int)(((long)a.max_q * group + rows - 1) / rows);
     const long items = (long)a.B * a.Hkv * a.tiles;
-    a.min_chunk = FEW_CHUNK;
-    long n = (long)FEW_PER_CU * num_cus / items;
+    a.min_chunk = a.split_rows ? FEW_CHUNK : MANY_CHUNK;
+    long n = (long)(a.split_rows ? FEW_PER_CU : MANY_PER_CU) * num_cus / items;
     const long most = (a.max_pages + a.min_chunk - 1) / a.min_chunk;
     n = n < 1 ? 1 : n > KV16_MAX_SPLIT ? KV16_MAX_SPLIT : n;
     a.nsplit = (int)(n > most ? most : n);
@@ -81,7 +88,7 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
 size_t thi_kv16_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages, int weights)
 {
     if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_q > 65535 || max_pages < 1 || max_pages > MAX_PAGES) return 0;
-    return bytes_of_rows(most_rows(B, Hq, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, max_q) : 0);
+    return bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, max_q) : 0);
 }
 
 int thi_kv16_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, int window, int sinks,

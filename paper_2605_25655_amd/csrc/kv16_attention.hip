@@ -84,16 +84,17 @@ __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < __
 
 // The sum of weights times values for one row, from the definition: only positions that it sees, each weight above zero.  For rows whose result is not finite in some
 // column: matrix products multiply a weight of zero with a value that the row does not see, and a NaN there must not come through; and a weight that underflows
-// turns an infinity into a NaN.  Called by all THREADS threads of a workgroup; thread d < D returns column d.
+// turns an infinity into a NaN.  Called by all THREADS threads of a workgroup; thread d < D returns column d, and the sum of the weights.
 template <int D, int THREADS>
-__device__ __forceinline__ float slow_row(const Kv16AttnArgs& a, const Request& rq, int b, int g, int head_row, int token, int v0, int v1, float m, float* s_w)
+__device__ __forceinline__ float slow_row(const Kv16AttnArgs& a, const Request& rq, int b, int g, size_t head_row, int token, int v0, int v1, float m, float* s_w, float& total)
 {
     const int tid = threadIdx.x;
     const Sight sight = sight_of(a, rq, token);
-    const uint16_t* const q = a.q + (size_t)head_row * D;
+    const uint16_t* const q = a.q + head_row * D;
     const int* const table = a.page_table + (size_t)b * a.max_pages;
     const float ms = m == -__builtin_inff() ? 0.f : m;
     float sum = 0.f;
+    total = 0.f;
     for (int v = v0; v < v1; ++v) {
         const int number = page_number(rq, v), page = table[number];
         if (page < 0 || page >= a.num_pages) continue;                        // (uniform)
@@ -113,7 +114,10 @@ __device__ __forceinline__ float slow_row(const Kv16AttnArgs& a, const Request& 
         if (tid < D)
             for (int p = 0; p < KV16_PAGE; ++p) {
                 const float w = s_w[p];
-                if (w != -1.f) sum += w * half_bits_to_float(head[kv16_value_at(p, tid, D)]);
+                if (w != -1.f) {
+                    sum += w * half_bits_to_float(head[kv16_value_at(p, tid, D)]);
+                    total += w;
+                }
             }
     }
     __syncthreads();
@@ -308,9 +312,9 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
                 a.stats[2 * pr + 1] = lf == 0.f ? 0.f : 1.0f / lf;
             }
         } else {
-            float* const po = a.part + (pr * a.nsplit + chunk) * (D + 2);
+            float* const po = a.part + (pr * a.nsplit + chunk) * kv16_part(D);
             po[d] = of;
-            if (d == 0) { po[D] = mn; po[D + 1] = lf; }
+            if (d == 0) { po[D] = mn; po[D + 1] = po[D + 2] = lf; }
         }
     };
     auto merge = [&](int c, float (&cw)[KD_WAVES], float& lf) {      // fixed order: waves 0..3
@@ -342,8 +346,8 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
         if (!(odd >> c & 1)) continue;           // (uniform)
         float cw[KD_WAVES], lf;
         const float mn = merge(c, cw, lf);
-        const float of = slow_row<D, KD_THREADS>(a, rq, b, g, (int)row_of_column(c), (r0 + c) / group, c0, c1, mn, s_w) * 512.0f;
-        if (tid < D) finish(c, tid, of, lf, mn);
+        const float of = slow_row<D, KD_THREADS>(a, rq, b, g, row_of_column(c), (r0 + c) / group, c0, c1, mn, s_w, lf);
+        if (tid < D) finish(c, tid, of * 512.0f, lf * 512.0f, mn);
     }
 }
 
@@ -362,12 +366,12 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
     if (rq.pages <= size) return;               // one chunk: the first pass has written this output
     const int live = (rq.pages + size - 1) / size;
     const size_t row = (size_t)(rq.first + i) * a.Hq + h, pr = part_row(a, b, i, h, 1);
-    const float* const first = a.part + pr * a.nsplit * (D + 2);
-    const float m = lane < live ? first[(size_t)lane * (D + 2) + D] : -__builtin_inff();
-    const float w = lane < live ? first[(size_t)lane * (D + 2) + D + 1] : 0.f;
+    const float* const first = a.part + pr * a.nsplit * kv16_part(D);
+    const float m = lane < live ? first[(size_t)lane * kv16_part(D) + D] : -__builtin_inff();
+    const float w = lane < live ? first[(size_t)lane * kv16_part(D) + D + 1] : 0.f;
     float v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = grp + k * GROUPS < live ? first[(size_t)(grp + k * GROUPS) * (D + 2) + d] : 0.f;
+    for (int k = 0; k < 8; ++k) v[k] = grp + k * GROUPS < live ? first[(size_t)(grp + k * GROUPS) * kv16_part(D) + d] : 0.f;
     float top = m;
 #pragma unroll
     for (int sh = 1; sh < 64; sh <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, sh));
@@ -385,7 +389,7 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
         k0 += 8;
         if (k0 * GROUPS >= live) break;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = grp + (k0 + k) * GROUPS < live ? first[(size_t)(grp + (k0 + k) * GROUPS) * (D + 2) + d] : 0.f;
+        for (int k = 0; k < 8; ++k) v[k] = grp + (k0 + k) * GROUPS < live ? first[(size_t)(grp + (k0 + k) * GROUPS) * kv16_part(D) + d] : 0.f;
     }
     s_o[grp][d] = o;
     __syncthreads();
@@ -395,8 +399,302 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
     for (int k = 1; k < GROUPS; ++k) sum += s_o[k][d];
     a.out[row * D + d] = l == 0.f ? 0 : to_half_bits(sum / l);
     if (d == 0 && a.stats) {
+        float exact = 0.f;
+        for (int k = 0; k < live; ++k) exact += first[(size_t)k * kv16_part(D) + D + 2] * s_w[k];
         a.stats[2 * pr] = top == -__builtin_inff() ? 0.f : top;
-        a.stats[2 * pr + 1] = l == 0.f ? 0.f : 1.0f / l;
+        a.stats[2 * pr + 1] = exact == 0.f ? 0.f : 1.0f / exact;
+    }
+}
+
+// ---- many rows of a cache head: prompts and chunks of them ----------------------------------------------------------
+//
+// A workgroup takes 256 rows of one cache head, 32 a wave, and walks the pages that any of them sees.  Pages come straight into LDS as they lie in memory
+// (three buffers for keys, three for values), which is the order in which the operands of v_mfma_f32_32x32x16_f16 are read: 256 bytes in a row for 16 lanes, no bank conflicts:
+//   S = K Q^T     : 32 positions x 32 rows; register 4 a + r of a lane is position 8 a + 4 (lane / 32) + r of its row;
+//   O^T = V^T P^T : the page holds for hi = 2 s + lane / 32 the positions 16 i + 4 hi + r, which are the registers 8 i + 4 s + r: the B operand as it stands.
+constexpr int KP_THREADS = 512, KP_WAVES = 8, KP_ROWS = 32 * KP_WAVES, KP_BUFS = 3;
+template <int D> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2;
+
+// 64 x 16 bytes from `base` + 16 * lane to LDS
+__device__ __forceinline__ void kp_bring(const uint16_t* base, unsigned lane_bytes, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(lane_bytes), "s"(base), "s"(lds) : "memory");
+}
+__device__ __forceinline__ void kp_barrier()      // (loads into LDS stay in flight; kp_wait is for them)
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+template <int N> __device__ __forceinline__ void kp_wait() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+// The result is divided by the sum of the weights as they were multiplied, rounded to fp16; STATS: the sum of the weights themselves, too, for kv16_attn_weights.
+template <int D, bool STATS>
+__global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a)
+{
+    constexpr int NK = D / 16, NT = D / 32;      // steps of 16 columns of the scores' product, tiles of 32 columns of the result
+    constexpr int PART = 64 * D * 2;             // bytes of a page's keys, or values, of a head
+    constexpr int MINE = PART / 1024 / KP_WAVES; // loads of each that a wave makes
+    extern __shared__ uintx4 kp_smem[];
+    __shared__ unsigned s_odd[KP_WAVES];
+    __shared__ float s_m[KP_ROWS], s_exact[KP_ROWS], s_w[KV16_PAGE];
+
+    const int tid = threadIdx.x, lane = tid & 63, row_lane = lane & 31, h = lane >> 5, lo = lane & 15;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = a.Hq / a.Hkv;
+    // the last rows first: they see the most
+    const int g = blockIdx.x % a.Hkv, r0 = (a.tiles - 1 - (int)blockIdx.x / a.Hkv) * KP_ROWS, b = blockIdx.y, chunk = blockIdx.z;
+    const Request rq = find_request(a, b);
+    const int all_rows = rq.n * group;
+    if (r0 >= all_rows) return;
+    const int size = chunk_pages(a, rq.pages);
+    if (chunk > 0 && chunk * size >= rq.pages) return;
+    const bool whole = rq.pages <= size;
+    const int c0 = chunk * size, c1 = c0 + size < rq.pages ? c0 + size : rq.pages;
+    if (tid < KP_WAVES) s_odd[tid] = 0;
+
+    const int w0 = r0 + wv * 32;                 // this wave's first row
+    const int r = w0 + row_lane < all_rows ? w0 + row_lane : all_rows - 1;
+    auto row_at = [&](int rr) { return (size_t)(rq.first + rr / group) * a.Hq + (size_t)g * group + rr % group; };
+    const Sight mine = sight_of(a, rq, r / group);
+    const Sight low = sight_of(a, rq, (w0 < all_rows ? w0 : all_rows - 1) / group), high = sight_of(a, rq, (w0 + 31 < all_rows ? w0 + 31 : all_rows - 1) / group);
+    const int tile_from = sight_of(a, rq, r0 / group).from, tile_end = sight_of(a, rq, (r0 + KP_ROWS - 1 < all_rows ? r0 + KP_ROWS - 1 : all_rows - 1) / group).end;
+    const bool rows_here = w0 < all_rows;
+
+    // The pages of this chunk that some row of the tile sees: of the sinks, then from the first row's window to the last row's own
+    int first = tile_from / KV16_PAGE - rq.skip, past = (tile_end + KV16_PAGE - 1) / KV16_PAGE - rq.skip;
+    int lead = a.sinks / KV16_PAGE + (a.sinks % KV16_PAGE != 0);      // (more than the request's where an earlier tile's window begins among them: nothing is skipped then)
+    lead = lead < first ? lead : first;
+    lead = lead < c1 ? lead : c1;
+    first = first > c0 ? first : c0;
+    past = past < c1 ? past : c1;
+    const int n_lead = lead > c0 ? lead - c0 : 0, n_it = n_lead + (past > first ? past - first : 0);
+    auto number_of = [&](int it) { return page_number(rq, it < n_lead ? c0 + it : first + it - n_lead); };
+    int entries = -1;
+    const int* const table = a.page_table + (size_t)b * a.max_pages;
+    auto page_at = [&](int it) {                 // asked for in order; -1: not there
+        if ((it & 63) == 0) {
+            entries = it + lane < n_it ? table[number_of(it + lane)] : -1;
+            asm volatile("" : "+v"(entries));    // waited for here
+        }
+        const int e = __builtin_amdgcn_readlane(entries, it & 63);
+        return e >= 0 && e < a.num_pages ? e : -1;
+    };
+
+    half8 queries[NK];
+#pragma unroll
+    for (int k = 0; k < NK; ++k) queries[k] = __builtin_bit_cast(half8, ld_cached(a.q + row_at(r) * D + k * 16 + h * 8));
+
+    const unsigned smem_at = (unsigned)(size_t)(__attribute__((address_space(3))) void*)kp_smem, lane16 = lane * 16;
+    const uint16_t* const heads = a.pages + (size_t)g * kv16_head_values(D);
+    const size_t page_values = (size_t)a.Hkv * kv16_head_values(D);
+    auto bring = [&](int page, int buf, bool values) __attribute__((always_inline)) {      // this wave's share (a page that is not there: of page 0, for nobody)
+        const uint16_t* const from = heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_values + (values ? kv16_values(D) : 0);
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) kp_bring(from + (wv + j * KP_WAVES) * 512, lane16, smem_at + ((values ? KP_BUFS : 0) + buf) * PART + (wv + j * KP_WAVES) * 1024);
+    };
+
+    float m = -__builtin_inff(), start = 0.f, l = 0.f, exact = 0.f;      // sums: of this lane's positions only
+    bool fresh = true;
+    floatx16 o[NT], s[2];
+    half8 pw[4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+
+    // where a lane's operands begin: keys of position lane % 32 of a tile of 32, columns 8 h .. of a step; values of column lane % 32 of a tile, positions of hi = 2 s + h
+    const unsigned k_lane = ((lane >> 4 & 1) * (D / 32) * 64 + h * 16 + lo) * 16, v_lane = ((lane >> 4 & 1) * 64 + h * 16 + lo) * 16;
+    auto key_at = [&](const char* keys, int t, int k) __attribute__((always_inline)) {
+        return *reinterpret_cast<const half8*>(keys + k_lane + (t * 2 * (D / 32) + k / 2) * 1024 + (k & 1) * 512);
+    };
+    auto value_at = [&](const char* values, int t, int k) __attribute__((always_inline)) {      // step k: positions 32 (k / 2) .., s = k % 2
+        return *reinterpret_cast<const half8*>(values + v_lane + ((k >> 1) * (D / 16) + t * 2) * 1024 + (k & 1) * 512);
+    };
+    auto multiply_keys = [&](int buf) __attribute__((always_inline)) {
+        const char* const keys = reinterpret_cast<const char*>(kp_smem) + buf * PART;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_at(keys, t, k), queries[k], s[t], 0, 0, 0);
+    };
+    auto multiply_values = [&](int buf) __attribute__((always_inline)) {
+        const char* const values = reinterpret_cast<const char*>(kp_smem) + (KP_BUFS + buf) * PART;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value_at(values, t, k), pw[k], o[t], 0, 0, 0);
+    };
+    auto soften = [&](int base) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], a.scale2, start);
+        if (base + KV16_PAGE > low.end || (base < high.from && base + KV16_PAGE > a.sinks)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!sees(mine, a.sinks, base + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3))) s[t][i] = -__builtin_inff();
+        }
+        float sum;
+        auto weights = [&]() __attribute__((always_inline)) {
+            sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float w = __builtin_amdgcn_exp2f(s[k >> 1][8 * (e >> 2) + 4 * (k & 1) + (e & 3)]);
+                    if (STATS) sum += w;
+                    pw[k][e] = (_Float16)w;
+                }
+        };
+        weights();
+        half2v top = {0, 0};
+        const half2v one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) top = __builtin_elementwise_maximum(top, half2v{pw[k][e], pw[k][e + 1]});
+        // a weight past 2^15, or no maximum yet: as in the few-rows kernel
+        if (fresh || __builtin_amdgcn_ballot_w64(((__builtin_bit_cast(unsigned, top) + 0x08000800u) & 0x80008000u) != 0) != 0ull) {
+            float mb = s[0][0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) mb = __builtin_elementwise_maximum(mb, s[i >> 4][i & 15]);
+            mb = __builtin_elementwise_maximum(mb, __shfl_xor(mb, 32));
+            const float mn = __builtin_elementwise_maximum(m, mb - start);
+            const bool none = mn == -__builtin_inff();
+            const float corr = __builtin_amdgcn_exp2f(m - (none ? 0.f : mn)), now = none ? 0.f : WEIGHT_LOG2 - mn;
+            fresh = __builtin_amdgcn_ballot_w64(none) != 0ull;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = s[i >> 4][i & 15] - start + now;
+            m = mn;
+            start = now;
+            l *= corr;
+            if (STATS) exact *= corr;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[t] *= corr;
+            weights();
+        }
+        if (STATS) exact += sum;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) l = __builtin_amdgcn_fdot2(half2v{pw[k][e], pw[k][e + 1]}, one, l, false);
+    };
+    // Values that nobody may read -- behind the request's last position, or of a page that is not there -- become zeros: a weight of zero times a NaN is one.
+    auto scrub = [&](int base, bool there, int buf) {
+        char* const values = reinterpret_cast<char*>(kp_smem) + (KP_BUFS + buf) * PART;
+        for (int i = tid; i < PART / 16; i += KP_THREADS / 2) {
+            const int first_pos = base + i / (PART / 32) * 32 + (i / 16 & 3) * 4;
+            uintx4 x = reinterpret_cast<uintx4*>(values)[i];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!there || first_pos + 16 * (e >> 2) + (e & 3) >= rq.len) x[e >> 1] &= ~(0xffffu << (16 * (e & 1)));
+            reinterpret_cast<uintx4*>(values)[i] = x;
+        }
+    };
+
+    // The two halves of the waves (one of each on every SIMD) take turns: in slot 2 p the first half multiplies (the weights of page p - 1 with their values, then the keys of page p),
+    // in slot 2 p + 1 the second half, and the other has its exponentials meanwhile.  At the beginning of its turn p a wave asks for its share of the keys of page p + 2 and of the
+    // values of page p + 1: the buffers' former contents were read in slot 2 p - 1 for the last time, and the new ones are needed from slot 2 p + 4 on.
+    int page[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) page[i] = i < n_it ? page_at(i) : -1;
+    bring(page[0], 0, false);
+    bring(page[0], 0, true);
+    bring(page[1], 1, false);
+    kp_wait<0>();
+    const bool second = wv >= 4;
+    kp_barrier();
+    if (second) kp_barrier();
+    auto works = [&](int base, bool there) { return there && rows_here && base < high.end && (base + KV16_PAGE > low.from || base < a.sinks); };
+    bool before = false;                         // has this wave weights of page p - 1?
+    int kb = 0, vb = 2;                          // buffers of the keys of page p and of the values of page p - 1
+    for (int p = 0; p <= n_it; ++p) {
+        const int base = p < n_it ? number_of(p) * KV16_PAGE : 0;
+        const bool there = p < n_it && page[0] >= 0, now = works(base, there);
+        const int v_next = vb == 2 ? 0 : vb + 1; // of the values of page p
+        bring(page[2], kb == 0 ? 2 : kb - 1, false);
+        bring(page[1], v_next == 2 ? 0 : v_next + 1, true);
+        if (before) multiply_values(vb);
+        if (now) multiply_keys(kb);
+        kp_wait<2 * MINE>();
+        kp_barrier();
+        if (now) soften(base);
+        if (!second && p < n_it && (!there || base + KV16_PAGE > rq.len)) scrub(base, there, v_next);
+        if (p + 1 < n_it && (page[1] < 0 || (number_of(p + 1) + 1) * KV16_PAGE > rq.len)) kp_wait<0>();
+        else kp_wait<2 * MINE>();
+        kp_barrier();
+        before = now;
+        kb = kb == 2 ? 0 : kb + 1;
+        vb = v_next;
+        page[0] = page[1];
+        page[1] = page[2];
+        page[2] = p + 3 < n_it ? page_at(p + 3) : -1;
+    }
+    if (!second) kp_barrier();
+    kp_wait<0>();                                // (nothing may be on its way into LDS that is no longer this workgroup's)
+
+    l += __shfl_xor(l, 32);
+    if (STATS) exact += __shfl_xor(exact, 32);
+    bool odd = false;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd = odd || !finite(o[t][i]);
+    const bool mine_here = w0 + row_lane < all_rows;
+    const unsigned long long odd_lanes = __builtin_amdgcn_ballot_w64(odd && mine_here);
+    const unsigned odd_rows = (unsigned)odd_lanes | (unsigned)(odd_lanes >> 32);
+    if (lane == 0) s_odd[wv] = odd_rows;
+    if (h == 0) { s_m[wv * 32 + row_lane] = m; s_exact[wv * 32 + row_lane] = exact; }
+    auto put_stats = [&](int rr, float mm, float ll) {
+        float* const to = a.stats + 2 * part_row(a, b, rr, g, group);
+        to[0] = mm == -__builtin_inff() ? 0.f : mm;
+        to[1] = ll == 0.f ? 0.f : 1.0f / ll;
+    };
+    if (mine_here && !(odd_rows >> row_lane & 1)) {
+        if (whole) {
+            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            uint16_t* const out = a.out + row_at(r) * D;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const half4 y = {(_Float16)(o[t][4 * i] * inv), (_Float16)(o[t][4 * i + 1] * inv), (_Float16)(o[t][4 * i + 2] * inv), (_Float16)(o[t][4 * i + 3] * inv)};
+                    *reinterpret_cast<half4*>(out + 32 * t + 8 * i + 4 * h) = y;
+                }
+            if (STATS && h == 0) put_stats(r, m, exact);
+        } else {
+            float* const po = a.part + (part_row(a, b, r, g, group) * a.nsplit + chunk) * kv16_part(D);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) po[32 * t + 8 * (i >> 2) + 4 * h + (i & 3)] = o[t][i];
+            if (h == 0) { po[D] = m; po[D + 1] = l; po[D + 2] = exact; }
+        }
+    }
+    __syncthreads();
+    for (int w = 0; w < KP_WAVES; ++w) {
+        unsigned rows = s_odd[w];                // (the same for all threads)
+        while (rows) {
+            const int c = w * 32 + __builtin_ctz(rows), rr = r0 + c;
+            rows &= rows - 1;
+            const float mm = s_m[c];
+            float ll;
+            const float of = slow_row<D, KP_THREADS>(a, rq, b, g, row_at(rr), rr / group, c0, c1, mm, s_w, ll) * 512.0f;
+            ll *= 512.0f;
+            if (whole) {
+                if (tid < D) a.out[row_at(rr) * D + tid] = ll == 0.f ? 0 : to_half_bits(of / ll);
+                if (STATS && tid == 0) put_stats(rr, mm, s_exact[c]);
+            } else {
+                float* const po = a.part + (part_row(a, b, rr, g, group) * a.nsplit + chunk) * kv16_part(D);
+                if (tid < D) po[tid] = of;
+                if (tid == 0) { po[D] = mm; po[D + 1] = ll; po[D + 2] = s_exact[c]; }
+            }
+        }
     }
 }
 
@@ -469,11 +767,23 @@ __global__ __launch_bounds__(KW_THREADS) void kv16_attn_weights(Kv16AttnArgs a)
     a.weights_out[at] = (a.weights_in && pos < before ? a.weights_in[at] : 0.f) + mine;
 }
 
+template <int D, bool STATS>
+void launch_prompt(const Kv16AttnArgs& a, dim3 grid, hipStream_t stream)
+{
+    static std::once_flag attr_once;
+    std::call_once(attr_once, [] {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&kv16_attn_prompt<D, STATS>), hipFuncAttributeMaxDynamicSharedMemorySize, KP_LDS<D>);
+    });
+    hipLaunchKernelGGL((kv16_attn_prompt<D, STATS>), grid, dim3(KP_THREADS), KP_LDS<D>, stream, a);
+}
+
 template <int D>
 hipError_t launch(const Kv16AttnArgs& a, hipStream_t stream)
 {
     const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.B, (unsigned)a.nsplit);
-    hipLaunchKernelGGL((kv16_attn_decode<D>), grid, dim3(KD_THREADS), 0, stream, a);
+    if (a.split_rows) hipLaunchKernelGGL((kv16_attn_decode<D>), grid, dim3(KD_THREADS), 0, stream, a);
+    else if (a.weights_out) launch_prompt<D, true>(a, grid, stream);
+    else launch_prompt<D, false>(a, grid, stream);
     if (a.nsplit > 1) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
     if (a.weights_out)
         hipLaunchKernelGGL((kv16_attn_weights<D>), dim3((unsigned)((a.max_pages + 3) / 4), (unsigned)a.Hkv, (unsigned)a.B), dim3(KW_THREADS), 0, stream, a);

@@ -128,7 +128,7 @@ hipError_t launch_kv16_attention(const Kv16AttnArgs& a, hipStream_t)
 {
     NEED(a.B >= 1 && a.T >= 1 && a.max_q >= 1 && a.max_q <= a.T && a.nsplit >= 1 && a.nsplit <= KV16_MAX_SPLIT && a.window >= 0 && a.sinks >= 0);
     const size_t rows = (size_t)a.B * a.max_q * a.Hq;
-    NEED(a.nsplit == 1 || (char*)a.part + rows * a.nsplit * (a.D + 2) * 4 <= space + given);
+    NEED(a.nsplit == 1 || (char*)a.part + rows * a.nsplit * kv16_part(a.D) * 4 <= space + given);
     NEED(!a.weights_out || ((char*)a.stats == space && (char*)a.stats + rows * 8 <= (char*)a.part));
     return hipSuccess;
 }
