@@ -412,8 +412,8 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
 // (three buffers for keys, three for values), which is the order in which the operands of v_mfma_f32_32x32x16_f16 are read: 256 bytes in a row for 16 lanes, no bank conflicts:
 //   S = K Q^T     : 32 positions x 32 rows; register 4 a + r of a lane is position 8 a + 4 (lane / 32) + r of its row;
 //   O^T = V^T P^T : the page holds for hi = 2 s + lane / 32 the positions 16 i + 4 hi + r, which are the registers 8 i + 4 s + r: the B operand as it stands.
-constexpr int KP_THREADS = 512, KP_WAVES = 8, KP_ROWS = 32 * KP_WAVES, KP_BUFS = 3;
-template <int D> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2;
+constexpr int KP_THREADS = 512, KP_WAVES = 8, KP_ROWS = 32 * KP_WAVES, KP_BUFS = 3, KP_AHEAD = 6;
+template <int D> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2 + KP_WAVES * 4096;
 
 // 64 x 16 bytes from `base` + 16 * lane to LDS
 __device__ __forceinline__ void kp_bring(const uint16_t* base, unsigned lane_bytes, unsigned lds)
@@ -467,29 +467,39 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
     first = first > c0 ? first : c0;
     past = past < c1 ? past : c1;
     const int n_lead = lead > c0 ? lead - c0 : 0, n_it = n_lead + (past > first ? past - first : 0);
-    auto number_of = [&](int it) { return page_number(rq, it < n_lead ? c0 + it : first + it - n_lead); };
+    // (what the loop needs of it, in few scalar registers: the position at which turn `it`'s page begins)
+    const int from_lead = c0 * KV16_PAGE, from_window = (first - n_lead + rq.skip) * KV16_PAGE;
+    auto base_of = [&](int it) { return it * KV16_PAGE + (it < n_lead ? from_lead : from_window); };
     int entries = -1;
     const int* const table = a.page_table + (size_t)b * a.max_pages;
-    auto page_at = [&](int it) {                 // asked for in order; -1: not there
-        if ((it & 63) == 0) {
-            entries = it + lane < n_it ? table[number_of(it + lane)] : -1;
-            asm volatile("" : "+v"(entries));    // waited for here
-        }
+    auto list = [&](int it) {                    // the table's entries of turns it .. it + 63, one a lane; waited for here
+        const int at = it + lane < n_it ? it + lane : n_it - 1;      // (no branch, here and in scrub: a loop with one that lanes take apart is put together anew, and accumulators are copied)
+        const int e = table[at < 0 ? 0 : base_of(at) / KV16_PAGE];
+        entries = it + lane < n_it ? e : -1;
+        asm volatile("" : "+v"(entries));
+    };
+    auto page_at = [&](int it) __attribute__((always_inline)) {      // -1: not there
         const int e = __builtin_amdgcn_readlane(entries, it & 63);
-        return e >= 0 && e < a.num_pages ? e : -1;
+        return e < a.num_pages ? e : -1;
     };
 
     half8 queries[NK];
 #pragma unroll
     for (int k = 0; k < NK; ++k) queries[k] = __builtin_bit_cast(half8, ld_cached(a.q + row_at(r) * D + k * 16 + h * 8));
+#pragma unroll
+    for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(queries[k]));      // waited for here, and not in every turn behind what is on its way into LDS
 
     const unsigned smem_at = (unsigned)(size_t)(__attribute__((address_space(3))) void*)kp_smem, lane16 = lane * 16;
     const uint16_t* const heads = a.pages + (size_t)g * kv16_head_values(D);
     const size_t page_values = (size_t)a.Hkv * kv16_head_values(D);
-    auto bring = [&](int page, int buf, bool values) __attribute__((always_inline)) {      // this wave's share (a page that is not there: of page 0, for nobody)
-        const uint16_t* const from = heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_values + (values ? kv16_values(D) : 0);
-#pragma unroll
-        for (int j = 0; j < MINE; ++j) kp_bring(from + (wv + j * KP_WAVES) * 512, lane16, smem_at + ((values ? KP_BUFS : 0) + buf) * PART + (wv + j * KP_WAVES) * 1024);
+    // where a page's keys begin (a page that is not there: page 0, for nobody), and the j-th load of this wave's share of its keys or values
+    auto head = [&](int page) __attribute__((always_inline)) { return heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_values; };
+    const unsigned lds_at = smem_at + wv * 1024;
+    auto bring_keys = [&](const uint16_t* from, unsigned buf, int j) __attribute__((always_inline)) {
+        kp_bring(from + (wv + j * KP_WAVES) * 512, lane16, lds_at + buf + j * KP_WAVES * 1024);
+    };
+    auto bring_values = [&](const uint16_t* from, unsigned buf, int j) __attribute__((always_inline)) {
+        kp_bring(from + kv16_values(D) + (wv + j * KP_WAVES) * 512, lane16, lds_at + KP_BUFS * PART + buf + j * KP_WAVES * 1024);
     };
 
     float m = -__builtin_inff(), start = 0.f, l = 0.f, exact = 0.f;      // sums: of this lane's positions only
@@ -509,85 +519,112 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
     auto value_at = [&](const char* values, int t, int k) __attribute__((always_inline)) {      // step k: positions 32 (k / 2) .., s = k % 2
         return *reinterpret_cast<const half8*>(values + v_lane + ((k >> 1) * (D / 16) + t * 2) * 1024 + (k & 1) * 512);
     };
-    auto multiply_keys = [&](int buf) __attribute__((always_inline)) {
-        const char* const keys = reinterpret_cast<const char*>(kp_smem) + buf * PART;
+    // The weights of a page times its values (not FIRST), then the keys of the next page times the queries.  Operands are asked for KP_AHEAD products ahead, in this order, or
+    // the compiler would ask for each where it is needed and wait.
+    auto multiply = [&](auto first_one, unsigned v_buf, unsigned k_buf, auto between) __attribute__((always_inline)) {
+        constexpr int V = decltype(first_one)::value ? 0 : 4 * NT, N = V + 2 * NK;
+        const char* const keys = reinterpret_cast<const char*>(kp_smem) + k_buf;
+        const char* const values = reinterpret_cast<const char*>(kp_smem) + KP_BUFS * PART + v_buf;
+        half8 f[KP_AHEAD];
+        auto fetch = [&](int i) __attribute__((always_inline)) {
+            f[i % KP_AHEAD] = i < V ? value_at(values, i % NT, i / NT) : key_at(keys, (i - V) & 1, (i - V) >> 1);
+        };
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int i = 0; i < KP_AHEAD; ++i) fetch(i);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
-#pragma unroll
-        for (int k = 0; k < NK; ++k)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_at(keys, t, k), queries[k], s[t], 0, 0, 0);
-    };
-    auto multiply_values = [&](int buf) __attribute__((always_inline)) {
-        const char* const values = reinterpret_cast<const char*>(kp_smem) + (KP_BUFS + buf) * PART;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value_at(values, t, k), pw[k], o[t], 0, 0, 0);
+        for (int i = 0; i < N; ++i) {
+            const floatx16 none = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (i < V) o[i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % KP_AHEAD], pw[i / NT], o[i % NT], 0, 0, 0);
+            else s[(i - V) & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % KP_AHEAD], queries[(i - V) >> 1], i - V < 2 ? none : s[(i - V) & 1], 0, 0, 0);
+            if (i + KP_AHEAD < N) fetch(i + KP_AHEAD);
+            between(i);                          // (for the time that a product takes)
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     auto soften = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], a.scale2, start);
-        if (base + KV16_PAGE > low.end || (base < high.from && base + KV16_PAGE > a.sinks)) {
+        if (base + KV16_PAGE > low.end) {        // some row's end is in front of the page's
+            const int end = mine.end - base - 4 * h;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!sees(mine, a.sinks, base + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3))) s[t][i] = -__builtin_inff();
+            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = end > 8 * (i >> 2) + (i & 3) ? s[i >> 4][i & 15] : -__builtin_inff();
         }
-        float sum;
-        auto weights = [&]() __attribute__((always_inline)) {
-            sum = 0.f;
+        if (base < high.from && base + KV16_PAGE > a.sinks) {      // some row's window begins behind the page's first position, and not all of them are sinks
+            const int hidden = a.sinks - base - 4 * h, span = mine.from > a.sinks ? mine.from - a.sinks : 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(s[k >> 1][8 * (e >> 2) + 4 * (k & 1) + (e & 3)]);
-                    if (STATS) sum += w;
-                    pw[k][e] = (_Float16)w;
-                }
-        };
-        weights();
-        half2v top = {0, 0};
-        const half2v one = {(_Float16)1.0f, (_Float16)1.0f};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) top = __builtin_elementwise_maximum(top, half2v{pw[k][e], pw[k][e + 1]});
+            for (int i = 0; i < 32; ++i)
+                s[i >> 4][i & 15] = (unsigned)(8 * (i >> 2) + (i & 3) - hidden) < (unsigned)span ? -__builtin_inff() : s[i >> 4][i & 15];
+        }
         // a weight past 2^15, or no maximum yet: as in the few-rows kernel
-        if (fresh || __builtin_amdgcn_ballot_w64(((__builtin_bit_cast(unsigned, top) + 0x08000800u) & 0x80008000u) != 0) != 0ull) {
-            float mb = s[0][0];
+        float mb = s[0][0];
 #pragma unroll
-            for (int i = 1; i < 32; ++i) mb = __builtin_elementwise_maximum(mb, s[i >> 4][i & 15]);
-            mb = __builtin_elementwise_maximum(mb, __shfl_xor(mb, 32));
-            const float mn = __builtin_elementwise_maximum(m, mb - start);
+        for (int i = 1; i < 32; ++i) mb = __builtin_fmaxf(mb, s[i >> 4][i & 15]);      // (a NaN does not show, but its row's sums are not numbers)
+        if (fresh || __builtin_amdgcn_ballot_w64(mb > 15.0f) != 0ull) {
+            mb = __builtin_fmaxf(mb, __shfl_xor(mb, 32));
+            const float mn = __builtin_fmaxf(m, mb - start);
             const bool none = mn == -__builtin_inff();
             const float corr = __builtin_amdgcn_exp2f(m - (none ? 0.f : mn)), now = none ? 0.f : WEIGHT_LOG2 - mn;
             fresh = __builtin_amdgcn_ballot_w64(none) != 0ull;
 #pragma unroll
             for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = s[i >> 4][i & 15] - start + now;
+            const bool some = __builtin_amdgcn_ballot_w64(m != -__builtin_inff()) != 0ull;      // (else all sums are zeros)
             m = mn;
             start = now;
             l *= corr;
             if (STATS) exact *= corr;
+            // By way of LDS, a tile at a time: the compiler gives products of the accumulators registers of their own, and copies all of them to and fro on the other path (64 moves
+            // of pairs a page, each a time in which no matrix product runs).
+            if (some) {
+                uintx4* const own = kp_smem + 2 * KP_BUFS * PART / 16 + wv * 256 + lane;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) o[t] *= corr;
-            weights();
+                for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const floatx4 y = {o[t][4 * i] * corr, o[t][4 * i + 1] * corr, o[t][4 * i + 2] * corr, o[t][4 * i + 3] * corr};
+                        own[i * 64] = __builtin_bit_cast(uintx4, y);
+                    }
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const floatx4 y = __builtin_bit_cast(floatx4, own[i * 64]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[t][4 * i + k] = y[k];
+                    }
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                }
+            }
         }
-        if (STATS) exact += sum;
+        // Weights are cut to fp16's bits, not rounded to the nearest: their sum is one of cut weights too, so that what all are too small by cancels, and what is left is half
+        // a step of each as with the other rounding; that one's conversion, of two values to the nearest, keeps matrix products of the SIMD's other wave from running for half of its time,
+        // this one's does not.  (So do exponentials, for all of theirs; and products of fp16 pairs, which is why the sum is one of single values.)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) l = __builtin_amdgcn_fdot2(half2v{pw[k][e], pw[k][e + 1]}, one, l, false);
+            for (int e = 0; e < 8; e += 2) {
+                const float w0 = __builtin_amdgcn_exp2f(s[k >> 1][8 * (e >> 2) + 4 * (k & 1) + (e & 3)]), w1 = __builtin_amdgcn_exp2f(s[k >> 1][8 * (e >> 2) + 4 * (k & 1) + (e & 3) + 1]);
+                if (STATS) exact += w0 + w1;
+                const half2v w = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w0, w1));
+                pw[k][e] = w[0];
+                pw[k][e + 1] = w[1];
+                const unsigned both = __builtin_bit_cast(unsigned, w);
+                asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel_hi:[1,0,0]" : "+v"(l) : "v"(both));                       // (the low one, the high one)
+                asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l) : "v"(both));
+            }
+        // (vector work may be moved past a barrier, which concerns memory only; here it is what the turns are about)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(pw[k]));
+        asm volatile("" : "+v"(l));
     };
     // Values that nobody may read -- behind the request's last position, or of a page that is not there -- become zeros: a weight of zero times a NaN is one.
-    auto scrub = [&](int base, bool there, int buf) {
-        char* const values = reinterpret_cast<char*>(kp_smem) + (KP_BUFS + buf) * PART;
-        for (int i = tid; i < PART / 16; i += KP_THREADS / 2) {
+    auto scrub = [&](int base, bool there, unsigned buf) {
+        char* const values = reinterpret_cast<char*>(kp_smem) + KP_BUFS * PART + buf;
+        asm volatile("" : "+s"(base));           // (what depends on it stays here, under the caller's condition)
+#pragma unroll
+        for (int j = 0; j < PART / 16 / (KP_THREADS / 2); ++j) {
+            const int i = j * (KP_THREADS / 2) + (tid & (KP_THREADS / 2 - 1));
             const int first_pos = base + i / (PART / 32) * 32 + (i / 16 & 3) * 4;
             uintx4 x = reinterpret_cast<uintx4*>(values)[i];
 #pragma unroll
@@ -598,42 +635,76 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
     };
 
     // The two halves of the waves (one of each on every SIMD) take turns: in slot 2 p the first half multiplies (the weights of page p - 1 with their values, then the keys of page p),
-    // in slot 2 p + 1 the second half, and the other has its exponentials meanwhile.  At the beginning of its turn p a wave asks for its share of the keys of page p + 2 and of the
+    // in slot 2 p + 1 the second half, and the other has its exponentials meanwhile.  During its products of turn p a wave asks for its share of the keys of page p + 2 and of the
     // values of page p + 1: the buffers' former contents were read in slot 2 p - 1 for the last time, and the new ones are needed from slot 2 p + 4 on.
-    int page[3];
+    // (A wave works on all pages up to its last row's own; behind the last one it multiplies keys of whatever is there, for nobody: accumulators under a condition are copied.)
+    const int here_end = rows_here ? high.end : 0;
+    auto turns_to = [&](int end, int from, int most) { const int n = (end - from + KV16_PAGE - 1) / KV16_PAGE; return end <= from ? 0 : n < most ? n : most; };
+    const int lead_turns = turns_to(here_end, from_lead, n_lead);
+    const int n_wave = lead_turns < n_lead ? lead_turns : n_it > n_lead ? n_lead + turns_to(here_end, from_window + n_lead * KV16_PAGE, n_it - n_lead) : n_lead;
+    list(0);
+    int page = page_at(0), page1 = page_at(1), page2 = page_at(2), page3 = page_at(3);      // of turns it, it + 1, it + 2, it + 3
 #pragma unroll
-    for (int i = 0; i < 3; ++i) page[i] = i < n_it ? page_at(i) : -1;
-    bring(page[0], 0, false);
-    bring(page[0], 0, true);
-    bring(page[1], 1, false);
+    for (int j = 0; j < MINE; ++j) {
+        bring_keys(head(page), 0, j);
+        bring_values(head(page), 0, j);
+        bring_keys(head(page1), PART, j);
+    }
+    const uint16_t *from1 = head(page1), *from2 = head(page2), *from3 = head(page3);
     kp_wait<0>();
     const bool second = wv >= 4;
     kp_barrier();
     if (second) kp_barrier();
-    auto works = [&](int base, bool there) { return there && rows_here && base < high.end && (base + KV16_PAGE > low.from || base < a.sinks); };
-    bool before = false;                         // has this wave weights of page p - 1?
-    int kb = 0, vb = 2;                          // buffers of the keys of page p and of the values of page p - 1
-    for (int p = 0; p <= n_it; ++p) {
-        const int base = p < n_it ? number_of(p) * KV16_PAGE : 0;
-        const bool there = p < n_it && page[0] >= 0, now = works(base, there);
-        const int v_next = vb == 2 ? 0 : vb + 1; // of the values of page p
-        bring(page[2], kb == 0 ? 2 : kb - 1, false);
-        bring(page[1], v_next == 2 ? 0 : v_next + 1, true);
-        if (before) multiply_values(vb);
-        if (now) multiply_keys(kb);
+    unsigned b0 = 0, b1 = PART, b2 = 2 * PART;   // buffers of pages it, it + 1, it + 2
+    multiply(std::true_type{}, 0u, 0u, [&](int i) __attribute__((always_inline)) {
+        if (i < MINE) bring_keys(from2, 2 * PART, i);
+        else if (i < 2 * MINE) bring_values(from1, PART, i - MINE);
+    });
+    kp_wait<2 * MINE>();
+    kp_barrier();
+    // beside a wave's own work: in the turn of the exponentials of page `it`, during the products, and behind them
+    auto tend = [&](int it) __attribute__((always_inline)) {
+        const int base = base_of(it);
+        if (page < 0 || base + KV16_PAGE > rq.len) {
+            if (!second) scrub(base, page >= 0, b0);
+        }
+        if (it + 1 < n_it && (page1 < 0 || base_of(it + 1) + KV16_PAGE > rq.len)) kp_wait<0>();      // (the next one is to be scrubbed)
+        if (((it + 4) & 63) == 0) list(it + 4);
+        kp_barrier();
+    };
+    auto bring = [&](int i) __attribute__((always_inline)) {
+        if (i < MINE) bring_keys(from3, b0, i);
+        else if (i < 2 * MINE) bring_values(from2, b2, i - MINE);
+    };
+    auto advance = [&](int it) __attribute__((always_inline)) {
+        page = page1;
+        page1 = page2;
+        page2 = page3;
+        page3 = page_at(it + 4);
+        from2 = from3;
+        from3 = head(page3);
+        const unsigned b = b0;
+        b0 = b1;
+        b1 = b2;
+        b2 = b;
         kp_wait<2 * MINE>();
         kp_barrier();
-        if (now) soften(base);
-        if (!second && p < n_it && (!there || base + KV16_PAGE > rq.len)) scrub(base, there, v_next);
-        if (p + 1 < n_it && (page[1] < 0 || (number_of(p + 1) + 1) * KV16_PAGE > rq.len)) kp_wait<0>();
-        else kp_wait<2 * MINE>();
-        kp_barrier();
-        before = now;
-        kb = kb == 2 ? 0 : kb + 1;
-        vb = v_next;
-        page[0] = page[1];
-        page[1] = page[2];
-        page[2] = p + 3 < n_it ? page_at(p + 3) : -1;
+    };
+    // (tested at its end: a loop that is left at its head has the accumulators live in two places, and copies them)
+    if (n_wave > 0) {
+        int it = 0;
+        do {
+            soften(page < 0 ? 0x7fffff00 : base_of(it));      // (nothing of a page that is not there is seen)
+            tend(it);
+            multiply(std::false_type{}, b0, b1, bring);
+            advance(it);
+        } while (++it < n_wave);
+    }
+    for (int it = n_wave; it < n_it; ++it) {
+        tend(it);
+#pragma unroll
+        for (int i = 0; i < 2 * MINE; ++i) bring(i);
+        advance(it);
     }
     if (!second) kp_barrier();
     kp_wait<0>();                                // (nothing may be on its way into LDS that is no longer this workgroup's)
