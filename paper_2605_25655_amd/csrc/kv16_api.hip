@@ -15,7 +15,7 @@ bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff /
 
 constexpr int MAX_PAGES = 1 << 24;      // of a row of the page table: positions stay below 2^30
 
-constexpr int FEW_ROWS = 64, FEW_CHUNK = 4, FEW_PER_CU = 2, MANY_CHUNK = 8, MANY_PER_CU = 1;      // kv16_plan
+constexpr int FEW_ROWS = 64, FEW_CHUNK = 4, FEW_PER_CU = 2, MANY_CHUNK = 8, MANY_PER_CU = 2;      // kv16_plan
 
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -30,7 +30,7 @@ size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
     };
     const int group = Hq / Hkv, q_few = FEW_ROWS / group;
     const long few = at_most(max_q < q_few ? max_q : q_few, FEW_CHUNK, 16L * FEW_PER_CU * num_cus);
-    const long many = (long)max_q * group <= FEW_ROWS ? 0 : at_most(max_q, MANY_CHUNK, 256L * MANY_PER_CU * num_cus);
+    const long many = (long)max_q * group <= FEW_ROWS ? 0 : at_most(max_q, MANY_CHUNK, 128L * MANY_PER_CU * num_cus);
     return (size_t)(few > many ? few : many);
 }
 size_t bytes_of_rows(size_t rows, int D) { return rows ? round_up(rows * kv16_part(D) * sizeof(float)) : 256; }
@@ -44,7 +44,7 @@ void thi::kv16_plan(Kv16AttnArgs& a, int num_cus)
 {
     const int group = a.Hq / a.Hkv;
     a.split_rows = (long)a.max_q * group <= FEW_ROWS;
-    const int rows = a.split_rows ? 16 : 256;
+    const int rows = a.split_rows ? 16 : 128;
     a.tiles = (int)(((long)a.max_q * group + rows - 1) / rows);
     const long items = (long)a.B * a.Hkv * a.tiles;
     a.min_chunk = a.split_rows ? FEW_CHUNK : MANY_CHUNK;

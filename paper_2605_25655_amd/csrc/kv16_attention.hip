@@ -412,8 +412,8 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
 // (three buffers for keys, three for values), which is the order in which the operands of v_mfma_f32_32x32x16_f16 are read: 256 bytes in a row for 16 lanes, no bank conflicts:
 //   S = K Q^T     : 32 positions x 32 rows; register 4 a + r of a lane is position 8 a + 4 (lane / 32) + r of its row;
 //   O^T = V^T P^T : the page holds for hi = 2 s + lane / 32 the positions 16 i + 4 hi + r, which are the registers 8 i + 4 s + r: the B operand as it stands.
-constexpr int KP_THREADS = 512, KP_WAVES = 8, KP_ROWS = 32 * KP_WAVES, KP_BUFS = 3, KP_AHEAD = 6;
-template <int D> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2 + KP_WAVES * 4096;
+constexpr int KP_WAVES = 4, KP_AHEAD = 6, KP_BUFS = 2;
+template <int D, int WAVES> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2 + WAVES * 2048;
 
 // 64 x 16 bytes from `base` + 16 * lane to LDS
 __device__ __forceinline__ void kp_bring(const uint16_t* base, unsigned lane_bytes, unsigned lds)
@@ -426,37 +426,60 @@ __device__ __forceinline__ void kp_barrier()      // (loads into LDS stay in fli
 }
 template <int N> __device__ __forceinline__ void kp_wait() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 
+// What a workgroup of WAVES waves works on: 32 WAVES rows of a cache head from row r0 on, and of the pages its request looks at c0 .. c1 - 1.
+struct Tile {
+    Request rq;
+    int group, g, b, chunk, r0, all_rows, c0, c1;
+    bool whole;
+    __device__ __forceinline__ size_t row(const Kv16AttnArgs& a, int r) const { return (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group; }      // of q and out
+};
+template <int WAVES> __device__ __forceinline__ Tile find_tile(const Kv16AttnArgs& a)
+{
+    Tile t;
+    t.group = a.Hq / a.Hkv;
+    // the last rows first: they see the most
+    t.g = blockIdx.x % a.Hkv;
+    t.r0 = (a.tiles - 1 - (int)blockIdx.x / a.Hkv) * 32 * WAVES;
+    t.b = blockIdx.y;
+    t.chunk = blockIdx.z;
+    t.rq = find_request(a, t.b);
+    t.all_rows = t.rq.n * t.group;
+    const int size = chunk_pages(a, t.rq.pages);
+    t.whole = t.rq.pages <= size;
+    t.c0 = t.chunk * size;
+    t.c1 = t.c0 + size < t.rq.pages ? t.c0 + size : t.rq.pages;
+    return t;
+}
+__device__ __forceinline__ const Kv16AttnArgs& arguments_again()
+{
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const Kv16AttnArgs*)(const void*)p;
+}
+
 // The result is divided by the sum of the weights as they were multiplied, rounded to fp16; STATS: the sum of the weights themselves, too, for kv16_attn_weights.
-template <int D, bool STATS>
-__global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a)
+template <int D, int WAVES, bool STATS>
+__global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a)
 {
     constexpr int NK = D / 16, NT = D / 32;      // steps of 16 columns of the scores' product, tiles of 32 columns of the result
     constexpr int PART = 64 * D * 2;             // bytes of a page's keys, or values, of a head
-    constexpr int MINE = PART / 1024 / KP_WAVES; // loads of each that a wave makes
+    constexpr int MINE = PART / 1024 / WAVES; // loads of each that a wave makes
     extern __shared__ uintx4 kp_smem[];
-    __shared__ unsigned s_odd[KP_WAVES];
-    __shared__ float s_m[KP_ROWS], s_exact[KP_ROWS], s_w[KV16_PAGE];
+    __shared__ unsigned s_odd[WAVES];
+    __shared__ float s_m[32 * WAVES], s_exact[32 * WAVES], s_w[KV16_PAGE];
 
     const int tid = threadIdx.x, lane = tid & 63, row_lane = lane & 31, h = lane >> 5, lo = lane & 15;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int group = a.Hq / a.Hkv;
-    // the last rows first: they see the most
-    const int g = blockIdx.x % a.Hkv, r0 = (a.tiles - 1 - (int)blockIdx.x / a.Hkv) * KP_ROWS, b = blockIdx.y, chunk = blockIdx.z;
-    const Request rq = find_request(a, b);
-    const int all_rows = rq.n * group;
-    if (r0 >= all_rows) return;
-    const int size = chunk_pages(a, rq.pages);
-    if (chunk > 0 && chunk * size >= rq.pages) return;
-    const bool whole = rq.pages <= size;
-    const int c0 = chunk * size, c1 = c0 + size < rq.pages ? c0 + size : rq.pages;
-    if (tid < KP_WAVES) s_odd[tid] = 0;
+    const Tile tile = find_tile<WAVES>(a);
+    const Request& rq = tile.rq;
+    const int group = tile.group, r0 = tile.r0, all_rows = tile.all_rows, c0 = tile.c0, c1 = tile.c1;
+    if (r0 >= all_rows || c0 > c1 || (tile.chunk > 0 && c0 >= rq.pages)) return;
 
     const int w0 = r0 + wv * 32;                 // this wave's first row
     const int r = w0 + row_lane < all_rows ? w0 + row_lane : all_rows - 1;
-    auto row_at = [&](int rr) { return (size_t)(rq.first + rr / group) * a.Hq + (size_t)g * group + rr % group; };
     const Sight mine = sight_of(a, rq, r / group);
     const Sight low = sight_of(a, rq, (w0 < all_rows ? w0 : all_rows - 1) / group), high = sight_of(a, rq, (w0 + 31 < all_rows ? w0 + 31 : all_rows - 1) / group);
-    const int tile_from = sight_of(a, rq, r0 / group).from, tile_end = sight_of(a, rq, (r0 + KP_ROWS - 1 < all_rows ? r0 + KP_ROWS - 1 : all_rows - 1) / group).end;
+    const int tile_from = sight_of(a, rq, r0 / group).from, tile_end = sight_of(a, rq, (r0 + 32 * WAVES - 1 < all_rows ? r0 + 32 * WAVES - 1 : all_rows - 1) / group).end;
     const bool rows_here = w0 < all_rows;
 
     // The pages of this chunk that some row of the tile sees: of the sinks, then from the first row's window to the last row's own
@@ -471,7 +494,7 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
     const int from_lead = c0 * KV16_PAGE, from_window = (first - n_lead + rq.skip) * KV16_PAGE;
     auto base_of = [&](int it) { return it * KV16_PAGE + (it < n_lead ? from_lead : from_window); };
     int entries = -1;
-    const int* const table = a.page_table + (size_t)b * a.max_pages;
+    const int* const table = a.page_table + (size_t)tile.b * a.max_pages;
     auto list = [&](int it) {                    // the table's entries of turns it .. it + 63, one a lane; waited for here
         const int at = it + lane < n_it ? it + lane : n_it - 1;      // (no branch, here and in scrub: a loop with one that lanes take apart is put together anew, and accumulators are copied)
         const int e = table[at < 0 ? 0 : base_of(at) / KV16_PAGE];
@@ -485,21 +508,21 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
 
     half8 queries[NK];
 #pragma unroll
-    for (int k = 0; k < NK; ++k) queries[k] = __builtin_bit_cast(half8, ld_cached(a.q + row_at(r) * D + k * 16 + h * 8));
+    for (int k = 0; k < NK; ++k) queries[k] = __builtin_bit_cast(half8, ld_cached(a.q + tile.row(a, r) * D + k * 16 + h * 8));
 #pragma unroll
     for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(queries[k]));      // waited for here, and not in every turn behind what is on its way into LDS
 
     const unsigned smem_at = (unsigned)(size_t)(__attribute__((address_space(3))) void*)kp_smem, lane16 = lane * 16;
-    const uint16_t* const heads = a.pages + (size_t)g * kv16_head_values(D);
+    const uint16_t* const heads = a.pages + (size_t)tile.g * kv16_head_values(D);
     const size_t page_values = (size_t)a.Hkv * kv16_head_values(D);
     // where a page's keys begin (a page that is not there: page 0, for nobody), and the j-th load of this wave's share of its keys or values
     auto head = [&](int page) __attribute__((always_inline)) { return heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_values; };
     const unsigned lds_at = smem_at + wv * 1024;
     auto bring_keys = [&](const uint16_t* from, unsigned buf, int j) __attribute__((always_inline)) {
-        kp_bring(from + (wv + j * KP_WAVES) * 512, lane16, lds_at + buf + j * KP_WAVES * 1024);
+        kp_bring(from + (wv + j * WAVES) * 512, lane16, lds_at + buf + j * WAVES * 1024);
     };
     auto bring_values = [&](const uint16_t* from, unsigned buf, int j) __attribute__((always_inline)) {
-        kp_bring(from + kv16_values(D) + (wv + j * KP_WAVES) * 512, lane16, lds_at + KP_BUFS * PART + buf + j * KP_WAVES * 1024);
+        kp_bring(from + kv16_values(D) + (wv + j * WAVES) * 512, lane16, lds_at + KP_BUFS * PART + buf + j * WAVES * 1024);
     };
 
     float m = -__builtin_inff(), start = 0.f, l = 0.f, exact = 0.f;      // sums: of this lane's positions only
@@ -521,7 +544,7 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
     };
     // The weights of a page times its values (not FIRST), then the keys of the next page times the queries.  Operands are asked for KP_AHEAD products ahead, in this order, or
     // the compiler would ask for each where it is needed and wait.
-    auto multiply = [&](auto first_one, unsigned v_buf, unsigned k_buf, auto between) __attribute__((always_inline)) {
+    auto multiply = [&](auto first_one, unsigned v_buf, unsigned k_buf) __attribute__((always_inline)) {
         constexpr int V = decltype(first_one)::value ? 0 : 4 * NT, N = V + 2 * NK;
         const char* const keys = reinterpret_cast<const char*>(kp_smem) + k_buf;
         const char* const values = reinterpret_cast<const char*>(kp_smem) + KP_BUFS * PART + v_buf;
@@ -538,7 +561,6 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
             if (i < V) o[i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % KP_AHEAD], pw[i / NT], o[i % NT], 0, 0, 0);
             else s[(i - V) & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % KP_AHEAD], queries[(i - V) >> 1], i - V < 2 ? none : s[(i - V) & 1], 0, 0, 0);
             if (i + KP_AHEAD < N) fetch(i + KP_AHEAD);
-            between(i);                          // (for the time that a product takes)
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -578,20 +600,21 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
             // By way of LDS, a tile at a time: the compiler gives products of the accumulators registers of their own, and copies all of them to and fro on the other path (64 moves
             // of pairs a page, each a time in which no matrix product runs).
             if (some) {
-                uintx4* const own = kp_smem + 2 * KP_BUFS * PART / 16 + wv * 256 + lane;
+                uintx4* const own = kp_smem + 2 * KP_BUFS * PART / 16 + wv * 128 + lane;
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
+                for (int t = 0; t < 2 * NT; ++t) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const floatx4 y = {o[t][4 * i] * corr, o[t][4 * i + 1] * corr, o[t][4 * i + 2] * corr, o[t][4 * i + 3] * corr};
+                    for (int i = 0; i < 2; ++i) {
+                        const int k = (t & 1) * 8 + 4 * i;
+                        const floatx4 y = {o[t / 2][k] * corr, o[t / 2][k + 1] * corr, o[t / 2][k + 2] * corr, o[t / 2][k + 3] * corr};
                         own[i * 64] = __builtin_bit_cast(uintx4, y);
                     }
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 2; ++i) {
                         const floatx4 y = __builtin_bit_cast(floatx4, own[i * 64]);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) o[t][4 * i + k] = y[k];
+                        for (int k = 0; k < 4; ++k) o[t / 2][(t & 1) * 8 + 4 * i + k] = y[k];
                     }
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 }
@@ -623,8 +646,8 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
         char* const values = reinterpret_cast<char*>(kp_smem) + KP_BUFS * PART + buf;
         asm volatile("" : "+s"(base));           // (what depends on it stays here, under the caller's condition)
 #pragma unroll
-        for (int j = 0; j < PART / 16 / (KP_THREADS / 2); ++j) {
-            const int i = j * (KP_THREADS / 2) + (tid & (KP_THREADS / 2 - 1));
+        for (int j = 0; j < PART / 16 / (64 * WAVES); ++j) {
+            const int i = j * 64 * WAVES + tid;
             const int first_pos = base + i / (PART / 32) * 32 + (i / 16 & 3) * 4;
             uintx4 x = reinterpret_cast<uintx4*>(values)[i];
 #pragma unroll
@@ -634,81 +657,72 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
         }
     };
 
-    // The two halves of the waves (one of each on every SIMD) take turns: in slot 2 p the first half multiplies (the weights of page p - 1 with their values, then the keys of page p),
-    // in slot 2 p + 1 the second half, and the other has its exponentials meanwhile.  During its products of turn p a wave asks for its share of the keys of page p + 2 and of the
-    // values of page p + 1: the buffers' former contents were read in slot 2 p - 1 for the last time, and the new ones are needed from slot 2 p + 4 on.
+    // A wave's work is a chain: the scores of page 0, its exponentials, then the products behind page `it` (its weights with its values, and the scores of page it + 1), the exponentials of
+    // page it + 1, and so on.  The two halves of the waves (one of each on every SIMD) meet once a page, at different places: the first half behind its products, the
+    // second in front of them.  So between two meetings, k and k + 1, the first half has the exponentials of page k while the second multiplies, and then the other way round, and all of them
+    // read the values of page k and the keys of page k + 1.  What comes in meanwhile are values of page k + 2 and keys of page k + 3, into the buffers that were read
+    // in front of meeting k; they are waited for in front of meeting k + 2.
     // (A wave works on all pages up to its last row's own; behind the last one it multiplies keys of whatever is there, for nobody: accumulators under a condition are copied.)
     const int here_end = rows_here ? high.end : 0;
     auto turns_to = [&](int end, int from, int most) { const int n = (end - from + KV16_PAGE - 1) / KV16_PAGE; return end <= from ? 0 : n < most ? n : most; };
     const int lead_turns = turns_to(here_end, from_lead, n_lead);
     const int n_wave = lead_turns < n_lead ? lead_turns : n_it > n_lead ? n_lead + turns_to(here_end, from_window + n_lead * KV16_PAGE, n_it - n_lead) : n_lead;
     list(0);
-    int page = page_at(0), page1 = page_at(1), page2 = page_at(2), page3 = page_at(3);      // of turns it, it + 1, it + 2, it + 3
+    int page = page_at(0), page1 = page_at(1), page2 = page_at(2);      // of pages it, it + 1, it + 2
+    const uint16_t *from1 = head(page1), *from2 = head(page2);
 #pragma unroll
     for (int j = 0; j < MINE; ++j) {
         bring_keys(head(page), 0, j);
         bring_values(head(page), 0, j);
-        bring_keys(head(page1), PART, j);
+        bring_keys(from1, PART, j);
     }
-    const uint16_t *from1 = head(page1), *from2 = head(page2), *from3 = head(page3);
     kp_wait<0>();
-    const bool second = wv >= 4;
     kp_barrier();
-    if (second) kp_barrier();
-    unsigned b0 = 0, b1 = PART, b2 = 2 * PART;   // buffers of pages it, it + 1, it + 2
-    multiply(std::true_type{}, 0u, 0u, [&](int i) __attribute__((always_inline)) {
-        if (i < MINE) bring_keys(from2, 2 * PART, i);
-        else if (i < 2 * MINE) bring_values(from1, PART, i - MINE);
-    });
-    kp_wait<2 * MINE>();
+    multiply(std::true_type{}, 0u, 0u);
     kp_barrier();
-    // beside a wave's own work: in the turn of the exponentials of page `it`, during the products, and behind them
-    auto tend = [&](int it) __attribute__((always_inline)) {
-        const int base = base_of(it);
-        if (page < 0 || base + KV16_PAGE > rq.len) {
-            if (!second) scrub(base, page >= 0, b0);
+    unsigned b0 = 0, b1 = PART;                  // buffers of pages it and it + 1
+    auto begin = [&](int it) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) bring_keys(from2, b0, j);
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) bring_values(from1, b1, j);
+        if (page < 0 || base_of(it) + KV16_PAGE > rq.len) {
+            scrub(base_of(it), page >= 0, b0);
+            kp_barrier();
         }
-        if (it + 1 < n_it && (page1 < 0 || base_of(it + 1) + KV16_PAGE > rq.len)) kp_wait<0>();      // (the next one is to be scrubbed)
-        if (((it + 4) & 63) == 0) list(it + 4);
-        kp_barrier();
+        if (((it + 3) & 63) == 0) list(it + 3);
     };
-    auto bring = [&](int i) __attribute__((always_inline)) {
-        if (i < MINE) bring_keys(from3, b0, i);
-        else if (i < 2 * MINE) bring_values(from2, b2, i - MINE);
-    };
-    auto advance = [&](int it) __attribute__((always_inline)) {
+    auto end = [&](int it) __attribute__((always_inline)) {
         page = page1;
         page1 = page2;
-        page2 = page3;
-        page3 = page_at(it + 4);
-        from2 = from3;
-        from3 = head(page3);
+        page2 = page_at(it + 3);
+        from1 = from2;
+        from2 = head(page2);
         const unsigned b = b0;
         b0 = b1;
-        b1 = b2;
-        b2 = b;
-        kp_wait<2 * MINE>();
+        b1 = b;
+        kp_wait<0>();
         kp_barrier();
     };
     // (tested at its end: a loop that is left at its head has the accumulators live in two places, and copies them)
     if (n_wave > 0) {
         int it = 0;
         do {
+            begin(it);
             soften(page < 0 ? 0x7fffff00 : base_of(it));      // (nothing of a page that is not there is seen)
-            tend(it);
-            multiply(std::false_type{}, b0, b1, bring);
-            advance(it);
+            multiply(std::false_type{}, b0, b1);
+            end(it);
         } while (++it < n_wave);
     }
     for (int it = n_wave; it < n_it; ++it) {
-        tend(it);
-#pragma unroll
-        for (int i = 0; i < 2 * MINE; ++i) bring(i);
-        advance(it);
+        begin(it);
+        end(it);
     }
-    if (!second) kp_barrier();
     kp_wait<0>();                                // (nothing may be on its way into LDS that is no longer this workgroup's)
 
+    // What follows is made of the arguments anew: kept over the loop, it would take the scalar registers that the loop needs.
+    const Kv16AttnArgs& e = arguments_again();
+    const Tile at = find_tile<WAVES>(e);
     l += __shfl_xor(l, 32);
     if (STATS) exact += __shfl_xor(exact, 32);
     bool odd = false;
@@ -716,20 +730,22 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = odd || !finite(o[t][i]);
-    const bool mine_here = w0 + row_lane < all_rows;
+    const int own = wv * 32 + row_lane;
+    const bool mine_here = at.r0 + own < at.all_rows;
     const unsigned long long odd_lanes = __builtin_amdgcn_ballot_w64(odd && mine_here);
     const unsigned odd_rows = (unsigned)odd_lanes | (unsigned)(odd_lanes >> 32);
     if (lane == 0) s_odd[wv] = odd_rows;
-    if (h == 0) { s_m[wv * 32 + row_lane] = m; s_exact[wv * 32 + row_lane] = exact; }
-    auto put_stats = [&](int rr, float mm, float ll) {
-        float* const to = a.stats + 2 * part_row(a, b, rr, g, group);
+    if (h == 0) { s_m[own] = m; s_exact[own] = exact; }
+    auto put_stats = [&](int r, float mm, float ll) {
+        float* const to = e.stats + 2 * part_row(e, at.b, r, at.g, at.group);
         to[0] = mm == -__builtin_inff() ? 0.f : mm;
         to[1] = ll == 0.f ? 0.f : 1.0f / ll;
     };
     if (mine_here && !(odd_rows >> row_lane & 1)) {
-        if (whole) {
+        const int r = at.r0 + own;
+        if (at.whole) {
             const float inv = l == 0.f ? 0.f : 1.0f / l;
-            uint16_t* const out = a.out + row_at(r) * D;
+            uint16_t* const out = e.out + at.row(e, r) * D;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -739,29 +755,29 @@ __global__ __launch_bounds__(KP_THREADS, 2) void kv16_attn_prompt(Kv16AttnArgs a
                 }
             if (STATS && h == 0) put_stats(r, m, exact);
         } else {
-            float* const po = a.part + (part_row(a, b, r, g, group) * a.nsplit + chunk) * kv16_part(D);
+            float* const po = e.part + (part_row(e, at.b, r, at.g, at.group) * e.nsplit + at.chunk) * kv16_part(D);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) po[32 * t + 8 * (i >> 2) + 4 * h + (i & 3)] = o[t][i];
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<floatx4*>(po + 32 * t + 8 * i + 4 * h) = floatx4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
             if (h == 0) { po[D] = m; po[D + 1] = l; po[D + 2] = exact; }
         }
     }
     __syncthreads();
-    for (int w = 0; w < KP_WAVES; ++w) {
-        unsigned rows = s_odd[w];                // (the same for all threads)
+    for (int w = 0; w < WAVES; ++w) {
+        unsigned rows = __builtin_amdgcn_readfirstlane(s_odd[w]);
         while (rows) {
-            const int c = w * 32 + __builtin_ctz(rows), rr = r0 + c;
+            const int c = w * 32 + __builtin_ctz(rows), r = at.r0 + c;
             rows &= rows - 1;
             const float mm = s_m[c];
             float ll;
-            const float of = slow_row<D, KP_THREADS>(a, rq, b, g, row_at(rr), rr / group, c0, c1, mm, s_w, ll) * 512.0f;
+            const float of = slow_row<D, 64 * WAVES>(e, at.rq, at.b, at.g, at.row(e, r), r / at.group, at.c0, at.c1, mm, s_w, ll) * 512.0f;
             ll *= 512.0f;
-            if (whole) {
-                if (tid < D) a.out[row_at(rr) * D + tid] = ll == 0.f ? 0 : to_half_bits(of / ll);
-                if (STATS && tid == 0) put_stats(rr, mm, s_exact[c]);
+            if (at.whole) {
+                if (tid < D) e.out[at.row(e, r) * D + tid] = ll == 0.f ? 0 : to_half_bits(of / ll);
+                if (STATS && tid == 0) put_stats(r, mm, s_exact[c]);
             } else {
-                float* const po = a.part + (part_row(a, b, rr, g, group) * a.nsplit + chunk) * kv16_part(D);
+                float* const po = e.part + (part_row(e, at.b, r, at.g, at.group) * e.nsplit + at.chunk) * kv16_part(D);
                 if (tid < D) po[tid] = of;
                 if (tid == 0) { po[D] = mm; po[D + 1] = ll; po[D + 2] = s_exact[c]; }
             }
@@ -843,9 +859,9 @@ void launch_prompt(const Kv16AttnArgs& a, dim3 grid, hipStream_t stream)
 {
     static std::once_flag attr_once;
     std::call_once(attr_once, [] {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&kv16_attn_prompt<D, STATS>), hipFuncAttributeMaxDynamicSharedMemorySize, KP_LDS<D>);
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&kv16_attn_prompt<D, KP_WAVES, STATS>), hipFuncAttributeMaxDynamicSharedMemorySize, KP_LDS<D, KP_WAVES>);
     });
-    hipLaunchKernelGGL((kv16_attn_prompt<D, STATS>), grid, dim3(KP_THREADS), KP_LDS<D>, stream, a);
+    hipLaunchKernelGGL((kv16_attn_prompt<D, KP_WAVES, STATS>), grid, dim3(64 * KP_WAVES), (KP_LDS<D, KP_WAVES>), stream, a);
 }
 
 template <int D>
