@@ -542,71 +542,100 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     auto value_at = [&](const char* values, int t, int k) __attribute__((always_inline)) {      // step k: positions 32 (k / 2) .., s = k % 2
         return *reinterpret_cast<const half8*>(values + v_lane + ((k >> 1) * (D / 16) + t * 2) * 1024 + (k & 1) * 512);
     };
-    // The weights of a page times its values (not FIRST), then the keys of the next page times the queries.  Operands are asked for KP_AHEAD products ahead, in this order, or
-    // the compiler would ask for each where it is needed and wait.
-    auto multiply = [&](auto first_one, unsigned v_buf, unsigned k_buf) __attribute__((always_inline)) {
-        constexpr int V = decltype(first_one)::value ? 0 : 4 * NT, N = V + 2 * NK;
-        const char* const keys = reinterpret_cast<const char*>(kp_smem) + k_buf;
-        const char* const values = reinterpret_cast<const char*>(kp_smem) + KP_BUFS * PART + v_buf;
+    // N products whose operands are asked for KP_AHEAD ahead, in this order, or the compiler would ask for each where it is needed and wait; `between` puts vector work into the time that
+    // the i-th takes.
+    auto products = [&](auto count, auto fetch, auto product, auto between) __attribute__((always_inline)) {
+        constexpr int N = decltype(count)::value;
         half8 f[KP_AHEAD];
-        auto fetch = [&](int i) __attribute__((always_inline)) {
-            f[i % KP_AHEAD] = i < V ? value_at(values, i % NT, i / NT) : key_at(keys, (i - V) & 1, (i - V) >> 1);
-        };
 #pragma unroll
-        for (int i = 0; i < KP_AHEAD; ++i) fetch(i);
+        for (int i = 0; i < KP_AHEAD; ++i) f[i] = fetch(i);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const floatx16 none = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (i < V) o[i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % KP_AHEAD], pw[i / NT], o[i % NT], 0, 0, 0);
-            else s[(i - V) & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i % KP_AHEAD], queries[(i - V) >> 1], i - V < 2 ? none : s[(i - V) & 1], 0, 0, 0);
-            if (i + KP_AHEAD < N) fetch(i + KP_AHEAD);
+            product(i, f[i % KP_AHEAD]);
+            if (i + KP_AHEAD < N) f[i % KP_AHEAD] = fetch(i + KP_AHEAD);
+            between(i);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto soften = [&](int base) __attribute__((always_inline)) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], a.scale2, start);
+    // the scores of a page, into s
+    auto multiply_keys = [&](unsigned buf, auto between) __attribute__((always_inline)) {
+        const char* const keys = reinterpret_cast<const char*>(kp_smem) + buf;
+        products(std::integral_constant<int, 2 * NK>{}, [&](int i) __attribute__((always_inline)) { return key_at(keys, i & 1, i >> 1); },
+                 [&](int i, half8 k) __attribute__((always_inline)) {
+                     const floatx16 none = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                     s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, queries[i >> 1], i < 2 ? none : s[i & 1], 0, 0, 0);
+                 },
+                 between);
+    };
+    // a page's weights times its values
+    auto multiply_values = [&](unsigned buf, auto between) __attribute__((always_inline)) {
+        const char* const values = reinterpret_cast<const char*>(kp_smem) + KP_BUFS * PART + buf;
+        products(std::integral_constant<int, 4 * NT>{}, [&](int i) __attribute__((always_inline)) { return value_at(values, i % NT, i / NT); },
+                 [&](int i, half8 v) __attribute__((always_inline)) { o[i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pw[i / NT], o[i % NT], 0, 0, 0); }, between);
+    };
+    // t: what the exponentials of a page are of; largest: the largest of the lane's
+    float t[32], largest = -__builtin_inff();
+    auto scale = [&](int i) __attribute__((always_inline)) { t[i] = __builtin_fmaf(s[i >> 4][i & 15], a.scale2, start); };
+    auto look = [&](int i) __attribute__((always_inline)) { largest = __builtin_fmaxf(__builtin_fmaxf(largest, t[2 * i]), t[2 * i + 1]); };      // (a NaN does not show, but its row's sums are not numbers)
+    // The i-th pair of weights.  They are cut to fp16's bits, not rounded to the nearest: their sum is one of cut weights too, so that what all are too small by cancels, and what is left is
+    // half a step of each as with the other rounding; that one's conversion, of two values to the nearest, keeps matrix products of the SIMD's other wave from running for half of its time,
+    // this one's does not.  (So do exponentials, for all of theirs; and products of fp16 pairs, which is why the sum is one of single values.)
+    auto weigh = [&](int i) __attribute__((always_inline)) {
+        const int k = i >> 2, e = 2 * (i & 3);
+        const float w0 = __builtin_amdgcn_exp2f(t[16 * (k >> 1) + 8 * (e >> 2) + 4 * (k & 1) + (e & 3)]), w1 = __builtin_amdgcn_exp2f(t[16 * (k >> 1) + 8 * (e >> 2) + 4 * (k & 1) + (e & 3) + 1]);
+        if (STATS) exact += w0 + w1;
+        const half2v w = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w0, w1));
+        pw[k][e] = w[0];
+        pw[k][e + 1] = w[1];
+    };
+    auto add = [&](int i) __attribute__((always_inline)) {
+        const unsigned both = __builtin_bit_cast(unsigned, half2v{pw[i >> 2][2 * (i & 3)], pw[i >> 2][2 * (i & 3) + 1]});
+        asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel_hi:[1,0,0]" : "+v"(l) : "v"(both));                       // (the low one, the high one)
+        asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l) : "v"(both));
+    };
+    // What a row does not see of the page, and a maximum that weights refer to if there is none or a weight would be past 2^15.
+    auto settle = [&](int base) __attribute__((always_inline)) {
+        bool masked = false;
         if (base + KV16_PAGE > low.end) {        // some row's end is in front of the page's
+            masked = true;
             const int end = mine.end - base - 4 * h;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = end > 8 * (i >> 2) + (i & 3) ? s[i >> 4][i & 15] : -__builtin_inff();
+            for (int i = 0; i < 32; ++i) t[i] = end > 8 * (i >> 2) + (i & 3) ? t[i] : -__builtin_inff();
         }
         if (base < high.from && base + KV16_PAGE > a.sinks) {      // some row's window begins behind the page's first position, and not all of them are sinks
+            masked = true;
             const int hidden = a.sinks - base - 4 * h, span = mine.from > a.sinks ? mine.from - a.sinks : 0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                s[i >> 4][i & 15] = (unsigned)(8 * (i >> 2) + (i & 3) - hidden) < (unsigned)span ? -__builtin_inff() : s[i >> 4][i & 15];
+            for (int i = 0; i < 32; ++i) t[i] = (unsigned)(8 * (i >> 2) + (i & 3) - hidden) < (unsigned)span ? -__builtin_inff() : t[i];
         }
-        // a weight past 2^15, or no maximum yet: as in the few-rows kernel
-        float mb = s[0][0];
+        if (masked) {
+            largest = -__builtin_inff();
 #pragma unroll
-        for (int i = 1; i < 32; ++i) mb = __builtin_fmaxf(mb, s[i >> 4][i & 15]);      // (a NaN does not show, but its row's sums are not numbers)
-        if (fresh || __builtin_amdgcn_ballot_w64(mb > 15.0f) != 0ull) {
-            mb = __builtin_fmaxf(mb, __shfl_xor(mb, 32));
-            const float mn = __builtin_fmaxf(m, mb - start);
+            for (int i = 0; i < 16; ++i) look(i);
+        }
+        if (fresh || __builtin_amdgcn_ballot_w64(largest > 15.0f) != 0ull) {
+            const float mb = __builtin_fmaxf(largest, __shfl_xor(largest, 32)), mn = __builtin_fmaxf(m, mb - start);
             const bool none = mn == -__builtin_inff();
             const float corr = __builtin_amdgcn_exp2f(m - (none ? 0.f : mn)), now = none ? 0.f : WEIGHT_LOG2 - mn;
             fresh = __builtin_amdgcn_ballot_w64(none) != 0ull;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s[i >> 4][i & 15] = s[i >> 4][i & 15] - start + now;
+            for (int i = 0; i < 32; ++i) t[i] = t[i] - start + now;
             const bool some = __builtin_amdgcn_ballot_w64(m != -__builtin_inff()) != 0ull;      // (else all sums are zeros)
             m = mn;
             start = now;
             l *= corr;
             if (STATS) exact *= corr;
-            // By way of LDS, a tile at a time: the compiler gives products of the accumulators registers of their own, and copies all of them to and fro on the other path (64 moves
+            // By way of LDS, half a tile at a time: the compiler gives products of the accumulators registers of their own, and copies all of them to and fro on the other path (64 moves
             // of pairs a page, each a time in which no matrix product runs).
             if (some) {
                 uintx4* const own = kp_smem + 2 * KP_BUFS * PART / 16 + wv * 128 + lane;
 #pragma unroll
-                for (int t = 0; t < 2 * NT; ++t) {
+                for (int k = 0; k < 2 * NT; ++k) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int k = (t & 1) * 8 + 4 * i;
-                        const floatx4 y = {o[t / 2][k] * corr, o[t / 2][k + 1] * corr, o[t / 2][k + 2] * corr, o[t / 2][k + 3] * corr};
+                        const int r = (k & 1) * 8 + 4 * i;
+                        const floatx4 y = {o[k / 2][r] * corr, o[k / 2][r + 1] * corr, o[k / 2][r + 2] * corr, o[k / 2][r + 3] * corr};
                         own[i * 64] = __builtin_bit_cast(uintx4, y);
                     }
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -614,32 +643,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
                     for (int i = 0; i < 2; ++i) {
                         const floatx4 y = __builtin_bit_cast(floatx4, own[i * 64]);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) o[t / 2][(t & 1) * 8 + 4 * i + k] = y[k];
+                        for (int r = 0; r < 4; ++r) o[k / 2][(k & 1) * 8 + 4 * i + r] = y[r];
                     }
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 }
             }
         }
-        // Weights are cut to fp16's bits, not rounded to the nearest: their sum is one of cut weights too, so that what all are too small by cancels, and what is left is half
-        // a step of each as with the other rounding; that one's conversion, of two values to the nearest, keeps matrix products of the SIMD's other wave from running for half of its time,
-        // this one's does not.  (So do exponentials, for all of theirs; and products of fp16 pairs, which is why the sum is one of single values.)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const float w0 = __builtin_amdgcn_exp2f(s[k >> 1][8 * (e >> 2) + 4 * (k & 1) + (e & 3)]), w1 = __builtin_amdgcn_exp2f(s[k >> 1][8 * (e >> 2) + 4 * (k & 1) + (e & 3) + 1]);
-                if (STATS) exact += w0 + w1;
-                const half2v w = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w0, w1));
-                pw[k][e] = w[0];
-                pw[k][e + 1] = w[1];
-                const unsigned both = __builtin_bit_cast(unsigned, w);
-                asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel_hi:[1,0,0]" : "+v"(l) : "v"(both));                       // (the low one, the high one)
-                asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l) : "v"(both));
-            }
-        // (vector work may be moved past a barrier, which concerns memory only; here it is what the turns are about)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(pw[k]));
-        asm volatile("" : "+v"(l));
+        largest = -__builtin_inff();
     };
     // Values that nobody may read -- behind the request's last position, or of a page that is not there -- become zeros: a weight of zero times a NaN is one.
     auto scrub = [&](int base, bool there, unsigned buf) {
@@ -678,14 +688,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     }
     kp_wait<0>();
     kp_barrier();
-    multiply(std::true_type{}, 0u, 0u);
+    auto nothing = [](int) {};
+    multiply_keys(0u, nothing);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) scale(i);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) look(i);
     kp_barrier();
     unsigned b0 = 0, b1 = PART;                  // buffers of pages it and it + 1
+    auto bring = [&](int j) __attribute__((always_inline)) {
+        if (j < MINE) bring_keys(from2, b0, j);
+        else if (j < 2 * MINE) bring_values(from1, b1, j - MINE);
+    };
     auto begin = [&](int it) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < MINE; ++j) bring_keys(from2, b0, j);
-#pragma unroll
-        for (int j = 0; j < MINE; ++j) bring_values(from1, b1, j);
         if (page < 0 || base_of(it) + KV16_PAGE > rq.len) {
             scrub(base_of(it), page >= 0, b0);
             kp_barrier();
@@ -708,14 +723,48 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     if (n_wave > 0) {
         int it = 0;
         do {
+            settle(page < 0 ? 0x7fffff00 : base_of(it));      // (nothing of a page that is not there is seen)
             begin(it);
-            soften(page < 0 ? 0x7fffff00 : base_of(it));      // (nothing of a page that is not there is seen)
-            multiply(std::false_type{}, b0, b1);
+            multiply_keys(b1, [&](int i) __attribute__((always_inline)) {
+                if (NK == 8) {
+                    weigh(i);
+                    if (i >= 8) add(i - 8);
+                } else {
+                    weigh(2 * i);
+                    weigh(2 * i + 1);
+                }
+                bring(i);
+            });
+            multiply_values(b0, [&](int i) __attribute__((always_inline)) {
+                if (NK == 8) {
+                    if (i < 4) {
+                        add(8 + 2 * i);
+                        add(9 + 2 * i);
+                    } else if (i < 12) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) scale(4 * (i - 4) + k);
+                        look(2 * (i - 4));
+                        look(2 * (i - 4) + 1);
+                    }
+                } else {
+                    if (i < 4) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) add(4 * i + k);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) scale(8 * (i - 4) + k);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) look(4 * (i - 4) + k);
+                    }
+                }
+            });
             end(it);
         } while (++it < n_wave);
     }
     for (int it = n_wave; it < n_it; ++it) {
         begin(it);
+#pragma unroll
+        for (int j = 0; j < 2 * MINE; ++j) bring(j);
         end(it);
     }
     kp_wait<0>();                                // (nothing may be on its way into LDS that is no longer this workgroup's)
