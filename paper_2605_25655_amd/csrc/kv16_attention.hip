@@ -461,14 +461,14 @@ __device__ __forceinline__ const Kv16AttnArgs& arguments_again()
 template <int D, int WAVES, bool STATS>
 __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a)
 {
-    constexpr int NK = D / 16, NT = D / 32;      // steps of 16 columns of the scores' product, tiles of 32 columns of the result
+    constexpr int NB = D / 32, NT = D / 16;      // steps of 32 columns of the scores' product, tiles of 16 columns of the result
     constexpr int PART = 64 * D * 2;             // bytes of a page's keys, or values, of a head
     constexpr int MINE = PART / 1024 / WAVES; // loads of each that a wave makes
     extern __shared__ uintx4 kp_smem[];
     __shared__ unsigned s_odd[WAVES];
     __shared__ float s_m[32 * WAVES], s_exact[32 * WAVES], s_w[KV16_PAGE];
 
-    const int tid = threadIdx.x, lane = tid & 63, row_lane = lane & 31, h = lane >> 5, lo = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Tile tile = find_tile<WAVES>(a);
     const Request& rq = tile.rq;
@@ -476,8 +476,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     if (r0 >= all_rows || c0 > c1 || (tile.chunk > 0 && c0 >= rq.pages)) return;
 
     const int w0 = r0 + wv * 32;                 // this wave's first row
-    const int r = w0 + row_lane < all_rows ? w0 + row_lane : all_rows - 1;
-    const Sight mine = sight_of(a, rq, r / group);
+    Sight mine[2];                               // of the lane's two rows, w0 + lo and 16 further on
+#pragma unroll
+    for (int c = 0; c < 2; ++c) mine[c] = sight_of(a, rq, (w0 + 16 * c + lo < all_rows ? w0 + 16 * c + lo : all_rows - 1) / group);
     const Sight low = sight_of(a, rq, (w0 < all_rows ? w0 : all_rows - 1) / group), high = sight_of(a, rq, (w0 + 31 < all_rows ? w0 + 31 : all_rows - 1) / group);
     const int tile_from = sight_of(a, rq, r0 / group).from, tile_end = sight_of(a, rq, (r0 + 32 * WAVES - 1 < all_rows ? r0 + 32 * WAVES - 1 : all_rows - 1) / group).end;
     const bool rows_here = w0 < all_rows;
@@ -506,11 +507,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
         return e < a.num_pages ? e : -1;
     };
 
-    half8 queries[NK];
+    half8 queries[2][NB];
 #pragma unroll
-    for (int k = 0; k < NK; ++k) queries[k] = __builtin_bit_cast(half8, ld_cached(a.q + tile.row(a, r) * D + k * 16 + h * 8));
+    for (int c = 0; c < 2; ++c) {
+        const int r = w0 + 16 * c + lo < all_rows ? w0 + 16 * c + lo : all_rows - 1;
 #pragma unroll
-    for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(queries[k]));      // waited for here, and not in every turn behind what is on its way into LDS
+        for (int b = 0; b < NB; ++b) queries[c][b] = __builtin_bit_cast(half8, ld_cached(a.q + tile.row(a, r) * D + b * 32 + hi * 8));
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) asm volatile("" : "+v"(queries[c][b]));      // waited for here, and not in every turn behind what is on its way into LDS
 
     const unsigned smem_at = (unsigned)(size_t)(__attribute__((address_space(3))) void*)kp_smem, lane16 = lane * 16;
     const uint16_t* const heads = a.pages + (size_t)tile.g * kv16_head_values(D);
@@ -525,23 +532,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
         kp_bring(from + kv16_values(D) + (wv + j * WAVES) * 512, lane16, lds_at + KP_BUFS * PART + buf + j * WAVES * 1024);
     };
 
-    float m = -__builtin_inff(), start = 0.f, l = 0.f, exact = 0.f;      // sums: of this lane's positions only
+    float m[2] = {-__builtin_inff(), -__builtin_inff()}, start[2] = {0.f, 0.f}, l[2] = {0.f, 0.f}, exact[2] = {0.f, 0.f};      // sums: of this lane's positions only
     bool fresh = true;
-    floatx16 o[NT], s[2];
-    half8 pw[4];
+    floatx4 o[2][NT], s[2][4];
+    half8 pw[2][2];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+        for (int t = 0; t < NT; ++t) o[c][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    // where a lane's operands begin: keys of position lane % 32 of a tile of 32, columns 8 h .. of a step; values of column lane % 32 of a tile, positions of hi = 2 s + h
-    const unsigned k_lane = ((lane >> 4 & 1) * (D / 32) * 64 + h * 16 + lo) * 16, v_lane = ((lane >> 4 & 1) * 64 + h * 16 + lo) * 16;
-    auto key_at = [&](const char* keys, int t, int k) __attribute__((always_inline)) {
-        return *reinterpret_cast<const half8*>(keys + k_lane + (t * 2 * (D / 32) + k / 2) * 1024 + (k & 1) * 512);
-    };
-    auto value_at = [&](const char* values, int t, int k) __attribute__((always_inline)) {      // step k: positions 32 (k / 2) .., s = k % 2
-        return *reinterpret_cast<const half8*>(values + v_lane + ((k >> 1) * (D / 16) + t * 2) * 1024 + (k & 1) * 512);
-    };
     // N products whose operands are asked for KP_AHEAD ahead, in this order, or the compiler would ask for each where it is needed and wait; `between` puts vector work into the time that
     // the i-th takes.
     auto products = [&](auto count, auto fetch, auto product, auto between) __attribute__((always_inline)) {
@@ -558,98 +557,105 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // the scores of a page, into s
+    // the scores of a page, into s: an operand for two products
     auto multiply_keys = [&](unsigned buf, auto between) __attribute__((always_inline)) {
-        const char* const keys = reinterpret_cast<const char*>(kp_smem) + buf;
-        products(std::integral_constant<int, 2 * NK>{}, [&](int i) __attribute__((always_inline)) { return key_at(keys, i & 1, i >> 1); },
+        const uintx4* const keys = kp_smem + buf / 16 + lane;
+        products(std::integral_constant<int, 4 * NB>{}, [&](int i) __attribute__((always_inline)) { return __builtin_bit_cast(half8, keys[((i & 3) * NB + (i >> 2)) * 64]); },
                  [&](int i, half8 k) __attribute__((always_inline)) {
-                     const floatx16 none = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                     s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, queries[i >> 1], i < 2 ? none : s[i & 1], 0, 0, 0);
+                     const floatx4 none = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                     for (int c = 0; c < 2; ++c) s[c][i & 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, queries[c][i >> 2], i < 4 ? none : s[c][i & 3], 0, 0, 0);
                  },
                  between);
     };
     // a page's weights times its values
     auto multiply_values = [&](unsigned buf, auto between) __attribute__((always_inline)) {
-        const char* const values = reinterpret_cast<const char*>(kp_smem) + KP_BUFS * PART + buf;
-        products(std::integral_constant<int, 4 * NT>{}, [&](int i) __attribute__((always_inline)) { return value_at(values, i % NT, i / NT); },
-                 [&](int i, half8 v) __attribute__((always_inline)) { o[i % NT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pw[i / NT], o[i % NT], 0, 0, 0); }, between);
+        const uintx4* const values = kp_smem + (KP_BUFS * PART + buf) / 16 + lane;
+        products(std::integral_constant<int, 2 * NT>{}, [&](int i) __attribute__((always_inline)) { return __builtin_bit_cast(half8, values[i * 64]); },
+                 [&](int i, half8 v) __attribute__((always_inline)) {
+#pragma unroll
+                     for (int c = 0; c < 2; ++c) o[c][i % NT] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pw[c][i / NT], o[c][i % NT], 0, 0, 0);
+                 },
+                 between);
     };
-    // t: what the exponentials of a page are of; largest: the largest of the lane's
-    float t[32], largest = -__builtin_inff();
-    auto scale = [&](int i) __attribute__((always_inline)) { t[i] = __builtin_fmaf(s[i >> 4][i & 15], a.scale2, start); };
-    auto look = [&](int i) __attribute__((always_inline)) { largest = __builtin_fmaxf(__builtin_fmaxf(largest, t[2 * i]), t[2 * i + 1]); };      // (a NaN does not show, but its row's sums are not numbers)
+    // t: what the exponentials of a page are of, 16 positions for each of the lane's rows; largest: the largest of them
+    float t[32], largest[2] = {-__builtin_inff(), -__builtin_inff()};
+    auto scale = [&](int i) __attribute__((always_inline)) { t[i] = __builtin_fmaf(s[i >> 4][(i >> 2) & 3][i & 3], a.scale2, start[i >> 4]); };
+    auto look = [&](int i) __attribute__((always_inline)) {      // (a NaN does not show, but its row's sums are not numbers)
+        largest[i >> 3] = __builtin_fmaxf(__builtin_fmaxf(largest[i >> 3], t[2 * i]), t[2 * i + 1]);
+    };
     // The i-th pair of weights.  They are cut to fp16's bits, not rounded to the nearest: their sum is one of cut weights too, so that what all are too small by cancels, and what is left is
     // half a step of each as with the other rounding; that one's conversion, of two values to the nearest, keeps matrix products of the SIMD's other wave from running for half of its time,
     // this one's does not.  (So do exponentials, for all of theirs; and products of fp16 pairs, which is why the sum is one of single values.)
     auto weigh = [&](int i) __attribute__((always_inline)) {
-        const int k = i >> 2, e = 2 * (i & 3);
-        const float w0 = __builtin_amdgcn_exp2f(t[16 * (k >> 1) + 8 * (e >> 2) + 4 * (k & 1) + (e & 3)]), w1 = __builtin_amdgcn_exp2f(t[16 * (k >> 1) + 8 * (e >> 2) + 4 * (k & 1) + (e & 3) + 1]);
-        if (STATS) exact += w0 + w1;
+        const int c = i >> 3, k = (i >> 2) & 1, e = 2 * (i & 3);
+        const float w0 = __builtin_amdgcn_exp2f(t[2 * i]), w1 = __builtin_amdgcn_exp2f(t[2 * i + 1]);
+        if (STATS) exact[c] += w0 + w1;
         const half2v w = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w0, w1));
-        pw[k][e] = w[0];
-        pw[k][e + 1] = w[1];
+        pw[c][k][e] = w[0];
+        pw[c][k][e + 1] = w[1];
     };
     auto add = [&](int i) __attribute__((always_inline)) {
-        const unsigned both = __builtin_bit_cast(unsigned, half2v{pw[i >> 2][2 * (i & 3)], pw[i >> 2][2 * (i & 3) + 1]});
-        asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel_hi:[1,0,0]" : "+v"(l) : "v"(both));                       // (the low one, the high one)
-        asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l) : "v"(both));
+        const int c = i >> 3, n = (i >> 2) & 1, e = 2 * (i & 3);
+        const unsigned both = __builtin_bit_cast(unsigned, half2v{pw[c][n][e], pw[c][n][e + 1]});
+        asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel_hi:[1,0,0]" : "+v"(l[c]) : "v"(both));                       // (the low one, the high one)
+        asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l[c]) : "v"(both));
     };
     // What a row does not see of the page, and a maximum that weights refer to if there is none or a weight would be past 2^15.
     auto settle = [&](int base) __attribute__((always_inline)) {
         bool masked = false;
         if (base + KV16_PAGE > low.end) {        // some row's end is in front of the page's
             masked = true;
-            const int end = mine.end - base - 4 * h;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) t[i] = end > 8 * (i >> 2) + (i & 3) ? t[i] : -__builtin_inff();
+            for (int i = 0; i < 32; ++i) t[i] = mine[i >> 4].end - base - 4 * hi > 16 * ((i >> 2) & 3) + (i & 3) ? t[i] : -__builtin_inff();
         }
         if (base < high.from && base + KV16_PAGE > a.sinks) {      // some row's window begins behind the page's first position, and not all of them are sinks
             masked = true;
-            const int hidden = a.sinks - base - 4 * h, span = mine.from > a.sinks ? mine.from - a.sinks : 0;
+            const int hidden = a.sinks - base - 4 * hi;
+            const int span[2] = {mine[0].from > a.sinks ? mine[0].from - a.sinks : 0, mine[1].from > a.sinks ? mine[1].from - a.sinks : 0};
 #pragma unroll
-            for (int i = 0; i < 32; ++i) t[i] = (unsigned)(8 * (i >> 2) + (i & 3) - hidden) < (unsigned)span ? -__builtin_inff() : t[i];
+            for (int i = 0; i < 32; ++i) t[i] = (unsigned)(16 * ((i >> 2) & 3) + (i & 3) - hidden) < (unsigned)span[i >> 4] ? -__builtin_inff() : t[i];
         }
         if (masked) {
-            largest = -__builtin_inff();
+            largest[0] = largest[1] = -__builtin_inff();
 #pragma unroll
             for (int i = 0; i < 16; ++i) look(i);
         }
-        if (fresh || __builtin_amdgcn_ballot_w64(largest > 15.0f) != 0ull) {
-            const float mb = __builtin_fmaxf(largest, __shfl_xor(largest, 32)), mn = __builtin_fmaxf(m, mb - start);
-            const bool none = mn == -__builtin_inff();
-            const float corr = __builtin_amdgcn_exp2f(m - (none ? 0.f : mn)), now = none ? 0.f : WEIGHT_LOG2 - mn;
-            fresh = __builtin_amdgcn_ballot_w64(none) != 0ull;
+        if (fresh || __builtin_amdgcn_ballot_w64(__builtin_fmaxf(largest[0], largest[1]) > 15.0f) != 0ull) {
+            fresh = false;
+            bool some = false;                   // (else all sums are zeros)
+            float corr[2];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) t[i] = t[i] - start + now;
-            const bool some = __builtin_amdgcn_ballot_w64(m != -__builtin_inff()) != 0ull;      // (else all sums are zeros)
-            m = mn;
-            start = now;
-            l *= corr;
-            if (STATS) exact *= corr;
-            // By way of LDS, half a tile at a time: the compiler gives products of the accumulators registers of their own, and copies all of them to and fro on the other path (64 moves
+            for (int c = 0; c < 2; ++c) {
+                const float mn = __builtin_fmaxf(m[c], max_over_hi(largest[c]) - start[c]);
+                const bool none = mn == -__builtin_inff();
+                corr[c] = __builtin_amdgcn_exp2f(m[c] - (none ? 0.f : mn));
+                const float now = none ? 0.f : WEIGHT_LOG2 - mn;
+                fresh = fresh || __builtin_amdgcn_ballot_w64(none) != 0ull;
+                some = some || __builtin_amdgcn_ballot_w64(m[c] != -__builtin_inff()) != 0ull;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) t[16 * c + i] = t[16 * c + i] - start[c] + now;
+                m[c] = mn;
+                start[c] = now;
+                l[c] *= corr[c];
+                if (STATS) exact[c] *= corr[c];
+            }
+            // By way of LDS, some at a time: the compiler gives products of the accumulators registers of their own, and copies all of them to and fro on the other path (64 moves
             // of pairs a page, each a time in which no matrix product runs).
             if (some) {
                 uintx4* const own = kp_smem + 2 * KP_BUFS * PART / 16 + wv * 128 + lane;
 #pragma unroll
-                for (int k = 0; k < 2 * NT; ++k) {
+                for (int n = 0; n < NT; ++n) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int r = (k & 1) * 8 + 4 * i;
-                        const floatx4 y = {o[k / 2][r] * corr, o[k / 2][r + 1] * corr, o[k / 2][r + 2] * corr, o[k / 2][r + 3] * corr};
-                        own[i * 64] = __builtin_bit_cast(uintx4, y);
-                    }
+                    for (int c = 0; c < 2; ++c) own[c * 64] = __builtin_bit_cast(uintx4, o[c][n] * corr[c]);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const floatx4 y = __builtin_bit_cast(floatx4, own[i * 64]);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[k / 2][(k & 1) * 8 + 4 * i + r] = y[r];
-                    }
+                    for (int c = 0; c < 2; ++c) o[c][n] = __builtin_bit_cast(floatx4, own[c * 64]);
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 }
             }
         }
-        largest = -__builtin_inff();
+        largest[0] = largest[1] = -__builtin_inff();
     };
     // Values that nobody may read -- behind the request's last position, or of a page that is not there -- become zeros: a weight of zero times a NaN is one.
     auto scrub = [&](int base, bool there, unsigned buf) {
@@ -726,7 +732,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
             settle(page < 0 ? 0x7fffff00 : base_of(it));      // (nothing of a page that is not there is seen)
             begin(it);
             multiply_keys(b1, [&](int i) __attribute__((always_inline)) {
-                if (NK == 8) {
+                if (NB == 4) {
                     weigh(i);
                     if (i >= 8) add(i - 8);
                 } else {
@@ -736,7 +742,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
                 bring(i);
             });
             multiply_values(b0, [&](int i) __attribute__((always_inline)) {
-                if (NK == 8) {
+                if (NB == 4) {
                     if (i < 4) {
                         add(8 + 2 * i);
                         add(9 + 2 * i);
@@ -772,44 +778,51 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     // What follows is made of the arguments anew: kept over the loop, it would take the scalar registers that the loop needs.
     const Kv16AttnArgs& e = arguments_again();
     const Tile at = find_tile<WAVES>(e);
-    l += __shfl_xor(l, 32);
-    if (STATS) exact += __shfl_xor(exact, 32);
-    bool odd = false;
+    unsigned odd_rows = 0;                       // of the wave's 32
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int c = 0; c < 2; ++c) {
+        l[c] += __shfl_xor(l[c], 16);
+        l[c] += __shfl_xor(l[c], 32);
+        if (STATS) {
+            exact[c] += __shfl_xor(exact[c], 16);
+            exact[c] += __shfl_xor(exact[c], 32);
+        }
+        bool odd = false;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) odd = odd || !finite(o[t][i]);
-    const int own = wv * 32 + row_lane;
-    const bool mine_here = at.r0 + own < at.all_rows;
-    const unsigned long long odd_lanes = __builtin_amdgcn_ballot_w64(odd && mine_here);
-    const unsigned odd_rows = (unsigned)odd_lanes | (unsigned)(odd_lanes >> 32);
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) odd = odd || !finite(o[c][t][i]);
+        unsigned long long lanes = __builtin_amdgcn_ballot_w64(odd);
+        lanes |= lanes >> 32;
+        odd_rows |= ((unsigned)(lanes | lanes >> 16) & 0xffffu) << (16 * c);
+    }
+    const int here = at.all_rows - at.r0 - wv * 32;          // rows of this wave
+    if (here < 32) odd_rows &= here <= 0 ? 0u : (1u << here) - 1u;
     if (lane == 0) s_odd[wv] = odd_rows;
-    if (h == 0) { s_m[own] = m; s_exact[own] = exact; }
     auto put_stats = [&](int r, float mm, float ll) {
         float* const to = e.stats + 2 * part_row(e, at.b, r, at.g, at.group);
         to[0] = mm == -__builtin_inff() ? 0.f : mm;
         to[1] = ll == 0.f ? 0.f : 1.0f / ll;
     };
-    if (mine_here && !(odd_rows >> row_lane & 1)) {
-        const int r = at.r0 + own;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const int own = 16 * c + lo, r = at.r0 + wv * 32 + own;
+        if (hi == 0) { s_m[wv * 32 + own] = m[c]; s_exact[wv * 32 + own] = exact[c]; }
+        if (own >= here || (odd_rows >> own & 1)) continue;
         if (at.whole) {
-            const float inv = l == 0.f ? 0.f : 1.0f / l;
+            const float inv = l[c] == 0.f ? 0.f : 1.0f / l[c];
             uint16_t* const out = e.out + at.row(e, r) * D;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const half4 y = {(_Float16)(o[t][4 * i] * inv), (_Float16)(o[t][4 * i + 1] * inv), (_Float16)(o[t][4 * i + 2] * inv), (_Float16)(o[t][4 * i + 3] * inv)};
-                    *reinterpret_cast<half4*>(out + 32 * t + 8 * i + 4 * h) = y;
-                }
-            if (STATS && h == 0) put_stats(r, m, exact);
+            for (int t = 0; t < NT; ++t) {
+                const half4 y = {(_Float16)(o[c][t][0] * inv), (_Float16)(o[c][t][1] * inv), (_Float16)(o[c][t][2] * inv), (_Float16)(o[c][t][3] * inv)};
+                *reinterpret_cast<half4*>(out + 16 * t + 4 * hi) = y;
+            }
+            if (STATS && hi == 0) put_stats(r, m[c], exact[c]);
         } else {
             float* const po = e.part + (part_row(e, at.b, r, at.g, at.group) * e.nsplit + at.chunk) * kv16_part(D);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) *reinterpret_cast<floatx4*>(po + 32 * t + 8 * i + 4 * h) = floatx4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
-            if (h == 0) { po[D] = m; po[D + 1] = l; po[D + 2] = exact; }
+            for (int t = 0; t < NT; ++t) *reinterpret_cast<floatx4*>(po + 16 * t + 4 * hi) = o[c][t];
+            if (hi == 0) { po[D] = m[c]; po[D + 1] = l[c]; po[D + 2] = exact[c]; }
         }
     }
     __syncthreads();
