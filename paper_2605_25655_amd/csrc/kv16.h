@@ -44,6 +44,7 @@ struct Kv16AttnArgs {
     float scale2;                    // softmax scale times log2(e)
     int window, sinks;               // window 0: everything in front of a token
     int B, T, Hq, Hkv, D, max_q, num_pages, max_pages;
+    int group;                       // Hq / Hkv query heads per cache head
     // how the rows are dealt (kv16_plan)
     float* part;                     // [B][max_q][Hq][nsplit][kv16_part(D)]: a chunk's unnormalised output, maximum, sum of the weights as they were multiplied, and as they are
     float* stats;                    // [B][max_q][Hq][2]: a row's maximum and one over its sum, with weights_out

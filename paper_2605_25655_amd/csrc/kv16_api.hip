@@ -42,7 +42,7 @@ int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 
 void thi::kv16_plan(Kv16AttnArgs& a, int num_cus)
 {
-    const int group = a.Hq / a.Hkv;
+    const int group = a.group = a.Hq / a.Hkv;
     a.split_rows = (long)a.max_q * group <= FEW_ROWS;
     const int rows = a.split_rows ? 16 : 128;
     a.tiles = (int)(((long)a.max_q * group + rows - 1) / rows);

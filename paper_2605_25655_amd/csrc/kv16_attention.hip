@@ -61,7 +61,7 @@ __device__ __forceinline__ bool sees(const Sight& s, int sinks, int pos) { retur
 // request's chunk borders, and with them the bits of its result, do not depend on its neighbours.
 __device__ __forceinline__ int chunk_pages(const Kv16AttnArgs& a, int pages)
 {
-    const int size = (pages + a.nsplit - 1) / a.nsplit;
+    const int size = a.nsplit == 1 ? pages : (pages + a.nsplit - 1) / a.nsplit;
     return size > a.min_chunk ? size : a.min_chunk;
 }
 
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
 
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int group = a.Hq / a.Hkv;
+    const int group = a.group;
     const int g = blockIdx.x / a.tiles, r0 = (blockIdx.x % a.tiles) * 16;      // first row of this tile: row r is token r / group, head r % group
     const int b = blockIdx.y, chunk = blockIdx.z;
     const Request rq = find_request(a, b);
@@ -429,27 +429,28 @@ template <int N> __device__ __forceinline__ void kp_wait() { asm volatile("s_wai
 // What a workgroup of WAVES waves works on: 32 WAVES rows of a cache head from row r0 on, and of the pages its request looks at c0 .. c1 - 1.
 struct Tile {
     Request rq;
-    int group, g, b, chunk, r0, all_rows, c0, c1;
+    int g, b, chunk, r0, all_rows, c0, c1;
     bool whole;
-    __device__ __forceinline__ size_t row(const Kv16AttnArgs& a, int r) const { return (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group; }      // of q and out
+    __device__ __forceinline__ size_t row(const Kv16AttnArgs& a, int r) const { return (size_t)(rq.first + r / a.group) * a.Hq + (size_t)g * a.group + r % a.group; }      // of q and out
 };
 template <int WAVES> __device__ __forceinline__ Tile find_tile(const Kv16AttnArgs& a)
 {
     Tile t;
-    t.group = a.Hq / a.Hkv;
     // the last rows first: they see the most
-    t.g = blockIdx.x % a.Hkv;
-    t.r0 = (a.tiles - 1 - (int)blockIdx.x / a.Hkv) * 32 * WAVES;
+    const int number = blockIdx.x / (unsigned)a.Hkv;
+    t.g = blockIdx.x - number * a.Hkv;
+    t.r0 = (a.tiles - 1 - number) * 32 * WAVES;
     t.b = blockIdx.y;
     t.chunk = blockIdx.z;
     t.rq = find_request(a, t.b);
-    t.all_rows = t.rq.n * t.group;
+    t.all_rows = t.rq.n * a.group;
     const int size = chunk_pages(a, t.rq.pages);
     t.whole = t.rq.pages <= size;
     t.c0 = t.chunk * size;
     t.c1 = t.c0 + size < t.rq.pages ? t.c0 + size : t.rq.pages;
     return t;
 }
+// The arguments, read again: kept over the loop, they would take the scalar registers that it needs.
 __device__ __forceinline__ const Kv16AttnArgs& arguments_again()
 {
     auto p = __builtin_amdgcn_kernarg_segment_ptr();
@@ -466,21 +467,32 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     constexpr int MINE = PART / 1024 / WAVES; // loads of each that a wave makes
     extern __shared__ uintx4 kp_smem[];
     __shared__ unsigned s_odd[WAVES];
+    __shared__ Tile s_tile;
     __shared__ float s_m[32 * WAVES], s_exact[32 * WAVES], s_w[KV16_PAGE];
 
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Tile tile = find_tile<WAVES>(a);
     const Request& rq = tile.rq;
-    const int group = tile.group, r0 = tile.r0, all_rows = tile.all_rows, c0 = tile.c0, c1 = tile.c1;
-    if (r0 >= all_rows || c0 > c1 || (tile.chunk > 0 && c0 >= rq.pages)) return;
+    const int r0 = tile.r0, all_rows = tile.all_rows, c0 = tile.c0, c1 = tile.c1;
+    if (r0 >= all_rows || (tile.chunk > 0 && c0 >= rq.pages)) return;
+    if (tid == 0) s_tile = tile;                 // (for the end)
 
-    const int w0 = r0 + wv * 32;                 // this wave's first row
-    Sight mine[2];                               // of the lane's two rows, w0 + lo and 16 further on
+    // The lane's two rows, w0 + lo and 16 further on (rows that are not there: the last one), and what they see.
+    const int w0 = r0 + wv * 32, first_token = r0 / a.group, first_head = r0 - first_token * a.group;
+    size_t row[2];                               // of q and out
+    int token[2];
+    Sight mine[2];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) mine[c] = sight_of(a, rq, (w0 + 16 * c + lo < all_rows ? w0 + 16 * c + lo : all_rows - 1) / group);
-    const Sight low = sight_of(a, rq, (w0 < all_rows ? w0 : all_rows - 1) / group), high = sight_of(a, rq, (w0 + 31 < all_rows ? w0 + 31 : all_rows - 1) / group);
-    const int tile_from = sight_of(a, rq, r0 / group).from, tile_end = sight_of(a, rq, (r0 + 32 * WAVES - 1 < all_rows ? r0 + 32 * WAVES - 1 : all_rows - 1) / group).end;
+    for (int c = 0; c < 2; ++c) {
+        const int r = w0 + 16 * c + lo < all_rows ? w0 + 16 * c + lo : all_rows - 1, n = (r - r0 + first_head) / a.group;
+        token[c] = first_token + n;
+        row[c] = (size_t)(rq.first + token[c]) * a.Hq + (size_t)tile.g * a.group + (r - r0 + first_head - n * a.group);
+        mine[c] = sight_of(a, rq, token[c]);
+    }
+    const Sight low = sight_of(a, rq, __builtin_amdgcn_readfirstlane(token[0])), high = sight_of(a, rq, __builtin_amdgcn_readlane(token[1], 15));
+    const int last_row = r0 + 32 * WAVES - 1 < all_rows ? r0 + 32 * WAVES - 1 : all_rows - 1;
+    const int tile_from = sight_of(a, rq, first_token).from, tile_end = sight_of(a, rq, first_token + (last_row - r0 + first_head) / a.group).end;
     const bool rows_here = w0 < all_rows;
 
     // The pages of this chunk that some row of the tile sees: of the sinks, then from the first row's window to the last row's own
@@ -496,28 +508,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     auto base_of = [&](int it) { return it * KV16_PAGE + (it < n_lead ? from_lead : from_window); };
     int entries = -1;
     const int* const table = a.page_table + (size_t)tile.b * a.max_pages;
-    auto list = [&](int it) {                    // the table's entries of turns it .. it + 63, one a lane; waited for here
+    auto list = [&](int it) {                    // the table's entries of turns it .. it + 63, one a lane
         const int at = it + lane < n_it ? it + lane : n_it - 1;      // (no branch, here and in scrub: a loop with one that lanes take apart is put together anew, and accumulators are copied)
         const int e = table[at < 0 ? 0 : base_of(at) / KV16_PAGE];
         entries = it + lane < n_it ? e : -1;
-        asm volatile("" : "+v"(entries));
     };
+    auto listed = [&]() { asm volatile("" : "+v"(entries)); };      // waited for here
     auto page_at = [&](int it) __attribute__((always_inline)) {      // -1: not there
         const int e = __builtin_amdgcn_readlane(entries, it & 63);
         return e < a.num_pages ? e : -1;
     };
 
+    list(0);
     half8 queries[2][NB];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int r = w0 + 16 * c + lo < all_rows ? w0 + 16 * c + lo : all_rows - 1;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) queries[c][b] = __builtin_bit_cast(half8, ld_cached(a.q + tile.row(a, r) * D + b * 32 + hi * 8));
-    }
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int b = 0; b < NB; ++b) asm volatile("" : "+v"(queries[c][b]));      // waited for here, and not in every turn behind what is on its way into LDS
+        for (int b = 0; b < NB; ++b) queries[c][b] = __builtin_bit_cast(half8, ld_cached(a.q + row[c] * D + b * 32 + hi * 8));
 
     const unsigned smem_at = (unsigned)(size_t)(__attribute__((address_space(3))) void*)kp_smem, lane16 = lane * 16;
     const uint16_t* const heads = a.pages + (size_t)tile.g * kv16_head_values(D);
@@ -683,7 +690,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     auto turns_to = [&](int end, int from, int most) { const int n = (end - from + KV16_PAGE - 1) / KV16_PAGE; return end <= from ? 0 : n < most ? n : most; };
     const int lead_turns = turns_to(here_end, from_lead, n_lead);
     const int n_wave = lead_turns < n_lead ? lead_turns : n_it > n_lead ? n_lead + turns_to(here_end, from_window + n_lead * KV16_PAGE, n_it - n_lead) : n_lead;
-    list(0);
+    listed();
     int page = page_at(0), page1 = page_at(1), page2 = page_at(2);      // of pages it, it + 1, it + 2
     const uint16_t *from1 = head(page1), *from2 = head(page2);
 #pragma unroll
@@ -692,6 +699,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
         bring_values(head(page), 0, j);
         bring_keys(from1, PART, j);
     }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) asm volatile("" : "+v"(queries[c][b]));      // waited for here, and not in every turn behind what is on its way into LDS
     kp_wait<0>();
     kp_barrier();
     auto nothing = [](int) {};
@@ -711,7 +722,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
             scrub(base_of(it), page >= 0, b0);
             kp_barrier();
         }
-        if (((it + 3) & 63) == 0) list(it + 3);
+        if (((it + 3) & 63) == 0) {
+            list(it + 3);
+            listed();
+        }
     };
     auto end = [&](int it) __attribute__((always_inline)) {
         page = page1;
@@ -775,9 +789,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     }
     kp_wait<0>();                                // (nothing may be on its way into LDS that is no longer this workgroup's)
 
-    // What follows is made of the arguments anew: kept over the loop, it would take the scalar registers that the loop needs.
     const Kv16AttnArgs& e = arguments_again();
-    const Tile at = find_tile<WAVES>(e);
+    const Tile& at = s_tile;
     unsigned odd_rows = 0;                       // of the wave's 32
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -800,7 +813,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     if (here < 32) odd_rows &= here <= 0 ? 0u : (1u << here) - 1u;
     if (lane == 0) s_odd[wv] = odd_rows;
     auto put_stats = [&](int r, float mm, float ll) {
-        float* const to = e.stats + 2 * part_row(e, at.b, r, at.g, at.group);
+        float* const to = e.stats + 2 * part_row(e, at.b, r, at.g, e.group);
         to[0] = mm == -__builtin_inff() ? 0.f : mm;
         to[1] = ll == 0.f ? 0.f : 1.0f / ll;
     };
@@ -811,7 +824,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
         if (own >= here || (odd_rows >> own & 1)) continue;
         if (at.whole) {
             const float inv = l[c] == 0.f ? 0.f : 1.0f / l[c];
-            uint16_t* const out = e.out + at.row(e, r) * D;
+            uint16_t* const out = e.out + row[c] * D;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const half4 y = {(_Float16)(o[c][t][0] * inv), (_Float16)(o[c][t][1] * inv), (_Float16)(o[c][t][2] * inv), (_Float16)(o[c][t][3] * inv)};
@@ -819,7 +832,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
             }
             if (STATS && hi == 0) put_stats(r, m[c], exact[c]);
         } else {
-            float* const po = e.part + (part_row(e, at.b, r, at.g, at.group) * e.nsplit + at.chunk) * kv16_part(D);
+            float* const po = e.part + (part_row(e, at.b, r, at.g, e.group) * e.nsplit + at.chunk) * kv16_part(D);
 #pragma unroll
             for (int t = 0; t < NT; ++t) *reinterpret_cast<floatx4*>(po + 16 * t + 4 * hi) = o[c][t];
             if (hi == 0) { po[D] = m[c]; po[D + 1] = l[c]; po[D + 2] = exact[c]; }
@@ -833,13 +846,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
             rows &= rows - 1;
             const float mm = s_m[c];
             float ll;
-            const float of = slow_row<D, 64 * WAVES>(e, at.rq, at.b, at.g, at.row(e, r), r / at.group, at.c0, at.c1, mm, s_w, ll) * 512.0f;
+            const float of = slow_row<D, 64 * WAVES>(e, at.rq, at.b, at.g, at.row(e, r), r / e.group, at.c0, at.c1, mm, s_w, ll) * 512.0f;
             ll *= 512.0f;
             if (at.whole) {
                 if (tid < D) e.out[at.row(e, r) * D + tid] = ll == 0.f ? 0 : to_half_bits(of / ll);
                 if (STATS && tid == 0) put_stats(r, mm, s_exact[c]);
             } else {
-                float* const po = e.part + (part_row(e, at.b, r, at.g, at.group) * e.nsplit + at.chunk) * kv16_part(D);
+                float* const po = e.part + (part_row(e, at.b, r, at.g, e.group) * e.nsplit + at.chunk) * kv16_part(D);
                 if (tid < D) po[tid] = of;
                 if (tid == 0) { po[D] = mm; po[D + 1] = ll; po[D + 2] = s_exact[c]; }
             }
@@ -861,7 +874,7 @@ __global__ __launch_bounds__(KW_THREADS) void kv16_attn_weights(Kv16AttnArgs a)
     const Request rq = find_request(a, b);
     const int p0 = number * KV16_PAGE;
     if (number >= a.max_pages || p0 >= rq.len) return;
-    const int group = a.Hq / a.Hkv, before = rq.len - rq.n;
+    const int group = a.group, before = rq.len - rq.n;
     const int page = a.page_table[(size_t)b * a.max_pages + number];
     float sum[16];
 #pragma unroll
