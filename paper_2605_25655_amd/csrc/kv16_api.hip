@@ -35,6 +35,12 @@ size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
 }
 size_t bytes_of_rows(size_t rows, int D) { return rows ? round_up(rows * kv16_part(D) * sizeof(float)) : 256; }
 size_t bytes_of_stats(int B, int Hq, int max_q) { return round_up((size_t)B * max_q * Hq * 2 * sizeof(float)); }
+// of the most that a call of up to so many leaves of its scores
+size_t bytes_of_scores(int B, int Hq, int Hkv, int max_q, int max_pages)
+{
+    const int group = Hq / Hkv, q = KV16_SCORE_ROWS / group < max_q ? KV16_SCORE_ROWS / group : max_q;
+    return round_up((size_t)B * q * Hq * max_pages * KV16_PAGE * sizeof(float));
+}
 
 int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 
@@ -88,7 +94,7 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
 size_t thi_kv16_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages, int weights)
 {
     if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_q > 65535 || max_pages < 1 || max_pages > MAX_PAGES) return 0;
-    return bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, max_q) : 0);
+    return bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, max_q) + bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0);
 }
 
 int thi_kv16_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, int window, int sinks,
@@ -107,7 +113,8 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     a.sinks = window ? sinks : 0;
     kv16_plan(a, device_cu_count());
     const size_t stats = weights_out ? bytes_of_stats(B, Hq, max_q) : 0;
-    if (workspace_bytes < stats + bytes_of_rows(a.nsplit > 1 ? (size_t)B * max_q * Hq * a.nsplit : 0, D)) return THI_ERR_WORKSPACE;
+    const size_t scores = weights_out && (long)max_q * a.group <= KV16_SCORE_ROWS ? bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0;
+    if (workspace_bytes < stats + scores + bytes_of_rows(a.nsplit > 1 ? (size_t)B * max_q * Hq * a.nsplit : 0, D)) return THI_ERR_WORKSPACE;
     (void)hipGetLastError();
     a.q = (const uint16_t*)q;
     a.pages = (const uint16_t*)pages;
@@ -120,7 +127,8 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     a.scale2 = scale * 1.44269504088896340736f;
     if (a.scale2 == 0.f) a.scale2 = 1e-30f;      // (all weights equal either way; a masked score of -inf stays what it is)
     a.stats = weights_out ? (float*)workspace : nullptr;
-    a.part = (float*)((char*)workspace + stats);
+    a.scores = scores ? (float*)((char*)workspace + stats) : nullptr;
+    a.part = (float*)((char*)workspace + stats + scores);
     return finish(launch_kv16_attention(a, (hipStream_t)hip_stream));
 }
 

@@ -149,7 +149,8 @@ __device__ __forceinline__ void split_weights(const float (&w)[4], half4& large,
 }
 __device__ __forceinline__ half8 join(half4 a, half4 b) { return half8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
 
-template <int D>
+// SCORES: they are left for kv16_attn_weigh.
+template <int D, bool SCORES>
 __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a)
 {
     constexpr int NB = D / 32, NT = D / 16;      // blocks of a key, tiles of a value's columns
@@ -251,6 +252,16 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
             for (int k = 0; k < NT; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) vx[k][i] &= keep[i];
+        }
+        if (SCORES && lo < rows) {
+            float* const to = a.scores + (((size_t)b * a.Hkv + g) * a.max_q * group + lo) * a.max_pages * KV16_PAGE + base + 4 * hi;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                floatx4 y;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[r] = t[4 * i + r] == -__builtin_inff() ? t[4 * i + r] : s[i][r] * a.scale2;
+                *reinterpret_cast<floatx4*>(to + 16 * i) = y;
+            }
         }
         half8 pl, ps;
         auto weights = [&]() __attribute__((always_inline)) {
@@ -862,71 +873,131 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
 
 // ---- what each position got of the rows' attention -------------------------------------------------------------------
 //
-// A wave takes a page of a cache head: its keys stay in registers (the A operand), the rows that see any of it come by, 16 at a time, with the maxima and sums that the
-// attention left behind.  Weights are made again, in fp32, and added up per lane (a lane keeps one row of each 16), then over the lanes: a fixed order.
-constexpr int KW_THREADS = 256;
-template <int D>
-__global__ __launch_bounds__(KW_THREADS) void kv16_attn_weights(Kv16AttnArgs a)
+// Up to 16 rows of a cache head: the few-rows kernel leaves its scores (4 bytes a row and position next to the 4 D that it reads); here they become weights with the maxima and sums that
+// the attention left behind, and are added up over the rows.  A thread takes four positions.
+constexpr int KS_THREADS = 256;
+__global__ __launch_bounds__(KS_THREADS) void kv16_attn_weigh(Kv16AttnArgs a)
 {
-    constexpr int NB = D / 32;
-    const int lane = threadIdx.x & 63, lo = lane & 15, hi = lane >> 4;
-    const int number = blockIdx.x * (KW_THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = blockIdx.y, b = blockIdx.z;
+    const int g = blockIdx.y, b = blockIdx.z, p0 = (blockIdx.x * KS_THREADS + threadIdx.x) * 4;
     const Request rq = find_request(a, b);
-    const int p0 = number * KV16_PAGE;
-    if (number >= a.max_pages || p0 >= rq.len) return;
-    const int group = a.group, before = rq.len - rq.n;
-    const int page = a.page_table[(size_t)b * a.max_pages + number];
-    float sum[16];
+    if (p0 >= rq.len) return;
+    const int number = p0 / KV16_PAGE, rows = rq.n * a.group, before = rq.len - rq.n;
+    const size_t at = ((size_t)b * a.Hkv + g) * a.max_pages * KV16_PAGE + p0;
+    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (number < rq.lead || number >= rq.lead + rq.skip) {
+        const size_t stride = (size_t)a.max_pages * KV16_PAGE;
+        const float* scores = a.scores + ((size_t)b * a.Hkv + g) * a.max_q * a.group * stride + p0;
+        for (int r = 0; r < rows; ++r, scores += stride) {
+            const floatx4 s = *reinterpret_cast<const floatx4*>(scores);
+            const float* const stats = a.stats + 2 * part_row(a, b, r, g, a.group);
+            const float m = stats[0], inv = stats[1] * 512.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-    // the tokens that see any of it: from the one at its first position on, to the last that has its last position in the window
-    int first = p0 > before ? p0 - before : 0, last = rq.n;
-    if (a.window > 0 && p0 >= a.sinks) {
-        const long most = (long)p0 + KV16_PAGE - 1 + a.window - before;      // token i sees from before + i + 1 - window on
-        last = most < last ? (most < 0 ? 0 : (int)most) : last;
+            for (int k = 0; k < 4; ++k) sum[k] = __builtin_fmaf(inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(s[k] - m), inv, sum[k]);
+        }
     }
-    if (page >= 0 && page < a.num_pages && first < last) {
-        const uint16_t* const head = a.pages + ((size_t)(unsigned)page * a.Hkv + g) * kv16_head_values(D);
-        half8 keys[4][NB];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (p0 + k < rq.len) a.weights_out[at + k] = (a.weights_in && p0 + k < before ? a.weights_in[at + k] : 0.f) + sum[k];
+}
+
+// More rows: the scores are made again.  A workgroup takes two pages of a cache head, whose keys stay in its waves' registers (the A operand); the rows that see any of them come by, 16
+// at a time, every fourth 16 in a wave.  Weights in fp32, added up per lane (a lane has one row of each 16), then over lanes and waves: a fixed order.
+constexpr int KW_THREADS = 256, KW_WAVES = 4;
+template <int D>
+__global__ __launch_bounds__(KW_THREADS, 2) void kv16_attn_weights(Kv16AttnArgs a)
+{
+    constexpr int NB = D / 32, TILES = 8;        // tiles of 16 positions
+    __shared__ float s_sum[KW_WAVES][4 * TILES][64];
+    const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int number = blockIdx.x * 2, g = blockIdx.y, b = blockIdx.z;
+    const Request rq = find_request(a, b);
+    const int p0 = number * KV16_PAGE, group = a.group, before = rq.len - rq.n;
+    if (p0 >= rq.len) return;
+    bool there[2];
+    half8 keys[TILES][NB];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int e = number + n < a.max_pages ? a.page_table[(size_t)b * a.max_pages + number + n] : -1;
+        there[n] = e >= 0 && e < a.num_pages;
+        const uint16_t* const head = a.pages + ((size_t)(unsigned)(there[n] ? e : 0) * a.Hkv + g) * kv16_head_values(D);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int k = 0; k < NB; ++k) keys[i][k] = __builtin_bit_cast(half8, ld_cached(head + (i * NB + k) * 512 + lane * 8));
-        for (int r0 = first * group; r0 < last * group; r0 += 16) {
-            const int r = r0 + lo < last * group ? r0 + lo : last * group - 1;
-            const uint16_t* const q = a.q + ((size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group) * D + hi * 8;
-            const float* const stats = a.stats + 2 * part_row(a, b, r, g, group);
-            const float m = stats[0], inv = r0 + lo < last * group ? stats[1] : 0.f;
-            const Sight mine = sight_of(a, rq, r / group);
-            floatx4 s[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < NB; ++k) {
-                const half8 x = __builtin_bit_cast(half8, ld_cached(q + k * 32));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys[i][k], x, s[i], 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int pos = p0 + 16 * (i >> 2) + 4 * hi + (i & 3);
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][i & 3], a.scale2, -m)) * 512.0f * inv;
-                sum[i] += inv != 0.f && sees(mine, a.sinks, pos) ? w : 0.f;
-            }
-        }
-#pragma unroll
-        for (int sh = 1; sh < 16; sh <<= 1)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sum[i] += __shfl_xor(sum[i], sh);
+            for (int k = 0; k < NB; ++k) keys[4 * n + i][k] = __builtin_bit_cast(half8, ld_cached(head + (i * NB + k) * 512 + lane * 8));
     }
-    // lane (lo, hi) writes tile lo / 4's position 4 hi + lo % 4
-    float mine = 0.f;
+    float sum[4 * TILES];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) mine = i == lo ? sum[i] : mine;
-    const int pos = p0 + 16 * (lo >> 2) + 4 * hi + (lo & 3);
+    for (int i = 0; i < 4 * TILES; ++i) sum[i] = 0.f;
+    // the tokens that see any of it: from the one at its first position on, to the last that has its last position in the window
+    const int first = p0 > before ? p0 - before : 0;
+    int last = rq.n;
+    if (a.window > 0 && p0 >= a.sinks) {
+        const long most = (long)p0 + 2 * KV16_PAGE - 1 + a.window - before;      // token i sees from before + i + 1 - window on
+        last = most < last ? (most < 0 ? 0 : (int)most) : last;
+    }
+    const int r_end = last * group;
+    struct Rows {
+        half8 q[NB];
+        float m, inv;
+        int token;
+    };
+    auto ask = [&](int r0, Rows& x) __attribute__((always_inline)) {      // rows r0 .. r0 + 15 (behind the last one: the last one, with no weight)
+        const int r = r0 + lo < r_end ? r0 + lo : r_end - 1;
+        x.token = r / group;
+        const uint16_t* const q = a.q + ((size_t)(rq.first + x.token) * a.Hq + (size_t)g * group + (r - x.token * group)) * D + hi * 8;
+#pragma unroll
+        for (int k = 0; k < NB; ++k) x.q[k] = __builtin_bit_cast(half8, ld_cached(q + k * 32));
+        const float* const stats = a.stats + 2 * part_row(a, b, r, g, group);
+        x.m = stats[0];
+        x.inv = r0 + lo < r_end ? stats[1] * 512.0f : 0.f;
+    };
+    const int r_first = first * group + wv * 16;
+    if (first < last && r_first < r_end) {
+        Rows now, next;
+        ask(r_first, now);
+        for (int r0 = r_first; r0 < r_end; r0 += 16 * KW_WAVES) {
+            ask(r0 + 16 * KW_WAVES < r_end ? r0 + 16 * KW_WAVES : r0, next);
+            const Sight mine = sight_of(a, rq, now.token), low = sight_of(a, rq, __builtin_amdgcn_readfirstlane(now.token)), high = sight_of(a, rq, __builtin_amdgcn_readlane(now.token, 15));
+            floatx4 s[TILES];
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < NB; ++k)
+#pragma unroll
+                for (int i = 0; i < TILES; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys[i][k], now.q[k], s[i], 0, 0, 0);
+            float w[4 * TILES];
+#pragma unroll
+            for (int i = 0; i < 4 * TILES; ++i) w[i] = __builtin_fmaf(s[i >> 2][i & 3], a.scale2, -now.m);
+            // does some row not see all of it, or is some row not there or not a number?
+            const bool odd = __builtin_amdgcn_ballot_w64(!(now.inv > 0.f)) != 0ull;
+            if (odd || !there[0] || !there[1] || p0 + 2 * KV16_PAGE > low.end || (p0 < high.from && p0 + 2 * KV16_PAGE > a.sinks)) {
+#pragma unroll
+                for (int i = 0; i < 4 * TILES; ++i)
+                    if (!there[i >> 4] || now.inv == 0.f || !sees(mine, a.sinks, p0 + 16 * (i >> 2) + 4 * hi + (i & 3))) w[i] = -__builtin_inff();
+                // (a sum that is not a number: what the row sees, and that only)
+#pragma unroll
+                for (int i = 0; i < 4 * TILES; ++i) sum[i] = w[i] == -__builtin_inff() ? sum[i] : __builtin_fmaf(__builtin_amdgcn_exp2f(w[i]), now.inv, sum[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4 * TILES; ++i) sum[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(w[i]), now.inv, sum[i]);
+            }
+            now = next;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * TILES; ++i) s_sum[wv][i][lane] = sum[i];
+    __syncthreads();
+    if (tid >= 2 * KV16_PAGE) return;
+    const int i = 4 * (tid >> 4) + (tid & 3), h = (tid >> 2) & 3;
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < KW_WAVES; ++w)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) total += s_sum[w][i][16 * h + ((k + tid) & 15)];      // (each thread in an order of its own, the same every time; no two of a bank at once)
+    const int pos = p0 + tid;
     if (pos >= rq.len) return;
     const size_t at = ((size_t)b * a.Hkv + g) * a.max_pages * KV16_PAGE + pos;
-    a.weights_out[at] = (a.weights_in && pos < before ? a.weights_in[at] : 0.f) + mine;
+    a.weights_out[at] = (a.weights_in && pos < before ? a.weights_in[at] : 0.f) + total;
 }
 
 template <int D, bool STATS>
@@ -943,12 +1014,16 @@ template <int D>
 hipError_t launch(const Kv16AttnArgs& a, hipStream_t stream)
 {
     const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.B, (unsigned)a.nsplit);
-    if (a.split_rows) hipLaunchKernelGGL((kv16_attn_decode<D>), grid, dim3(KD_THREADS), 0, stream, a);
+    const bool scores = a.weights_out && a.scores;
+    if (a.split_rows && scores) hipLaunchKernelGGL((kv16_attn_decode<D, true>), grid, dim3(KD_THREADS), 0, stream, a);
+    else if (a.split_rows) hipLaunchKernelGGL((kv16_attn_decode<D, false>), grid, dim3(KD_THREADS), 0, stream, a);
     else if (a.weights_out) launch_prompt<D, true>(a, grid, stream);
     else launch_prompt<D, false>(a, grid, stream);
     if (a.nsplit > 1) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
-    if (a.weights_out)
-        hipLaunchKernelGGL((kv16_attn_weights<D>), dim3((unsigned)((a.max_pages + 3) / 4), (unsigned)a.Hkv, (unsigned)a.B), dim3(KW_THREADS), 0, stream, a);
+    if (scores)
+        hipLaunchKernelGGL(kv16_attn_weigh, dim3((unsigned)((a.max_pages * (KV16_PAGE / 4) + KS_THREADS - 1) / KS_THREADS), (unsigned)a.Hkv, (unsigned)a.B), dim3(KS_THREADS), 0, stream, a);
+    else if (a.weights_out)
+        hipLaunchKernelGGL((kv16_attn_weights<D>), dim3((unsigned)((a.max_pages + 1) / 2), (unsigned)a.Hkv, (unsigned)a.B), dim3(KW_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
