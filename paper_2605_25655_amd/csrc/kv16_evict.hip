@@ -8,7 +8,7 @@ namespace {
 
 // ---- workspace (words) -----------------------------------------------------------------------------------------------
 struct Space {
-    int *kept, *begin, *fresh, *index;      // per row: positions kept (0: left as it is), its first fresh page's place in `fresh`; fresh pages; kept positions
+    int *kept, *begin, *fresh, *slots;      // per row: positions kept (-1: left as it is), its first fresh page's place in `fresh`; fresh pages; where kept positions are (page * KV16_PAGE + place)
 };
 __host__ __device__ inline Space space_of(const Kv16EvictArgs& a)
 {
@@ -16,7 +16,7 @@ __host__ __device__ inline Space space_of(const Kv16EvictArgs& a)
     s.kept = a.ws;
     s.begin = s.kept + a.rows;
     s.fresh = s.begin + a.rows;
-    s.index = s.fresh + a.num_pages;        // [layers][rows][Hkv][64 max_pages]
+    s.slots = s.fresh + a.num_pages;        // [layers][rows][Hkv][64 max_pages]
     return s;
 }
 
@@ -67,39 +67,42 @@ __device__ __forceinline__ int scan(int x, int* s_wave, int& total)
     return before + y - x;
 }
 
-// Who is evicted, which pages they get, and the tables and counts that follow: one workgroup.
-constexpr int KE_PLAN = 1024;
-__global__ __launch_bounds__(KE_PLAN) void kv16_evict_plan(Kv16EvictArgs a)
+// Positions that a row keeps (-1: it is within its budget), by one wave.
+__device__ __forceinline__ int kept_of(const Kv16EvictArgs& a, int b, int n, int lane)
 {
-    __shared__ int s_wave[KE_PLAN / 64];
+    if (n <= a.budget) return -1;
+    const int live = live_positions(a, b, n, lane);
+    return live < a.budget ? live : a.budget;
+}
+
+constexpr int KE_THREADS = 1024;
+
+// Who is evicted, which pages they get, and the tables and counts that follow: one workgroup.
+__device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave)
+{
     const Space ws = space_of(a);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    for (int b = wave; b < a.rows; b += KE_PLAN / 64) {
-        const int n = length_of(a, b);
-        int kept = 0;
-        if (n > a.budget) {
-            kept = live_positions(a, b, n, lane);
-            kept = kept < a.budget ? kept : a.budget;
-        }
-        if (lane == 0) ws.kept[b] = n > a.budget ? kept : -1;
+    for (int b = wave; b < a.rows; b += KE_THREADS / 64) {
+        const int kept = kept_of(a, b, length_of(a, b), lane);
+        if (lane == 0) ws.kept[b] = kept;
     }
     __syncthreads();
     // pages that they ask for, one row behind the other
     long asked = 0;
-    for (int b0 = 0; b0 < a.rows; b0 += KE_PLAN) {
+    for (int b0 = 0; b0 < a.rows; b0 += KE_THREADS) {
         const int b = b0 + tid, kept = b < a.rows ? ws.kept[b] : -1;
         int total;
-        const int before = scan<KE_PLAN>(kept >= 0 ? pages_for(a, kept) : 0, s_wave, total);
+        const int before = scan<KE_THREADS>(kept >= 0 ? pages_for(a, kept) : 0, s_wave, total);
         const long at = asked + before;
         if (b < a.rows) ws.begin[b] = at > a.num_pages ? a.num_pages : (int)at;      // (further than any free page)
         asked += total;
     }
     // the lowest free pages
     int free_pages = 0;
-    for (int p0 = 0; p0 < a.num_pages; p0 += KE_PLAN) {
+    for (int p0 = 0; p0 < a.num_pages; p0 += KE_THREADS) {
         const int p = p0 + tid, refs = p < a.num_pages ? a.refs_in[p] : 1;
         int total;
-        const int before = scan<KE_PLAN>(refs == 0 ? 1 : 0, s_wave, total);
+        const int before = scan<KE_THREADS>(refs == 0 ? 1 : 0, s_wave, total);
         if (refs == 0) ws.fresh[free_pages + before] = p;
         if (p < a.num_pages) a.refs_out[p] = refs;
         free_pages += total;
@@ -108,7 +111,7 @@ __global__ __launch_bounds__(KE_PLAN) void kv16_evict_plan(Kv16EvictArgs a)
     __syncthreads();
     // Rows whose pages are there: the lengths, tables and counts that they leave with.  (counts by atomic operations on integers: the same in any order)
     int done = 0, left = 0;
-    for (int b = wave; b < a.rows; b += KE_PLAN / 64) {
+    for (int b = wave; b < a.rows; b += KE_THREADS / 64) {
         const int kept = ws.kept[b], n = length_of(a, b), need = kept >= 0 ? pages_for(a, kept) : 0, begin = ws.begin[b];
         const bool moves = kept >= 0 && (long)begin + need <= free_pages;
         if (lane == 0) {
@@ -147,135 +150,178 @@ __device__ __forceinline__ unsigned order_of(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Which positions of a row a cache head of a layer keeps, in their order: a workgroup each.  The k-th largest weight by its bits, eight at a time from the top.
-constexpr int KE_SELECT = 1024;
-__global__ __launch_bounds__(KE_SELECT) void kv16_evict_select(Kv16EvictArgs a)
+// Which positions of a row a cache head of a layer keeps, in their order: a workgroup each (and one in front of them all for the plan, which nothing here waits for).  The k-th
+// largest weight by its bits, 11, 11 and 10 of them at a time from the top: with 8 at a time, most weights fall on a few counters.  A thread takes four neighbouring positions at a time.
+constexpr int KE_DIGIT = 11;
+__global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
 {
-    __shared__ int s_wave[KE_SELECT / 64];
-    __shared__ int s_count[256];
+    __shared__ int s_wave[KE_THREADS / 64];
+    __shared__ int s_count[1 << KE_DIGIT];
     __shared__ unsigned s_prefix;
-    __shared__ int s_left;
+    __shared__ int s_left, s_kept;
+    if (blockIdx.x == 0) {
+        if (blockIdx.y == 0 && blockIdx.z == 0) evict_plan(a, s_wave);
+        return;
+    }
     const Space ws = space_of(a);
-    const int tid = threadIdx.x, lane = tid & 63, g = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
-    const int kept = ws.kept[b];
-    if (kept < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, g = blockIdx.x - 1, b = blockIdx.y, layer = blockIdx.z;
     const int n = length_of(a, b);
+    if (n <= a.budget) return;
+    if (tid < 64) {
+        const int kept = kept_of(a, b, n, lane);
+        if (tid == 0) s_kept = kept;
+    }
     const size_t at = (((size_t)layer * a.rows + b) * a.Hkv + g) * a.max_pages * KV16_PAGE;
     const float* const weights = a.weights_in + at;
-    int* const index = ws.index + at;
+    int* const slots = ws.slots + at;
     const int* const table = a.table_in + (size_t)b * a.max_pages;
-    auto live = [&](int p) { return p < n && is_page(a, table[p / KV16_PAGE]); };
-    auto guarded = [&](int p) { return p < a.sinks || p >= n - a.recent; };
-    // what is left of the budget for the others
+    // four positions from p on, of one page: which are there, which are guarded, their weights' order
+    struct Four {
+        unsigned there, guarded, u[4];
+    };
+    auto ask = [&](int p) {
+        Four f{0, 0, {0, 0, 0, 0}};
+        if (p >= n || !is_page(a, table[p / KV16_PAGE])) return f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int q = p + k;
+            if (q >= n) continue;
+            f.there |= 1u << k;
+            if (q < a.sinks || q >= n - a.recent) f.guarded |= 1u << k;
+            f.u[k] = order_of(weights[q]);
+        }
+        return f;
+    };
+    // what is left of the budget for those that are not guarded
     int mine = 0;
-    for (int p = tid; p < n; p += KE_SELECT) mine += live(p) && guarded(p) ? 1 : 0;
+    for (int p = tid * 4; p < n; p += KE_THREADS * 4) mine += __builtin_popcount(ask(p).guarded);
     int sure;
-    scan<KE_SELECT>(mine, s_wave, sure);
-    int want = kept - sure;                      // >= 0: no more than the budget is guarded
+    scan<KE_THREADS>(mine, s_wave, sure);
+    int want = s_kept - sure;                    // >= 0: no more than the budget is guarded
     unsigned prefix = 0, mask = 0;               // weights above the prefix are kept, of those equal to it (in the end) `want`
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) s_count[tid] = 0;
+    for (int shift = 32 - KE_DIGIT, bits = KE_DIGIT; bits > 0;) {
+        for (int i = tid; i < 1 << KE_DIGIT; i += KE_THREADS) s_count[i] = 0;
         __syncthreads();
-        for (int p = tid; p < n; p += KE_SELECT) {
-            const unsigned u = order_of(weights[p]);
-            if (live(p) && !guarded(p) && (u & mask) == prefix) atomicAdd(&s_count[u >> shift & 255u], 1);
+        const unsigned digit = (1u << bits) - 1;
+        for (int p = tid * 4; p < n; p += KE_THREADS * 4) {
+            const Four f = ask(p);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if ((f.there & ~f.guarded) >> k & 1 && (f.u[k] & mask) == prefix) atomicAdd(&s_count[f.u[k] >> shift & digit], 1);
         }
         __syncthreads();
-        if (tid < 64) {                          // from the top: lane 0 the four highest
-            int c[4], all = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) all += c[k] = s_count[255 - (lane * 4 + k)];
-            int upto = all;
-#pragma unroll
-            for (int sh = 1; sh < 64; sh <<= 1) {
-                const int z = __shfl_up(upto, sh);
-                if (lane >= sh) upto += z;
-            }
-            int above = upto - all;
-            const unsigned long long who = __builtin_amdgcn_ballot_w64(upto >= want);
-            const int first = who ? __builtin_ctzll(who) : 63;      // (want is at most the number of candidates)
-            if (lane == first) {
-                int k = 0;
-                while (k < 3 && above + c[k] < want) above += c[k++];
-                s_prefix = prefix | (unsigned)(255 - (lane * 4 + k)) << shift;
-                s_left = want - above;
-            }
+        // from the top: thread 0 the two highest
+        const int hi = (1 << KE_DIGIT) - 1 - 2 * tid, c0 = s_count[hi], c1 = s_count[hi - 1];
+        int total;
+        const int above = scan<KE_THREADS>(c0 + c1, s_wave, total);
+        // the one counter with which the sum from the top reaches what is wanted (want 0: the highest; it is at most the number of candidates)
+        const bool first = above < want ? above + c0 >= want : (want == 0 && tid == 0), second = above + c0 < want && above + c0 + c1 >= want;
+        if (first || second) {
+            s_prefix = prefix | (unsigned)(first ? hi : hi - 1) << shift;
+            s_left = want - above - (first ? 0 : c0);
         }
         __syncthreads();
         prefix = s_prefix;
         want = s_left;
-        mask |= 255u << shift;
-        __syncthreads();
+        mask |= digit << shift;
+        bits = shift < KE_DIGIT ? shift : KE_DIGIT;
+        shift -= bits;
     }
     int placed = 0, equal = 0;
-    for (int p0 = 0; p0 < n; p0 += KE_SELECT) {
-        const int p = p0 + tid;
-        const bool there = p < n && live(p), guard = guarded(p);
-        const unsigned u = there ? order_of(weights[p]) : 0u;
-        const bool even = there && !guard && u == prefix;
+    for (int p0 = 0; p0 < n; p0 += KE_THREADS * 4) {
+        const int p = p0 + tid * 4;
+        const Four f = ask(p);
+        unsigned same = 0, keep = f.guarded;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool other = (f.there & ~f.guarded) >> k & 1;
+            same |= (other && f.u[k] == prefix ? 1u : 0u) << k;
+            keep |= (other && f.u[k] > prefix ? 1u : 0u) << k;
+        }
         int total;
-        const int rank = scan<KE_SELECT>(even ? 1 : 0, s_wave, total) + equal;
+        int rank = scan<KE_THREADS>(__builtin_popcount(same), s_wave, total) + equal;
         equal += total;
-        const bool keep = there && (guard || u > prefix || (even && rank < want));
-        const int to = scan<KE_SELECT>(keep ? 1 : 0, s_wave, total) + placed;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (same >> k & 1 && rank++ < want) keep |= 1u << k;
+        int to = scan<KE_THREADS>(__builtin_popcount(keep), s_wave, total) + placed;
         placed += total;
-        if (keep) index[to] = p;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (keep >> k & 1) {
+                slots[to] = table[p / KV16_PAGE] * KV16_PAGE + ((p + k) & (KV16_PAGE - 1));
+                a.weights_out[at + to++] = weights[p + k];      // (written over where the row stays after all)
+            }
     }
 }
 
-// The move: a workgroup takes one fresh page of one cache head of a layer, 64 kept positions from wherever they were.
-constexpr int KE_MOVE = 256;
+// The move: a workgroup takes one fresh page of one cache head of a layer, 64 kept positions from wherever they were.  All that it reads is asked for at once, the pieces of 16 bytes of
+// the keys and the single values, for a workgroup is short and the wait for memory most of it.
+constexpr int KE_MOVE = 512;
 template <int D>
 __global__ __launch_bounds__(KE_MOVE) void kv16_evict_move(Kv16EvictArgs a)
 {
+    constexpr int KEYS = KV16_PAGE * D / 8 / KE_MOVE, VALUES = KV16_PAGE / 8 * D / KE_MOVE;      // 16 bytes each
     __shared__ long s_from[KV16_PAGE];           // where the head's block of the position's page begins
     __shared__ int s_pos[KV16_PAGE];
     const Space ws = space_of(a);
     const int tid = threadIdx.x, g = blockIdx.y, b = blockIdx.z % a.rows, layer = blockIdx.z / a.rows;
-    const int kept = ws.kept[b];
     const size_t at = (((size_t)layer * a.rows + b) * a.Hkv + g) * a.max_pages * KV16_PAGE;
+    const int p0 = blockIdx.x * KV16_PAGE;
+    const int slot = tid < KV16_PAGE && p0 + tid < a.max_pages * KV16_PAGE ? ws.slots[at + p0 + tid] : 0;      // (of a row that keeps as many)
+    const int kept = ws.kept[b], begin = ws.begin[b];
     if (kept < 0) {                              // left as it is
         const int n = length_of(a, b);
         for (int p = blockIdx.x * KE_MOVE + tid; p < n; p += gridDim.x * KE_MOVE) a.weights_out[at + p] = a.weights_in[at + p];
         return;
     }
-    const int p0 = blockIdx.x * KV16_PAGE, count = kept - p0 < KV16_PAGE ? kept - p0 : KV16_PAGE;
+    const int count = kept - p0 < KV16_PAGE ? kept - p0 : KV16_PAGE;
     if (count <= 0) return;
     uint16_t* const pool = a.pages + (size_t)layer * a.layer_values;
     const size_t page_values = (size_t)a.Hkv * kv16_head_values(D);
+    const int page = ws.fresh[begin + blockIdx.x];
     if (tid < KV16_PAGE) {
-        const int p = tid < count ? ws.index[at + p0 + tid] : -1;
-        s_pos[tid] = p & (KV16_PAGE - 1);
-        s_from[tid] = p < 0 ? 0 : (long)((size_t)a.table_in[(size_t)b * a.max_pages + p / KV16_PAGE] * page_values + (size_t)g * kv16_head_values(D));
-        if (p >= 0) a.weights_out[at + p0 + tid] = a.weights_in[at + p];
+        const int from = tid < count ? slot : 0;
+        s_pos[tid] = from & (KV16_PAGE - 1);
+        s_from[tid] = (long)((size_t)(unsigned)(from / KV16_PAGE) * page_values + (size_t)g * kv16_head_values(D));
     }
     __syncthreads();
-    uint16_t* const to = pool + (size_t)ws.fresh[ws.begin[b] + blockIdx.x] * page_values + (size_t)g * kv16_head_values(D);
-#pragma unroll 4
-    for (int i = tid; i < KV16_PAGE * D / 8; i += KE_MOVE) {
-        const int p = i & (KV16_PAGE - 1), part = i / KV16_PAGE;
-        if (p < count) *reinterpret_cast<uintx4*>(to + kv16_key_at(p, part, D)) = ld_stream(pool + s_from[p] + kv16_key_at(s_pos[p], part, D));
-    }
+    uint16_t* const to = pool + (size_t)(unsigned)page * page_values + (size_t)g * kv16_head_values(D);
+    uintx4 keys[KEYS];
+    uint16_t x[VALUES][8];
+    // (a position that is not there: of the first one, which is)
+    const int key = tid & (KV16_PAGE - 1), part = tid / KV16_PAGE, key_from = key < count ? key : 0;
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) keys[i] = ld_stream(pool + s_from[key_from] + kv16_key_at(s_pos[key_from], part + i * (KE_MOVE / KV16_PAGE), D));
     // eight positions of a column are 16 bytes
-#pragma unroll 2
-    for (int i = tid; i < KV16_PAGE / 8 * D; i += KE_MOVE) {
-        const int col = i % D, oct = i / D, first = (oct >> 2) * 32 + (oct & 3) * 4;      // positions first + 0 .. 3 and first + 16 + 0 .. 3
-        uint16_t x[8];
+    const int col = tid % D;
+    int first[VALUES];                           // positions first + 0 .. 3 and first + 16 + 0 .. 3
+#pragma unroll
+    for (int i = 0; i < VALUES; ++i) {
+        const int oct = tid / D + i * (KE_MOVE / D);
+        first[i] = (oct >> 2) * 32 + (oct & 3) * 4;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int p = first + (k >> 2) * 16 + (k & 3);
-            x[k] = p < count ? pool[s_from[p] + kv16_value_at(s_pos[p], col, D)] : 0;
+            int p = first[i] + (k >> 2) * 16 + (k & 3);
+            p = p < count ? p : 0;
+            x[i][k] = pool[s_from[p] + kv16_value_at(s_pos[p], col, D)];
         }
-        uint16_t* const put = to + kv16_value_at(first, col, D);
-        if (first + 19 < count) {
+    }
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i)
+        if (key < count) *reinterpret_cast<uintx4*>(to + kv16_key_at(key, part + i * (KE_MOVE / KV16_PAGE), D)) = keys[i];
+#pragma unroll
+    for (int i = 0; i < VALUES; ++i) {
+        uint16_t* const put = to + kv16_value_at(first[i], col, D);
+        if (first[i] + 19 < count) {
             uintx4 y;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = x[2 * k] | (unsigned)x[2 * k + 1] << 16;
+            for (int k = 0; k < 4; ++k) y[k] = x[i][2 * k] | (unsigned)x[i][2 * k + 1] << 16;
             *reinterpret_cast<uintx4*>(put) = y;
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (first + (k >> 2) * 16 + (k & 3) < count) put[k] = x[k];
+                if (first[i] + (k >> 2) * 16 + (k & 3) < count) put[k] = x[i][k];
         }
     }
 }
@@ -290,8 +336,7 @@ size_t kv16_evict_words(int layers, int rows, int Hkv, int max_pages, int num_pa
 hipError_t launch_kv16_evict(const Kv16EvictArgs& a, int num_cus, hipStream_t stream)
 {
     (void)num_cus;
-    hipLaunchKernelGGL(kv16_evict_plan, dim3(1), dim3(KE_PLAN), 0, stream, a);
-    hipLaunchKernelGGL(kv16_evict_select, dim3((unsigned)a.Hkv, (unsigned)a.rows, (unsigned)a.layers), dim3(KE_SELECT), 0, stream, a);
+    hipLaunchKernelGGL(kv16_evict_select, dim3((unsigned)a.Hkv + 1, (unsigned)a.rows, (unsigned)a.layers), dim3(KE_THREADS), 0, stream, a);
     const long most = (long)a.max_pages * KV16_PAGE < a.budget ? (long)a.max_pages * KV16_PAGE : a.budget;
     const dim3 grid((unsigned)((most + KV16_PAGE - 1) / KV16_PAGE), (unsigned)a.Hkv, (unsigned)(a.rows * a.layers));
     if (a.D == 128) hipLaunchKernelGGL((kv16_evict_move<128>), grid, dim3(KE_MOVE), 0, stream, a);
