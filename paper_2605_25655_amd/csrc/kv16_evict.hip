@@ -192,9 +192,19 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
         }
         return f;
     };
+    // (rows of up to 8192 positions: asked for once)
+    constexpr int HELD = 2;
+    Four held[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) held[i] = ask((i * KE_THREADS + tid) * 4);
+    auto each = [&](auto what) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) what(held[i]);
+        for (int p = (HELD * KE_THREADS + tid) * 4; p < n; p += KE_THREADS * 4) what(ask(p));
+    };
     // what is left of the budget for those that are not guarded
     int mine = 0;
-    for (int p = tid * 4; p < n; p += KE_THREADS * 4) mine += __builtin_popcount(ask(p).guarded);
+    each([&](const Four& f) { mine += __builtin_popcount(f.guarded); });
     int sure;
     scan<KE_THREADS>(mine, s_wave, sure);
     int want = s_kept - sure;                    // >= 0: no more than the budget is guarded
@@ -203,12 +213,11 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
         for (int i = tid; i < 1 << KE_DIGIT; i += KE_THREADS) s_count[i] = 0;
         __syncthreads();
         const unsigned digit = (1u << bits) - 1;
-        for (int p = tid * 4; p < n; p += KE_THREADS * 4) {
-            const Four f = ask(p);
+        each([&](const Four& f) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if ((f.there & ~f.guarded) >> k & 1 && (f.u[k] & mask) == prefix) atomicAdd(&s_count[f.u[k] >> shift & digit], 1);
-        }
+        });
         __syncthreads();
         // from the top: thread 0 the two highest
         const int hi = (1 << KE_DIGIT) - 1 - 2 * tid, c0 = s_count[hi], c1 = s_count[hi - 1];
@@ -228,9 +237,7 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
         shift -= bits;
     }
     int placed = 0, equal = 0;
-    for (int p0 = 0; p0 < n; p0 += KE_THREADS * 4) {
-        const int p = p0 + tid * 4;
-        const Four f = ask(p);
+    auto place = [&](int p, const Four& f) __attribute__((always_inline)) {
         unsigned same = 0, keep = f.guarded;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -252,7 +259,11 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
                 slots[to] = table[p / KV16_PAGE] * KV16_PAGE + ((p + k) & (KV16_PAGE - 1));
                 a.weights_out[at + to++] = weights[p + k];      // (written over where the row stays after all)
             }
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (i * KE_THREADS * 4 < n) place((i * KE_THREADS + tid) * 4, held[i]);
+    for (int p0 = HELD * KE_THREADS * 4; p0 < n; p0 += KE_THREADS * 4) place(p0 + tid * 4, ask(p0 + tid * 4));
 }
 
 // The move: a workgroup takes one fresh page of one cache head of a layer, 64 kept positions from wherever they were.  All that it reads is asked for at once, the pieces of 16 bytes of
