@@ -344,7 +344,8 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
  * where before is weights_in[b,g,j] (the same shape, or the same buffer; NULL: 0) for the positions in front of the new tokens and 0 for theirs.  Entries from seq_lens[b] on
  * are not written.
  *
- * Scores, statistics and sums are fp32, weights reach the matrix cores as fp16 (two summands up to 64 rows of a cache head, one beyond).  Workspace:
+ * Scores, statistics and sums are fp32.  Weights reach the matrix cores as fp16: up to 16 rows of a request and cache head (max_q Hq / Hkv) as two summands, beyond as one,
+ * cut to its bits, as is the sum that divides the result.  Workspace:
  * thi_kv16_attention_workspace_bytes(), 256-byte aligned; what that says for the largest B, T, max_q and max_pages does for every smaller call with these heads
  * (weights != 0: with weights_out).  Reproducible bit for bit.
  */

@@ -48,13 +48,13 @@ struct Kv16AttnArgs {
     // how the rows are dealt (kv16_plan)
     float* part;                     // [B][max_q][Hq][nsplit][kv16_part(D)]: a chunk's unnormalised output, maximum, sum of the weights as they were multiplied, and as they are
     float* stats;                    // [B][max_q][Hq][2]: a row's maximum and one over its sum, with weights_out
-    float* scores;                   // [B][Hkv][max_q group][64 max_pages]: scores in powers of two, with weights_out and up to KV16_SCORE_ROWS rows of a cache head, or nullptr
-    bool split_rows;                 // 16 rows of a cache head at a time, cut along the positions
-    int tiles;                       // tiles of 16 rows
+    float* scores;                   // [B][Hkv][16 max_pages][max_q group][4]: four positions' scores in powers of two, with weights_out, for few rows
+    bool few;                        // all rows of a request and cache head at once, at most KV16_FEW_ROWS
+    int tiles;                       // else: tiles of KV16_TILE_ROWS
     int nsplit, min_chunk;           // chunks per request at most, pages per chunk at least
 };
 constexpr int KV16_MAX_SPLIT = 64;
-constexpr int KV16_SCORE_ROWS = 16;
+constexpr int KV16_FEW_ROWS = 16, KV16_TILE_ROWS = 128;
 constexpr int kv16_part(int D) { return D + 4; }
 void kv16_plan(Kv16AttnArgs& a, int num_cus);
 hipError_t launch_kv16_attention(const Kv16AttnArgs& a, hipStream_t stream);

@@ -15,7 +15,8 @@ bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff /
 
 constexpr int MAX_PAGES = 1 << 24;      // of a row of the page table: positions stay below 2^30
 
-constexpr int FEW_ROWS = 64, FEW_CHUNK = 4, FEW_PER_CU = 2, MANY_CHUNK = 8, MANY_PER_CU = 2;      // kv16_plan
+// Pages of a chunk at least, chunks' workgroups for every compute unit, and tables times columns that are not cut (kv16_plan)
+constexpr int CHUNK = 4, FEW_PER_CU = 3, MANY_PER_CU = 2, FEW_UNCUT = 1280;
 
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -23,14 +24,14 @@ size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 // workgroups of 16 (256) rows for every compute unit, so no batch has more rows than these hold; and no more than its own times the chunks of the longest table.
 size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
 {
-    auto at_most = [&](long q, int chunk, long held) {
-        const long chunks = (max_pages + chunk - 1) / chunk, own = (long)B * q * Hq;
+    auto at_most = [&](long q, long held) {
+        const long chunks = (max_pages + CHUNK - 1) / CHUNK, own = (long)B * q * Hq;
         const long rows = chunks < 2 ? 0 : own > held ? held : own * (chunks < KV16_MAX_SPLIT ? chunks : KV16_MAX_SPLIT);
         return rows < held ? rows : held;
     };
-    const int group = Hq / Hkv, q_few = FEW_ROWS / group;
-    const long few = at_most(max_q < q_few ? max_q : q_few, FEW_CHUNK, 16L * FEW_PER_CU * num_cus);
-    const long many = (long)max_q * group <= FEW_ROWS ? 0 : at_most(max_q, MANY_CHUNK, 128L * MANY_PER_CU * num_cus);
+    const int group = Hq / Hkv, q_few = KV16_FEW_ROWS / group;
+    const long few = at_most(max_q < q_few ? max_q : q_few, (long)KV16_FEW_ROWS * FEW_PER_CU * num_cus);
+    const long many = (long)max_q * group <= KV16_FEW_ROWS ? 0 : at_most(max_q, (long)KV16_TILE_ROWS * MANY_PER_CU * num_cus);
     return (size_t)(few > many ? few : many);
 }
 size_t bytes_of_rows(size_t rows, int D) { return rows ? round_up(rows * kv16_part(D) * sizeof(float)) : 256; }
@@ -38,7 +39,7 @@ size_t bytes_of_stats(int B, int Hq, int max_q) { return round_up((size_t)B * ma
 // of the most that a call of up to so many leaves of its scores
 size_t bytes_of_scores(int B, int Hq, int Hkv, int max_q, int max_pages)
 {
-    const int group = Hq / Hkv, q = KV16_SCORE_ROWS / group < max_q ? KV16_SCORE_ROWS / group : max_q;
+    const int group = Hq / Hkv, q = KV16_FEW_ROWS / group < max_q ? KV16_FEW_ROWS / group : max_q;
     return round_up((size_t)B * q * Hq * max_pages * KV16_PAGE * sizeof(float));
 }
 
@@ -46,16 +47,28 @@ int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 
 }  // namespace
 
+// How the rows are dealt: up to KV16_FEW_ROWS of a request and cache head to kv16_attn_decode, more, KV16_TILE_ROWS at a time, to kv16_attn_prompt; and where that gives fewer
+// workgroups than the compute units hold, requests are cut into chunks of at least CHUNK pages, whose results one more launch puts together.
+// Measured, us a pass (requests of up to that many positions each; 64/8: query heads / cache heads of 128 columns):
+//   the second kernel from 8, 16, 32, 64 rows on: 16 rows of 64/8, 4 x 9000: 32.5 29.8 29.7 29.7; 24 rows: 33 33 42 42; 32 rows: 34 34 40 40; 64 rows: 40 40 40 64; 16 rows of 32/32, 5 x 1500:
+//     28.0 25.9 25.9 25.9; 64 rows: 38 38 38 54; 30 rows of 2 heads of 64 columns, 8 x 2000: 17.3 17.3 15.9 15.9.  16 is also what one matrix tile holds.
+//   two, three, four workgroups for a compute unit (which holds three): 64/8, 24 x 5000: 57.6 50.1 47.9; 3 x 131000: 85 86 123; 16 x 32000, 4096 seen: 46.9 48.0 49.0; 32/32, 5 x 1500: 22.1
+//     22.8 20.8
+//   more rows: one, two, three (it holds two): 300 tokens of 64/8 behind 7700: 161 113 119; 128 of 32/32 behind 1872: 30 29 29; 64 of 64/8, 3 x 6000: 85 56 60; 128 of 64/8, 5 x 20000, 4096
+//     seen: 128 128 111; 1000 of 32/32 behind 5000: 128 139 149
+//   chunks of 2, 4, 8 pages at least: 128 tokens of 32/32 behind 1872: 36.1 25.5 29.8; 300 of 64/8 behind 7700: 110 111 113; one of 64/8, 1 x 3000: 11.3 12.0 13.4; 10 rows of 8 heads of 64
+//     columns, 8 x 2000: 14.3 12.5 12.3
+//   not cut, cut: 2 x 468 of 8 heads of 64 columns: 6.8 9.9; 2 x 1200 of these: 9.1 10.0; 2 x 1500 of these (past FEW_UNCUT): 10.4 8.5; 4 x 600 of 32/32: 10.3 13.1; 2 x 600 of 64/8: 10.5 11.6;
+//     2 x 760 of 64/8 (past it): 11.4 10.8
 void thi::kv16_plan(Kv16AttnArgs& a, int num_cus)
 {
-    const int group = a.group = a.Hq / a.Hkv;
-    a.split_rows = (long)a.max_q * group <= FEW_ROWS;
-    const int rows = a.split_rows ? 16 : 128;
-    a.tiles = (int)(((long)a.max_q * group + rows - 1) / rows);
+    a.group = a.Hq / a.Hkv;
+    a.few = (long)a.max_q * a.group <= KV16_FEW_ROWS;
+    a.tiles = a.few ? 1 : (int)(((long)a.max_q * a.group + KV16_TILE_ROWS - 1) / KV16_TILE_ROWS);
     const long items = (long)a.B * a.Hkv * a.tiles;
-    a.min_chunk = a.split_rows ? FEW_CHUNK : MANY_CHUNK;
-    long n = (long)(a.split_rows ? FEW_PER_CU : MANY_PER_CU) * num_cus / items;
-    const long most = (a.max_pages + a.min_chunk - 1) / a.min_chunk;
+    const long most = a.few && (long)a.max_pages * a.D <= FEW_UNCUT ? 1 : (a.max_pages + CHUNK - 1) / CHUNK;
+    a.min_chunk = CHUNK;
+    long n = (long)(a.few ? FEW_PER_CU : MANY_PER_CU) * num_cus / items;
     n = n < 1 ? 1 : n > KV16_MAX_SPLIT ? KV16_MAX_SPLIT : n;
     a.nsplit = (int)(n > most ? most : n);
 }
@@ -102,7 +115,8 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
                        void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     if (!q || !pages || !page_table || !seq_lens || !out || !workspace || (weights_in && !weights_out)) return THI_ERR_NULL;
-    if (!thi_kv16_attention_workspace_bytes(B, T, Hq, Hkv, D, max_q, max_pages, 0) || !pool_ok(num_pages) || (!q_offsets && (T != B || max_q != 1))) return THI_ERR_SHAPE;
+    const size_t need = thi_kv16_attention_workspace_bytes(B, T, Hq, Hkv, D, max_q, max_pages, weights_out != nullptr);
+    if (!need || !pool_ok(num_pages) || (!q_offsets && (T != B || max_q != 1))) return THI_ERR_SHAPE;
     if (window < 0 || sinks < 0) return THI_ERR_SHAPE;
     if (misaligned(q, 16) || misaligned(pages, 16) || misaligned(out, 16) || misaligned(page_table, 4) || misaligned(seq_lens, 4) ||
         misaligned(q_offsets, 4) || misaligned(weights_in, 4) || misaligned(weights_out, 4) || misaligned(workspace, 256))
@@ -113,8 +127,8 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     a.sinks = window ? sinks : 0;
     kv16_plan(a, device_cu_count());
     const size_t stats = weights_out ? bytes_of_stats(B, Hq, max_q) : 0;
-    const size_t scores = weights_out && (long)max_q * a.group <= KV16_SCORE_ROWS ? bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0;
-    if (workspace_bytes < stats + scores + bytes_of_rows(a.nsplit > 1 ? (size_t)B * max_q * Hq * a.nsplit : 0, D)) return THI_ERR_WORKSPACE;
+    const size_t scores = weights_out && a.few ? bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0;
+    if (workspace_bytes < need) return THI_ERR_WORKSPACE;
     (void)hipGetLastError();
     a.q = (const uint16_t*)q;
     a.pages = (const uint16_t*)pages;

@@ -126,8 +126,8 @@ __device__ __forceinline__ float slow_row(const Kv16AttnArgs& a, const Request& 
 
 // ---- one token per request, or a few: 16 rows of a cache head at a time, cut along the positions --------------------
 //
-// A workgroup (4 waves) takes a chunk of the pages that one request looks at, for one cache head; a wave takes a page at a time, in halves of 32 positions, straight from
-// memory into registers, the next half in flight behind it.  Rows are (new token, query head of the group) pairs, 16 of them the columns of two matrix products
+// A workgroup (4 waves) takes a chunk of the pages that one request looks at, for one cache head; a wave takes half of every second page, 32 positions, straight from
+// memory into registers, its next half in flight behind it.  Rows are (new token, query head of the group) pairs, 16 of them the columns of two matrix products
 // (v_mfma_f32_16x16x32_f16):
 //   S = K Q^T     : 16 positions x 16 rows;
 //   O^T = V^T P^T : a lane has the weights of positions 16 i + 4 hi + r of its row, which is the B operand as it stands, for the page holds the values in that order.
@@ -162,10 +162,9 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = a.group;
-    const int g = blockIdx.x / a.tiles, r0 = (blockIdx.x % a.tiles) * 16;      // first row of this tile: row r is token r / group, head r % group
-    const int b = blockIdx.y, chunk = blockIdx.z;
+    const int g = blockIdx.x, b = blockIdx.y, chunk = blockIdx.z;
     const Request rq = find_request(a, b);
-    const int rows = rq.n * group - r0 < 16 ? rq.n * group - r0 : 16;
+    const int rows = rq.n * group;               // at most 16: row r is token r / group, head r % group
     if (rows <= 0) return;
     const int size = chunk_pages(a, rq.pages);
     const int c0 = chunk * size, c1 = c0 + size < rq.pages ? c0 + size : rq.pages;
@@ -173,48 +172,45 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
     const bool whole = rq.pages <= size;
     if (tid == 0) s_odd = 0;
 
-    auto row_of_column = [&](int c) {            // (token, head) row of q and out
-        const int r = r0 + c;
-        return (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group;
-    };
+    auto row_of_column = [&](int r) { return (size_t)(rq.first + r / group) * a.Hq + (size_t)g * group + r % group; };      // (token, head) row of q and out
     const int col = lo < rows ? lo : rows - 1;
     half8 queries[NB];
 #pragma unroll
     for (int k = 0; k < NB; ++k) queries[k] = __builtin_bit_cast(half8, ld_cached(a.q + row_of_column(col) * D + k * 32 + hi * 8));
-    const Sight mine = sight_of(a, rq, (r0 + col) / group);
-    const Sight low = sight_of(a, rq, r0 / group), high = sight_of(a, rq, (r0 + rows - 1) / group);      // of the tile's first and last row
+    const Sight mine = sight_of(a, rq, col / group);
+    const Sight low = sight_of(a, rq, 0), high = sight_of(a, rq, rq.n - 1);
 
-    // This wave's pages: c0 + wv, c0 + wv + 4, ...; an entry that is no page: -1.  Loads are unconditional (a page that is not there: page 0), so that nothing
+    // This wave's half of pages c0 + wv / 2, c0 + wv / 2 + 2, ...; an entry that is no page: -1.  Loads are unconditional (a page that is not there: page 0), so that nothing
     // waits for a load but what uses it.
-    const int n_it = (c1 - c0 - wv + KD_WAVES - 1) / KD_WAVES;
+    const int half = wv & 1, v0 = c0 + (wv >> 1), n_it = (c1 - v0 + 1) >> 1;
     int entries = -1;                            // of the 64 pages from iteration `it` & ~63 on, one per lane
     const int* const table = a.page_table + (size_t)b * a.max_pages;
     auto page_at = [&](int it) {                 // asked for in order
         if ((it & 63) == 0) {
-            const int v = c0 + wv + (it + lane) * KD_WAVES;
+            const int v = v0 + (it + lane) * 2;
             entries = v < c1 ? table[page_number(rq, v)] : -1;
             asm volatile("" : "+v"(entries));    // waited for here, and not in every iteration behind whatever else is in flight
         }
         const int e = __builtin_amdgcn_readlane(entries, it & 63);
         return e >= 0 && e < a.num_pages ? e : -1;
     };
-    const uint16_t* const heads = a.pages + (size_t)g * kv16_head_values(D);
+    const uint16_t* const heads = a.pages + (size_t)g * kv16_head_values(D) + half * HALF * D;
     const size_t page_values = (size_t)a.Hkv * kv16_head_values(D);
     auto head = [&](int page) { return heads + (size_t)(unsigned)(page < 0 ? 0 : page) * page_values; };
-    uintx4 kx[2 * NB], vx[NT];                   // half a page: keys of two tiles of positions, values
-    auto ask_keys = [&](int page, int half) __attribute__((always_inline)) {
-        const uint16_t* const from = head(page) + half * HALF * D;
+    uintx4 kx[2 * NB], vx[NT];                   // keys of two tiles of positions, values
+    auto ask_keys = [&](int page) __attribute__((always_inline)) {
+        const uint16_t* const from = head(page);
 #pragma unroll
         for (int i = 0; i < 2 * NB; ++i) kx[i] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + i * 512 + lane * 8));
     };
-    auto ask_values = [&](int page, int half, int t) __attribute__((always_inline)) {
-        const uint16_t* const from = head(page) + kv16_values(D) + half * HALF * D;
+    auto ask_values = [&](int page, int t) __attribute__((always_inline)) {
+        const uint16_t* const from = head(page) + kv16_values(D);
         vx[t] = __builtin_nontemporal_load(reinterpret_cast<const uintx4*>(from + t * 512 + lane * 8));
     };
     int page = n_it > 0 ? page_at(0) : -1;
-    ask_keys(page, 0);
+    ask_keys(page);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) ask_values(page, 0, t);
+    for (int t = 0; t < NT; ++t) ask_values(page, t);
 
     // m: the maximum that the row's weights refer to; start: WEIGHT_LOG2 - m, so that a weight is 2^(score + start); l: the weights' sum, as a product with ones
     // (every element is the lane's row's)
@@ -226,9 +222,9 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
 #pragma unroll
     for (int t = 0; t < NT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    for (int step = 0; step < 2 * n_it; ++step) {
-        const int half = step & 1, it = step >> 1, number = page_number(rq, c0 + wv + it * KD_WAVES);
-        const int next = !half ? page : it + 1 < n_it ? page_at(it + 1) : -1;
+    for (int it = 0; it < n_it; ++it) {
+        const int number = page_number(rq, v0 + it * 2);
+        const int next = it + 1 < n_it ? page_at(it + 1) : -1;
         const bool there = page >= 0;
         const int base = number * KV16_PAGE + half * HALF;
         floatx4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -236,7 +232,7 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
         for (int k = 0; k < NB; ++k)
 #pragma unroll
             for (int i = 0; i < 2; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kx[i * NB + k]), queries[k], s[i], 0, 0, 0);
-        ask_keys(next, half ^ 1);
+        ask_keys(next);
         float t[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) t[i] = __builtin_fmaf(s[i >> 2][i & 3], a.scale2, start);
@@ -253,16 +249,12 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
 #pragma unroll
                 for (int i = 0; i < 4; ++i) vx[k][i] &= keep[i];
         }
-        if (SCORES && lo < rows) {
-            float* const to = a.scores + (((size_t)b * a.Hkv + g) * a.max_q * group + lo) * a.max_pages * KV16_PAGE + base + 4 * hi;
+        floatx4 score[2];                        // stored behind the values' loads: those of the next half are waited for in order, and a store takes longer
+        if (SCORES)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                floatx4 y;
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = t[4 * i + r] == -__builtin_inff() ? t[4 * i + r] : s[i][r] * a.scale2;
-                *reinterpret_cast<floatx4*>(to + 16 * i) = y;
-            }
-        }
+                for (int r = 0; r < 4; ++r) score[i][r] = t[4 * i + r] == -__builtin_inff() ? t[4 * i + r] : s[i][r] * a.scale2;
         half8 pl, ps;
         auto weights = [&]() __attribute__((always_inline)) {
             half4 large[2], small[2];
@@ -305,7 +297,12 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
             const half8 v = __builtin_bit_cast(half8, vx[k]);
             o[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl, o[k], 0, 0, 0);
             o[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ps, o[k], 0, 0, 0);
-            ask_values(next, half ^ 1, k);
+            ask_values(next, k);
+        }
+        if (SCORES && lo < rows) {
+            float* const to = a.scores + (((size_t)b * a.Hkv + g) * a.max_q * group + lo) * a.max_pages * KV16_PAGE + base + 4 * hi;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) *reinterpret_cast<floatx4*>(to + 16 * i) = score[i];
         }
         page = next;
     }
@@ -315,7 +312,7 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
     if (hi == 0) { s_m[wv][lo] = m; s_l[wv][lo] = l[0]; }
     __syncthreads();
     auto finish = [&](int c, int d, float of, float lf, float mn) {
-        const size_t row = row_of_column(c), pr = part_row(a, b, r0 + c, g, group);
+        const size_t row = row_of_column(c), pr = part_row(a, b, c, g, group);
         if (whole) {
             a.out[row * D + d] = lf == 0.f ? 0 : to_half_bits(of / lf);
             if (d == 0 && a.stats) {
@@ -357,32 +354,42 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
         if (!(odd >> c & 1)) continue;           // (uniform)
         float cw[KD_WAVES], lf;
         const float mn = merge(c, cw, lf);
-        const float of = slow_row<D, KD_THREADS>(a, rq, b, g, row_of_column(c), (r0 + c) / group, c0, c1, mn, s_w, lf);
+        const float of = slow_row<D, KD_THREADS>(a, rq, b, g, row_of_column(c), c / group, c0, c1, mn, s_w, lf);
         if (tid < D) finish(c, tid, of * 512.0f, lf * 512.0f, mn);
     }
 }
 
-// The chunks' (sum, maximum, weight) triples of a row.  Groups of D threads take every GROUPS-th chunk each, eight loads in flight, and meet in LDS:
-// a fixed order.
-constexpr int KC_THREADS = 512;
+// The chunks' (sum, maximum, weight) triples of a request's rows, (token, head) pairs in the order of q.  A group of D threads has a row of up to eight chunks to itself; of more, all
+// groups take every GROUPS-th chunk each, eight loads in flight, and meet in LDS: a fixed order.  The loads come before anything is known of the request (what lies behind its last
+// chunk is the workspace's, and not used).
+constexpr int KC_THREADS = 512, KC_AHEAD = 8;
+template <int D> __host__ __device__ int combine_blocks(const Kv16AttnArgs& a)
+{
+    const int rows = a.Hq * a.max_q, each = a.nsplit <= KC_AHEAD ? KC_THREADS / D : 1;
+    return a.nsplit > 1 ? (rows + each - 1) / each : 0;
+}
 template <int D>
-__global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
+__device__ __forceinline__ void combine_rows(const Kv16AttnArgs& a, int block, int b)
 {
     constexpr int GROUPS = KC_THREADS / D;
-    __shared__ float s_o[GROUPS][D], s_w[KV16_MAX_SPLIT];
-    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63, d = threadIdx.x % D, grp = threadIdx.x / D;
-    const Request rq = find_request(a, b);
-    if (i >= rq.n) return;
-    const int size = chunk_pages(a, rq.pages);
-    if (rq.pages <= size) return;               // one chunk: the first pass has written this output
-    const int live = (rq.pages + size - 1) / size;
-    const size_t row = (size_t)(rq.first + i) * a.Hq + h, pr = part_row(a, b, i, h, 1);
-    const float* const first = a.part + pr * a.nsplit * kv16_part(D);
-    const float m = lane < live ? first[(size_t)lane * kv16_part(D) + D] : -__builtin_inff();
-    const float w = lane < live ? first[(size_t)lane * kv16_part(D) + D + 1] : 0.f;
-    float v[8];
+    __shared__ float s_o[GROUPS][D], s_w[GROUPS][KV16_MAX_SPLIT];
+    const int lane = threadIdx.x & 63, d = threadIdx.x % D, grp = threadIdx.x / D;
+    const bool alone = a.nsplit <= KC_AHEAD;
+    if (block >= combine_blocks<D>(a)) return;
+    const int row = alone ? block * GROUPS + grp : block, chunk = alone ? 0 : grp, stride = alone ? 1 : GROUPS, own = alone ? grp : 0;
+    const bool exists = row < a.max_q * a.Hq;
+    const int i = row / a.Hq;
+    const float* const first = a.part + ((size_t)b * a.max_q * a.Hq + (exists ? row : 0)) * a.nsplit * kv16_part(D);
+    float m = lane < a.nsplit ? first[(size_t)lane * kv16_part(D) + D] : 0.f;
+    float w = lane < a.nsplit ? first[(size_t)lane * kv16_part(D) + D + 1] : 0.f;
+    float v[KC_AHEAD];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = grp + k * GROUPS < live ? first[(size_t)(grp + k * GROUPS) * kv16_part(D) + d] : 0.f;
+    for (int k = 0; k < KC_AHEAD; ++k) v[k] = chunk + k * stride < a.nsplit ? first[(size_t)(chunk + k * stride) * kv16_part(D) + d] : 0.f;
+    const Request rq = find_request(a, b);
+    const int size = chunk_pages(a, rq.pages), live = (rq.pages + size - 1) / size;
+    const bool cut = exists && i < rq.n && rq.pages > size;      // (one chunk: the first pass has written this output)
+    m = lane < live ? m : -__builtin_inff();
+    w = lane < live ? w : 0.f;
     float top = m;
 #pragma unroll
     for (int sh = 1; sh < 64; sh <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, sh));
@@ -390,31 +397,39 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
     float l = w * c;
 #pragma unroll
     for (int sh = 1; sh < 64; sh <<= 1) l += __shfl_xor(l, sh);
-    if (threadIdx.x < 64) s_w[lane] = __builtin_fmaxf(c, 1e-37f);      // (an infinity in a chunk whose weights underflow stays one)
+    if (alone || grp == 0) s_w[own][lane] = __builtin_fmaxf(c, 1e-37f);      // (an infinity in a chunk whose weights underflow stays one; a group's waves write the same)
     __syncthreads();
-    float o = 0.f;
-    for (int k0 = 0;;) {
+    float sum = 0.f;
+    for (int k0 = chunk;;) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (grp + (k0 + k) * GROUPS < live) o += v[k] * s_w[grp + (k0 + k) * GROUPS];
-        k0 += 8;
-        if (k0 * GROUPS >= live) break;
+        for (int k = 0; k < KC_AHEAD; ++k)
+            if (k0 + k * stride < live) sum += v[k] * s_w[own][k0 + k * stride];
+        k0 += KC_AHEAD * stride;
+        if (k0 >= live) break;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = grp + (k0 + k) * GROUPS < live ? first[(size_t)(grp + (k0 + k) * GROUPS) * kv16_part(D) + d] : 0.f;
+        for (int k = 0; k < KC_AHEAD; ++k) v[k] = k0 + k * stride < live ? first[(size_t)(k0 + k * stride) * kv16_part(D) + d] : 0.f;
     }
-    s_o[grp][d] = o;
-    __syncthreads();
-    if (threadIdx.x >= D) return;
-    float sum = s_o[0][d];
+    if (!alone) {
+        s_o[grp][d] = sum;
+        __syncthreads();
+        sum = s_o[0][d];
 #pragma unroll
-    for (int k = 1; k < GROUPS; ++k) sum += s_o[k][d];
-    a.out[row * D + d] = l == 0.f ? 0 : to_half_bits(sum / l);
-    if (d == 0 && a.stats) {
+        for (int k = 1; k < GROUPS; ++k) sum += s_o[k][d];
+    }
+    if (!cut || (!alone && grp > 0)) return;
+    a.out[((size_t)rq.first * a.Hq + row) * D + d] = l == 0.f ? 0 : to_half_bits(sum / l);
+    if (d == 0 && a.stats && !a.scores) {
         float exact = 0.f;
-        for (int k = 0; k < live; ++k) exact += first[(size_t)k * kv16_part(D) + D + 2] * s_w[k];
-        a.stats[2 * pr] = top == -__builtin_inff() ? 0.f : top;
-        a.stats[2 * pr + 1] = exact == 0.f ? 0.f : 1.0f / exact;
+        for (int k = 0; k < live; ++k) exact += first[(size_t)k * kv16_part(D) + D + 2] * s_w[own][k];
+        float* const to = a.stats + 2 * ((size_t)b * a.max_q * a.Hq + row);
+        to[0] = top == -__builtin_inff() ? 0.f : top;
+        to[1] = exact == 0.f ? 0.f : 1.0f / exact;
     }
+}
+template <int D>
+__global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
+{
+    combine_rows<D>(a, blockIdx.x, blockIdx.y);
 }
 
 // ---- many rows of a cache head: prompts and chunks of them ----------------------------------------------------------
@@ -873,27 +888,71 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
 
 // ---- what each position got of the rows' attention -------------------------------------------------------------------
 //
-// Up to 16 rows of a cache head: the few-rows kernel leaves its scores (4 bytes a row and position next to the 4 D that it reads); here they become weights with the maxima and sums that
-// the attention left behind, and are added up over the rows.  A thread takes four positions.
-constexpr int KS_THREADS = 256;
-__global__ __launch_bounds__(KS_THREADS) void kv16_attn_weigh(Kv16AttnArgs a)
+// Up to 16 rows of a cache head: the few-rows kernel leaves its scores (4 bytes a row and position next to the 4 D that it reads); here they become weights with the rows' maxima and sums,
+// and are added up over the rows.  A thread takes four positions.  Where requests are cut, the last workgroups put the rows' chunks together (combine_rows), and the others find the
+// maxima and sums of their rows by themselves, so that neither waits for the other.
+template <int D>
+__global__ __launch_bounds__(KC_THREADS) void kv16_attn_weigh(Kv16AttnArgs a, int weighing)
 {
-    const int g = blockIdx.y, b = blockIdx.z, p0 = (blockIdx.x * KS_THREADS + threadIdx.x) * 4;
+    const int block = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+    if (block >= weighing) {
+        combine_rows<D>(a, (block - weighing) * a.Hkv + g, b);
+        return;
+    }
+    __shared__ float s_m[KV16_FEW_ROWS], s_inv[KV16_FEW_ROWS];
+    const int p0 = (block * KC_THREADS + threadIdx.x) * 4, wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const Request rq = find_request(a, b);
-    if (p0 >= rq.len) return;
+    if (block * KC_THREADS * 4 >= rq.len) return;
     const int number = p0 / KV16_PAGE, rows = rq.n * a.group, before = rq.len - rq.n;
     const size_t at = ((size_t)b * a.Hkv + g) * a.max_pages * KV16_PAGE + p0;
-    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (number < rq.lead || number >= rq.lead + rq.skip) {
-        const size_t stride = (size_t)a.max_pages * KV16_PAGE;
-        const float* scores = a.scores + ((size_t)b * a.Hkv + g) * a.max_q * a.group * stride + p0;
-        for (int r = 0; r < rows; ++r, scores += stride) {
-            const floatx4 s = *reinterpret_cast<const floatx4*>(scores);
-            const float* const stats = a.stats + 2 * part_row(a, b, r, g, a.group);
-            const float m = stats[0], inv = stats[1] * 512.0f;
+    const size_t stride = (size_t)a.max_pages * KV16_PAGE;
+    const float* const scores = a.scores + ((size_t)b * a.Hkv + g) * a.max_q * a.group * stride + p0;
+    const bool looked = p0 < rq.len && (number < rq.lead || number >= rq.lead + rq.skip);
+    floatx4 s[8];
+    auto ask = [&](int from) __attribute__((always_inline)) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum[k] = __builtin_fmaf(inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(s[k] - m), inv, sum[k]);
+        for (int r = 0; r < 8; ++r) s[r] = looked && from + r < rows ? *reinterpret_cast<const floatx4*>(scores + (from + r) * stride) : floatx4{0.f, 0.f, 0.f, 0.f};
+    };
+    ask(0);
+    const int size = chunk_pages(a, rq.pages), live = (rq.pages + size - 1) / size;
+    for (int r = wv; r < rows; r += KC_THREADS / 64) {
+        const size_t pr = part_row(a, b, r, g, a.group);
+        float m, inv;
+        if (live <= 1) {
+            m = a.stats[2 * pr];
+            inv = a.stats[2 * pr + 1];
+        } else {
+            const float* const mine = a.part + (pr * a.nsplit + lane) * kv16_part(D) + D;
+            const float x = lane < live ? mine[0] : -__builtin_inff();
+            float sum = lane < live ? mine[2] : 0.f;
+            m = x;
+#pragma unroll
+            for (int sh = 1; sh < 64; sh <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, sh));
+            m = m == -__builtin_inff() ? 0.f : m;
+            sum *= __builtin_amdgcn_exp2f(x - m);
+#pragma unroll
+            for (int sh = 1; sh < 64; sh <<= 1) sum += __shfl_xor(sum, sh);
+            inv = sum == 0.f ? 0.f : 1.0f / sum;
         }
+        if (lane == 0) {
+            s_m[r] = m;
+            s_inv[r] = inv * 512.0f;             // (sums are of 2^WEIGHT_LOG2 times the weights)
+        }
+    }
+    __syncthreads();
+    if (p0 >= rq.len) return;
+    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int from = 0;;) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            if (!looked || from + r >= rows) continue;
+            const float m = s_m[from + r], inv = s_inv[from + r];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] = __builtin_fmaf(inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(s[r][k] - m), inv, sum[k]);
+        }
+        from += 8;
+        if (from >= rows) break;
+        ask(from);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -1014,14 +1073,14 @@ template <int D>
 hipError_t launch(const Kv16AttnArgs& a, hipStream_t stream)
 {
     const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.B, (unsigned)a.nsplit);
-    const bool scores = a.weights_out && a.scores;
-    if (a.split_rows && scores) hipLaunchKernelGGL((kv16_attn_decode<D, true>), grid, dim3(KD_THREADS), 0, stream, a);
-    else if (a.split_rows) hipLaunchKernelGGL((kv16_attn_decode<D, false>), grid, dim3(KD_THREADS), 0, stream, a);
+    const bool scores = a.few && a.weights_out;
+    if (scores) hipLaunchKernelGGL((kv16_attn_decode<D, true>), grid, dim3(KD_THREADS), 0, stream, a);
+    else if (a.few) hipLaunchKernelGGL((kv16_attn_decode<D, false>), grid, dim3(KD_THREADS), 0, stream, a);
     else if (a.weights_out) launch_prompt<D, true>(a, grid, stream);
     else launch_prompt<D, false>(a, grid, stream);
-    if (a.nsplit > 1) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)a.Hq, (unsigned)a.max_q, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
-    if (scores)
-        hipLaunchKernelGGL(kv16_attn_weigh, dim3((unsigned)((a.max_pages * (KV16_PAGE / 4) + KS_THREADS - 1) / KS_THREADS), (unsigned)a.Hkv, (unsigned)a.B), dim3(KS_THREADS), 0, stream, a);
+    const int combining = combine_blocks<D>(a), weighing = (a.max_pages * (KV16_PAGE / 4) + KC_THREADS - 1) / KC_THREADS;
+    if (combining && !scores) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)combining, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
+    if (scores) hipLaunchKernelGGL((kv16_attn_weigh<D>), dim3((unsigned)(weighing + (combining + a.Hkv - 1) / a.Hkv), (unsigned)a.Hkv, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a, weighing);
     else if (a.weights_out)
         hipLaunchKernelGGL((kv16_attn_weights<D>), dim3((unsigned)((a.max_pages + 1) / 2), (unsigned)a.Hkv, (unsigned)a.B), dim3(KW_THREADS), 0, stream, a);
     return hipGetLastError();

@@ -174,8 +174,9 @@ def run_attention(thi, c, scale, window=0, sinks=0, decode=False, weights=False,
 
 
 def one_or_two(c):
+    # (past 16 rows, weights are cut by (1 - d) with 0 <= d <= 2^-10: as one of 2^-11 around a mean of 2^-11, and what all have in common the sum cancels)
     group = c["q"].shape[1] // c["pages"].shape[1]
-    return ref.TWO_SUMMANDS if c["max_q"] * group <= 64 else ref.ONE_SUMMAND
+    return ref.TWO_SUMMANDS if c["max_q"] * group <= 16 else ref.ONE_SUMMAND
 
 
 def check_attention(thi, c, window=0, sinks=0, decode=False, weights=False, weights_in=None, scale=None):
