@@ -342,7 +342,7 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
  * weights_out (or NULL) [B][Hkv][64 max_pages] fp32: what each position got of the attention, for thi_kv16_evict:
  *   weights_out[b,g,j] = before + sum of p_j over the request's rows and the query heads of cache head g,  j < seq_lens[b]
  * where before is weights_in[b,g,j] (the same shape, or the same buffer; NULL: 0) for the positions in front of the new tokens and 0 for theirs.  Entries from seq_lens[b] on
- * are not written.
+ * are not written.  With weights, Hkv max_pages <= 2^23.
  *
  * Scores, statistics and sums are fp32.  Weights reach the matrix cores as fp16: up to 16 rows of a request and cache head (max_q Hq / Hkv) as two summands, beyond as one,
  * cut to its bits, as is the sum that divides the result.  Workspace:

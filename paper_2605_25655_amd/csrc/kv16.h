@@ -47,11 +47,13 @@ struct Kv16AttnArgs {
     int group;                       // Hq / Hkv query heads per cache head
     // how the rows are dealt (kv16_plan)
     float* part;                     // [B][max_q][Hq][nsplit][kv16_part(D)]: a chunk's unnormalised output, maximum, sum of the weights as they were multiplied, and as they are
-    float* stats;                    // [B][max_q][Hq][2]: a row's maximum and one over its sum, with weights_out
+    float* stats;                    // [B][Hkv][tiles KV16_TILE_ROWS][2]: a row's maximum and one over its sum, with weights_out
+    uint16_t* queries;               // [B][Hkv][tiles KV16_TILE_ROWS / 16][D / 32][64][8]: queries as matrix operands, with weights_out, for more rows than few
     float* scores;                   // [B][Hkv][16 max_pages][max_q group][4]: four positions' scores in powers of two, with weights_out, for few rows
     bool few;                        // all rows of a request and cache head at once, at most KV16_FEW_ROWS
-    int tiles;                       // else: tiles of KV16_TILE_ROWS
+    int tiles;                       // of KV16_TILE_ROWS rows
     int nsplit, min_chunk;           // chunks per request at most, pages per chunk at least
+    int num_cus;
 };
 constexpr int KV16_MAX_SPLIT = 64;
 constexpr int KV16_FEW_ROWS = 16, KV16_TILE_ROWS = 128;

@@ -14,6 +14,7 @@ bool heads_ok(int Hq, int Hkv, int D) { return Hq >= 1 && Hkv >= 1 && Hq <= 6553
 bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff / KV16_PAGE; }
 
 constexpr int MAX_PAGES = 1 << 24;      // of a row of the page table: positions stay below 2^30
+constexpr long MAX_WEIGHED = 1 << 23;   // pages of a row times cache heads, with weights: a launch's threads stay below 2^32
 
 // Pages of a chunk at least, chunks' workgroups for every compute unit, and tables times columns that are not cut (kv16_plan)
 constexpr int CHUNK = 4, FEW_PER_CU = 3, MANY_PER_CU = 2, FEW_UNCUT = 1280;
@@ -35,7 +36,12 @@ size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
     return (size_t)(few > many ? few : many);
 }
 size_t bytes_of_rows(size_t rows, int D) { return rows ? round_up(rows * kv16_part(D) * sizeof(float)) : 256; }
-size_t bytes_of_stats(int B, int Hq, int max_q) { return round_up((size_t)B * max_q * Hq * 2 * sizeof(float)); }
+size_t tiles_of(int Hq, int Hkv, int max_q) { return ((size_t)max_q * (Hq / Hkv) + KV16_TILE_ROWS - 1) / KV16_TILE_ROWS; }
+size_t bytes_of_stats(int B, int Hq, int Hkv, int max_q) { return tiles_of(Hq, Hkv, max_q) * B * Hkv * KV16_TILE_ROWS * 2 * sizeof(float); }
+size_t bytes_of_queries(int B, int Hq, int Hkv, int D, int max_q)
+{
+    return (size_t)max_q * (Hq / Hkv) <= KV16_FEW_ROWS ? 0 : tiles_of(Hq, Hkv, max_q) * B * Hkv * KV16_TILE_ROWS * D * 2;
+}
 // of the most that a call of up to so many leaves of its scores
 size_t bytes_of_scores(int B, int Hq, int Hkv, int max_q, int max_pages)
 {
@@ -64,13 +70,14 @@ void thi::kv16_plan(Kv16AttnArgs& a, int num_cus)
 {
     a.group = a.Hq / a.Hkv;
     a.few = (long)a.max_q * a.group <= KV16_FEW_ROWS;
-    a.tiles = a.few ? 1 : (int)(((long)a.max_q * a.group + KV16_TILE_ROWS - 1) / KV16_TILE_ROWS);
+    a.tiles = (int)(((long)a.max_q * a.group + KV16_TILE_ROWS - 1) / KV16_TILE_ROWS);
     const long items = (long)a.B * a.Hkv * a.tiles;
     const long most = a.few && (long)a.max_pages * a.D <= FEW_UNCUT ? 1 : (a.max_pages + CHUNK - 1) / CHUNK;
     a.min_chunk = CHUNK;
     long n = (long)(a.few ? FEW_PER_CU : MANY_PER_CU) * num_cus / items;
     n = n < 1 ? 1 : n > KV16_MAX_SPLIT ? KV16_MAX_SPLIT : n;
     a.nsplit = (int)(n > most ? most : n);
+    a.num_cus = num_cus;
 }
 
 extern "C" {
@@ -106,8 +113,10 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
 
 size_t thi_kv16_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages, int weights)
 {
-    if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_q > 65535 || max_pages < 1 || max_pages > MAX_PAGES) return 0;
-    return bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, max_q) + bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0);
+    if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_q > 65535 || max_pages < 1 || max_pages > MAX_PAGES ||
+        (weights && (long)max_pages * Hkv > MAX_WEIGHED))
+        return 0;
+    return bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, Hkv, max_q) + bytes_of_queries(B, Hq, Hkv, D, max_q) + bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0);
 }
 
 int thi_kv16_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, int window, int sinks,
@@ -126,7 +135,7 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     a.window = window;
     a.sinks = window ? sinks : 0;
     kv16_plan(a, device_cu_count());
-    const size_t stats = weights_out ? bytes_of_stats(B, Hq, max_q) : 0;
+    const size_t stats = weights_out ? bytes_of_stats(B, Hq, Hkv, max_q) : 0, queries = weights_out ? bytes_of_queries(B, Hq, Hkv, D, max_q) : 0;
     const size_t scores = weights_out && a.few ? bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0;
     if (workspace_bytes < need) return THI_ERR_WORKSPACE;
     (void)hipGetLastError();
@@ -141,8 +150,9 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     a.scale2 = scale * 1.44269504088896340736f;
     if (a.scale2 == 0.f) a.scale2 = 1e-30f;      // (all weights equal either way; a masked score of -inf stays what it is)
     a.stats = weights_out ? (float*)workspace : nullptr;
+    a.queries = queries ? (uint16_t*)((char*)workspace + stats) : nullptr;
     a.scores = scores ? (float*)((char*)workspace + stats) : nullptr;
-    a.part = (float*)((char*)workspace + stats + scores);
+    a.part = (float*)((char*)workspace + stats + queries + scores);
     return finish(launch_kv16_attention(a, (hipStream_t)hip_stream));
 }
 

@@ -72,6 +72,9 @@ __device__ __forceinline__ size_t part_row(const Kv16AttnArgs& a, int b, int r, 
     return ((size_t)b * a.max_q + r / group) * a.Hq + (size_t)g * group + r % group;
 }
 
+// The same by cache head, for what kv16_attn_weights and kv16_attn_weigh read.
+__device__ __forceinline__ size_t stats_row(const Kv16AttnArgs& a, int b, int g, int r) { return ((size_t)b * a.Hkv + g) * a.tiles * KV16_TILE_ROWS + r; }
+
 // over the lanes of the same lo (the four hi)
 __device__ __forceinline__ float max_over_hi(float x)
 {
@@ -316,8 +319,9 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
         if (whole) {
             a.out[row * D + d] = lf == 0.f ? 0 : to_half_bits(of / lf);
             if (d == 0 && a.stats) {
-                a.stats[2 * pr] = mn == -__builtin_inff() ? 0.f : mn;
-                a.stats[2 * pr + 1] = lf == 0.f ? 0.f : 1.0f / lf;
+                float* const to = a.stats + 2 * stats_row(a, b, g, c);
+                to[0] = mn == -__builtin_inff() ? 0.f : mn;
+                to[1] = lf == 0.f ? 0.f : 1.0f / lf;
             }
         } else {
             float* const po = a.part + (pr * a.nsplit + chunk) * kv16_part(D);
@@ -421,7 +425,8 @@ __device__ __forceinline__ void combine_rows(const Kv16AttnArgs& a, int block, i
     if (d == 0 && a.stats && !a.scores) {
         float exact = 0.f;
         for (int k = 0; k < live; ++k) exact += first[(size_t)k * kv16_part(D) + D + 2] * s_w[own][k];
-        float* const to = a.stats + 2 * ((size_t)b * a.max_q * a.Hq + row);
+        const int h = row - i * a.Hq, g = h / a.group;
+        float* const to = a.stats + 2 * stats_row(a, b, g, i * a.group + h - g * a.group);
         to[0] = top == -__builtin_inff() ? 0.f : top;
         to[1] = exact == 0.f ? 0.f : 1.0f / exact;
     }
@@ -729,6 +734,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int b = 0; b < NB; ++b) asm volatile("" : "+v"(queries[c][b]));      // waited for here, and not in every turn behind what is on its way into LDS
+    if (STATS && tile.chunk == 0 && rows_here)      // as operands, for kv16_attn_weights
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                *reinterpret_cast<half8*>(a.queries + (stats_row(a, tile.b, tile.g, w0 + 16 * c) / 16 * NB + b) * 512 + lane * 8) = queries[c][b];
     kp_wait<0>();
     kp_barrier();
     auto nothing = [](int) {};
@@ -839,7 +850,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     if (here < 32) odd_rows &= here <= 0 ? 0u : (1u << here) - 1u;
     if (lane == 0) s_odd[wv] = odd_rows;
     auto put_stats = [&](int r, float mm, float ll) {
-        float* const to = e.stats + 2 * part_row(e, at.b, r, at.g, e.group);
+        float* const to = e.stats + 2 * stats_row(e, at.b, at.g, r);
         to[0] = mm == -__builtin_inff() ? 0.f : mm;
         to[1] = ll == 0.f ? 0.f : 1.0f / ll;
     };
@@ -919,8 +930,9 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_weigh(Kv16AttnArgs a, in
         const size_t pr = part_row(a, b, r, g, a.group);
         float m, inv;
         if (live <= 1) {
-            m = a.stats[2 * pr];
-            inv = a.stats[2 * pr + 1];
+            const float* const mine = a.stats + 2 * stats_row(a, b, g, r);
+            m = mine[0];
+            inv = mine[1];
         } else {
             const float* const mine = a.part + (pr * a.nsplit + lane) * kv16_part(D) + D;
             const float x = lane < live ? mine[0] : -__builtin_inff();
@@ -959,31 +971,31 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_weigh(Kv16AttnArgs a, in
         if (p0 + k < rq.len) a.weights_out[at + k] = (a.weights_in && p0 + k < before ? a.weights_in[at + k] : 0.f) + sum[k];
 }
 
-// More rows: the scores are made again.  A workgroup takes two pages of a cache head, whose keys stay in its waves' registers (the A operand); the rows that see any of them come by, 16
-// at a time, every fourth 16 in a wave.  Weights in fp32, added up per lane (a lane has one row of each 16), then over lanes and waves: a fixed order.
-constexpr int KW_THREADS = 256, KW_WAVES = 4;
-template <int D>
-__global__ __launch_bounds__(KW_THREADS, 2) void kv16_attn_weights(Kv16AttnArgs a)
+// More rows: the scores are made again.  A workgroup takes a page of a cache head, whose keys stay in its waves' registers (the A operand); the rows that see any of it come by, 16
+// at a time, every WAVES-th 16 in a wave.  Weights in fp32, added up per lane (a lane has one row of each 16), then over lanes and waves: a fixed order.
+// For each 16 rows and 64 positions 262 kFLOP of matrix products (D = 128), 1024 exponentials and 4 KB of queries; the last is what bounds it.  So kv16_attn_prompt leaves the queries as operands, a
+// KB at a time: from where they stand, 16 rows a load, the rows of 32 heads 8 KB apart fall on one channel of the cache (2001 tokens of 32/32 heads of 128, all of the call: 102 us, like this 87).
+// Two pages in a workgroup, which halve the queries' way, leave too few of them (2001 tokens of 64/8 heads 317 us against 212); products of the next rows between the weights of the last: no gain
+// (89).  Eight waves instead of four where the workgroups are few: 2001 tokens of 64/8 heads 188 -> 170 us; where they are not, it is the other way round (of 32/32: 87 -> 93).
+constexpr int KW_PER_CU = 2;                     // up to so many workgroups for a compute unit: of eight waves instead of four
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs a)
 {
-    constexpr int NB = D / 32, TILES = 8;        // tiles of 16 positions
-    __shared__ float s_sum[KW_WAVES][4 * TILES][64];
+    constexpr int NB = D / 32, TILES = 4, SPAN = KV16_PAGE;      // tiles of 16 positions
+    __shared__ float s_sum[WAVES][4 * TILES][64];
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int number = blockIdx.x * 2, g = blockIdx.y, b = blockIdx.z;
+    const int number = blockIdx.x / (unsigned)a.Hkv, g = blockIdx.x - number * a.Hkv, b = blockIdx.y;      // the first pages first: the most rows see them
     const Request rq = find_request(a, b);
     const int p0 = number * KV16_PAGE, group = a.group, before = rq.len - rq.n;
     if (p0 >= rq.len) return;
-    bool there[2];
+    const int page = a.page_table[(size_t)b * a.max_pages + number];
+    const bool there = page >= 0 && page < a.num_pages;
+    const uint16_t* const from = a.pages + ((size_t)(unsigned)(there ? page : 0) * a.Hkv + g) * kv16_head_values(D);
     half8 keys[TILES][NB];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        const int e = number + n < a.max_pages ? a.page_table[(size_t)b * a.max_pages + number + n] : -1;
-        there[n] = e >= 0 && e < a.num_pages;
-        const uint16_t* const head = a.pages + ((size_t)(unsigned)(there[n] ? e : 0) * a.Hkv + g) * kv16_head_values(D);
+    for (int i = 0; i < TILES; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < NB; ++k) keys[4 * n + i][k] = __builtin_bit_cast(half8, ld_cached(head + (i * NB + k) * 512 + lane * 8));
-    }
+        for (int k = 0; k < NB; ++k) keys[i][k] = __builtin_bit_cast(half8, ld_cached(from + (i * NB + k) * 512 + lane * 8));
     float sum[4 * TILES];
 #pragma unroll
     for (int i = 0; i < 4 * TILES; ++i) sum[i] = 0.f;
@@ -991,66 +1003,90 @@ __global__ __launch_bounds__(KW_THREADS, 2) void kv16_attn_weights(Kv16AttnArgs 
     const int first = p0 > before ? p0 - before : 0;
     int last = rq.n;
     if (a.window > 0 && p0 >= a.sinks) {
-        const long most = (long)p0 + 2 * KV16_PAGE - 1 + a.window - before;      // token i sees from before + i + 1 - window on
+        const long most = (long)p0 + SPAN - 1 + a.window - before;      // token i sees from before + i + 1 - window on
         last = most < last ? (most < 0 ? 0 : (int)most) : last;
     }
-    const int r_end = last * group;
+    // rows of (token, head) pairs, 16 at a time as the attention left them
+    const int tile0 = first * group / 16 + wv, tile_end = (last * group + 15) / 16;
+    int token = (tile0 * 16 + lo) / group, rest = (tile0 * 16 + lo) % group;
+    const int token_step = 16 * WAVES / group, rest_step = 16 * WAVES - token_step * group;
+    const size_t row0 = stats_row(a, b, g, 0) + tile0 * 16;
+    const uint16_t* q = a.queries + row0 * D + lane * 8;
+    const float* stats = a.stats + 2 * (row0 + lo);
     struct Rows {
         half8 q[NB];
-        float m, inv;
+        float2 stats;
         int token;
     };
-    auto ask = [&](int r0, Rows& x) __attribute__((always_inline)) {      // rows r0 .. r0 + 15 (behind the last one: the last one, with no weight)
-        const int r = r0 + lo < r_end ? r0 + lo : r_end - 1;
-        x.token = r / group;
-        const uint16_t* const q = a.q + ((size_t)(rq.first + x.token) * a.Hq + (size_t)g * group + (r - x.token * group)) * D + hi * 8;
+    int left = tile_end - tile0;                 // (the last ones are asked for again, for nobody)
+    auto ask = [&](Rows& x) __attribute__((always_inline)) {
+        x.token = token;
 #pragma unroll
-        for (int k = 0; k < NB; ++k) x.q[k] = __builtin_bit_cast(half8, ld_cached(q + k * 32));
-        const float* const stats = a.stats + 2 * part_row(a, b, r, g, group);
-        x.m = stats[0];
-        x.inv = r0 + lo < r_end ? stats[1] * 512.0f : 0.f;
-    };
-    const int r_first = first * group + wv * 16;
-    if (first < last && r_first < r_end) {
-        Rows now, next;
-        ask(r_first, now);
-        for (int r0 = r_first; r0 < r_end; r0 += 16 * KW_WAVES) {
-            ask(r0 + 16 * KW_WAVES < r_end ? r0 + 16 * KW_WAVES : r0, next);
-            const Sight mine = sight_of(a, rq, now.token), low = sight_of(a, rq, __builtin_amdgcn_readfirstlane(now.token)), high = sight_of(a, rq, __builtin_amdgcn_readlane(now.token, 15));
-            floatx4 s[TILES];
-#pragma unroll
-            for (int i = 0; i < TILES; ++i) s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < NB; ++k)
-#pragma unroll
-                for (int i = 0; i < TILES; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys[i][k], now.q[k], s[i], 0, 0, 0);
-            float w[4 * TILES];
-#pragma unroll
-            for (int i = 0; i < 4 * TILES; ++i) w[i] = __builtin_fmaf(s[i >> 2][i & 3], a.scale2, -now.m);
-            // does some row not see all of it, or is some row not there or not a number?
-            const bool odd = __builtin_amdgcn_ballot_w64(!(now.inv > 0.f)) != 0ull;
-            if (odd || !there[0] || !there[1] || p0 + 2 * KV16_PAGE > low.end || (p0 < high.from && p0 + 2 * KV16_PAGE > a.sinks)) {
-#pragma unroll
-                for (int i = 0; i < 4 * TILES; ++i)
-                    if (!there[i >> 4] || now.inv == 0.f || !sees(mine, a.sinks, p0 + 16 * (i >> 2) + 4 * hi + (i & 3))) w[i] = -__builtin_inff();
-                // (a sum that is not a number: what the row sees, and that only)
-#pragma unroll
-                for (int i = 0; i < 4 * TILES; ++i) sum[i] = w[i] == -__builtin_inff() ? sum[i] : __builtin_fmaf(__builtin_amdgcn_exp2f(w[i]), now.inv, sum[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4 * TILES; ++i) sum[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(w[i]), now.inv, sum[i]);
-            }
-            now = next;
+        for (int k = 0; k < NB; ++k) x.q[k] = __builtin_bit_cast(half8, ld_cached(q + k * 512));
+        x.stats = *reinterpret_cast<const float2*>(stats);
+        left -= WAVES;
+        token += token_step;
+        rest += rest_step;
+        if (rest >= group) {
+            rest -= group;
+            ++token;
         }
+        if (left > 0) {
+            q += 16 * WAVES * D;
+            stats += 2 * 16 * WAVES;
+        }
+    };
+    auto weigh = [&](const Rows& x) __attribute__((always_inline)) {
+        const Sight mine = sight_of(a, rq, x.token), low = sight_of(a, rq, __builtin_amdgcn_readfirstlane(x.token)), high = sight_of(a, rq, __builtin_amdgcn_readlane(x.token, 15));
+        floatx4 s[TILES];
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+#pragma unroll
+            for (int i = 0; i < TILES; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(keys[i][k], x.q[k], k == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[i], 0, 0, 0);
+        // (a sum that is not a number: a maximum that is not one, so that what the row sees becomes one, and that only)
+        const bool number = finite(x.stats.y);
+        const float m = number ? x.stats.x : __builtin_nanf(""), inv = x.token >= last ? 0.f : number ? x.stats.y * 512.0f : 1.0f;
+        float w[4 * TILES];
+#pragma unroll
+        for (int i = 0; i < 4 * TILES; ++i) w[i] = __builtin_fmaf(s[i >> 2][i & 3], a.scale2, -m);
+        const bool none = inv == 0.f;            // a row that is not there, or sees nothing
+        if (__builtin_amdgcn_ballot_w64(none) != 0ull || p0 + SPAN > low.end) {
+            const int seen = (none ? 0 : mine.end) - p0 - 4 * hi;
+#pragma unroll
+            for (int i = 0; i < 4 * TILES; ++i) w[i] = seen > 16 * (i >> 2) + (i & 3) ? w[i] : -__builtin_inff();
+        }
+        if (p0 < high.from && p0 + SPAN > a.sinks) {
+            const int hidden = a.sinks - p0 - 4 * hi, span = mine.from > a.sinks ? mine.from - a.sinks : 0;
+#pragma unroll
+            for (int i = 0; i < 4 * TILES; ++i) w[i] = (unsigned)(16 * (i >> 2) + (i & 3) - hidden) < (unsigned)span ? -__builtin_inff() : w[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4 * TILES; ++i) sum[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(w[i]), inv, sum[i]);
+    };
+    const int turns = there && first < last ? (tile_end - tile0 + WAVES - 1) / WAVES : 0;
+    if (turns > 0) {
+        Rows one, other;
+        ask(one);
+        int it = 0;
+        do {                                     // (two turns: no copies from one to the other, each of which would wait for the load)
+            ask(other);
+            __builtin_amdgcn_sched_barrier(0);
+            weigh(one);
+            __builtin_amdgcn_sched_barrier(0);
+            ask(one);
+            __builtin_amdgcn_sched_barrier(0);
+            weigh(other);                        // (of rows behind the last, in the end)
+            __builtin_amdgcn_sched_barrier(0);
+        } while ((it += 2) < turns);
     }
 #pragma unroll
     for (int i = 0; i < 4 * TILES; ++i) s_sum[wv][i][lane] = sum[i];
     __syncthreads();
-    if (tid >= 2 * KV16_PAGE) return;
+    if (tid >= SPAN) return;
     const int i = 4 * (tid >> 4) + (tid & 3), h = (tid >> 2) & 3;
     float total = 0.f;
 #pragma unroll
-    for (int w = 0; w < KW_WAVES; ++w)
+    for (int w = 0; w < WAVES; ++w)
 #pragma unroll
         for (int k = 0; k < 16; ++k) total += s_sum[w][i][16 * h + ((k + tid) & 15)];      // (each thread in an order of its own, the same every time; no two of a bank at once)
     const int pos = p0 + tid;
@@ -1081,8 +1117,11 @@ hipError_t launch(const Kv16AttnArgs& a, hipStream_t stream)
     const int combining = combine_blocks<D>(a), weighing = (a.max_pages * (KV16_PAGE / 4) + KC_THREADS - 1) / KC_THREADS;
     if (combining && !scores) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)combining, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
     if (scores) hipLaunchKernelGGL((kv16_attn_weigh<D>), dim3((unsigned)(weighing + (combining + a.Hkv - 1) / a.Hkv), (unsigned)a.Hkv, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a, weighing);
-    else if (a.weights_out)
-        hipLaunchKernelGGL((kv16_attn_weights<D>), dim3((unsigned)((a.max_pages + 1) / 2), (unsigned)a.Hkv, (unsigned)a.B), dim3(KW_THREADS), 0, stream, a);
+    else if (a.weights_out) {
+        const dim3 pages((unsigned)(a.max_pages * a.Hkv), (unsigned)a.B);
+        if ((long)a.max_pages * a.Hkv * a.B <= KW_PER_CU * a.num_cus) hipLaunchKernelGGL((kv16_attn_weights<D, 8>), pages, dim3(512), 0, stream, a);
+        else hipLaunchKernelGGL((kv16_attn_weights<D, 4>), pages, dim3(256), 0, stream, a);
+    }
     return hipGetLastError();
 }
 

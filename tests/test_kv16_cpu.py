@@ -54,6 +54,7 @@ def test_attention_refusals(lib):
     big = 1 << 40
     #       0  1  2  3  4  5    6  7  8  9  10 11 12 13 14 15   16 17 18 19 20   21
     good = [p, p, p, p, p, 0.1, 5, 1, p, p, p, 2, 5, 8, 2, 128, 4, 9, 3, p, big, None]
+    refused(lib.thi_kv16_attention, [*good[:18], (1 << 22) + 1, *good[19:]], [((10, p), SHAPE)])      # (of two cache heads, with weights)
     refused(lib.thi_kv16_attention, good, [
         ((0, None), NULL), ((1, None), NULL), ((2, None), NULL), ((3, None), NULL), ((8, None), NULL), ((10, None), NULL), ((19, None), NULL),
         ((6, -1), SHAPE), ((7, -1), SHAPE),
@@ -82,6 +83,7 @@ def test_sizes(lib):
     assert lib.thi_kv16_page_bytes(8, 96) == 0 and lib.thi_kv16_page_bytes(0, 64) == 0
     f = lib.thi_kv16_attention_workspace_bytes
     assert f(2, 2, 8, 2, 128, 1, 100, 0) > 0 and f(2, 2, 8, 2, 128, 1, 100, 0) % 256 == 0 and f(2, 2, 8, 2, 128, 1, 100, 1) > f(2, 2, 8, 2, 128, 1, 100, 0)
+    assert f(2, 2, 8, 8, 128, 1, 1 << 20, 1) > 0 and f(2, 2, 8, 8, 128, 1, (1 << 20) + 1, 1) == 0 and f(2, 2, 8, 8, 128, 1, (1 << 20) + 1, 0) > 0
     assert f(2, 2, 8, 3, 128, 1, 100, 0) == 0 and f(2, 2, 8, 2, 100, 1, 100, 0) == 0 and f(2, 2, 8, 2, 128, 3, 100, 0) == 0 and f(0, 2, 8, 2, 128, 1, 100, 0) == 0
     f = lib.thi_kv16_evict_workspace_bytes
     assert f(2, 4, 8, 10, 1000) >= 4 * 2 * 4 * 8 * 10 * 64 and f(2, 4, 8, 10, 0) == 0 and f(0, 4, 8, 10, 10) == 0 and f(256, 256, 8, 1, 1) == 0

@@ -262,6 +262,17 @@ def test_weights_add_to_what_was_there(thi):
         assert np.array_equal(got[written], want[written]) and np.array_equal(got[~written].astype(np.float32), before[~written])
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 70)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_weights_of_many_pages(thi, D, window, sinks):
+    """Weights of more rows than a tile where pages times cache heads are more than twice the compute units, and entries that are no page."""
+    c = attention_case(60 + D, 8, 8, D, [500, 64, 1, 0, 130, 20, 300, 65, 33], [150, 20, 1, 0, 17, 20, 40, 3, 33])
+    c["table"][0, [1, 6]] = [-1, 2 ** 31 - 1]
+    check_attention(thi, c, window, sinks, weights=True)
+    d = attention_case(61 + D, 24, 8, D, [500, 64, 1, 0, 130, 20, 300, 65, 33], [50, 20, 1, 0, 17, 20, 40, 3, 33])
+    check_attention(thi, d, window, sinks, weights=True)
+
+
 @pytest.mark.parametrize("new", [1, 4, 90])
 def test_missing_pages(thi, new):
     """Entries that are no page (-1, past the pool, negative) are positions that are not there: at the front, in the middle, at the end, all of them."""
