@@ -137,7 +137,7 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     kv16_plan(a, device_cu_count());
     const size_t stats = weights_out ? bytes_of_stats(B, Hq, Hkv, max_q) : 0, queries = weights_out ? bytes_of_queries(B, Hq, Hkv, D, max_q) : 0;
     const size_t scores = weights_out && a.few ? bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0;
-    if (workspace_bytes < need) return THI_ERR_WORKSPACE;
+    if (workspace_bytes < need || workspace_bytes < stats + queries + scores + bytes_of_rows(a.nsplit > 1 ? (size_t)B * max_q * Hq * a.nsplit : 0, D)) return THI_ERR_WORKSPACE;
     (void)hipGetLastError();
     a.q = (const uint16_t*)q;
     a.pages = (const uint16_t*)pages;
