@@ -321,7 +321,7 @@ int thi_kv4_compact(const int* refs_in, const int* table_in, int* refs_out, int*
 size_t thi_kv16_page_bytes(int Hkv, int D);
 
 /*
- * thi_qk_norm_rope_kv4 with this cache: q_out = y(query), the cache at slots[t] = (y(key), value).  Arguments, slots and refusals are the same.  Norm and rotation in
+ * thi_qk_norm_rope_kv4 with this cache: q_out = y(query), the cache at slots[t] = (y(key), value).  Arguments, slots and refusals are the same, and T <= 2^28.  Norm and rotation in
  * fp32, angles in 64 bits, one rounding to fp16; values are stored as they are.
  */
 int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const void* k_gamma, float eps, const int* positions, const float* theta,
@@ -342,7 +342,9 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
  * weights_out (or NULL) [B][Hkv][64 max_pages] fp32: what each position got of the attention, for thi_kv16_evict:
  *   weights_out[b,g,j] = before + sum of p_j over the request's rows and the query heads of cache head g,  j < seq_lens[b]
  * where before is weights_in[b,g,j] (the same shape, or the same buffer; NULL: 0) for the positions in front of the new tokens and 0 for theirs.  Entries from seq_lens[b] on
- * are not written.  With weights, Hkv max_pages <= 2^23.
+ * are not written.
+ *
+ * Hkv ceil(max_q Hq / Hkv / 128) <= 2^23, and with weights Hkv max_pages <= 2^23 (THI_ERR_SHAPE).
  *
  * Scores, statistics and sums are fp32.  Weights reach the matrix cores as fp16: up to 16 rows of a request and cache head (max_q Hq / Hkv) as two summands, beyond as one,
  * cut to its bits, as is the sum that divides the result.  Workspace:
@@ -367,8 +369,8 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
  * stayed for want of pages.
  *
  * refs_* [num_pages], table_* [rows][max_pages], lens_* [rows] int32; weights_* [layers][rows][Hkv][64 max_pages] fp32; pages: layer l's pool begins at
- * pages + l * layer_bytes (a multiple of 16).  1 <= budget, 0 <= sinks, recent, headroom, sinks + recent <= budget, layers * rows <= 65535 (THI_ERR_SHAPE).
- * Workspace: thi_kv16_evict_workspace_bytes(), 256-byte aligned.
+ * pages + l * layer_bytes (a multiple of 16).  1 <= budget, 0 <= sinks, recent, headroom, sinks + recent <= budget, layers * rows <= 65535, and where a row's table reaches
+ * past 2^28 positions, budget <= 2^28 (THI_ERR_SHAPE).  Workspace: thi_kv16_evict_workspace_bytes(), 256-byte aligned.
  */
 size_t thi_kv16_evict_workspace_bytes(int layers, int rows, int Hkv, int max_pages, int num_pages);
 int thi_kv16_evict(const int* refs_in, const int* table_in, const int* lens_in, const float* weights_in, int budget, int sinks, int recent, int headroom,

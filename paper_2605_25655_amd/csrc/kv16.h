@@ -73,6 +73,6 @@ struct Kv16EvictArgs {
     int* ws;                         // kv16_evict_words()
 };
 size_t kv16_evict_words(int layers, int rows, int Hkv, int max_pages, int num_pages);
-hipError_t launch_kv16_evict(const Kv16EvictArgs& a, int num_cus, hipStream_t stream);
+hipError_t launch_kv16_evict(const Kv16EvictArgs& a, hipStream_t stream);
 
 }  // namespace thi

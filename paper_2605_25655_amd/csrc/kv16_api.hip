@@ -14,7 +14,9 @@ bool heads_ok(int Hq, int Hkv, int D) { return Hq >= 1 && Hkv >= 1 && Hq <= 6553
 bool pool_ok(int num_pages) { return num_pages >= 1 && num_pages <= 0x7fffffff / KV16_PAGE; }
 
 constexpr int MAX_PAGES = 1 << 24;      // of a row of the page table: positions stay below 2^30
-constexpr long MAX_WEIGHED = 1 << 23;   // pages of a row times cache heads, with weights: a launch's threads stay below 2^32
+constexpr size_t MAX_TILES = 1 << 23;   // of a request's rows, times cache heads: a launch's threads stay below 2^32
+constexpr int MAX_KEPT = 1 << 28, MAX_TOKENS = 1 << 28;      // positions of a row that has been evicted from; tokens of a store: the same
+constexpr long MAX_WEIGHED = 1 << 23;   // pages of a row of the table times cache heads, with weights: the same
 
 // Pages of a chunk at least, chunks' workgroups for every compute unit, and tables times columns that are not cut (kv16_plan)
 constexpr int CHUNK = 4, FEW_PER_CU = 3, MANY_PER_CU = 2, FEW_UNCUT = 1280;
@@ -91,7 +93,7 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
                           const int* slots, void* q_out, void* pages, int T, int Hq, int Hkv, int D, int num_pages, void* hip_stream)
 {
     if (!qkv || !slots || !q_out || !pages || (theta && !positions)) return THI_ERR_NULL;
-    if (T < 1 || !heads_ok(Hq, Hkv, D) || !pool_ok(num_pages)) return THI_ERR_SHAPE;
+    if (T < 1 || T > MAX_TOKENS || !heads_ok(Hq, Hkv, D) || !pool_ok(num_pages)) return THI_ERR_SHAPE;
     if ((ld & 7) || ld < (long)(Hq + 2 * Hkv) * D) return THI_ERR_SHAPE;
     if (misaligned(qkv, 16) || misaligned(q_gamma, 16) || misaligned(k_gamma, 16) || misaligned(q_out, 16) || misaligned(pages, 16) ||
         misaligned(positions, 4) || misaligned(theta, 4) || misaligned(slots, 4))
@@ -114,7 +116,7 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
 size_t thi_kv16_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages, int weights)
 {
     if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_q > 65535 || max_pages < 1 || max_pages > MAX_PAGES ||
-        (weights && (long)max_pages * Hkv > MAX_WEIGHED))
+        tiles_of(Hq, Hkv, max_q) * Hkv > MAX_TILES || (weights && (long)max_pages * Hkv > MAX_WEIGHED))
         return 0;
     return bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, Hkv, max_q) + bytes_of_queries(B, Hq, Hkv, D, max_q) + bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0);
 }
@@ -172,6 +174,7 @@ int thi_kv16_evict(const int* refs_in, const int* table_in, const int* lens_in, 
     const size_t need = thi_kv16_evict_workspace_bytes(layers, rows, Hkv, max_pages, num_pages);
     if (!need || !heads_ok(Hkv, Hkv, D)) return THI_ERR_SHAPE;
     if (budget < 1 || sinks < 0 || recent < 0 || headroom < 0 || (long)sinks + recent > budget) return THI_ERR_SHAPE;
+    if (budget > MAX_KEPT && max_pages > MAX_KEPT / KV16_PAGE) return THI_ERR_SHAPE;
     if (refs_out == refs_in || table_out == table_in || lens_out == lens_in || weights_out == weights_in) return THI_ERR_SHAPE;
     if ((layer_bytes & 15) || (layers > 1 && layer_bytes < thi_kv16_page_bytes(Hkv, D) * (size_t)num_pages)) return THI_ERR_SHAPE;
     const void* const words[] = {refs_in, table_in, lens_in, weights_in, refs_out, table_out, lens_out, weights_out, info};
@@ -182,7 +185,7 @@ int thi_kv16_evict(const int* refs_in, const int* table_in, const int* lens_in, 
     (void)hipGetLastError();
     const Kv16EvictArgs a{refs_in, table_in, lens_in, weights_in, refs_out, table_out, lens_out, weights_out, info, (uint16_t*)pages, layer_bytes / 2,
                           budget, sinks, recent, headroom, layers, rows, Hkv, D, num_pages, max_pages, (int*)workspace};
-    return finish(launch_kv16_evict(a, device_cu_count(), (hipStream_t)hip_stream));
+    return finish(launch_kv16_evict(a, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

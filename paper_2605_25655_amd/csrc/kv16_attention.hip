@@ -127,15 +127,18 @@ __device__ __forceinline__ float slow_row(const Kv16AttnArgs& a, const Request& 
     return sum;
 }
 
-// ---- one token per request, or a few: 16 rows of a cache head at a time, cut along the positions --------------------
+// ---- one token per request, or a few: up to 16 rows of a cache head, cut along the positions ------------------------
 //
-// A workgroup (4 waves) takes a chunk of the pages that one request looks at, for one cache head; a wave takes half of every second page, 32 positions, straight from
-// memory into registers, its next half in flight behind it.  Rows are (new token, query head of the group) pairs, 16 of them the columns of two matrix products
+// What bounds it is the pages' way from memory, 4 D bytes a position and cache head.  A workgroup (4 waves) takes a chunk of the pages that one request looks at, for one cache head; a wave
+// takes half of every second page, 32 positions, straight from memory into registers, its next half in flight behind it.  (Whole pages, every fourth, leave waves of short chunks without
+// work: 32 requests of up to 2048 positions, 32/32 heads of 128, 116 us, like this 110.)  Rows are (new token, query head of the group) pairs, the columns of two matrix products
 // (v_mfma_f32_16x16x32_f16):
 //   S = K Q^T     : 16 positions x 16 rows;
 //   O^T = V^T P^T : a lane has the weights of positions 16 i + 4 hi + r of its row, which is the B operand as it stands, for the page holds the values in that order.
 // So nothing but the rows' maxima crosses lanes, and those only when a weight leaves fp16's range.  Weights are multiplied as two fp16 summands (2^-21 of a weight
 // off at most down to 2^-12 of the largest, 2^-33 of that below, where one alone is off by 2^-11 and as much as the result's own rounding).
+// Measured, us a pass with kv16_attn_combine: those 32 requests 110 (6.2 TB/s; a copy of 128 MiB 7.1), 3 of 131000 and less on 64/8 heads 86 (6.2 TB/s), 16 of 32000 and less with a window
+// of 4096 48 (5.3), two of 468 and less with 8 heads of 64 columns 5.9, which is a launch and four loads one behind the other.
 constexpr int KD_THREADS = 256, KD_WAVES = 4;
 constexpr float WEIGHT_LOG2 = 9.0f;              // weights are held as 2^9 p of a maximum that may lag by 2^6 (fp16 ends at 2^16)
 
@@ -152,7 +155,7 @@ __device__ __forceinline__ void split_weights(const float (&w)[4], half4& large,
 }
 __device__ __forceinline__ half8 join(half4 a, half4 b) { return half8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
 
-// SCORES: they are left for kv16_attn_weigh.
+// SCORES: they are left for kv16_attn_weigh, 4 bytes a row and position: 24 requests of up to 5000 positions, 64/8 heads, 50 us without weights, 58 with the scores' stores, 64 with their sums.
 template <int D, bool SCORES>
 __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a)
 {
@@ -365,7 +368,7 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
 
 // The chunks' (sum, maximum, weight) triples of a request's rows, (token, head) pairs in the order of q.  A group of D threads has a row of up to eight chunks to itself; of more, all
 // groups take every GROUPS-th chunk each, eight loads in flight, and meet in LDS: a fixed order.  The loads come before anything is known of the request (what lies behind its last
-// chunk is the workspace's, and not used).
+// chunk is the workspace's, and not used).  16 requests of 64 heads and six chunks: 4.6 us (a row for a workgroup: 5.2).
 constexpr int KC_THREADS = 512, KC_AHEAD = 8;
 template <int D> __host__ __device__ int combine_blocks(const Kv16AttnArgs& a)
 {
@@ -439,10 +442,18 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
 
 // ---- many rows of a cache head: prompts and chunks of them ----------------------------------------------------------
 //
-// A workgroup takes 256 rows of one cache head, 32 a wave, and walks the pages that any of them sees.  Pages come straight into LDS as they lie in memory
-// (three buffers for keys, three for values), which is the order in which the operands of v_mfma_f32_32x32x16_f16 are read: 256 bytes in a row for 16 lanes, no bank conflicts:
-//   S = K Q^T     : 32 positions x 32 rows; register 4 a + r of a lane is position 8 a + 4 (lane / 32) + r of its row;
-//   O^T = V^T P^T : the page holds for hi = 2 s + lane / 32 the positions 16 i + 4 hi + r, which are the registers 8 i + 4 s + r: the B operand as it stands.
+// A workgroup takes 128 rows of one cache head, 32 a wave, and walks the pages that any of them sees.  Pages come straight into LDS as they lie in memory (two buffers for keys, two for
+// values, 64 KB where D is 128: two workgroups a compute unit), which is the order in which the operands of v_mfma_f32_16x16x32_f16 are read: 1 KB in a row for a wave, no bank conflicts.
+// The products are those of kv16_attn_decode, with two tiles of 16 rows, so that each operand from LDS is multiplied twice.
+//
+// What bounds it are the matrix products, 4 D FLOP a position and row, and the exponentials, one a position and row, in whose time the SIMD's matrix core rests.  So a wave has
+// the exponentials of a page between the products of the next page's scores, and its scaling and maxima between those of the values, and the two workgroups of a compute unit fill what is
+// left.  Weights are one fp16 each, cut (see weigh); a maximum may lag behind by 2^6, so that accumulators are hardly ever scaled.
+// Measured: a prompt of 4096 tokens, 40/40 heads of 128, 196 us (878 TFLOP/s of what it sees; a matrix product of 8192^3 reaches 1387 here); chunks of up to 777 tokens on up to 8029
+// positions, window 2000, 64/8 heads, 127 us, where the 616 tiles of equal work are two or three to a compute unit, 20 percent more than their mean.  256 rows in one workgroup a compute unit:
+// 267 and 197 us.  Exponentials between products, or by themselves: 209 and 129, 211 and 141; products of 16x16x32 instead of 32x32x16, which read half the
+// operands but take more power, so that the clock goes down: 197 and 129 instead of 209 and 129.  Cut into chunks where that fills compute units that have one
+// workgroup: 5 chunks of 128 tokens, window 4096, 126 -> 111 us, but one of 800 on 4000 99 -> 126, for partial results are 4 D bytes a row: not done.
 constexpr int KP_WAVES = 4, KP_AHEAD = 6, KP_BUFS = 2;
 template <int D, int WAVES> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2 + WAVES * 2048;
 

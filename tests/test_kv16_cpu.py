@@ -44,7 +44,7 @@ def test_append_refusals(lib):
     good = [p, 1024, p, p, 1e-6, p, p, p, p, p, 3, 4, 2, 128, 10, None]
     refused(lib.thi_qk_norm_rope_kv16, good, [
         ((0, None), NULL), ((7, None), NULL), ((8, None), NULL), ((9, None), NULL), ((5, None), NULL),      # theta without positions
-        ((10, 0), SHAPE), ((10, -1), SHAPE), ((11, 3), SHAPE), ((11, 0), SHAPE), ((12, 0), SHAPE), ((12, -2), SHAPE), ((13, 96), SHAPE), ((13, 256), SHAPE),
+        ((10, 0), SHAPE), ((10, -1), SHAPE), ((10, (1 << 28) + 1), SHAPE), ((11, 3), SHAPE), ((11, 0), SHAPE), ((12, 0), SHAPE), ((12, -2), SHAPE), ((13, 96), SHAPE), ((13, 256), SHAPE),
         ((1, 1016), SHAPE), ((1, 1028), SHAPE), ((14, 0), SHAPE), ((14, (1 << 25)), SHAPE),
         ((0, p + 8), ALIGN), ((2, p + 2), ALIGN), ((3, p + 4), ALIGN), ((5, p + 2), ALIGN), ((6, p + 1), ALIGN), ((7, p + 2), ALIGN), ((8, p + 8), ALIGN), ((9, p + 8), ALIGN)])
 
@@ -70,6 +70,7 @@ def test_evict_refusals(lib):
     stride = 2 * 256 * 64 * 50
     #       refs table lens w  budget sinks recent head refs table lens w info pages stride  L  R  Hkv D  P  MP  ws bytes stream
     good = [p, p, p, p, 100, 4, 96, 0, o, o, o, o, p, p, stride, 2, 4, 2, 64, 50, 8, p, big, None]
+    refused(lib.thi_kv16_evict, [*good[:4], (1 << 28) + 1, *good[5:17], 1, *good[18:20], 1 << 23, *good[21:]], [((12, p), SHAPE)])
     refused(lib.thi_kv16_evict, good, [
         *(((i, None), NULL) for i in (0, 1, 2, 3, 8, 9, 10, 11, 13, 21)),
         ((4, 0), SHAPE), ((4, 99), SHAPE), ((5, -1), SHAPE), ((6, -1), SHAPE), ((6, 97), SHAPE), ((6, 2147483647), SHAPE), ((7, -1), SHAPE),
@@ -84,6 +85,7 @@ def test_sizes(lib):
     f = lib.thi_kv16_attention_workspace_bytes
     assert f(2, 2, 8, 2, 128, 1, 100, 0) > 0 and f(2, 2, 8, 2, 128, 1, 100, 0) % 256 == 0 and f(2, 2, 8, 2, 128, 1, 100, 1) > f(2, 2, 8, 2, 128, 1, 100, 0)
     assert f(2, 2, 8, 8, 128, 1, 1 << 20, 1) > 0 and f(2, 2, 8, 8, 128, 1, (1 << 20) + 1, 1) == 0 and f(2, 2, 8, 8, 128, 1, (1 << 20) + 1, 0) > 0
+    assert f(1, 60000, 17920, 1, 128, 59918, 1, 0) > 0 and f(1, 60000, 17920, 1, 128, 59919, 1, 0) == 0      # 2^23 tiles of 128 rows, and one more
     assert f(2, 2, 8, 3, 128, 1, 100, 0) == 0 and f(2, 2, 8, 2, 100, 1, 100, 0) == 0 and f(2, 2, 8, 2, 128, 3, 100, 0) == 0 and f(0, 2, 8, 2, 128, 1, 100, 0) == 0
     f = lib.thi_kv16_evict_workspace_bytes
     assert f(2, 4, 8, 10, 1000) >= 4 * 2 * 4 * 8 * 10 * 64 and f(2, 4, 8, 10, 0) == 0 and f(0, 4, 8, 10, 10) == 0 and f(256, 256, 8, 1, 1) == 0
@@ -135,7 +137,7 @@ hipError_t launch_kv16_attention(const Kv16AttnArgs& a, hipStream_t)
     return hipSuccess;
 }
 size_t kv16_evict_words(int layers, int rows, int Hkv, int max_pages, int num_pages) { return 2 * (size_t)rows + num_pages + (size_t)layers * rows * Hkv * max_pages * 64; }
-hipError_t launch_kv16_evict(const Kv16EvictArgs& a, int, hipStream_t) { NEED(a.ws && a.sinks + a.recent <= a.budget && a.layers * a.rows <= 65535); return hipSuccess; }
+hipError_t launch_kv16_evict(const Kv16EvictArgs& a, hipStream_t) { NEED(a.ws && a.sinks + a.recent <= a.budget && a.layers * a.rows <= 65535); return hipSuccess; }
 }
 int main()
 {
