@@ -46,11 +46,12 @@ struct Kv16AttnArgs {
     int B, T, Hq, Hkv, D, max_q, num_pages, max_pages;
     int group;                       // Hq / Hkv query heads per cache head
     // how the rows are dealt (kv16_plan)
-    float* part;                     // [B][max_q][Hq][nsplit][kv16_part(D)]: a chunk's unnormalised output, maximum, sum of the weights as they were multiplied, and as they are
+    enum Whose { EVERYONES, THOSE_OF_FEW_ROWS, THOSE_OF_MORE } whose;      // requests of this launch
+    int part_q;                      // the most tokens of one of them
+    float* part;                     // [B][part_q][Hq][nsplit][kv16_part(D)]: a chunk's unnormalised output, maximum, sum of the weights as they were multiplied, and as they are
     float* stats;                    // [B][Hkv][tiles KV16_TILE_ROWS][2]: a row's maximum and one over its sum, with weights_out
-    uint16_t* queries;               // [B][Hkv][tiles KV16_TILE_ROWS / 16][D / 32][64][8]: queries as matrix operands, with weights_out, for more rows than few
-    float* scores;                   // [B][Hkv][16 max_pages][max_q group][4]: four positions' scores in powers of two, with weights_out, for few rows
-    bool few;                        // all rows of a request and cache head at once, at most KV16_FEW_ROWS
+    uint16_t* queries;               // [B][Hkv][tiles KV16_TILE_ROWS / 16][D / 32][64][8]: queries as matrix operands, with weights_out, unless there are scores
+    float* scores;                   // [B][Hkv][max_q group][64 max_pages]: scores in powers of two, with weights_out, if nobody has more rows than few
     int tiles;                       // of KV16_TILE_ROWS rows
     int nsplit, min_chunk;           // chunks per request at most, pages per chunk at least
     int num_cus;
@@ -58,8 +59,8 @@ struct Kv16AttnArgs {
 constexpr int KV16_MAX_SPLIT = 64;
 constexpr int KV16_FEW_ROWS = 16, KV16_TILE_ROWS = 128;
 constexpr int kv16_part(int D) { return D + 4; }
-void kv16_plan(Kv16AttnArgs& a, int num_cus);
-hipError_t launch_kv16_attention(const Kv16AttnArgs& a, hipStream_t stream);
+// few: requests of up to KV16_FEW_ROWS rows of a cache head, many: more; nullptr: nobody
+hipError_t launch_kv16_attention(const Kv16AttnArgs* few, const Kv16AttnArgs* many, hipStream_t stream);
 
 struct Kv16EvictArgs {
     const int *refs_in, *table_in, *lens_in;

@@ -18,13 +18,13 @@ constexpr size_t MAX_TILES = 1 << 23;   // of a request's rows, times cache head
 constexpr int MAX_KEPT = 1 << 28, MAX_TOKENS = 1 << 28;      // positions of a row that has been evicted from; tokens of a store: the same
 constexpr long MAX_WEIGHED = 1 << 23;   // pages of a row of the table times cache heads, with weights: the same
 
-// Pages of a chunk at least, chunks' workgroups for every compute unit, and tables times columns that are not cut (kv16_plan)
-constexpr int CHUNK = 4, FEW_PER_CU = 3, MANY_PER_CU = 2, FEW_UNCUT = 1280;
+// Pages of a chunk at least, chunks' workgroups for every compute unit, and tables times columns that are not cut (plan)
+constexpr int CHUNK = 4, FEW_PER_CU = 3, MANY_PER_CU = 2, FEW_UNCUT = 1280, APART = 72;
 
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
-// The most rows of partial results that a call of up to B requests, max_q rows and max_pages pages has.  Where kv16_plan cuts, the chunks are at most FEW_PER_CU (MANY_PER_CU)
-// workgroups of 16 (256) rows for every compute unit, so no batch has more rows than these hold; and no more than its own times the chunks of the longest table.
+// The most rows of partial results that a call of up to B requests, max_q rows and max_pages pages has.  Where plan() cuts, the chunks are at most FEW_PER_CU (MANY_PER_CU)
+// workgroups of KV16_FEW_ROWS (KV16_TILE_ROWS) rows for every compute unit, so no batch has more rows than these hold; and no more than its own times the chunks of the longest table.
 size_t most_rows(int B, int Hq, int Hkv, int max_q, int max_pages, int num_cus)
 {
     auto at_most = [&](long q, long held) {
@@ -51,10 +51,6 @@ size_t bytes_of_scores(int B, int Hq, int Hkv, int max_q, int max_pages)
     return round_up((size_t)B * q * Hq * max_pages * KV16_PAGE * sizeof(float));
 }
 
-int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
-
-}  // namespace
-
 // How the rows are dealt: up to KV16_FEW_ROWS of a request and cache head to kv16_attn_decode, more, KV16_TILE_ROWS at a time, to kv16_attn_prompt; and where that gives fewer
 // workgroups than the compute units hold, requests are cut into chunks of at least CHUNK pages, whose results one more launch puts together.
 // Measured, us a pass (requests of up to that many positions each; 64/8: query heads / cache heads of 128 columns):
@@ -68,19 +64,33 @@ int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 //     columns, 8 x 2000: 14.3 12.5 12.3
 //   not cut, cut: 2 x 468 of 8 heads of 64 columns: 6.8 9.9; 2 x 1200 of these: 9.1 10.0; 2 x 1500 of these (past FEW_UNCUT): 10.4 8.5; 4 x 600 of 32/32: 10.3 13.1; 2 x 600 of 64/8: 10.5 11.6;
 //     2 x 760 of 64/8 (past it): 11.4 10.8
-void thi::kv16_plan(Kv16AttnArgs& a, int num_cus)
+void plan(Kv16AttnArgs& a, bool few, int num_cus)
 {
     a.group = a.Hq / a.Hkv;
-    a.few = (long)a.max_q * a.group <= KV16_FEW_ROWS;
-    a.tiles = (int)(((long)a.max_q * a.group + KV16_TILE_ROWS - 1) / KV16_TILE_ROWS);
-    const long items = (long)a.B * a.Hkv * a.tiles;
-    const long most = a.few && (long)a.max_pages * a.D <= FEW_UNCUT ? 1 : (a.max_pages + CHUNK - 1) / CHUNK;
+    a.tiles = (int)tiles_of(a.Hq, a.Hkv, a.max_q);
+    a.part_q = few && KV16_FEW_ROWS / a.group < a.max_q ? KV16_FEW_ROWS / a.group : a.max_q;
+    const long items = (long)a.B * a.Hkv * (few ? 1 : a.tiles);
+    const long most = few && (long)a.max_pages * a.D <= FEW_UNCUT ? 1 : (a.max_pages + CHUNK - 1) / CHUNK;
     a.min_chunk = CHUNK;
-    long n = (long)(a.few ? FEW_PER_CU : MANY_PER_CU) * num_cus / items;
+    long n = (long)(few ? FEW_PER_CU : MANY_PER_CU) * num_cus / items;
     n = n < 1 ? 1 : n > KV16_MAX_SPLIT ? KV16_MAX_SPLIT : n;
     a.nsplit = (int)(n > most ? most : n);
     a.num_cus = num_cus;
 }
+size_t rows_of(const Kv16AttnArgs& a) { return a.nsplit > 1 ? (size_t)a.B * a.part_q * a.Hq * a.nsplit : 0; }
+// Are requests of few rows in a call of more dealt as if they were alone?  Some has to be there, by the number of tokens, and what a row sees has to be APART pages at least, for a tile of
+// one row walks them as one of 128 does.  With all dealt alike / apart, us a pass, 512 new tokens and single ones (64/8 heads of 128 where nothing is said): 8000 positions and 3 x 131000:
+// 2232 / 408; 8000 and 3 x 30000: 563 / 223; 5 x 8000: 202 / 194; 33 x 8000: 524 / 331; 33 x 30000, 4000 seen: 308 / 190; 17 x 8000 of 32/32: 460 / 472; below APART 5 x 4000: 107 / 115;
+// 17 x 4000 of 32/32: 235 / 249; 9 x 2000: 57 / 74; 9 x 2000 of 32/32: 65 / 104.
+bool apart(const Kv16AttnArgs& a)
+{
+    const long q_few = KV16_FEW_ROWS / a.group, seen = a.window ? ((long)a.window + a.sinks + a.max_q) / KV16_PAGE + 3 : a.max_pages;
+    return q_few > 0 && a.T <= (a.B - 1L) * a.max_q + q_few && (seen < a.max_pages ? seen : a.max_pages) >= APART;
+}
+
+int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
+
+}  // namespace
 
 extern "C" {
 
@@ -132,15 +142,13 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     if (misaligned(q, 16) || misaligned(pages, 16) || misaligned(out, 16) || misaligned(page_table, 4) || misaligned(seq_lens, 4) ||
         misaligned(q_offsets, 4) || misaligned(weights_in, 4) || misaligned(weights_out, 4) || misaligned(workspace, 256))
         return THI_ERR_ALIGN;
+    const bool few = (long)max_q * (Hq / Hkv) <= KV16_FEW_ROWS;
+    const size_t stats = weights_out ? bytes_of_stats(B, Hq, Hkv, max_q) : 0, queries = weights_out ? bytes_of_queries(B, Hq, Hkv, D, max_q) : 0;
+    const size_t scores = weights_out && few ? bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0;
     Kv16AttnArgs a{};
     a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.max_q = max_q; a.num_pages = num_pages; a.max_pages = max_pages;
     a.window = window;
     a.sinks = window ? sinks : 0;
-    kv16_plan(a, device_cu_count());
-    const size_t stats = weights_out ? bytes_of_stats(B, Hq, Hkv, max_q) : 0, queries = weights_out ? bytes_of_queries(B, Hq, Hkv, D, max_q) : 0;
-    const size_t scores = weights_out && a.few ? bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0;
-    if (workspace_bytes < need || workspace_bytes < stats + queries + scores + bytes_of_rows(a.nsplit > 1 ? (size_t)B * max_q * Hq * a.nsplit : 0, D)) return THI_ERR_WORKSPACE;
-    (void)hipGetLastError();
     a.q = (const uint16_t*)q;
     a.pages = (const uint16_t*)pages;
     a.page_table = page_table;
@@ -155,7 +163,19 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     a.queries = queries ? (uint16_t*)((char*)workspace + stats) : nullptr;
     a.scores = scores ? (float*)((char*)workspace + stats) : nullptr;
     a.part = (float*)((char*)workspace + stats + queries + scores);
-    return finish(launch_kv16_attention(a, (hipStream_t)hip_stream));
+    plan(a, few, device_cu_count());
+    size_t rows = rows_of(a);
+    Kv16AttnArgs other = a;                      // of requests of few rows in a call of more; their partial results are put together before the others' are there
+    const bool both = !few && apart(a);
+    if (both) {
+        plan(other, true, a.num_cus);
+        other.whose = Kv16AttnArgs::THOSE_OF_FEW_ROWS;
+        a.whose = Kv16AttnArgs::THOSE_OF_MORE;
+        rows = rows_of(other) > rows ? rows_of(other) : rows;
+    }
+    if (workspace_bytes < need || workspace_bytes < stats + queries + scores + bytes_of_rows(rows, D)) return THI_ERR_WORKSPACE;
+    (void)hipGetLastError();
+    return finish(launch_kv16_attention(few ? &a : both ? &other : nullptr, few ? nullptr : &a, (hipStream_t)hip_stream));
 }
 
 size_t thi_kv16_evict_workspace_bytes(int layers, int rows, int Hkv, int max_pages, int num_pages)

@@ -44,6 +44,8 @@ __device__ __forceinline__ Request find_request(const Kv16AttnArgs& a, int b)
     }
     return r;
 }
+// Is it this launch's?
+__device__ __forceinline__ bool ours(const Kv16AttnArgs& a, const Request& r) { return a.whose == Kv16AttnArgs::EVERYONES || (r.n * a.group <= KV16_FEW_ROWS) == (a.whose == Kv16AttnArgs::THOSE_OF_FEW_ROWS); }
 __device__ __forceinline__ int page_number(const Request& r, int v) { return v < r.lead ? v : v + r.skip; }
 
 // What a row sees: positions below `end`, from `from` on or below the sinks.
@@ -69,7 +71,7 @@ __device__ __forceinline__ int chunk_pages(const Kv16AttnArgs& a, int pages)
 // take what the largest request asks for and not what all tokens of the call do.
 __device__ __forceinline__ size_t part_row(const Kv16AttnArgs& a, int b, int r, int g, int group)
 {
-    return ((size_t)b * a.max_q + r / group) * a.Hq + (size_t)g * group + r % group;
+    return ((size_t)b * a.part_q + r / group) * a.Hq + (size_t)g * group + r % group;
 }
 
 // The same by cache head, for what kv16_attn_weights and kv16_attn_weigh read.
@@ -171,7 +173,7 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
     const int g = blockIdx.x, b = blockIdx.y, chunk = blockIdx.z;
     const Request rq = find_request(a, b);
     const int rows = rq.n * group;               // at most 16: row r is token r / group, head r % group
-    if (rows <= 0) return;
+    if (rows <= 0 || !ours(a, rq)) return;
     const int size = chunk_pages(a, rq.pages);
     const int c0 = chunk * size, c1 = c0 + size < rq.pages ? c0 + size : rq.pages;
     if (chunk > 0 && c0 >= rq.pages) return;
@@ -183,6 +185,9 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
     half8 queries[NB];
 #pragma unroll
     for (int k = 0; k < NB; ++k) queries[k] = __builtin_bit_cast(half8, ld_cached(a.q + row_of_column(col) * D + k * 32 + hi * 8));
+    if (a.queries && chunk == 0 && wv == 0)      // as operands, for kv16_attn_weights
+#pragma unroll
+        for (int k = 0; k < NB; ++k) *reinterpret_cast<half8*>(a.queries + (stats_row(a, b, g, 0) / 16 * NB + k) * 512 + lane * 8) = queries[k];
     const Sight mine = sight_of(a, rq, col / group);
     const Sight low = sight_of(a, rq, 0), high = sight_of(a, rq, rq.n - 1);
 
@@ -372,7 +377,7 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
 constexpr int KC_THREADS = 512, KC_AHEAD = 8;
 template <int D> __host__ __device__ int combine_blocks(const Kv16AttnArgs& a)
 {
-    const int rows = a.Hq * a.max_q, each = a.nsplit <= KC_AHEAD ? KC_THREADS / D : 1;
+    const int rows = a.Hq * a.part_q, each = a.nsplit <= KC_AHEAD ? KC_THREADS / D : 1;
     return a.nsplit > 1 ? (rows + each - 1) / each : 0;
 }
 template <int D>
@@ -384,9 +389,9 @@ __device__ __forceinline__ void combine_rows(const Kv16AttnArgs& a, int block, i
     const bool alone = a.nsplit <= KC_AHEAD;
     if (block >= combine_blocks<D>(a)) return;
     const int row = alone ? block * GROUPS + grp : block, chunk = alone ? 0 : grp, stride = alone ? 1 : GROUPS, own = alone ? grp : 0;
-    const bool exists = row < a.max_q * a.Hq;
+    const bool exists = row < a.part_q * a.Hq;
     const int i = row / a.Hq;
-    const float* const first = a.part + ((size_t)b * a.max_q * a.Hq + (exists ? row : 0)) * a.nsplit * kv16_part(D);
+    const float* const first = a.part + ((size_t)b * a.part_q * a.Hq + (exists ? row : 0)) * a.nsplit * kv16_part(D);
     float m = lane < a.nsplit ? first[(size_t)lane * kv16_part(D) + D] : 0.f;
     float w = lane < a.nsplit ? first[(size_t)lane * kv16_part(D) + D + 1] : 0.f;
     float v[KC_AHEAD];
@@ -394,7 +399,7 @@ __device__ __forceinline__ void combine_rows(const Kv16AttnArgs& a, int block, i
     for (int k = 0; k < KC_AHEAD; ++k) v[k] = chunk + k * stride < a.nsplit ? first[(size_t)(chunk + k * stride) * kv16_part(D) + d] : 0.f;
     const Request rq = find_request(a, b);
     const int size = chunk_pages(a, rq.pages), live = (rq.pages + size - 1) / size;
-    const bool cut = exists && i < rq.n && rq.pages > size;      // (one chunk: the first pass has written this output)
+    const bool cut = exists && i < rq.n && rq.pages > size && ours(a, rq);      // (one chunk: the first pass has written this output)
     m = lane < live ? m : -__builtin_inff();
     w = lane < live ? w : 0.f;
     float top = m;
@@ -517,7 +522,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     const Tile tile = find_tile<WAVES>(a);
     const Request& rq = tile.rq;
     const int r0 = tile.r0, all_rows = tile.all_rows, c0 = tile.c0, c1 = tile.c1;
-    if (r0 >= all_rows || (tile.chunk > 0 && c0 >= rq.pages)) return;
+    if (r0 >= all_rows || !ours(a, rq) || (tile.chunk > 0 && c0 >= rq.pages)) return;
     if (tid == 0) s_tile = tile;                 // (for the end)
 
     // The lane's two rows, w0 + lo and 16 further on (rows that are not there: the last one), and what they see.
@@ -1117,30 +1122,47 @@ void launch_prompt(const Kv16AttnArgs& a, dim3 grid, hipStream_t stream)
 }
 
 template <int D>
-hipError_t launch(const Kv16AttnArgs& a, hipStream_t stream)
+void launch_few(const Kv16AttnArgs& a, hipStream_t stream)
+{
+    const dim3 grid((unsigned)a.Hkv, (unsigned)a.B, (unsigned)a.nsplit);
+    const int combining = combine_blocks<D>(a), weighing = (a.max_pages * (KV16_PAGE / 4) + KC_THREADS - 1) / KC_THREADS;
+    if (a.scores) {
+        hipLaunchKernelGGL((kv16_attn_decode<D, true>), grid, dim3(KD_THREADS), 0, stream, a);
+        hipLaunchKernelGGL((kv16_attn_weigh<D>), dim3((unsigned)(weighing + (combining + a.Hkv - 1) / a.Hkv), (unsigned)a.Hkv, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a, weighing);
+        return;
+    }
+    hipLaunchKernelGGL((kv16_attn_decode<D, false>), grid, dim3(KD_THREADS), 0, stream, a);
+    if (combining) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)combining, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
+}
+
+template <int D>
+void launch_many(const Kv16AttnArgs& a, hipStream_t stream)
 {
     const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.B, (unsigned)a.nsplit);
-    const bool scores = a.few && a.weights_out;
-    if (scores) hipLaunchKernelGGL((kv16_attn_decode<D, true>), grid, dim3(KD_THREADS), 0, stream, a);
-    else if (a.few) hipLaunchKernelGGL((kv16_attn_decode<D, false>), grid, dim3(KD_THREADS), 0, stream, a);
-    else if (a.weights_out) launch_prompt<D, true>(a, grid, stream);
+    const int combining = combine_blocks<D>(a);
+    if (a.weights_out) launch_prompt<D, true>(a, grid, stream);
     else launch_prompt<D, false>(a, grid, stream);
-    const int combining = combine_blocks<D>(a), weighing = (a.max_pages * (KV16_PAGE / 4) + KC_THREADS - 1) / KC_THREADS;
-    if (combining && !scores) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)combining, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
-    if (scores) hipLaunchKernelGGL((kv16_attn_weigh<D>), dim3((unsigned)(weighing + (combining + a.Hkv - 1) / a.Hkv), (unsigned)a.Hkv, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a, weighing);
-    else if (a.weights_out) {
-        const dim3 pages((unsigned)(a.max_pages * a.Hkv), (unsigned)a.B);
-        if ((long)a.max_pages * a.Hkv * a.B <= KW_PER_CU * a.num_cus) hipLaunchKernelGGL((kv16_attn_weights<D, 8>), pages, dim3(512), 0, stream, a);
-        else hipLaunchKernelGGL((kv16_attn_weights<D, 4>), pages, dim3(256), 0, stream, a);
+    if (combining) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)combining, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
+}
+
+template <int D>
+hipError_t launch(const Kv16AttnArgs* few, const Kv16AttnArgs* many, hipStream_t stream)
+{
+    if (few) launch_few<D>(*few, stream);
+    if (many) launch_many<D>(*many, stream);
+    if (many && many->weights_out) {
+        const dim3 pages((unsigned)(many->max_pages * many->Hkv), (unsigned)many->B);
+        if ((long)many->max_pages * many->Hkv * many->B <= KW_PER_CU * many->num_cus) hipLaunchKernelGGL((kv16_attn_weights<D, 8>), pages, dim3(512), 0, stream, *many);
+        else hipLaunchKernelGGL((kv16_attn_weights<D, 4>), pages, dim3(256), 0, stream, *many);
     }
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_kv16_attention(const Kv16AttnArgs& a, hipStream_t stream)
+hipError_t launch_kv16_attention(const Kv16AttnArgs* few, const Kv16AttnArgs* many, hipStream_t stream)
 {
-    return a.D == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+    return (few ? few : many)->D == 128 ? launch<128>(few, many, stream) : launch<64>(few, many, stream);
 }
 
 }  // namespace thi

@@ -123,17 +123,34 @@ def test_host_side_under_sanitizers(tmp_path):
 #include <cstdio>
 #include <cstdlib>
 namespace thi {
-static long launches = 0;
+static long launches = 0, both = 0;
 static size_t given = (size_t)1 << 50;
 static char* space;
 #define NEED(x) do { ++launches; if (!(x)) { std::printf("stand-in %%s\n", #x); std::exit(1); } } while (0)
 hipError_t launch_kv16_append(const Kv16AppendArgs& a, int, hipStream_t) { NEED(a.ld >= (a.Hq + 2L * a.Hkv) * a.D && a.T >= 1); return hipSuccess; }
-hipError_t launch_kv16_attention(const Kv16AttnArgs& a, hipStream_t)
+static void look(const Kv16AttnArgs& a, long q)
 {
     NEED(a.B >= 1 && a.T >= 1 && a.max_q >= 1 && a.max_q <= a.T && a.nsplit >= 1 && a.nsplit <= KV16_MAX_SPLIT && a.window >= 0 && a.sinks >= 0);
-    const size_t rows = (size_t)a.B * a.max_q * a.Hq;
-    NEED(a.nsplit == 1 || (char*)a.part + rows * a.nsplit * kv16_part(a.D) * 4 <= space + given);
-    NEED(!a.weights_out || ((char*)a.stats == space && (char*)a.stats + rows * 8 <= (char*)a.part));
+    const size_t rows = (size_t)a.B * a.Hkv * a.tiles * KV16_TILE_ROWS;
+    NEED(a.tiles * (long)KV16_TILE_ROWS >= a.max_q * (long)a.group && a.part_q == q);
+    NEED(a.nsplit == 1 || (char*)a.part + (size_t)a.B * q * a.Hq * a.nsplit * kv16_part(a.D) * 4 <= space + given);
+    NEED((char*)a.part <= space + given);
+    NEED(!a.weights_out || ((char*)a.stats == space && space + rows * 8 <= (char*)a.part));
+    NEED(!a.queries || ((char*)a.queries >= space + rows * 8 && (char*)a.queries + rows * a.D * 2 <= (char*)a.part));
+    NEED(!a.scores || ((char*)a.scores >= space + rows * 8 && (char*)a.scores + (size_t)a.B * a.max_q * a.Hq * a.max_pages * 256 <= (char*)a.part));
+}
+hipError_t launch_kv16_attention(const Kv16AttnArgs* few, const Kv16AttnArgs* many, hipStream_t)
+{
+    NEED(few || many);
+    const Kv16AttnArgs& a = few ? *few : *many;
+    const long q_few = KV16_FEW_ROWS / a.group;
+    if (few) look(*few, many ? q_few : a.max_q);
+    if (many) look(*many, a.max_q);
+    NEED((many == nullptr) == ((long)a.max_q * a.group <= KV16_FEW_ROWS));
+    NEED(few && many ? few->whose == Kv16AttnArgs::THOSE_OF_FEW_ROWS && many->whose == Kv16AttnArgs::THOSE_OF_MORE && !few->scores && few->queries == many->queries && few->tiles == many->tiles
+                     : a.whose == Kv16AttnArgs::EVERYONES);
+    NEED(!a.weights_out || (few && !many ? a.scores && !a.queries : a.queries && !a.scores));
+    if (few && many) ++both;
     return hipSuccess;
 }
 size_t kv16_evict_words(int layers, int rows, int Hkv, int max_pages, int num_pages) { return 2 * (size_t)rows + num_pages + (size_t)layers * rows * Hkv * max_pages * 64; }
@@ -183,13 +200,14 @@ int main()
                         for (int b : {1, 2, 5, 17, 300})
                             for (int r : {1, 2, 7, 64, 500})
                                 for (int m : {1, 3, 16, 17, 100, 3000})
-                                    if (b <= B && r <= q && m <= mp) {
-                                        const int rc = thi_kv16_attention(p, p, w, w, w, 0.1f, 0, 0, p, nullptr, weights ? f : nullptr, b, b * r, h[0], h[1], h[2], r, 7, m, p, thi::given, nullptr);
+                                    for (int t : {b * r, (b - 1) * r + 1})
+                                    if (b <= B && r <= q && m <= mp && t >= r) {
+                                        const int rc = thi_kv16_attention(p, p, w, w, w, 0.1f, 0, 0, p, nullptr, weights ? f : nullptr, b, t, h[0], h[1], h[2], r, 7, m, p, thi::given, nullptr);
                                         if (rc != 0) { std::printf("%%d for %%d %%d %%d in %%d %%d %%d\n", rc, b, r, m, B, q, mp); return 1; }
                                     }
                     }
     std::printf("ok %%ld calls, %%ld launches\n", calls, thi::launches);
-    return thi::launches > 100 ? 0 : 1;
+    return thi::launches > 100 && thi::both > 100 ? 0 : 1;
 }
 ''' % dict(root=ROOT))
     exe = str(tmp_path / "kv16_san")

@@ -228,6 +228,19 @@ def test_prompts(thi, window, sinks, Hq, Hkv, D):
     check_attention(thi, c, window, sinks, weights=True)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,window,sinks", [(4, 1, 64, 0, 0), (8, 2, 128, 0, 0), (4, 4, 64, 4500, 70), (16, 1, 64, 0, 0), (17, 1, 64, 0, 0)])
+def test_single_tokens_next_to_chunks_far_behind(thi, Hq, Hkv, D, window, sinks):
+    """Long tables: requests of few rows of a call with larger ones are dealt as if they were alone, and their result is as near as then (17 rows are not few)."""
+    c = attention_case(Hq + D, Hq, Hkv, D, [150, 4700, 0, 1, 4650, 70], [40, 1, 1, 1, 16 // min(16, Hq // Hkv), 0])
+    c["table"][4, 3] = -1
+    got = check_attention(thi, c, window, sinks, weights=True)
+    if Hq // Hkv <= 16:
+        y, tol, _, _ = ref.attention(c, D ** -0.5, window, sinks, ref.TWO_SUMMANDS)
+        assert (np.abs(got - y) <= tol)[40:].all()
+    without = run_attention(thi, c, D ** -0.5, window, sinks)[0]
+    assert np.array_equal(without[40:], got[40:])
+
+
 def test_prompt_of_one_long_request(thi):
     check_attention(thi, attention_case(17, 2, 1, 128, [700], [700]), weights=True)
 
