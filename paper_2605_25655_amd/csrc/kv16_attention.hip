@@ -459,7 +459,7 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
 // 267 and 197 us.  Exponentials between products, or by themselves: 209 and 129, 211 and 141; products of 16x16x32 instead of 32x32x16, which read half the
 // operands but take more power, so that the clock goes down: 197 and 129 instead of 209 and 129.  Cut into chunks where that fills compute units that have one
 // workgroup: 5 chunks of 128 tokens, window 4096, 126 -> 111 us, but one of 800 on 4000 99 -> 126, for partial results are 4 D bytes a row: not done.
-constexpr int KP_WAVES = 4, KP_AHEAD = 6, KP_BUFS = 2;
+constexpr int KP_WAVES = 4, KP_AHEAD = 4, KP_BUFS = 2;
 template <int D, int WAVES> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2 + WAVES * 2048;
 
 // 64 x 16 bytes from `base` + 16 * lane to LDS
@@ -586,7 +586,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
         kp_bring(from + kv16_values(D) + (wv + j * WAVES) * 512, lane16, lds_at + KP_BUFS * PART + buf + j * WAVES * 1024);
     };
 
-    float m[2] = {-__builtin_inff(), -__builtin_inff()}, start[2] = {0.f, 0.f}, l[2] = {0.f, 0.f}, exact[2] = {0.f, 0.f};      // sums: of this lane's positions only
+    float m[2] = {-__builtin_inff(), -__builtin_inff()}, start[2] = {0.f, 0.f}, exact[2] = {0.f, 0.f};      // exact: of this lane's positions only
+    floatx4 l[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};      // the weights' sum, as a product with ones (every element is the lane's row's)
+    const half8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
     bool fresh = true;
     floatx4 o[2][NT], s[2][4];
     half8 pw[2][2];
@@ -595,42 +597,40 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[c][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    // N products whose operands are asked for KP_AHEAD ahead, in this order, or the compiler would ask for each where it is needed and wait; `between` puts vector work into the time that
-    // the i-th takes.
-    auto products = [&](auto count, auto fetch, auto product, auto between) __attribute__((always_inline)) {
-        constexpr int N = decltype(count)::value;
-        half8 f[KP_AHEAD];
+    // A turn's operands, each for two products, in the order in which they are multiplied: 4 NB of the next page's keys, 2 NT of this page's values.  They are asked for KP_AHEAD ahead, in this
+    // order, or the compiler would ask for each where it is needed and wait; the first ones in front of what the turn begins with.  `between` puts vector work into the time that the
+    // i-th takes.
+    constexpr int KEYS = 4 * NB, VALUES = 2 * NT;
+    half8 f[KP_AHEAD];
+    auto key = [&](unsigned buf, int i) __attribute__((always_inline)) { return __builtin_bit_cast(half8, kp_smem[buf / 16 + lane + ((i & 3) * NB + (i >> 2)) * 64]); };
+    auto value = [&](unsigned buf, int i) __attribute__((always_inline)) { return __builtin_bit_cast(half8, kp_smem[(KP_BUFS * PART + buf) / 16 + lane + i * 64]); };
+    auto ask_keys = [&](unsigned buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < KP_AHEAD; ++i) f[i] = fetch(i);
+        for (int i = 0; i < KP_AHEAD; ++i) f[i] = key(buf, i);
         __builtin_amdgcn_sched_barrier(0);
+    };
+    // the scores of a page, into s; then values of another one are asked for
+    auto multiply_keys = [&](unsigned buf, unsigned values, auto between) __attribute__((always_inline)) {
+        const floatx4 none = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            product(i, f[i % KP_AHEAD]);
-            if (i + KP_AHEAD < N) f[i % KP_AHEAD] = fetch(i + KP_AHEAD);
+        for (int i = 0; i < KEYS; ++i) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) s[c][i & 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[i % KP_AHEAD], queries[c][i >> 2], i < 4 ? none : s[c][i & 3], 0, 0, 0);
+            f[i % KP_AHEAD] = i + KP_AHEAD < KEYS ? key(buf, i + KP_AHEAD) : value(values, i + KP_AHEAD - KEYS);
             between(i);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // the scores of a page, into s: an operand for two products
-    auto multiply_keys = [&](unsigned buf, auto between) __attribute__((always_inline)) {
-        const uintx4* const keys = kp_smem + buf / 16 + lane;
-        products(std::integral_constant<int, 4 * NB>{}, [&](int i) __attribute__((always_inline)) { return __builtin_bit_cast(half8, keys[((i & 3) * NB + (i >> 2)) * 64]); },
-                 [&](int i, half8 k) __attribute__((always_inline)) {
-                     const floatx4 none = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                     for (int c = 0; c < 2; ++c) s[c][i & 3] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, queries[c][i >> 2], i < 4 ? none : s[c][i & 3], 0, 0, 0);
-                 },
-                 between);
-    };
     // a page's weights times its values
     auto multiply_values = [&](unsigned buf, auto between) __attribute__((always_inline)) {
-        const uintx4* const values = kp_smem + (KP_BUFS * PART + buf) / 16 + lane;
-        products(std::integral_constant<int, 2 * NT>{}, [&](int i) __attribute__((always_inline)) { return __builtin_bit_cast(half8, values[i * 64]); },
-                 [&](int i, half8 v) __attribute__((always_inline)) {
 #pragma unroll
-                     for (int c = 0; c < 2; ++c) o[c][i % NT] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pw[c][i / NT], o[c][i % NT], 0, 0, 0);
-                 },
-                 between);
+        for (int i = 0; i < VALUES; ++i) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) o[c][i % NT] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[(KEYS + i) % KP_AHEAD], pw[c][i / NT], o[c][i % NT], 0, 0, 0);
+            if (i + KP_AHEAD < VALUES) f[(KEYS + i) % KP_AHEAD] = value(buf, i + KP_AHEAD);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     // t: what the exponentials of a page are of, 16 positions for each of the lane's rows; largest: the largest of them
     float t[32], largest[2] = {-__builtin_inff(), -__builtin_inff()};
@@ -640,7 +640,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     };
     // The i-th pair of weights.  They are cut to fp16's bits, not rounded to the nearest: their sum is one of cut weights too, so that what all are too small by cancels, and what is left is
     // half a step of each as with the other rounding; that one's conversion, of two values to the nearest, keeps matrix products of the SIMD's other wave from running for half of its time,
-    // this one's does not.  (So do exponentials, for all of theirs; and products of fp16 pairs, which is why the sum is one of single values.)
+    // this one's does not.  (So do exponentials, for all of theirs.)
     auto weigh = [&](int i) __attribute__((always_inline)) {
         const int c = i >> 3, k = (i >> 2) & 1, e = 2 * (i & 3);
         const float w0 = __builtin_amdgcn_exp2f(t[2 * i]), w1 = __builtin_amdgcn_exp2f(t[2 * i + 1]);
@@ -648,12 +648,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
         const half2v w = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(w0, w1));
         pw[c][k][e] = w[0];
         pw[c][k][e + 1] = w[1];
-    };
-    auto add = [&](int i) __attribute__((always_inline)) {
-        const int c = i >> 3, n = (i >> 2) & 1, e = 2 * (i & 3);
-        const unsigned both = __builtin_bit_cast(unsigned, half2v{pw[c][n][e], pw[c][n][e + 1]});
-        asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel_hi:[1,0,0]" : "+v"(l[c]) : "v"(both));                       // (the low one, the high one)
-        asm("v_fma_mix_f32 %0, %1, 1.0, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l[c]) : "v"(both));
     };
     // What a row does not see of the page, and a maximum that weights refer to if there is none or a weight would be past 2^15.
     auto settle = [&](int base) __attribute__((always_inline)) {
@@ -727,11 +721,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
         }
     };
 
-    // A wave's work is a chain: the scores of page 0, its exponentials, then the products behind page `it` (its weights with its values, and the scores of page it + 1), the exponentials of
-    // page it + 1, and so on.  The two halves of the waves (one of each on every SIMD) meet once a page, at different places: the first half behind its products, the
-    // second in front of them.  So between two meetings, k and k + 1, the first half has the exponentials of page k while the second multiplies, and then the other way round, and all of them
-    // read the values of page k and the keys of page k + 1.  What comes in meanwhile are values of page k + 2 and keys of page k + 3, into the buffers that were read
-    // in front of meeting k; they are waited for in front of meeting k + 2.
+    // A wave's work is a chain: the scores of page 0, and then a turn for every page: it settles the weights' exponents, takes the exponentials between the products of the next page's scores, and
+    // multiplies the weights with its values.  The waves meet at a turn's end; in turn `it` they read the values of page it and the keys of page it + 1, and what comes in meanwhile are
+    // values of page it + 1 and keys of page it + 2, into the buffers that were read in the turn before.
     // (A wave works on all pages up to its last row's own; behind the last one it multiplies keys of whatever is there, for nobody: accumulators under a condition are copied.)
     const int here_end = rows_here ? high.end : 0;
     auto turns_to = [&](int end, int from, int most) { const int n = (end - from + KV16_PAGE - 1) / KV16_PAGE; return end <= from ? 0 : n < most ? n : most; };
@@ -758,8 +750,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
                 *reinterpret_cast<half8*>(a.queries + (stats_row(a, tile.b, tile.g, w0 + 16 * c) / 16 * NB + b) * 512 + lane * 8) = queries[c][b];
     kp_wait<0>();
     kp_barrier();
-    auto nothing = [](int) {};
-    multiply_keys(0u, nothing);
+    ask_keys(0u);
+    multiply_keys(0u, 0u, [](int) {});
 #pragma unroll
     for (int i = 0; i < 32; ++i) scale(i);
 #pragma unroll
@@ -796,39 +788,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     if (n_wave > 0) {
         int it = 0;
         do {
+            ask_keys(b1);
             settle(page < 0 ? 0x7fffff00 : base_of(it));      // (nothing of a page that is not there is seen)
             begin(it);
-            multiply_keys(b1, [&](int i) __attribute__((always_inline)) {
-                if (NB == 4) {
-                    weigh(i);
-                    if (i >= 8) add(i - 8);
-                } else {
-                    weigh(2 * i);
-                    weigh(2 * i + 1);
-                }
+            multiply_keys(b1, b0, [&](int i) __attribute__((always_inline)) {
+                weigh(i * (16 / KEYS));
+                if (KEYS == 8) weigh(2 * i + 1);
                 bring(i);
             });
+            // (the sum of the weights: by products, or each weight would be a vector instruction more)
             multiply_values(b0, [&](int i) __attribute__((always_inline)) {
-                if (NB == 4) {
-                    if (i < 4) {
-                        add(8 + 2 * i);
-                        add(9 + 2 * i);
-                    } else if (i < 12) {
+                constexpr int BEGIN = 4, EACH = 16 / VALUES;      // of the next scores, 4 EACH at a time
+                if (i < BEGIN) l[i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pw[i & 1][i >> 1], l[i & 1], 0, 0, 0);
+                else if (i < BEGIN + 16 / (2 * EACH)) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) scale(4 * (i - 4) + k);
-                        look(2 * (i - 4));
-                        look(2 * (i - 4) + 1);
-                    }
-                } else {
-                    if (i < 4) {
+                    for (int k = 0; k < 4 * EACH; ++k) scale(4 * EACH * (i - BEGIN) + k);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) add(4 * i + k);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) scale(8 * (i - 4) + k);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) look(4 * (i - 4) + k);
-                    }
+                    for (int k = 0; k < 2 * EACH; ++k) look(2 * EACH * (i - BEGIN) + k);
                 }
             });
             end(it);
@@ -847,8 +823,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
     unsigned odd_rows = 0;                       // of the wave's 32
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-        l[c] += __shfl_xor(l[c], 16);
-        l[c] += __shfl_xor(l[c], 32);
         if (STATS) {
             exact[c] += __shfl_xor(exact[c], 16);
             exact[c] += __shfl_xor(exact[c], 32);
@@ -876,7 +850,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
         if (hi == 0) { s_m[wv * 32 + own] = m[c]; s_exact[wv * 32 + own] = exact[c]; }
         if (own >= here || (odd_rows >> own & 1)) continue;
         if (at.whole) {
-            const float inv = l[c] == 0.f ? 0.f : 1.0f / l[c];
+            const float inv = l[c][0] == 0.f ? 0.f : 1.0f / l[c][0];
             uint16_t* const out = e.out + row[c] * D;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -888,7 +862,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_prompt(Kv16AttnArgs a
             float* const po = e.part + (part_row(e, at.b, r, at.g, e.group) * e.nsplit + at.chunk) * kv16_part(D);
 #pragma unroll
             for (int t = 0; t < NT; ++t) *reinterpret_cast<floatx4*>(po + 16 * t + 4 * hi) = o[c][t];
-            if (hi == 0) { po[D] = m[c]; po[D + 1] = l[c]; po[D + 2] = exact[c]; }
+            if (hi == 0) { po[D] = m[c]; po[D + 1] = l[c][0]; po[D + 2] = exact[c]; }
         }
     }
     __syncthreads();
