@@ -966,7 +966,7 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_weigh(Kv16AttnArgs a, in
 // For each 16 rows and 64 positions 262 kFLOP of matrix products (D = 128), 1024 exponentials and 4 KB of queries; the last is what bounds it.  So kv16_attn_prompt leaves the queries as operands, a
 // KB at a time: from where they stand, 16 rows a load, the rows of 32 heads 8 KB apart fall on one channel of the cache (2001 tokens of 32/32 heads of 128, all of the call: 102 us, like this 87).
 // Two pages in a workgroup, which halve the queries' way, leave too few of them (2001 tokens of 64/8 heads 317 us against 212); products of the next rows between the weights of the last: no gain
-// (89).  Eight waves instead of four where the workgroups are few: 2001 tokens of 64/8 heads 188 -> 170 us; where they are not, it is the other way round (of 32/32: 87 -> 93).
+// (89); four pages in a workgroup, a page a wave, queries by way of LDS and rows in parts of 512 whose sums one more launch adds: less for them (161 as against 169), more for 32/32 heads (97).  Eight waves instead of four where the workgroups are few: 2001 tokens of 64/8 heads 188 -> 170 us; where they are not, it is the other way round (of 32/32: 87 -> 93).
 constexpr int KW_PER_CU = 2;                     // up to so many workgroups for a compute unit: of eight waves instead of four
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs a)
@@ -1041,17 +1041,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs 
         for (int i = 0; i < 4 * TILES; ++i) w[i] = __builtin_fmaf(s[i >> 2][i & 3], a.scale2, -m);
         const bool none = inv == 0.f;            // a row that is not there, or sees nothing
         if (__builtin_amdgcn_ballot_w64(none) != 0ull || p0 + SPAN > low.end) {
-            const int seen = (none ? 0 : mine.end) - p0 - 4 * hi;
+            int seen = (none ? 0 : mine.end) - p0 - 4 * hi;
+            asm volatile("" : "+v"(seen));      // (here, under the condition, and what depends on it)
 #pragma unroll
             for (int i = 0; i < 4 * TILES; ++i) w[i] = seen > 16 * (i >> 2) + (i & 3) ? w[i] : -__builtin_inff();
         }
         if (p0 < high.from && p0 + SPAN > a.sinks) {
-            const int hidden = a.sinks - p0 - 4 * hi, span = mine.from > a.sinks ? mine.from - a.sinks : 0;
+            const int span = mine.from > a.sinks ? mine.from - a.sinks : 0;
+            int hidden = a.sinks - p0 - 4 * hi;
+            asm volatile("" : "+v"(hidden));
 #pragma unroll
             for (int i = 0; i < 4 * TILES; ++i) w[i] = (unsigned)(16 * (i >> 2) + (i & 3) - hidden) < (unsigned)span ? -__builtin_inff() : w[i];
         }
 #pragma unroll
         for (int i = 0; i < 4 * TILES; ++i) sum[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(w[i]), inv, sum[i]);
+#pragma unroll
+        for (int i = 0; i < 4 * TILES; ++i) asm volatile("" : "+v"(sum[i]));      // (now: next to the following products)
     };
     const int turns = there && first < last ? (tile_end - tile0 + WAVES - 1) / WAVES : 0;
     if (turns > 0) {
