@@ -369,8 +369,8 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
  * stayed for want of pages.
  *
  * refs_* [num_pages], table_* [rows][max_pages], lens_* [rows] int32; weights_* [layers][rows][Hkv][64 max_pages] fp32; pages: layer l's pool begins at
- * pages + l * layer_bytes (a multiple of 16).  1 <= budget, 0 <= sinks, recent, headroom, sinks + recent <= budget, layers * rows <= 65535, and where a row's table reaches
- * past 2^28 positions, budget <= 2^28 (THI_ERR_SHAPE).  Workspace: thi_kv16_evict_workspace_bytes(), 256-byte aligned.
+ * pages + l * layer_bytes (a multiple of 16).  1 <= budget, 0 <= sinks, recent, headroom, sinks + recent <= budget, layers * rows <= 65535, rows * max_pages < 2^31, and where
+ * a row's table reaches past 2^28 positions, budget <= 2^28 (THI_ERR_SHAPE).  Workspace: thi_kv16_evict_workspace_bytes(), 256-byte aligned.
  */
 size_t thi_kv16_evict_workspace_bytes(int layers, int rows, int Hkv, int max_pages, int num_pages);
 int thi_kv16_evict(const int* refs_in, const int* table_in, const int* lens_in, const float* weights_in, int budget, int sinks, int recent, int headroom,

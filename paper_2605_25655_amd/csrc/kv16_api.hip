@@ -181,6 +181,7 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
 size_t thi_kv16_evict_workspace_bytes(int layers, int rows, int Hkv, int max_pages, int num_pages)
 {
     if (layers < 1 || rows < 1 || layers > 65535 || rows > 65535 || (long)layers * rows > 65535 || !heads_ok(Hkv, Hkv, 64) || max_pages < 1 || max_pages > MAX_PAGES ||
+        (long)rows * max_pages > 0x7fffffff ||      // (the pages that all rows ask for are counted in 32 bits)
         !pool_ok(num_pages))
         return 0;
     return round_up(kv16_evict_words(layers, rows, Hkv, max_pages, num_pages) * 4);

@@ -88,6 +88,7 @@ def test_sizes(lib):
     assert f(1, 60000, 17920, 1, 128, 59918, 1, 0) > 0 and f(1, 60000, 17920, 1, 128, 59919, 1, 0) == 0      # 2^23 tiles of 128 rows, and one more
     assert f(2, 2, 8, 3, 128, 1, 100, 0) == 0 and f(2, 2, 8, 2, 100, 1, 100, 0) == 0 and f(2, 2, 8, 2, 128, 3, 100, 0) == 0 and f(0, 2, 8, 2, 128, 1, 100, 0) == 0
     f = lib.thi_kv16_evict_workspace_bytes
+    assert f(1, 128, 8, 1 << 24, 10) == 0 and f(1, 127, 8, 1 << 24, 10) > 0
     assert f(2, 4, 8, 10, 1000) >= 4 * 2 * 4 * 8 * 10 * 64 and f(2, 4, 8, 10, 0) == 0 and f(0, 4, 8, 10, 10) == 0 and f(256, 256, 8, 1, 1) == 0
 
 

@@ -650,6 +650,54 @@ def test_on_a_stream_of_its_own_and_in_graphs(thi):
             assert torch.equal(pages.view(torch.int16), want[k][1].view(torch.int16)), (i, k)
 
 
+def test_prompts_and_mixed_calls_in_graphs(thi):
+    """Two captured calls with weights that share a workspace, one of prompts and one of single tokens next to a chunk far behind, replayed in turn, with eager calls of a third kind between."""
+    import torch
+    cases = [(attention_case(50, 8, 2, 64, [300, 70, 128], [300, 33, 0]), 100, 4), (attention_case(51, 8, 2, 64, [4700, 200], [1, 40]), 0, 0), (attention_case(52, 8, 2, 64, [500, 66], [1, 1]), 0, 0)]
+    need = max(thi.thi_kv16_attention_workspace_bytes(*c["table"].shape[:1], len(c["q"]), 8, 2, 64, c["max_q"], c["table"].shape[1], True) for c, _, _ in cases)
+    ws = thi.Workspace(need, init=False)
+    calls = []
+    for c, window, sinks in cases:
+        t = {k: dev(c[k]) for k in ("q", "pages", "table", "lens", "offsets")}
+        o = dict(out=torch.empty_like(t["q"]), w=torch.zeros(len(c["lens"]), 2, c["table"].shape[1] * PAGE, device="cuda"))
+        calls.append((lambda t=t, o=o, c=c, window=window, sinks=sinks: thi.thi_kv16_attention(t["q"], t["pages"], t["table"], t["lens"], t["offsets"], 0.1, window, sinks, o["out"], c["max_q"],
+                                                                                              ws, None, o["w"]), o))
+    want, graphs = [], []
+    for call, o in calls:
+        call()
+        want.append({k: x.clone() for k, x in o.items()})
+    torch.cuda.synchronize()
+    for call, _ in calls[:2]:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        graphs.append(graph)
+    for i in range(3):
+        for k in (0, 1):
+            calls[k][1]["out"].fill_(7)
+            calls[k][1]["w"].zero_()
+            calls[2][0]()
+            graphs[k].replay()
+            torch.cuda.synchronize()
+            for j in (k, 2):
+                for name, x in calls[j][1].items():
+                    assert torch.equal(x, want[j][name]), (i, k, j, name)
+
+
+@pytest.mark.parametrize("new", [[1, 1, 2], [40, 1, 17]])
+def test_rows_behind_the_last_request_are_left(thi, new):
+    """A batch padded to more rows than its requests have: those rows are not written, and the others are what they are without them."""
+    import torch
+    c = attention_case(53, 4, 2, 128, [100, 70, 64], new)
+    T = sum(new)
+    want, w = run_attention(thi, c, 0.125, weights=True)
+    q = dev(np.concatenate([c["q"], np.full((5, 4, 128), np.nan, np.float16)]))
+    out, got = torch.full_like(q, 7.0), torch.full((3, 2, c["table"].shape[1] * PAGE), float("nan"), device="cuda")
+    ws = thi.Workspace(thi.thi_kv16_attention_workspace_bytes(3, T + 5, 4, 2, 128, max(new), c["table"].shape[1], True), init=False)
+    thi.thi_kv16_attention(q, dev(c["pages"]), dev(c["table"]), dev(c["lens"]), dev(c["offsets"]), 0.125, 0, 0, out, max(new), ws, None, got)
+    assert np.array_equal(host(out)[:T].astype(np.float64), want) and (host(out)[T:] == 7).all() and np.array_equal(host(got).astype(np.float64), w, equal_nan=True)
+
+
 def test_the_same_bits_every_time(thi):
     import torch
     c = attention_case(40, 8, 2, 64, [900, 333], [5, 70])
