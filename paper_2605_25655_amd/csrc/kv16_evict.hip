@@ -1,6 +1,6 @@
 // Requests of the fp16 cache brought back to a number of positions: which stay, fresh pages for them, and the move.  Memory-bound: kept keys and values are read and
 // written once, the accumulated weights read a few times, the later ones from the caches.  Two launches: the plan next to the selection, then the move.
-// Measured: 16 requests of up to 4000 positions brought to 1200 in four layers of 8 heads of 128, 204 us (24 + 180); two of up to 300 of 8 heads of 64, 12.3.
+// Measured: 16 requests of up to 4000 positions brought to 1200 in four layers of 8 heads of 128, 201 us (21 + 180); two of up to 300 of 8 heads of 64, 11.3 (9 + 2.7).
 #include "kv16.h"
 
 namespace thi {
@@ -78,33 +78,50 @@ __device__ __forceinline__ int kept_of(const Kv16EvictArgs& a, int b, int n, int
 
 constexpr int KE_THREADS = 1024;
 
-// Who is evicted, which pages they get, and the tables and counts that follow: one workgroup.
-__device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave)
+// Who is evicted, which pages they get, and the tables and counts that follow: one workgroup.  What it writes and reads back is in LDS, too, as far as it fits: a chain of loads and stores is
+// what it takes its time for.
+constexpr int KE_ROWS = 1024, KE_PAGES = 8192;
+struct PlanSpace {
+    int kept[KE_ROWS], begin[KE_ROWS], fresh[KE_PAGES];
+};
+__device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave, PlanSpace& s)
 {
     const Space ws = space_of(a);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int first_refs = tid < a.num_pages ? a.refs_in[tid] : 1;
     for (int b = wave; b < a.rows; b += KE_THREADS / 64) {
         const int kept = kept_of(a, b, length_of(a, b), lane);
-        if (lane == 0) ws.kept[b] = kept;
+        if (lane == 0) {
+            ws.kept[b] = kept;
+            if (b < KE_ROWS) s.kept[b] = kept;
+        }
     }
     __syncthreads();
+    auto kept_by = [&](int b) { return b < KE_ROWS ? s.kept[b] : ws.kept[b]; };
     // pages that they ask for, one row behind the other
     long asked = 0;
     for (int b0 = 0; b0 < a.rows; b0 += KE_THREADS) {
-        const int b = b0 + tid, kept = b < a.rows ? ws.kept[b] : -1;
+        const int b = b0 + tid, kept = b < a.rows ? kept_by(b) : -1;
         int total;
         const int before = scan<KE_THREADS>(kept >= 0 ? pages_for(a, kept) : 0, s_wave, total);
         const long at = asked + before;
-        if (b < a.rows) ws.begin[b] = at > a.num_pages ? a.num_pages : (int)at;      // (further than any free page)
+        if (b < a.rows) {
+            const int begin = at > a.num_pages ? a.num_pages : (int)at;      // (further than any free page)
+            ws.begin[b] = begin;
+            if (b < KE_ROWS) s.begin[b] = begin;
+        }
         asked += total;
     }
     // the lowest free pages
     int free_pages = 0;
     for (int p0 = 0; p0 < a.num_pages; p0 += KE_THREADS) {
-        const int p = p0 + tid, refs = p < a.num_pages ? a.refs_in[p] : 1;
+        const int p = p0 + tid, refs = p0 == 0 ? first_refs : p < a.num_pages ? a.refs_in[p] : 1;
         int total;
         const int before = scan<KE_THREADS>(refs == 0 ? 1 : 0, s_wave, total);
-        if (refs == 0) ws.fresh[free_pages + before] = p;
+        if (refs == 0) {
+            ws.fresh[free_pages + before] = p;
+            if (free_pages + before < KE_PAGES) s.fresh[free_pages + before] = p;
+        }
         if (p < a.num_pages) a.refs_out[p] = refs;
         free_pages += total;
     }
@@ -113,7 +130,7 @@ __device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave)
     // Rows whose pages are there: the lengths, tables and counts that they leave with.  (counts by atomic operations on integers: the same in any order)
     int done = 0, left = 0;
     for (int b = wave; b < a.rows; b += KE_THREADS / 64) {
-        const int kept = ws.kept[b], n = length_of(a, b), need = kept >= 0 ? pages_for(a, kept) : 0, begin = ws.begin[b];
+        const int kept = kept_by(b), n = length_of(a, b), need = kept >= 0 ? pages_for(a, kept) : 0, begin = b < KE_ROWS ? s.begin[b] : ws.begin[b];
         const bool moves = kept >= 0 && (long)begin + need <= free_pages;
         if (lane == 0) {
             a.lens_out[b] = moves ? kept : n;
@@ -125,7 +142,7 @@ __device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave)
             const int e = a.table_in[at];
             int f = e;
             if (moves) {
-                f = j < need ? ws.fresh[begin + j] : -1;
+                f = j >= need ? -1 : begin + j < KE_PAGES ? s.fresh[begin + j] : ws.fresh[begin + j];
                 if (is_page(a, e)) atomicSub(&a.refs_out[e], 1);
                 if (j < need) atomicAdd(&a.refs_out[f], 1);
             }
@@ -156,22 +173,25 @@ __device__ __forceinline__ unsigned order_of(float w)
 constexpr int KE_DIGIT = 11;
 __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
 {
+    constexpr int DIGITS = 3;
+    union Shared {
+        int count[DIGITS][1 << KE_DIGIT];
+        PlanSpace plan;
+    };
+    __shared__ Shared shared;
     __shared__ int s_wave[KE_THREADS / 64];
-    __shared__ int s_count[1 << KE_DIGIT];
     __shared__ unsigned s_prefix;
-    __shared__ int s_left, s_kept;
+    __shared__ int s_left, s_kept, s_sure;
     if (blockIdx.x == 0) {
-        if (blockIdx.y == 0 && blockIdx.z == 0) evict_plan(a, s_wave);
+        if (blockIdx.y == 0 && blockIdx.z == 0) evict_plan(a, s_wave, shared.plan);
         return;
     }
     const Space ws = space_of(a);
     const int tid = threadIdx.x, lane = tid & 63, g = blockIdx.x - 1, b = blockIdx.y, layer = blockIdx.z;
     const int n = length_of(a, b);
     if (n <= a.budget) return;
-    if (tid < 64) {
-        const int kept = kept_of(a, b, n, lane);
-        if (tid == 0) s_kept = kept;
-    }
+    for (int i = tid; i < DIGITS << KE_DIGIT; i += KE_THREADS) shared.count[0][i] = 0;
+    if (tid == 0) s_sure = 0;
     const size_t at = (((size_t)layer * a.rows + b) * a.Hkv + g) * a.max_pages * KV16_PAGE;
     const float* const weights = a.weights_in + at;
     int* const slots = ws.slots + at;
@@ -182,14 +202,19 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
     };
     auto ask = [&](int p) {
         Four f{0, 0, {0, 0, 0, 0}};
-        if (p >= n || !is_page(a, table[p / KV16_PAGE])) return f;
+        if (p >= n) return f;
+        // (both asked for at once: a page has weights for all of its positions)
+        const int page = table[p / KV16_PAGE];
+        float w[4];
+        __builtin_memcpy(w, weights + p, sizeof(w));
+        const bool there = is_page(a, page);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int q = p + k;
-            if (q >= n) continue;
+            if (!there || q >= n) continue;
             f.there |= 1u << k;
             if (q < a.sinks || q >= n - a.recent) f.guarded |= 1u << k;
-            f.u[k] = order_of(weights[q]);
+            f.u[k] = order_of(w[k]);
         }
         return f;
     };
@@ -203,25 +228,31 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
         for (int i = 0; i < HELD; ++i) what(held[i]);
         for (int p = (HELD * KE_THREADS + tid) * 4; p < n; p += KE_THREADS * 4) what(ask(p));
     };
+    if (tid < 64) {
+        const int kept = kept_of(a, b, n, lane);
+        if (tid == 0) s_kept = kept;
+    }
+    __syncthreads();
     // what is left of the budget for those that are not guarded
     int mine = 0;
     each([&](const Four& f) { mine += __builtin_popcount(f.guarded); });
-    int sure;
-    scan<KE_THREADS>(mine, s_wave, sure);
-    int want = s_kept - sure;                    // >= 0: no more than the budget is guarded
+#pragma unroll
+    for (int sh = 1; sh < 64; sh <<= 1) mine += __shfl_xor(mine, sh);
+    if (lane == 0 && mine) atomicAdd(&s_sure, mine);
+    int want = 0;                                // >= 0 once it is known: no more than the budget is guarded
     unsigned prefix = 0, mask = 0;               // weights above the prefix are kept, of those equal to it (in the end) `want`
-    for (int shift = 32 - KE_DIGIT, bits = KE_DIGIT; bits > 0;) {
-        for (int i = tid; i < 1 << KE_DIGIT; i += KE_THREADS) s_count[i] = 0;
-        __syncthreads();
+    for (int shift = 32 - KE_DIGIT, bits = KE_DIGIT, turn = 0; bits > 0; ++turn) {
+        int* const count = shared.count[turn];
         const unsigned digit = (1u << bits) - 1;
         each([&](const Four& f) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if ((f.there & ~f.guarded) >> k & 1 && (f.u[k] & mask) == prefix) atomicAdd(&s_count[f.u[k] >> shift & digit], 1);
+                if ((f.there & ~f.guarded) >> k & 1 && (f.u[k] & mask) == prefix) atomicAdd(&count[f.u[k] >> shift & digit], 1);
         });
         __syncthreads();
+        if (turn == 0) want = s_kept - s_sure;
         // from the top: thread 0 the two highest
-        const int hi = (1 << KE_DIGIT) - 1 - 2 * tid, c0 = s_count[hi], c1 = s_count[hi - 1];
+        const int hi = (1 << KE_DIGIT) - 1 - 2 * tid, c0 = count[hi], c1 = count[hi - 1];
         int total;
         const int above = scan<KE_THREADS>(c0 + c1, s_wave, total);
         // the one counter with which the sum from the top reaches what is wanted (want 0: the highest; it is at most the number of candidates)
@@ -237,7 +268,7 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
         bits = shift < KE_DIGIT ? shift : KE_DIGIT;
         shift -= bits;
     }
-    int placed = 0, equal = 0;
+    int placed = 0, equal = 0;                   // of those above the prefix, or guarded; of those equal to it
     auto place = [&](int p, const Four& f) __attribute__((always_inline)) {
         unsigned same = 0, keep = f.guarded;
 #pragma unroll
@@ -246,14 +277,15 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
             same |= (other && f.u[k] == prefix ? 1u : 0u) << k;
             keep |= (other && f.u[k] > prefix ? 1u : 0u) << k;
         }
+        // (both counted at once: no more than 4096 of each)
         int total;
-        int rank = scan<KE_THREADS>(__builtin_popcount(same), s_wave, total) + equal;
-        equal += total;
+        const int before = scan<KE_THREADS>(__builtin_popcount(keep) | __builtin_popcount(same) << 16, s_wave, total);
+        int rank = equal + (before >> 16), to = placed + (before & 0xffff) + (rank < want ? rank : want);
+        placed += total & 0xffff;
+        equal += total >> 16;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (same >> k & 1 && rank++ < want) keep |= 1u << k;
-        int to = scan<KE_THREADS>(__builtin_popcount(keep), s_wave, total) + placed;
-        placed += total;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (keep >> k & 1) {
@@ -270,7 +302,7 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
 // The move: a workgroup takes one fresh page of one cache head of a layer, 64 kept positions from wherever they were.  All that it reads is asked for at once, the pieces of 16 bytes of
 // the keys and the single values, for a workgroup is short and the wait for memory most of it.  A key's pieces lie beside those of seven neighbours in a cache line, a value's beside those of
 // 31, so that where every third position is kept, nearly all lines of the pages come: of the batch above 0.7 GB, with the 0.3 that are written 140 us at a copy's rate.  (180; of
-// neighbouring positions 149; through LDS, to have the values' lines once, 212 with the selection as against 208.)
+// neighbouring positions 149; through LDS, to have the values' lines once: 4 us more.)
 constexpr int KE_MOVE = 512;
 template <int D>
 __global__ __launch_bounds__(KE_MOVE) void kv16_evict_move(Kv16EvictArgs a)
