@@ -454,10 +454,11 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
 // What bounds it are the matrix products, 4 D FLOP a position and row, and the exponentials, one a position and row, in whose time the SIMD's matrix core rests.  So a wave has
 // the exponentials of a page between the products of the next page's scores, and its scaling and maxima between those of the values, and the two workgroups of a compute unit fill what is
 // left.  Weights are one fp16 each, cut (see weigh); a maximum may lag behind by 2^6, so that accumulators are hardly ever scaled.
-// Measured: a prompt of 4096 tokens, 40/40 heads of 128, 196 us (878 TFLOP/s of what it sees; a matrix product of 8192^3 reaches 1387 here); chunks of up to 777 tokens on up to 8029
-// positions, window 2000, 64/8 heads, 127 us, where the 616 tiles of equal work are two or three to a compute unit, 20 percent more than their mean.  256 rows in one workgroup a compute unit:
+// Measured: a prompt of 4096 tokens, 40/40 heads of 128, 190 to 195 us from card to card (880 to 910 TFLOP/s of what it sees; a matrix product of 8192^3 reaches 1387 here); chunks of up to 777 tokens on up to 8029
+// positions, window 2000, 64/8 heads, 126 us, where the 616 tiles of equal work are two or three to a compute unit, 20 percent more than their mean.  256 rows in one workgroup a compute unit:
 // 267 and 197 us.  Exponentials between products, or by themselves: 209 and 129, 211 and 141; products of 16x16x32 instead of 32x32x16, which read half the
-// operands but take more power, so that the clock goes down: 197 and 129 instead of 209 and 129.  Cut into chunks where that fills compute units that have one
+// operands but take more power, so that the clock goes down: 197 and 129 instead of 209 and 129.  The weights' sum as a product with ones instead of 32 instructions a page: 200.6 -> 196.7 on one card; operands of
+// both products asked for in one stream, over what a turn begins with: -> 194, and 129 -> 125.  Cut into chunks where that fills compute units that have one
 // workgroup: 5 chunks of 128 tokens, window 4096, 126 -> 111 us, but one of 800 on 4000 99 -> 126, for partial results are 4 D bytes a row: not done.
 constexpr int KP_WAVES = 4, KP_AHEAD = 4, KP_BUFS = 2;
 template <int D, int WAVES> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2 + WAVES * 2048;
@@ -964,7 +965,7 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_weigh(Kv16AttnArgs a, in
 // More rows: the scores are made again.  A workgroup takes a page of a cache head, whose keys stay in its waves' registers (the A operand); the rows that see any of it come by, 16
 // at a time, every WAVES-th 16 in a wave.  Weights in fp32, added up per lane (a lane has one row of each 16), then over lanes and waves: a fixed order.
 // For each 16 rows and 64 positions 262 kFLOP of matrix products (D = 128), 1024 exponentials and 4 KB of queries; the last is what bounds it.  So kv16_attn_prompt leaves the queries as operands, a
-// KB at a time: from where they stand, 16 rows a load, the rows of 32 heads 8 KB apart fall on one channel of the cache (2001 tokens of 32/32 heads of 128, all of the call: 102 us, like this 87).
+// KB at a time: from where they stand, 16 rows a load, the rows of 32 heads 8 KB apart fall on one channel of the cache (2001 tokens of 32/32 heads of 128, all of the call: 102 us, like this 87; 80 to 85 with the attention as it is now).
 // Two pages in a workgroup, which halve the queries' way, leave too few of them (2001 tokens of 64/8 heads 317 us against 212); products of the next rows between the weights of the last: no gain
 // (89); four pages in a workgroup, a page a wave, queries by way of LDS and rows in parts of 512 whose sums one more launch adds: less for them (161 as against 169), more for 32/32 heads (97).  Eight waves instead of four where the workgroups are few: 2001 tokens of 64/8 heads 188 -> 170 us; where they are not, it is the other way round (of 32/32: 87 -> 93).
 constexpr int KW_PER_CU = 2;                     // up to so many workgroups for a compute unit: of eight waves instead of four
@@ -1065,11 +1066,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs 
         int it = 0;
         do {                                     // (two turns: no copies from one to the other, each of which would wait for the load)
             ask(other);
-            __builtin_amdgcn_sched_barrier(0);
             weigh(one);
-            __builtin_amdgcn_sched_barrier(0);
             ask(one);
-            __builtin_amdgcn_sched_barrier(0);
             weigh(other);                        // (of rows behind the last, in the end)
             __builtin_amdgcn_sched_barrier(0);
         } while ((it += 2) < turns);
