@@ -64,6 +64,8 @@ size_t bytes_of_scores(int B, int Hq, int Hkv, int max_q, int max_pages)
 //     columns, 8 x 2000: 14.3 12.5 12.3
 //   not cut, cut: 2 x 468 of 8 heads of 64 columns: 6.8 9.9; 2 x 1200 of these: 9.1 10.0; 2 x 1500 of these (past FEW_UNCUT): 10.4 8.5; 4 x 600 of 32/32: 10.3 13.1; 2 x 600 of 64/8: 10.5 11.6;
 //     2 x 760 of 64/8 (past it): 11.4 10.8
+//   few rows, four, eight waves a workgroup, where there are more of them than the compute units hold: 32 x 2048 of 32/32: 110.5 107.0; 64 x 2000 of these 204 196; 96 x 3000 of 64/8: 117 105; 20 x 2000
+//     of 40/40: 82.6 75.1; where there are not: 24 x 4000 of 32/32: 150 155; 16 x 4000 112 116; 24 x 5000 of 64/8: 50.0 53.3; and of short tables (not past FEW_UNCUT), 32 x 500 of 32/32: 32.0 34.9
 void plan(Kv16AttnArgs& a, bool few, int num_cus)
 {
     a.group = a.Hq / a.Hkv;
@@ -76,6 +78,7 @@ void plan(Kv16AttnArgs& a, bool few, int num_cus)
     n = n < 1 ? 1 : n > KV16_MAX_SPLIT ? KV16_MAX_SPLIT : n;
     a.nsplit = (int)(n > most ? most : n);
     a.num_cus = num_cus;
+    a.wide = few && items > (long)FEW_PER_CU * num_cus && (long)a.max_pages * a.D > FEW_UNCUT;
 }
 size_t rows_of(const Kv16AttnArgs& a) { return a.nsplit > 1 ? (size_t)a.B * a.part_q * a.Hq * a.nsplit : 0; }
 // Are requests of few rows in a call of more dealt as if they were alone?  Some has to be there, by the number of tokens, and what a row sees has to be APART pages at least, for a tile of

@@ -131,17 +131,17 @@ __device__ __forceinline__ float slow_row(const Kv16AttnArgs& a, const Request& 
 
 // ---- one token per request, or a few: up to 16 rows of a cache head, cut along the positions ------------------------
 //
-// What bounds it is the pages' way from memory, 4 D bytes a position and cache head.  A workgroup (4 waves) takes a chunk of the pages that one request looks at, for one cache head; a wave
-// takes half of every second page, 32 positions, straight from memory into registers, its next half in flight behind it.  (Whole pages, every fourth, leave waves of short chunks without
+// What bounds it is the pages' way from memory, 4 D bytes a position and cache head.  A workgroup (four waves, or eight) takes a chunk of the pages that one request looks at, for one cache head; a
+// wave takes half of every second page (or fourth), 32 positions, straight from memory into registers, its next half in flight behind it.  (Whole pages, every fourth, leave waves of short chunks without
 // work: 32 requests of up to 2048 positions, 32/32 heads of 128, 116 us, like this 110.)  Rows are (new token, query head of the group) pairs, the columns of two matrix products
 // (v_mfma_f32_16x16x32_f16):
 //   S = K Q^T     : 16 positions x 16 rows;
 //   O^T = V^T P^T : a lane has the weights of positions 16 i + 4 hi + r of its row, which is the B operand as it stands, for the page holds the values in that order.
 // So nothing but the rows' maxima crosses lanes, and those only when a weight leaves fp16's range.  Weights are multiplied as two fp16 summands (2^-21 of a weight
 // off at most down to 2^-12 of the largest, 2^-33 of that below, where one alone is off by 2^-11 and as much as the result's own rounding).
-// Measured, us a pass with kv16_attn_combine: those 32 requests 110 (6.2 TB/s; a copy of 128 MiB 7.1), 3 of 131000 and less on 64/8 heads 86 (6.2 TB/s), 16 of 32000 and less with a window
+// Measured, us a pass with kv16_attn_combine: those 32 requests 107 with eight waves (6.4 TB/s; a copy of 128 MiB 7.1), 3 of 131000 and less on 64/8 heads 86 (6.2 TB/s), 16 of 32000 and less with a window
 // of 4096 48 (5.3), two of 468 and less with 8 heads of 64 columns 5.9, which is a launch and four loads one behind the other.
-constexpr int KD_THREADS = 256, KD_WAVES = 4;
+template <int D, int WAVES> constexpr int KD_LDS = WAVES * 16 * (D + 4) * 4;
 constexpr float WEIGHT_LOG2 = 9.0f;              // weights are held as 2^9 p of a maximum that may lag by 2^6 (fp16 ends at 2^16)
 
 // Two fp16 summands of four weights (the large one truncated, so that the small one is not negative).
@@ -158,13 +158,14 @@ __device__ __forceinline__ void split_weights(const float (&w)[4], half4& large,
 __device__ __forceinline__ half8 join(half4 a, half4 b) { return half8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
 
 // SCORES: they are left for kv16_attn_weigh, 4 bytes a row and position: 24 requests of up to 5000 positions, 64/8 heads, 50 us without weights, 58 with the scores' stores, 64 with their sums.
-template <int D, bool SCORES>
-__global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a)
+template <int D, int WAVES, bool SCORES>
+__global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_decode(Kv16AttnArgs a)
 {
     constexpr int NB = D / 32, NT = D / 16;      // blocks of a key, tiles of a value's columns
     constexpr int HALF = 32;                     // positions of half a page
-    __shared__ float s_o[KD_WAVES][16][D + 4];
-    __shared__ float s_m[KD_WAVES][16], s_l[KD_WAVES][16], s_w[KV16_PAGE];
+    extern __shared__ uintx4 kd_smem[];
+    float (*const s_o)[16][D + 4] = reinterpret_cast<float (*)[16][D + 4]>(kd_smem);      // of each wave
+    __shared__ float s_m[WAVES][16], s_l[WAVES][16], s_w[KV16_PAGE];
     __shared__ unsigned s_odd;
 
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
@@ -191,14 +192,14 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
     const Sight mine = sight_of(a, rq, col / group);
     const Sight low = sight_of(a, rq, 0), high = sight_of(a, rq, rq.n - 1);
 
-    // This wave's half of pages c0 + wv / 2, c0 + wv / 2 + 2, ...; an entry that is no page: -1.  Loads are unconditional (a page that is not there: page 0), so that nothing
+    // This wave's half of pages c0 + wv / 2, then every WAVES / 2-th; an entry that is no page: -1.  Loads are unconditional (a page that is not there: page 0), so that nothing
     // waits for a load but what uses it.
-    const int half = wv & 1, v0 = c0 + (wv >> 1), n_it = (c1 - v0 + 1) >> 1;
+    const int half = wv & 1, v0 = c0 + (wv >> 1), n_it = (c1 - v0 + WAVES / 2 - 1) / (WAVES / 2);
     int entries = -1;                            // of the 64 pages from iteration `it` & ~63 on, one per lane
     const int* const table = a.page_table + (size_t)b * a.max_pages;
     auto page_at = [&](int it) {                 // asked for in order
         if ((it & 63) == 0) {
-            const int v = v0 + (it + lane) * 2;
+            const int v = v0 + (it + lane) * (WAVES / 2);
             entries = v < c1 ? table[page_number(rq, v)] : -1;
             asm volatile("" : "+v"(entries));    // waited for here, and not in every iteration behind whatever else is in flight
         }
@@ -234,7 +235,7 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
     for (int t = 0; t < NT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
     for (int it = 0; it < n_it; ++it) {
-        const int number = page_number(rq, v0 + it * 2);
+        const int number = page_number(rq, v0 + it * (WAVES / 2));
         const int next = it + 1 < n_it ? page_at(it + 1) : -1;
         const bool there = page >= 0;
         const int base = number * KV16_PAGE + half * HALF;
@@ -337,25 +338,25 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
             if (d == 0) { po[D] = mn; po[D + 1] = po[D + 2] = lf; }
         }
     };
-    auto merge = [&](int c, float (&cw)[KD_WAVES], float& lf) {      // fixed order: waves 0..3
+    auto merge = [&](int c, float (&cw)[WAVES], float& lf) {      // fixed order: waves 0..3
         float mn = s_m[0][c];
 #pragma unroll
-        for (int w = 1; w < KD_WAVES; ++w) mn = __builtin_fmaxf(mn, s_m[w][c]);
+        for (int w = 1; w < WAVES; ++w) mn = __builtin_fmaxf(mn, s_m[w][c]);
         const float ms = mn == -__builtin_inff() ? 0.f : mn;
         lf = 0.f;
 #pragma unroll
-        for (int w = 0; w < KD_WAVES; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             cw[w] = __builtin_amdgcn_exp2f(s_m[w][c] - ms);
             lf += s_l[w][c] * cw[w];
         }
         return mn;
     };
-    for (int idx = tid; idx < rows * D; idx += KD_THREADS) {
+    for (int idx = tid; idx < rows * D; idx += 64 * WAVES) {
         const int c = idx / D, d = idx % D;
-        float cw[KD_WAVES], lf, of = 0.f;
+        float cw[WAVES], lf, of = 0.f;
         const float mn = merge(c, cw, lf);
 #pragma unroll
-        for (int w = 0; w < KD_WAVES; ++w) of += s_o[w][c][d] * cw[w];
+        for (int w = 0; w < WAVES; ++w) of += s_o[w][c][d] * cw[w];
         // (weights are 2^WEIGHT_LOG2 times what they stand for, all of them)
         if (finite(of)) finish(c, d, of, lf, mn);
         else atomicOr(&s_odd, 1u << c);
@@ -364,9 +365,9 @@ __global__ __launch_bounds__(KD_THREADS, 2) void kv16_attn_decode(Kv16AttnArgs a
     const unsigned odd = s_odd;
     for (int c = 0; c < rows; ++c) {
         if (!(odd >> c & 1)) continue;           // (uniform)
-        float cw[KD_WAVES], lf;
+        float cw[WAVES], lf;
         const float mn = merge(c, cw, lf);
-        const float of = slow_row<D, KD_THREADS>(a, rq, b, g, row_of_column(c), c / group, c0, c1, mn, s_w, lf);
+        const float of = slow_row<D, 64 * WAVES>(a, rq, b, g, row_of_column(c), c / group, c0, c1, mn, s_w, lf);
         if (tid < D) finish(c, tid, of * 512.0f, lf * 512.0f, mn);
     }
 }
@@ -1098,17 +1099,22 @@ void launch_prompt(const Kv16AttnArgs& a, dim3 grid, hipStream_t stream)
     hipLaunchKernelGGL((kv16_attn_prompt<D, KP_WAVES, STATS>), grid, dim3(64 * KP_WAVES), (KP_LDS<D, KP_WAVES>), stream, a);
 }
 
-template <int D>
+template <int D, int WAVES>
 void launch_few(const Kv16AttnArgs& a, hipStream_t stream)
 {
+    static std::once_flag attr_once;
+    std::call_once(attr_once, [] {
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&kv16_attn_decode<D, WAVES, false>), hipFuncAttributeMaxDynamicSharedMemorySize, KD_LDS<D, WAVES>);
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&kv16_attn_decode<D, WAVES, true>), hipFuncAttributeMaxDynamicSharedMemorySize, KD_LDS<D, WAVES>);
+    });
     const dim3 grid((unsigned)a.Hkv, (unsigned)a.B, (unsigned)a.nsplit);
     const int combining = combine_blocks<D>(a), weighing = (a.max_pages * (KV16_PAGE / 4) + KC_THREADS - 1) / KC_THREADS;
     if (a.scores) {
-        hipLaunchKernelGGL((kv16_attn_decode<D, true>), grid, dim3(KD_THREADS), 0, stream, a);
+        hipLaunchKernelGGL((kv16_attn_decode<D, WAVES, true>), grid, dim3(64 * WAVES), (KD_LDS<D, WAVES>), stream, a);
         hipLaunchKernelGGL((kv16_attn_weigh<D>), dim3((unsigned)(weighing + (combining + a.Hkv - 1) / a.Hkv), (unsigned)a.Hkv, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a, weighing);
         return;
     }
-    hipLaunchKernelGGL((kv16_attn_decode<D, false>), grid, dim3(KD_THREADS), 0, stream, a);
+    hipLaunchKernelGGL((kv16_attn_decode<D, WAVES, false>), grid, dim3(64 * WAVES), (KD_LDS<D, WAVES>), stream, a);
     if (combining) hipLaunchKernelGGL((kv16_attn_combine<D>), dim3((unsigned)combining, (unsigned)a.B), dim3(KC_THREADS), 0, stream, a);
 }
 
@@ -1125,7 +1131,8 @@ void launch_many(const Kv16AttnArgs& a, hipStream_t stream)
 template <int D>
 hipError_t launch(const Kv16AttnArgs* few, const Kv16AttnArgs* many, hipStream_t stream)
 {
-    if (few) launch_few<D>(*few, stream);
+    if (few && few->wide) launch_few<D, 8>(*few, stream);
+    else if (few) launch_few<D, 4>(*few, stream);
     if (many) launch_many<D>(*many, stream);
     if (many && many->weights_out) {
         const dim3 pages((unsigned)(many->max_pages * many->Hkv), (unsigned)many->B);

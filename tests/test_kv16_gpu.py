@@ -275,6 +275,14 @@ def test_weights_add_to_what_was_there(thi):
         assert np.array_equal(got[written], want[written]) and np.array_equal(got[~written].astype(np.float32), before[~written])
 
 
+@pytest.mark.parametrize("D,weights", [(64, False), (64, True), (128, True)])
+def test_more_requests_than_run_at_once(thi, D, weights):
+    """Cache heads of all requests that are more than three times the compute units, with a long table: workgroups of eight waves."""
+    lens = [1300 if D == 64 else 700] + [(7 * b) % 150 for b in range(96)]
+    check_attention(thi, attention_case(D, 8, 8, D, lens, [1] * 97), decode=True, weights=weights)
+    check_attention(thi, attention_case(D + 1, 16, 8, D, lens, [1] * 97), 100, 3, decode=True, weights=weights)
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (100, 70)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_weights_of_many_pages(thi, D, window, sinks):
