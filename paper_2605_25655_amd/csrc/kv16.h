@@ -55,7 +55,7 @@ struct Kv16AttnArgs {
     int tiles;                       // of KV16_TILE_ROWS rows
     int nsplit, min_chunk;           // chunks per request at most, pages per chunk at least
     int num_cus;
-    bool wide;                       // eight waves to a workgroup of few rows, not four
+    bool wide, sorted;               // few rows: eight waves to a workgroup, not four; requests by their length
 };
 constexpr int KV16_MAX_SPLIT = 64;
 constexpr int KV16_FEW_ROWS = 16, KV16_TILE_ROWS = 128;

@@ -18,8 +18,9 @@ constexpr size_t MAX_TILES = 1 << 23;   // of a request's rows, times cache head
 constexpr int MAX_KEPT = 1 << 28, MAX_TOKENS = 1 << 28;      // positions of a row that has been evicted from; tokens of a store: the same
 constexpr long MAX_WEIGHED = 1 << 23;   // pages of a row of the table times cache heads, with weights: the same
 
-// Pages of a chunk at least, chunks' workgroups for every compute unit, and tables times columns that are not cut (plan)
-constexpr int CHUNK = 4, FEW_PER_CU = 3, MANY_PER_CU = 2, FEW_UNCUT = 1280, APART = 72;
+// Pages of a chunk at least, chunks' workgroups for every compute unit, tables times columns that are not cut, pages in sight from which on requests of few rows are dealt apart, and requests and
+// pages from which on they are dealt by length (plan)
+constexpr int CHUNK = 4, FEW_PER_CU = 3, MANY_PER_CU = 2, FEW_UNCUT = 1280, APART = 72, SORTED = 4, SORTED_PAGES = 32;
 
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -66,6 +67,8 @@ size_t bytes_of_scores(int B, int Hq, int Hkv, int max_q, int max_pages)
 //     2 x 760 of 64/8 (past it): 11.4 10.8
 //   few rows, four, eight waves a workgroup, where there are more of them than the compute units hold: 32 x 2048 of 32/32: 110.5 107.0; 64 x 2000 of these 204 196; 96 x 3000 of 64/8: 117 105; 20 x 2000
 //     of 40/40: 82.6 75.1; where there are not: 24 x 4000 of 32/32: 150 155; 16 x 4000 112 116; 24 x 5000 of 64/8: 50.0 53.3; and of short tables (not past FEW_UNCUT), 32 x 500 of 32/32: 32.0 34.9
+//   in the order of the batch, by length: 24 x 5000 of 64/8: 50.1 45.7; 64 x 6000: 160 146; 30 x 8000: 104 102; 16 x 32000, 4096 seen: 47.6 48.4; 32 x 2048 of 32/32: 106.8 108.0; of fewer or shorter
+//     ones, 3 x 131000: 86.0 86.1; 8 x 1000: 12.6 13.2
 void plan(Kv16AttnArgs& a, bool few, int num_cus)
 {
     a.group = a.Hq / a.Hkv;
@@ -79,6 +82,7 @@ void plan(Kv16AttnArgs& a, bool few, int num_cus)
     a.nsplit = (int)(n > most ? most : n);
     a.num_cus = num_cus;
     a.wide = few && items > (long)FEW_PER_CU * num_cus && (long)a.max_pages * a.D > FEW_UNCUT;
+    a.sorted = few && a.B >= SORTED && a.B <= 64 && a.max_pages >= SORTED_PAGES;
 }
 size_t rows_of(const Kv16AttnArgs& a) { return a.nsplit > 1 ? (size_t)a.B * a.part_q * a.Hq * a.nsplit : 0; }
 // Are requests of few rows in a call of more dealt as if they were alone?  Some has to be there, by the number of tokens, and what a row sees has to be APART pages at least, for a tile of

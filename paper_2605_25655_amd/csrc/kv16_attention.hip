@@ -144,6 +144,19 @@ __device__ __forceinline__ float slow_row(const Kv16AttnArgs& a, const Request& 
 template <int D, int WAVES> constexpr int KD_LDS = WAVES * 16 * (D + 4) * 4;
 constexpr float WEIGHT_LOG2 = 9.0f;              // weights are held as 2^9 p of a maximum that may lag by 2^6 (fp16 ends at 2^16)
 
+// The n-th request by length, the longest first, of up to 64.  Workgroups that follow each other by as many as there are compute units share one, so with chunks in this order, every second one backwards,
+// each has long and short ones: 24 requests of up to 5000 positions, 64/8 heads of 128, 50 -> 46 us, with weights 64 -> 57; 64 of 6000 160 -> 146.
+__device__ __forceinline__ int request_in_order(const Kv16AttnArgs& a, int n)
+{
+    const int lane = threadIdx.x & 63, len = lane < a.B ? a.seq_lens[lane] : 0;
+    int before = 0;
+    for (int i = 0; i < a.B; ++i) {
+        const int other = __builtin_amdgcn_readlane(len, i);
+        before += other > len || (other == len && i < lane);
+    }
+    return __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < a.B && before == n));      // (the places are a permutation, so some lane has this one)
+}
+
 // Two fp16 summands of four weights (the large one truncated, so that the small one is not negative).
 __device__ __forceinline__ void split_weights(const float (&w)[4], half4& large, half4& small)
 {
@@ -171,7 +184,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_decode(Kv16AttnArgs a
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = a.group;
-    const int g = blockIdx.x, b = blockIdx.y, chunk = blockIdx.z;
+    const int g = blockIdx.x, chunk = blockIdx.z, b = a.sorted ? request_in_order(a, chunk & 1 ? a.B - 1 - (int)blockIdx.y : (int)blockIdx.y) : (int)blockIdx.y;
     const Request rq = find_request(a, b);
     const int rows = rq.n * group;               // at most 16: row r is token r / group, head r % group
     if (rows <= 0 || !ours(a, rq)) return;
