@@ -52,6 +52,29 @@ size_t bytes_of_scores(int B, int Hq, int Hkv, int max_q, int max_pages)
     return round_up((size_t)B * q * Hq * max_pages * KV16_PAGE * sizeof(float));
 }
 
+// The most pages that a request's rows look at
+long pages_in_sight(const Kv16AttnArgs& a)
+{
+    const long seen = a.window ? ((long)a.window + a.sinks + a.max_q) / KV16_PAGE + 3 : a.max_pages;
+    return seen < a.max_pages ? seen : a.max_pages;
+}
+// Into how many chunks, at most `most`, requests of more rows are cut, by what that takes in us: a page 1.4 where each workgroup has a compute unit to itself, 1.9 where some share one, and 1.2 for each of those that do
+// where most share; for partial results a launch and their bytes (of one chunk: `bytes`), written and read.
+int chunks_worth(long items, long pages, long bytes, int most, int num_cus)
+{
+    int best = 1;
+    double least = 0;
+    for (int n = 1; n <= most; ++n) {
+        const double each = 1.2 * (double)(items * n) / num_cus, page = items * n <= num_cus ? 1.4 : each > 1.9 ? each : 1.9;
+        const double time = (double)((pages + n - 1) / n) * page + (n > 1 ? 5.0 + n * (double)bytes / 5e6 : 0.0);
+        if (n == 1 || time < least) {
+            best = n;
+            least = time;
+        }
+    }
+    return best;
+}
+
 // How the rows are dealt: up to KV16_FEW_ROWS of a request and cache head to kv16_attn_decode, more, KV16_TILE_ROWS at a time, to kv16_attn_prompt; and where that gives fewer
 // workgroups than the compute units hold, requests are cut into chunks of at least CHUNK pages, whose results one more launch puts together.
 // Measured, us a pass (requests of up to that many positions each; 64/8: query heads / cache heads of 128 columns):
@@ -59,8 +82,10 @@ size_t bytes_of_scores(int B, int Hq, int Hkv, int max_q, int max_pages)
 //     28.0 25.9 25.9 25.9; 64 rows: 38 38 38 54; 30 rows of 2 heads of 64 columns, 8 x 2000: 17.3 17.3 15.9 15.9.  16 is also what one matrix tile holds.
 //   two, three, four workgroups for a compute unit (which holds three): 64/8, 24 x 5000: 57.6 50.1 47.9; 3 x 131000: 85 86 123; 16 x 32000, 4096 seen: 46.9 48.0 49.0; 32/32, 5 x 1500: 22.1
 //     22.8 20.8
-//   more rows: one, two, three (it holds two): 300 tokens of 64/8 behind 7700: 161 113 119; 128 of 32/32 behind 1872: 30 29 29; 64 of 64/8, 3 x 6000: 85 56 60; 128 of 64/8, 5 x 20000, 4096
-//     seen: 128 128 111; 1000 of 32/32 behind 5000: 128 139 149
+//   more rows: up to one, two, three workgroups for a compute unit (it holds two): 300 tokens of 64/8 behind 7700: 161 113 119; 128 of 32/32 behind 1872: 30 29 29; 64 of 64/8, 3 x 6000: 85 56
+//     60; 128 of 64/8, 5 x 20000, 4096 seen: 128 128 111, but 800 of 40/40 behind 3200: 99 99 126; 1000 of 32/32 behind 5000: 128 139 149
+//   more rows, up to two for a compute unit, and as many as chunks_worth() says: 157 of 40/40, 2 x 353: 29.0 18.6; 94 of 64/8, 610 seen of 7020: 39.9 24.7; 700 of 32/32, a prompt: 43.3 23.9; 642 of 8
+//     heads of 64 columns, 5 prompts: 27.6 17.3; those above: the same
 //   chunks of 2, 4, 8 pages at least: 128 tokens of 32/32 behind 1872: 36.1 25.5 29.8; 300 of 64/8 behind 7700: 110 111 113; one of 64/8, 1 x 3000: 11.3 12.0 13.4; 10 rows of 8 heads of 64
 //     columns, 8 x 2000: 14.3 12.5 12.3
 //   not cut, cut: 2 x 468 of 8 heads of 64 columns: 6.8 9.9; 2 x 1200 of these: 9.1 10.0; 2 x 1500 of these (past FEW_UNCUT): 10.4 8.5; 4 x 600 of 32/32: 10.3 13.1; 2 x 600 of 64/8: 10.5 11.6;
@@ -74,12 +99,13 @@ void plan(Kv16AttnArgs& a, bool few, int num_cus)
     a.group = a.Hq / a.Hkv;
     a.tiles = (int)tiles_of(a.Hq, a.Hkv, a.max_q);
     a.part_q = few && KV16_FEW_ROWS / a.group < a.max_q ? KV16_FEW_ROWS / a.group : a.max_q;
-    const long items = (long)a.B * a.Hkv * (few ? 1 : a.tiles);
-    const long most = few && (long)a.max_pages * a.D <= FEW_UNCUT ? 1 : (a.max_pages + CHUNK - 1) / CHUNK;
+    const long items = (long)a.B * a.Hkv * (few ? 1 : a.tiles), pages = pages_in_sight(a);
+    const long most = few && pages * a.D <= FEW_UNCUT ? 1 : (pages + CHUNK - 1) / CHUNK;
     a.min_chunk = CHUNK;
     long n = (long)(few ? FEW_PER_CU : MANY_PER_CU) * num_cus / items;
     n = n < 1 ? 1 : n > KV16_MAX_SPLIT ? KV16_MAX_SPLIT : n;
-    a.nsplit = (int)(n > most ? most : n);
+    n = n > most ? most : n;
+    a.nsplit = (int)(few ? n : chunks_worth(items, pages, (long)a.B * a.max_q * a.Hq * kv16_part(a.D) * 8, (int)n, num_cus));
     a.num_cus = num_cus;
     a.wide = few && items > (long)FEW_PER_CU * num_cus && (long)a.max_pages * a.D > FEW_UNCUT;
     a.sorted = few && a.B >= SORTED && a.B <= 64 && a.max_pages >= SORTED_PAGES;
@@ -91,8 +117,8 @@ size_t rows_of(const Kv16AttnArgs& a) { return a.nsplit > 1 ? (size_t)a.B * a.pa
 // 17 x 4000 of 32/32: 235 / 249; 9 x 2000: 57 / 74; 9 x 2000 of 32/32: 65 / 104.
 bool apart(const Kv16AttnArgs& a)
 {
-    const long q_few = KV16_FEW_ROWS / a.group, seen = a.window ? ((long)a.window + a.sinks + a.max_q) / KV16_PAGE + 3 : a.max_pages;
-    return q_few > 0 && a.T <= (a.B - 1L) * a.max_q + q_few && (seen < a.max_pages ? seen : a.max_pages) >= APART;
+    const long q_few = KV16_FEW_ROWS / a.group;
+    return q_few > 0 && a.T <= (a.B - 1L) * a.max_q + q_few && pages_in_sight(a) >= APART;
 }
 
 int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }

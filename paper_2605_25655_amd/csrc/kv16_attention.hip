@@ -385,13 +385,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_decode(Kv16AttnArgs a
     }
 }
 
-// The chunks' (sum, maximum, weight) triples of a request's rows, (token, head) pairs in the order of q.  A group of D threads has a row of up to eight chunks to itself; of more, all
+// The chunks' (sum, maximum, weight) triples of a request's rows, (token, head) pairs in the order of q.  A group of D threads has a row of up to eight chunks to itself, or any where there are many rows; else all
 // groups take every GROUPS-th chunk each, eight loads in flight, and meet in LDS: a fixed order.  The loads come before anything is known of the request (what lies behind its last
 // chunk is the workspace's, and not used).  16 requests of 64 heads and six chunks: 4.6 us (a row for a workgroup: 5.2).
-constexpr int KC_THREADS = 512, KC_AHEAD = 8;
+constexpr int KC_THREADS = 512, KC_AHEAD = 8, KC_ROWS = 4096;
+template <int D> __host__ __device__ bool combine_alone(const Kv16AttnArgs& a) { return a.nsplit <= KC_AHEAD || (long)a.B * a.Hq * a.part_q >= KC_ROWS; }
 template <int D> __host__ __device__ int combine_blocks(const Kv16AttnArgs& a)
 {
-    const int rows = a.Hq * a.part_q, each = a.nsplit <= KC_AHEAD ? KC_THREADS / D : 1;
+    const int rows = a.Hq * a.part_q, each = combine_alone<D>(a) ? KC_THREADS / D : 1;
     return a.nsplit > 1 ? (rows + each - 1) / each : 0;
 }
 template <int D>
@@ -400,7 +401,7 @@ __device__ __forceinline__ void combine_rows(const Kv16AttnArgs& a, int block, i
     constexpr int GROUPS = KC_THREADS / D;
     __shared__ float s_o[GROUPS][D], s_w[GROUPS][KV16_MAX_SPLIT];
     const int lane = threadIdx.x & 63, d = threadIdx.x % D, grp = threadIdx.x / D;
-    const bool alone = a.nsplit <= KC_AHEAD;
+    const bool alone = combine_alone<D>(a);
     if (block >= combine_blocks<D>(a)) return;
     const int row = alone ? block * GROUPS + grp : block, chunk = alone ? 0 : grp, stride = alone ? 1 : GROUPS, own = alone ? grp : 0;
     const bool exists = row < a.part_q * a.Hq;
