@@ -55,6 +55,7 @@ struct Kv16AttnArgs {
     int tiles;                       // of KV16_TILE_ROWS rows
     int nsplit, min_chunk;           // chunks per request at most, pages per chunk at least
     int num_cus;
+    int parts, part_tiles;           // of the rows, so many tiles of 16 each, whose weights are summed by themselves: [parts][B][Hkv][64 max_pages] in `part`, when that is done with
     bool wide, sorted;               // few rows: eight waves to a workgroup, not four; requests by their length
 };
 constexpr int KV16_MAX_SPLIT = 64;

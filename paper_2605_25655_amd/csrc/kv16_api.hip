@@ -121,6 +121,20 @@ bool apart(const Kv16AttnArgs& a)
     return q_few > 0 && a.T <= (a.B - 1L) * a.max_q + q_few && pages_in_sight(a) >= APART;
 }
 
+// Parts of the rows whose weights are summed by themselves: of at least WEIGHED_ROWS rows, and no more workgroups than WEIGHED_GROUPS for it, so that their sums, of a page each, stay small.
+// In one, of at least 4096, 2048, 1024 rows, us a pass with weights: a prompt of 2001 of 64/8 heads 168 158 148 147; of 2696, 86 seen and one sink (whose page all rows look at) 192 113 101 104; of 800
+// 65 56 51 51; more workgroups anyway, a prompt of 2001 of 32/32 86 86 87 91; of 4000 248 254 259 263; 6 of 4399, 57 seen 292 319 338 381.
+constexpr long WEIGHED_ROWS = 2048, WEIGHED_GROUPS = 2048;
+long parts_of(int Hq, int Hkv, int max_q) { return ((long)max_q * (Hq / Hkv) + WEIGHED_ROWS - 1) / WEIGHED_ROWS; }
+size_t bytes_of_parts(int Hq, int Hkv, int max_q) { return parts_of(Hq, Hkv, max_q) < 2 ? 0 : WEIGHED_GROUPS * KV16_PAGE * sizeof(float); }
+void plan_weights(Kv16AttnArgs& a)
+{
+    const long most = WEIGHED_GROUPS / ((long)a.B * a.Hkv * a.max_pages), n = parts_of(a.Hq, a.Hkv, a.max_q), parts = n < most ? n : most > 1 ? most : 1;
+    const long tiles = ((long)a.max_q * a.group + 15) / 16;
+    a.part_tiles = (int)((tiles + parts - 1) / parts);
+    a.parts = (int)((tiles + a.part_tiles - 1) / a.part_tiles);
+}
+
 int finish(hipError_t e) { return e == hipSuccess ? THI_OK : THI_ERR_HIP; }
 
 }  // namespace
@@ -161,7 +175,10 @@ size_t thi_kv16_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, 
     if (B < 1 || B > 65535 || T < 1 || !heads_ok(Hq, Hkv, D) || max_q < 1 || max_q > T || max_q > 65535 || max_pages < 1 || max_pages > MAX_PAGES ||
         tiles_of(Hq, Hkv, max_q) * Hkv > MAX_TILES || (weights && (long)max_pages * Hkv > MAX_WEIGHED))
         return 0;
-    return bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D) + (weights ? bytes_of_stats(B, Hq, Hkv, max_q) + bytes_of_queries(B, Hq, Hkv, D, max_q) + bytes_of_scores(B, Hq, Hkv, max_q, max_pages) : 0);
+    const size_t part = bytes_of_rows(most_rows(B, Hq, Hkv, max_q, max_pages, device_cu_count()), D);
+    if (!weights) return part;
+    const size_t sums = bytes_of_parts(Hq, Hkv, max_q);
+    return (sums > part ? sums : part) + bytes_of_stats(B, Hq, Hkv, max_q) + bytes_of_queries(B, Hq, Hkv, D, max_q) + bytes_of_scores(B, Hq, Hkv, max_q, max_pages);
 }
 
 int thi_kv16_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, int window, int sinks,
@@ -197,6 +214,7 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
     a.scores = scores ? (float*)((char*)workspace + stats) : nullptr;
     a.part = (float*)((char*)workspace + stats + queries + scores);
     plan(a, few, device_cu_count());
+    if (weights_out && !few) plan_weights(a);
     size_t rows = rows_of(a);
     Kv16AttnArgs other = a;                      // of requests of few rows in a call of more; their partial results are put together before the others' are there
     const bool both = !few && apart(a);
@@ -206,7 +224,8 @@ int thi_kv16_attention(const void* q, const void* pages, const int* page_table, 
         a.whose = Kv16AttnArgs::THOSE_OF_MORE;
         rows = rows_of(other) > rows ? rows_of(other) : rows;
     }
-    if (workspace_bytes < need || workspace_bytes < stats + queries + scores + bytes_of_rows(rows, D)) return THI_ERR_WORKSPACE;
+    const size_t sums = a.parts > 1 ? (size_t)a.parts * B * Hkv * max_pages * KV16_PAGE * sizeof(float) : 0, part = bytes_of_rows(rows, D);
+    if (workspace_bytes < need || workspace_bytes < stats + queries + scores + (sums > part ? sums : part)) return THI_ERR_WORKSPACE;
     (void)hipGetLastError();
     return finish(launch_kv16_attention(few ? &a : both ? &other : nullptr, few ? nullptr : &a, (hipStream_t)hip_stream));
 }

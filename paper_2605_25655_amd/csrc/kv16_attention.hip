@@ -978,7 +978,8 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_weigh(Kv16AttnArgs a, in
 }
 
 // More rows: the scores are made again.  A workgroup takes a page of a cache head, whose keys stay in its waves' registers (the A operand); the rows that see any of it come by, 16
-// at a time, every WAVES-th 16 in a wave.  Weights in fp32, added up per lane (a lane has one row of each 16), then over lanes and waves: a fixed order.
+// at a time, every WAVES-th 16 in a wave.  Weights in fp32, added up per lane (a lane has one row of each 16), then over lanes and waves: a fixed order.  Where the rows are in parts (plan_weights),
+// one more launch adds their sums.
 // For each 16 rows and 64 positions 262 kFLOP of matrix products (D = 128), 1024 exponentials and 4 KB of queries; the last is what bounds it.  So kv16_attn_prompt leaves the queries as operands, a
 // KB at a time: from where they stand, 16 rows a load, the rows of 32 heads 8 KB apart fall on one channel of the cache (2001 tokens of 32/32 heads of 128, all of the call: 102 us, like this 87; 80 to 85 with the attention as it is now).
 // Two pages in a workgroup, which halve the queries' way, leave too few of them (2001 tokens of 64/8 heads 317 us against 212); products of the next rows between the weights of the last: no gain
@@ -990,7 +991,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs 
     constexpr int NB = D / 32, TILES = 4, SPAN = KV16_PAGE;      // tiles of 16 positions
     __shared__ float s_sum[WAVES][4 * TILES][64];
     const int tid = threadIdx.x, lane = tid & 63, lo = lane & 15, hi = lane >> 4, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int number = blockIdx.x / (unsigned)a.Hkv, g = blockIdx.x - number * a.Hkv, b = blockIdx.y;      // the first pages first: the most rows see them
+    const int number = blockIdx.x / (unsigned)a.Hkv, g = blockIdx.x - number * a.Hkv, b = blockIdx.y, part = blockIdx.z;      // the first pages first: the most rows see them
     const Request rq = find_request(a, b);
     const int p0 = number * KV16_PAGE, group = a.group, before = rq.len - rq.n;
     if (p0 >= rq.len) return;
@@ -1013,7 +1014,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs 
         last = most < last ? (most < 0 ? 0 : (int)most) : last;
     }
     // rows of (token, head) pairs, 16 at a time as the attention left them
-    const int tile0 = first * group / 16 + wv, tile_end = (last * group + 15) / 16;
+    const int tile_first = first * group / 16, tile_last = (last * group + 15) / 16, part_first = part * a.part_tiles, part_last = part_first + a.part_tiles;
+    const int tile0 = (tile_first > part_first ? tile_first : part_first) + wv, tile_end = tile_last < part_last ? tile_last : part_last;
     int token = (tile0 * 16 + lo) / group, rest = (tile0 * 16 + lo) % group;
     const int token_step = 16 * WAVES / group, rest_step = 16 * WAVES - token_step * group;
     const size_t row0 = stats_row(a, b, g, 0) + tile0 * 16;
@@ -1074,7 +1076,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs 
 #pragma unroll
         for (int i = 0; i < 4 * TILES; ++i) asm volatile("" : "+v"(sum[i]));      // (now: next to the following products)
     };
-    const int turns = there && first < last ? (tile_end - tile0 + WAVES - 1) / WAVES : 0;
+    const int turns = there && first < last && tile0 < tile_end ? (tile_end - tile0 + WAVES - 1) / WAVES : 0;
     if (turns > 0) {
         Rows one, other;
         ask(one);
@@ -1100,7 +1102,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs 
     const int pos = p0 + tid;
     if (pos >= rq.len) return;
     const size_t at = ((size_t)b * a.Hkv + g) * a.max_pages * KV16_PAGE + pos;
-    a.weights_out[at] = (a.weights_in && pos < before ? a.weights_in[at] : 0.f) + total;
+    if (a.parts > 1) a.part[(size_t)part * a.B * a.Hkv * a.max_pages * KV16_PAGE + at] = total;
+    else a.weights_out[at] = (a.weights_in && pos < before ? a.weights_in[at] : 0.f) + total;
+}
+
+// The sums of the parts of the rows.
+constexpr int KA_THREADS = 256;
+__global__ __launch_bounds__(KA_THREADS) void kv16_attn_add(Kv16AttnArgs a)
+{
+    const int p0 = (blockIdx.x * KA_THREADS + threadIdx.x) * 4, g = blockIdx.y, b = blockIdx.z;
+    const size_t each = (size_t)a.B * a.Hkv * a.max_pages * KV16_PAGE, at = ((size_t)b * a.Hkv + g) * a.max_pages * KV16_PAGE + p0;
+    const Request rq = find_request(a, b);
+    if (p0 >= rq.len) return;
+    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int part = 0; part < a.parts; ++part) sum += *reinterpret_cast<const floatx4*>(a.part + part * each + at);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (p0 + k < rq.len) a.weights_out[at + k] = (a.weights_in && p0 + k < rq.len - rq.n ? a.weights_in[at + k] : 0.f) + sum[k];
 }
 
 template <int D, bool STATS>
@@ -1149,9 +1168,11 @@ hipError_t launch(const Kv16AttnArgs* few, const Kv16AttnArgs* many, hipStream_t
     else if (few) launch_few<D, 4>(*few, stream);
     if (many) launch_many<D>(*many, stream);
     if (many && many->weights_out) {
-        const dim3 pages((unsigned)(many->max_pages * many->Hkv), (unsigned)many->B);
-        if ((long)many->max_pages * many->Hkv * many->B <= KW_PER_CU * many->num_cus) hipLaunchKernelGGL((kv16_attn_weights<D, 8>), pages, dim3(512), 0, stream, *many);
+        const dim3 pages((unsigned)(many->max_pages * many->Hkv), (unsigned)many->B, (unsigned)many->parts);
+        if ((long)many->max_pages * many->Hkv * many->B * many->parts <= KW_PER_CU * many->num_cus) hipLaunchKernelGGL((kv16_attn_weights<D, 8>), pages, dim3(512), 0, stream, *many);
         else hipLaunchKernelGGL((kv16_attn_weights<D, 4>), pages, dim3(256), 0, stream, *many);
+        if (many->parts > 1)
+            hipLaunchKernelGGL(kv16_attn_add, dim3((unsigned)((many->max_pages * (KV16_PAGE / 4) + KA_THREADS - 1) / KA_THREADS), (unsigned)many->Hkv, (unsigned)many->B), dim3(KA_THREADS), 0, stream, *many);
     }
     return hipGetLastError();
 }

@@ -136,6 +136,8 @@ static void look(const Kv16AttnArgs& a, long q)
     NEED(a.tiles * (long)KV16_TILE_ROWS >= a.max_q * (long)a.group && a.part_q == q);
     NEED(a.nsplit == 1 || (char*)a.part + (size_t)a.B * q * a.Hq * a.nsplit * kv16_part(a.D) * 4 <= space + given);
     NEED((char*)a.part <= space + given);
+    NEED(a.parts <= 1 || (char*)a.part + (size_t)a.parts * a.B * a.Hkv * a.max_pages * 256 <= space + given);
+    NEED(!a.queries || a.whose == Kv16AttnArgs::THOSE_OF_FEW_ROWS || (a.parts >= 1 && a.part_tiles >= 1 && (long)a.parts * a.part_tiles * 16 >= (long)a.max_q * a.group));
     NEED(!a.weights_out || ((char*)a.stats == space && space + rows * 8 <= (char*)a.part));
     NEED(!a.queries || ((char*)a.queries >= space + rows * 8 && (char*)a.queries + rows * a.D * 2 <= (char*)a.part));
     NEED(!a.scores || ((char*)a.scores >= space + rows * 8 && (char*)a.scores + (size_t)a.B * a.max_q * a.Hq * a.max_pages * 256 <= (char*)a.part));

@@ -294,6 +294,15 @@ def test_weights_of_many_pages(thi, D, window, sinks):
     check_attention(thi, d, window, sinks, weights=True)
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 3), (130, 70)])
+@pytest.mark.parametrize("Hq,Hkv,D", [(16, 2, 64), (16, 1, 128)])
+def test_weights_of_rows_in_parts(thi, Hq, Hkv, D, window, sinks):
+    """Weights of more rows of a cache head than one part has, next to requests of fewer, with weights from before."""
+    c = attention_case(70 + D, Hq, Hkv, D, [330, 90, 64], [330 if Hkv == 2 else 200, 17, 64])
+    before = np.random.default_rng(6).standard_normal((3, Hkv, c["table"].shape[1] * PAGE)).astype(np.float32)
+    check_attention(thi, c, window, sinks, weights_in=before)
+
+
 @pytest.mark.parametrize("new", [1, 4, 90])
 def test_missing_pages(thi, new):
     """Entries that are no page (-1, past the pool, negative) are positions that are not there: at the front, in the middle, at the end, all of them."""
