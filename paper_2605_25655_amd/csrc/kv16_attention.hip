@@ -1028,7 +1028,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_weights(Kv16AttnArgs 
     };
     int left = tile_end - tile0;                 // (the last ones are asked for again, for nobody)
     auto ask = [&](Rows& x) __attribute__((always_inline)) {
-        x.token = token;
+        x.token = left > 0 ? token : last;      // (behind the last tile: of nobody)
 #pragma unroll
         for (int k = 0; k < NB; ++k) x.q[k] = __builtin_bit_cast(half8, ld_cached(q + k * 512));
         x.stats = *reinterpret_cast<const float2*>(stats);
