@@ -76,20 +76,19 @@ __device__ __forceinline__ int kept_of(const Kv16EvictArgs& a, int b, int n, int
     return live < a.budget ? live : a.budget;
 }
 
-constexpr int KE_THREADS = 1024;
-
 // Who is evicted, which pages they get, and the tables and counts that follow: one workgroup.  What it writes and reads back is in LDS, too, as far as it fits: a chain of loads and stores is
 // what it takes its time for.
-constexpr int KE_ROWS = 1024, KE_PAGES = 8192;
+constexpr int KE_ROWS = 512, KE_PAGES = 4096;
 struct PlanSpace {
     int kept[KE_ROWS], begin[KE_ROWS], fresh[KE_PAGES];
 };
+template <int THREADS>
 __device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave, PlanSpace& s)
 {
     const Space ws = space_of(a);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int first_refs = tid < a.num_pages ? a.refs_in[tid] : 1;
-    for (int b = wave; b < a.rows; b += KE_THREADS / 64) {
+    for (int b = wave; b < a.rows; b += THREADS / 64) {
         const int kept = kept_of(a, b, length_of(a, b), lane);
         if (lane == 0) {
             ws.kept[b] = kept;
@@ -100,10 +99,10 @@ __device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave, PlanSpace& s)
     auto kept_by = [&](int b) { return b < KE_ROWS ? s.kept[b] : ws.kept[b]; };
     // pages that they ask for, one row behind the other
     long asked = 0;
-    for (int b0 = 0; b0 < a.rows; b0 += KE_THREADS) {
+    for (int b0 = 0; b0 < a.rows; b0 += THREADS) {
         const int b = b0 + tid, kept = b < a.rows ? kept_by(b) : -1;
         int total;
-        const int before = scan<KE_THREADS>(kept >= 0 ? pages_for(a, kept) : 0, s_wave, total);
+        const int before = scan<THREADS>(kept >= 0 ? pages_for(a, kept) : 0, s_wave, total);
         const long at = asked + before;
         if (b < a.rows) {
             const int begin = at > a.num_pages ? a.num_pages : (int)at;      // (further than any free page)
@@ -114,10 +113,10 @@ __device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave, PlanSpace& s)
     }
     // the lowest free pages
     int free_pages = 0;
-    for (int p0 = 0; p0 < a.num_pages; p0 += KE_THREADS) {
+    for (int p0 = 0; p0 < a.num_pages; p0 += THREADS) {
         const int p = p0 + tid, refs = p0 == 0 ? first_refs : p < a.num_pages ? a.refs_in[p] : 1;
         int total;
-        const int before = scan<KE_THREADS>(refs == 0 ? 1 : 0, s_wave, total);
+        const int before = scan<THREADS>(refs == 0 ? 1 : 0, s_wave, total);
         if (refs == 0) {
             ws.fresh[free_pages + before] = p;
             if (free_pages + before < KE_PAGES) s.fresh[free_pages + before] = p;
@@ -129,7 +128,7 @@ __device__ void evict_plan(const Kv16EvictArgs& a, int* s_wave, PlanSpace& s)
     __syncthreads();
     // Rows whose pages are there: the lengths, tables and counts that they leave with.  (counts by atomic operations on integers: the same in any order)
     int done = 0, left = 0;
-    for (int b = wave; b < a.rows; b += KE_THREADS / 64) {
+    for (int b = wave; b < a.rows; b += THREADS / 64) {
         const int kept = kept_by(b), n = length_of(a, b), need = kept >= 0 ? pages_for(a, kept) : 0, begin = b < KE_ROWS ? s.begin[b] : ws.begin[b];
         const bool moves = kept >= 0 && (long)begin + need <= free_pages;
         if (lane == 0) {
@@ -169,9 +168,10 @@ __device__ __forceinline__ unsigned order_of(float w)
 }
 
 // Which positions of a row a cache head of a layer keeps, in their order: a workgroup each (and one in front of them all for the plan, which nothing here waits for).  The k-th
-// largest weight by its bits, 11, 11 and 10 of them at a time from the top: with 8 at a time, most weights fall on a few counters.  A thread takes four neighbouring positions at a time.
+// largest weight by its bits, 11, 11 and 10 of them at a time from the top: with 8 at a time, most weights fall on a few counters.  A thread takes four neighbouring positions at a time, twice (with longer tables again and again).
 constexpr int KE_DIGIT = 11;
-__global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void kv16_evict_select(Kv16EvictArgs a)
 {
     constexpr int DIGITS = 3;
     union Shared {
@@ -179,18 +179,18 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
         PlanSpace plan;
     };
     __shared__ Shared shared;
-    __shared__ int s_wave[KE_THREADS / 64];
+    __shared__ int s_wave[THREADS / 64];
     __shared__ unsigned s_prefix;
     __shared__ int s_left, s_kept, s_sure;
     if (blockIdx.x == 0) {
-        if (blockIdx.y == 0 && blockIdx.z == 0) evict_plan(a, s_wave, shared.plan);
+        if (blockIdx.y == 0 && blockIdx.z == 0) evict_plan<THREADS>(a, s_wave, shared.plan);
         return;
     }
     const Space ws = space_of(a);
     const int tid = threadIdx.x, lane = tid & 63, g = blockIdx.x - 1, b = blockIdx.y, layer = blockIdx.z;
     const int n = length_of(a, b);
     if (n <= a.budget) return;
-    for (int i = tid; i < DIGITS << KE_DIGIT; i += KE_THREADS) shared.count[0][i] = 0;
+    for (int i = tid; i < DIGITS << KE_DIGIT; i += THREADS) shared.count[0][i] = 0;
     if (tid == 0) s_sure = 0;
     const size_t at = (((size_t)layer * a.rows + b) * a.Hkv + g) * a.max_pages * KV16_PAGE;
     const float* const weights = a.weights_in + at;
@@ -222,11 +222,11 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
     constexpr int HELD = 2;
     Four held[HELD];
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) held[i] = ask((i * KE_THREADS + tid) * 4);
+    for (int i = 0; i < HELD; ++i) held[i] = ask((i * THREADS + tid) * 4);
     auto each = [&](auto what) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < HELD; ++i) what(held[i]);
-        for (int p = (HELD * KE_THREADS + tid) * 4; p < n; p += KE_THREADS * 4) what(ask(p));
+        for (int p = (HELD * THREADS + tid) * 4; p < n; p += THREADS * 4) what(ask(p));
     };
     if (tid < 64) {
         const int kept = kept_of(a, b, n, lane);
@@ -251,15 +251,21 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
         });
         __syncthreads();
         if (turn == 0) want = s_kept - s_sure;
-        // from the top: thread 0 the two highest
-        const int hi = (1 << KE_DIGIT) - 1 - 2 * tid, c0 = count[hi], c1 = count[hi - 1];
-        int total;
-        const int above = scan<KE_THREADS>(c0 + c1, s_wave, total);
+        // from the top: thread 0 the highest
+        constexpr int PER = (1 << KE_DIGIT) / THREADS;
+        const int top = (1 << KE_DIGIT) - 1 - PER * tid;
+        int c[PER], sum = 0, total;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) sum += c[k] = count[top - k];
+        int above = scan<THREADS>(sum, s_wave, total);
         // the one counter with which the sum from the top reaches what is wanted (want 0: the highest; it is at most the number of candidates)
-        const bool first = above < want ? above + c0 >= want : (want == 0 && tid == 0), second = above + c0 < want && above + c0 + c1 >= want;
-        if (first || second) {
-            s_prefix = prefix | (unsigned)(first ? hi : hi - 1) << shift;
-            s_left = want - above - (first ? 0 : c0);
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if ((above < want && above + c[k] >= want) || (want == 0 && tid == 0 && k == 0)) {
+                s_prefix = prefix | (unsigned)(top - k) << shift;
+                s_left = want - above;
+            }
+            above += c[k];
         }
         __syncthreads();
         prefix = s_prefix;
@@ -279,7 +285,7 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
         }
         // (both counted at once: no more than 4096 of each)
         int total;
-        const int before = scan<KE_THREADS>(__builtin_popcount(keep) | __builtin_popcount(same) << 16, s_wave, total);
+        const int before = scan<THREADS>(__builtin_popcount(keep) | __builtin_popcount(same) << 16, s_wave, total);
         int rank = equal + (before >> 16), to = placed + (before & 0xffff) + (rank < want ? rank : want);
         placed += total & 0xffff;
         equal += total >> 16;
@@ -295,8 +301,8 @@ __global__ __launch_bounds__(KE_THREADS) void kv16_evict_select(Kv16EvictArgs a)
     };
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
-        if (i * KE_THREADS * 4 < n) place((i * KE_THREADS + tid) * 4, held[i]);
-    for (int p0 = HELD * KE_THREADS * 4; p0 < n; p0 += KE_THREADS * 4) place(p0 + tid * 4, ask(p0 + tid * 4));
+        if (i * THREADS * 4 < n) place((i * THREADS + tid) * 4, held[i]);
+    for (int p0 = HELD * THREADS * 4; p0 < n; p0 += THREADS * 4) place(p0 + tid * 4, ask(p0 + tid * 4));
 }
 
 // The move: a workgroup takes one fresh page of one cache head of a layer, 64 kept positions from wherever they were.  All that it reads is asked for at once, the pieces of 16 bytes of
@@ -379,9 +385,14 @@ size_t kv16_evict_words(int layers, int rows, int Hkv, int max_pages, int num_pa
     return 2 * (size_t)rows + num_pages + (size_t)layers * rows * Hkv * max_pages * KV16_PAGE;
 }
 
+constexpr int KE_SMALL_PAGES = 32, KE_SMALL_POOL = 8192;
 hipError_t launch_kv16_evict(const Kv16EvictArgs& a, hipStream_t stream)
 {
-    hipLaunchKernelGGL(kv16_evict_select, dim3((unsigned)a.Hkv + 1, (unsigned)a.rows, (unsigned)a.layers), dim3(KE_THREADS), 0, stream, a);
+    // Short tables: small workgroups, of which more run at once and which meet in less time (the plan's walk over a large pool would take longer).  1024, 256 threads, us a call: 33 rows of 48 positions
+    // brought to 8 in two layers of 40 heads 94 48; 28 of 1033 to 185 in three of 32 heads 279 231; 16 of 1500 to 300 in four of 8 heads 80.5 69.9; 9 of 1500 in two of 32 heads 105 94.
+    const dim3 lists((unsigned)a.Hkv + 1, (unsigned)a.rows, (unsigned)a.layers);
+    if (a.max_pages <= KE_SMALL_PAGES && a.num_pages <= KE_SMALL_POOL) hipLaunchKernelGGL((kv16_evict_select<256>), lists, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((kv16_evict_select<1024>), lists, dim3(1024), 0, stream, a);
     const long most = (long)a.max_pages * KV16_PAGE < a.budget ? (long)a.max_pages * KV16_PAGE : a.budget;
     const dim3 grid((unsigned)((most + KV16_PAGE - 1) / KV16_PAGE), (unsigned)a.Hkv, (unsigned)(a.rows * a.layers));
     if (a.D == 128) hipLaunchKernelGGL((kv16_evict_move<128>), grid, dim3(KE_MOVE), 0, stream, a);
