@@ -1,6 +1,6 @@
 // Requests of the fp16 cache brought back to a number of positions: which stay, fresh pages for them, and the move.  Memory-bound: kept keys and values are read and
 // written once, the accumulated weights read a few times, the later ones from the caches.  Two launches: the plan next to the selection, then the move.
-// Measured: 16 requests of up to 4000 positions brought to 1200 in four layers of 8 heads of 128, 201 us (21 + 180); two of up to 300 of 8 heads of 64, 11.3 (9 + 2.7).
+// Measured: 16 requests of up to 4000 positions brought to 1200 in four layers of 8 heads of 128, 201 us (21 + 180); two of up to 300 of 8 heads of 64, 11.0 (8 + 2.7).
 #include "kv16.h"
 
 namespace thi {
