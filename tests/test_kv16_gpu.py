@@ -211,6 +211,27 @@ def test_decode_windows(thi, window, sinks):
     check_attention(thi, c, window, sinks, decode=True, weights=True)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,n,new", [(64, 8, 128, 7020, 94), (16, 1, 64, 9000, 260), (64, 8, 128, 1300, 3), (8, 8, 64, 3000, 150)])
+def test_many_rows_in_many_chunks(thi, Hq, Hkv, D, n, new):
+    """New tokens of one long request, which is cut, against the same tokens as requests of their own, one each.  Off by a rounding each, and by one of the weights (2^-11 of them, times a value's
+    distance to the mean, which is at most twice the largest)."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n)
+    P = -(-n // PAGE)
+    pages = torch.randn(P, Hkv, 128 * D, generator=g, device="cuda").half()
+    q = (torch.randn(new, Hq, D, generator=g, device="cuda") * 3).half()
+    table = torch.randperm(P, generator=g, device="cuda").int()[None].contiguous()
+    one, each = torch.empty_like(q), torch.empty_like(q)
+    w = torch.zeros(1, Hkv, P * PAGE, device="cuda")
+    ws = thi.Workspace(max(thi.thi_kv16_attention_workspace_bytes(1, new, Hq, Hkv, D, new, P, True), thi.thi_kv16_attention_workspace_bytes(new, new, Hq, Hkv, D, 1, P, False)), init=False)
+    thi.thi_kv16_attention(q, pages, table, dev(np.array([n], np.int32)), dev(np.array([0, new], np.int32)), D ** -0.5, 0, 0, one, new, ws, None, w)
+    thi.thi_kv16_attention(q, pages, table.repeat(new, 1), dev(np.arange(n - new + 1, n + 1, dtype=np.int32)), None, D ** -0.5, 0, 0, each, 1, ws)
+    a, b, v = host(one.double()), host(each.double()), float(pages[..., 64 * D:].abs().max())
+    assert (np.abs(a - b) <= 2.0 ** -10 * np.maximum(np.abs(a), np.abs(b)) + 2.0 ** -10 * v + 2.0 ** -20).all(), np.abs(a - b).max()
+    rows = new * Hq // Hkv                                          # every row's weights are one in all, but for sums of n and of all rows in 32 bits
+    assert np.abs(host(w.double()).sum(-1) - rows).max() <= rows * (n + rows + 128) * 2.0 ** -24
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (20, 3), (64, 64), (90, 70), (250, 1)])
 @pytest.mark.parametrize("Hq,Hkv,D", [(4, 4, 128), (8, 1, 128), (5, 1, 64)])
 def test_few_new_tokens(thi, window, sinks, Hq, Hkv, D):
