@@ -75,6 +75,18 @@ struct Kv16EvictArgs {
     int budget, sinks, recent, headroom, layers, rows, Hkv, D, num_pages, max_pages;
     int* ws;                         // kv16_evict_words()
 };
+// The move's workgroups of a cache head, a page of kept positions each, and which of a row's n weights thread `thread` of one copies where the row stays as it is: every
+// step-th from its own place on, in 64 bits, for a step is up to 2^31 (a budget of 2^28) and a place up to as much more.
+constexpr int KE_MOVE = 512;
+__host__ __device__ constexpr unsigned kv16_move_groups(int budget, int max_pages)
+{
+    const long held = (long)max_pages * KV16_PAGE, most = held < budget ? held : budget;
+    return (unsigned)((most + KV16_PAGE - 1) / KV16_PAGE);
+}
+template <class Copy> __host__ __device__ __forceinline__ void kv16_each_copied(unsigned group, unsigned groups, unsigned thread, int n, Copy copy)
+{
+    for (size_t p = (size_t)group * KE_MOVE + thread; p < (size_t)n; p += (size_t)groups * KE_MOVE) copy(p);
+}
 size_t kv16_evict_words(int layers, int rows, int Hkv, int max_pages, int num_pages);
 hipError_t launch_kv16_evict(const Kv16EvictArgs& a, hipStream_t stream);
 

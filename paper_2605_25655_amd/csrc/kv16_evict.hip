@@ -309,7 +309,6 @@ __global__ __launch_bounds__(THREADS) void kv16_evict_select(Kv16EvictArgs a)
 // the keys and the single values, for a workgroup is short and the wait for memory most of it.  A key's pieces lie beside those of seven neighbours in a cache line, a value's beside those of
 // 31, so that where every third position is kept, nearly all lines of the pages come: of the batch above 0.7 GB, with the 0.3 that are written 140 us at a copy's rate.  (180; of
 // neighbouring positions 149; through LDS, to have the values' lines once: 4 us more.)
-constexpr int KE_MOVE = 512;
 template <int D>
 __global__ __launch_bounds__(KE_MOVE) void kv16_evict_move(Kv16EvictArgs a)
 {
@@ -323,8 +322,7 @@ __global__ __launch_bounds__(KE_MOVE) void kv16_evict_move(Kv16EvictArgs a)
     const int slot = tid < KV16_PAGE && p0 + tid < a.max_pages * KV16_PAGE ? ws.slots[at + p0 + tid] : 0;      // (of a row that keeps as many)
     const int kept = ws.kept[b], begin = ws.begin[b];
     if (kept < 0) {                              // left as it is
-        const int n = length_of(a, b);
-        for (int p = blockIdx.x * KE_MOVE + tid; p < n; p += gridDim.x * KE_MOVE) a.weights_out[at + p] = a.weights_in[at + p];
+        kv16_each_copied(blockIdx.x, gridDim.x, tid, length_of(a, b), [&](size_t p) __attribute__((always_inline)) { a.weights_out[at + p] = a.weights_in[at + p]; });
         return;
     }
     const int count = kept - p0 < KV16_PAGE ? kept - p0 : KV16_PAGE;
@@ -393,8 +391,7 @@ hipError_t launch_kv16_evict(const Kv16EvictArgs& a, hipStream_t stream)
     const dim3 lists((unsigned)a.Hkv + 1, (unsigned)a.rows, (unsigned)a.layers);
     if (a.max_pages <= KE_SMALL_PAGES && a.num_pages <= KE_SMALL_POOL) hipLaunchKernelGGL((kv16_evict_select<256>), lists, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((kv16_evict_select<1024>), lists, dim3(1024), 0, stream, a);
-    const long most = (long)a.max_pages * KV16_PAGE < a.budget ? (long)a.max_pages * KV16_PAGE : a.budget;
-    const dim3 grid((unsigned)((most + KV16_PAGE - 1) / KV16_PAGE), (unsigned)a.Hkv, (unsigned)(a.rows * a.layers));
+    const dim3 grid(kv16_move_groups(a.budget, a.max_pages), (unsigned)a.Hkv, (unsigned)(a.rows * a.layers));
     if (a.D == 128) hipLaunchKernelGGL((kv16_evict_move<128>), grid, dim3(KE_MOVE), 0, stream, a);
     else hipLaunchKernelGGL((kv16_evict_move<64>), grid, dim3(KE_MOVE), 0, stream, a);
     return hipGetLastError();

@@ -223,3 +223,50 @@ int main()
     res = subprocess.run([exe], env=env, capture_output=True, text=True)
     assert res.returncode == 0 and res.stdout.startswith("ok "), res.stdout[-1000:] + res.stderr[-4000:]
     assert "runtime error" not in res.stderr and "AddressSanitizer" not in res.stderr, res.stderr[-4000:]
+
+
+@pytest.mark.skipif(shutil.which(HIPCC) is None, reason="hipcc not found")
+def test_rows_that_stay_are_copied_once_at_the_limits(tmp_path):
+    """Which weights the eviction's threads copy where a row stays as it is, at the largest budgets, tables and lengths that are not refused: every step-th from the thread's own place
+    on, all of them in the row, and no more; built with the undefined-behaviour sanitizer."""
+    driver = tmp_path / "driver.cpp"
+    driver.write_text(r'''
+#include "%(root)s/paper_2605_25655_amd/csrc/kv16.h"
+#include <cstdio>
+#include <cstdlib>
+using namespace thi;
+int main()
+{
+    long walks = 0;
+    for (int budget : {1, 64, 65, 100000, 1 << 26, (1 << 27) - 1, 1 << 27, (1 << 28) - 1, 1 << 28, 2147483647})
+        for (int max_pages : {1, 2, 1000, 1 << 20, 1 << 22, (1 << 22) + 1, 1 << 24}) {
+            if (budget > 1 << 28 && max_pages > 1 << 22) continue;      // refused
+            const unsigned groups = kv16_move_groups(budget, max_pages);
+            const long step = (long)groups * KE_MOVE, reach = (long)max_pages * KV16_PAGE;
+            if (groups < 1 || (long)groups * KV16_PAGE < (budget < reach ? budget : reach) || step >= 1L << 32) { std::printf("groups %%u of %%d %%d\n", groups, budget, max_pages); return 1; }
+            for (long n : {0L, 1L, 5L, 100L, 4000L, reach - 1, reach}) {
+                if (n < 0 || n > reach) continue;
+                for (unsigned group : {0u, 1u, groups / 2, groups - 1})
+                    for (unsigned thread : {0u, 5u, KE_MOVE - 1u}) {
+                        if (group >= groups) continue;
+                        long next = (long)group * KE_MOVE + thread, last = -1;
+                        kv16_each_copied(group, groups, thread, (int)n, [&](long p) {
+                            if (p != next || p < 0 || p >= n) { std::printf("%%ld, not %%ld, of %%ld; budget %%d, %%d pages\n", p, next, n, budget, max_pages); std::exit(1); }
+                            last = p;
+                            next += step;
+                        });
+                        if (next < n || (last >= 0 && last + step < n)) { std::printf("ends at %%ld of %%ld\n", last, n); return 1; }
+                        ++walks;
+                    }
+            }
+        }
+    std::printf("ok %%ld walks\n", walks);
+    return 0;
+}
+''' % dict(root=ROOT))
+    exe = str(tmp_path / "kv16_walks")
+    res = subprocess.run([HIPCC, "-O1", "-g", "-std=c++17", "--offload-arch=gfx950", "-Xarch_host", "-fsanitize=undefined", "-Wno-unused-command-line-argument", "-o", exe, "-x", "hip", str(driver)],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr[-6000:]
+    res = subprocess.run([exe], env=dict(os.environ, UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1"), capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and res.stdout.startswith("ok "), res.stdout[-1000:] + res.stderr[-4000:]

@@ -531,6 +531,28 @@ def test_evict_long_rows(thi):
     check_evict(thi, c, 9000, 4, 1000)
 
 
+@pytest.mark.parametrize("n", [1, 100, 1 << 28])
+def test_evict_row_that_stays_at_the_largest_budget(thi, n):
+    """A table of 2^28 positions and a budget as large: the row stays, and its weights are copied, all of them and nothing else."""
+    import torch
+    MP = 1 << 22
+    say(f"[case] evict MP={MP} budget={1 << 28} n={n}")
+    table = torch.full((1, MP), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    w = torch.rand(1, 1, 1, MP * PAGE, device="cuda")
+    ins = [dev(np.array([1], np.int32)), table, dev(np.array([n], np.int32)), w]
+    outs = [torch.full_like(x, 7) for x in ins]
+    info = torch.full((2,), 7, dtype=torch.int32, device="cuda")
+    pool = torch.ones(1, 1, 1, 128 * 64, dtype=torch.float16, device="cuda")
+    ws = thi.Workspace(thi.thi_kv16_evict_workspace_bytes(1, 1, 1, MP, 1), init=False)
+    thi.thi_kv16_evict(*ins, 1 << 28, 4, 100, 0, *outs, info, pool, ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(ins[:3], outs[:3])) and host(info).tolist() == [0, 0] and bool((pool == 1).all())
+    assert torch.equal(outs[3][..., :n], w[..., :n]) and bool((outs[3][..., n:] == 7).all())
+    del w, ins, outs, ws
+    torch.cuda.empty_cache()
+
+
 def test_evict_pages_past_32_bits(thi):
     import torch
     D, P = 128, 33000
