@@ -965,6 +965,14 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_weigh(Kv16AttnArgs a, in
         for (int r = 0; r < 8; ++r) {
             if (!looked || from + r >= rows) continue;
             const float m = s_m[from + r], inv = s_inv[from + r];
+            if (!finite(inv)) {                  // (the same for all threads) a sum that is not a number: what the row sees becomes one, and that only, for zero times it is one, too
+                const int page = a.page_table[(size_t)b * a.max_pages + number];
+                const Sight mine = sight_of(a, rq, (from + r) / a.group);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (page >= 0 && page < a.num_pages && sees(mine, a.sinks, p0 + k)) sum[k] = inv;
+                continue;
+            }
 #pragma unroll
             for (int k = 0; k < 4; ++k) sum[k] = __builtin_fmaf(inv == 0.f ? 0.f : __builtin_amdgcn_exp2f(s[r][k] - m), inv, sum[k]);
         }

@@ -384,6 +384,53 @@ def test_what_is_not_finite_reaches_the_rows_that_see_it(thi, new, window):
             assert (np.abs(w - u)[fine] <= utol[fine]).all()
 
 
+@pytest.mark.parametrize("window", [0, 30, 100])
+@pytest.mark.parametrize("new", [1, 3, 8, 70])
+@pytest.mark.parametrize("what", ["key", "query", "infinite"])
+def test_weights_of_rows_that_are_not_numbers(thi, what, new, window):
+    """Accumulated weights next to a row whose softmax is not a number (a NaN in a key that it sees, or in its query; a score of infinity, next to one of minus infinity): NaN at the
+    positions that such a row sees, and at no other -- later tokens', in front of the window, without a page, behind a longer request's cut."""
+    lens, sinks = [150, 150, 1500], 4
+    c = attention_case(28, 4, 2, 128, lens, [new] * 3)
+    c["table"][1, 1] = -1
+    if what == "infinite":
+        c["q"][..., 7] = np.abs(c["q"][..., 7]) + 1
+    before = np.random.default_rng(8).standard_normal((3, 2, c["table"].shape[1] * PAGE)).astype(np.float32)
+    _, _, u, utol = ref.attention(c, 0.1, window, sinks, one_or_two(c), before)
+    clean, tol, _, _ = ref.attention(c, 0.1, window, sinks, one_or_two(c))
+    marks, queries = [], []
+    if what == "key":
+        marks = [(0, 149 - new // 2, np.nan), (1, 149, np.nan), (2, 1496, np.nan), (2, 2, np.nan) if new == 8 else (2, 1400, np.nan)]
+    elif what == "query":
+        queries = [(0, new // 2), (1, 0), (2, new - 1)]
+    else:                                                         # (a position of the sinks is seen by every row, and one of them is enough)
+        marks = [(b, p, x) for b in (0, 2) for p, x in ((1, np.inf), (2, -np.inf))]
+    for b, p, x in marks:
+        slot = int(c["table"][b, p // PAGE]) * PAGE + p % PAGE
+        c["pages"][slot // PAGE, 1, ref.places(p % PAGE, 128)[0][7]] = x
+    for b, i in queries:
+        c["q"][b * new + i, 3, 5] = np.nan
+    got, w = run_attention(thi, c, 0.1, window, sinks, weights=True, weights_in=before)
+    none = np.zeros(w.shape, bool)
+    for b in range(3):
+        for i in range(new):
+            here = lens[b] - new + i
+            at = np.array([p for p in range(here + 1) if c["table"][b, p // PAGE] >= 0 and (not window or p > here - window or p < sinks)])
+            for h in range(4):
+                bad = (b, i) in queries and h == 3 or h // 2 == 1 and any(x == b and p in at for x, p, _ in marks)
+                t = b * new + i
+                if bad:
+                    none[b, 1, at] = True
+                    assert np.isnan(got[t, h]).all(), (b, i, h)
+                else:
+                    assert (np.abs(got[t, h] - clean[t, h]) <= tol[t, h]).all(), (b, i, h)
+    assert none.any()
+    there = ~np.isnan(u)
+    assert np.array_equal(np.isnan(w), none | ~there), [np.argwhere(np.isnan(w)[b, 1] != (none | ~there)[b, 1]).ravel().tolist()[:9] for b in range(3)]
+    fine = there & ~none
+    assert (np.abs(w - u)[fine] <= utol[fine]).all(), (np.abs(w - u)[fine] / utol[fine]).max()
+
+
 @pytest.mark.parametrize("new", [1, 30])
 def test_peaked_and_large_scores(thi, new):
     """Scores far apart, growing along the positions (the maximum moves on and on), and a scale of zero and below."""
