@@ -296,6 +296,35 @@ def test_weights_add_to_what_was_there(thi):
         assert np.array_equal(got[written], want[written]) and np.array_equal(got[~written].astype(np.float32), before[~written])
 
 
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("B,n", [(64, 16700), (100, 20000)])
+def test_long_requests_that_are_not_cut(thi, B, n, weights):
+    """As many requests as fill the compute units, one of them long: a workgroup of four waves (of eight, with 100) walks more pages than its waves' lists hold at once, some of them missing."""
+    c = attention_case(B, 8, 8, 64, [n] + [(11 * b) % 90 for b in range(1, B)], [1] * B)
+    c["table"][0, [3, 127, 128, 200, 257]] = [-1, 2 ** 31 - 1, -1, -7, -1]
+    check_attention(thi, c, decode=True, weights=weights)
+    check_attention(thi, c, 15000, 70, decode=True, weights=weights)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (7000, 70)])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 8, 64), (8, 8, 128), (16, 8, 64)])
+def test_many_rows_of_long_requests_that_are_not_cut(thi, Hq, Hkv, D, window, sinks):
+    """Chunks of as many requests as fill the compute units, one of them far behind: a workgroup walks more pages than its list holds at once, some of them missing behind the 64th."""
+    c = attention_case(Hq + D, Hq, Hkv, D, [8930] + [20 + 7 * b % 50 for b in range(1, 34)], [20] * 34)
+    c["table"][0, [0, 63, 66, 130]] = [-1, -1, 2 ** 31 - 1, -1]
+    check_attention(thi, c, window, sinks, weights=True)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,n,new", [(64, 8, 128, 12100, 1), (64, 8, 128, 12100, 2), (8, 2, 128, 19000, 3), (8, 2, 64, 19000, 1)])
+def test_requests_in_more_chunks_than_are_joined_at_once(thi, Hq, Hkv, D, n, new):
+    """One long request of few rows, cut into 48 or 64 chunks, some pages and a whole chunk's missing."""
+    c = attention_case(new + D, Hq, Hkv, D, [n], [new])
+    c["table"][0, 100:112] = -1
+    c["table"][0, 180] = -1
+    check_attention(thi, c, weights=True)
+    check_attention(thi, c, n - 500, 70)
+
+
 @pytest.mark.parametrize("D,weights", [(64, False), (64, True), (128, True)])
 def test_more_requests_than_run_at_once(thi, D, weights):
     """Cache heads of all requests that are more than three times the compute units, with a long table: workgroups of eight waves."""
@@ -571,6 +600,14 @@ def test_evict_lengths_outside_the_table(thi):
 def test_evict_large_pool_and_many_rows(thi):
     rng = np.random.default_rng(9)
     check_evict(thi, evict_case(9, 1, 1, 64, rng.integers(0, 130, 1100).tolist(), 3, 4000), 64, 2, 8)
+
+
+@pytest.mark.parametrize("rows,MP,P", [(40, 120, 5300), (40, 120, 4500), (200, 30, 6100), (200, 30, 5000)])
+def test_evict_into_more_pages_than_a_plan_holds(thi, rows, MP, P):
+    """Headroom for whole tables, so that rows get pages from the 4096th free one on; with the smaller pools the last rows stay."""
+    lens = np.random.default_rng(11).integers(50, 200, rows).tolist()
+    want = check_evict(thi, evict_case(11, 1, 1, 64, lens, MP, P), 64, 2, 8, headroom=100000)
+    assert want["refs"].sum() > 4096 + 200
 
 
 def test_evict_long_rows(thi):
