@@ -352,9 +352,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_decode(Kv16AttnArgs a
         }
     };
     auto merge = [&](int c, float (&cw)[WAVES], float& lf) {      // fixed order: waves 0..3
+        // (a maximum that is not a number stays one: a wave has it from a score of infinity or NaN, and behind one of the others' slow_row would make a sum of infinity of it, one over which is zero)
         float mn = s_m[0][c];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) mn = __builtin_fmaxf(mn, s_m[w][c]);
+        for (int w = 1; w < WAVES; ++w) mn = __builtin_elementwise_maximum(mn, s_m[w][c]);
         const float ms = mn == -__builtin_inff() ? 0.f : mn;
         lf = 0.f;
 #pragma unroll

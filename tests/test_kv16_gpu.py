@@ -460,6 +460,26 @@ def test_weights_of_rows_that_are_not_numbers(thi, what, new, window):
     assert (np.abs(w - u)[fine] <= utol[fine]).all(), (np.abs(w - u)[fine] / utol[fine]).max()
 
 
+@pytest.mark.parametrize("n", [600, 1500, 5000])
+@pytest.mark.parametrize("new", [1, 4, 30])
+def test_infinite_score_next_to_growing_ones(thi, new, n):
+    """A score of infinity early on in one query head's rows, whose softmax is not a number from there on, and in the other's, for whom it is minus infinity, scores that grow along the
+    positions, so that maxima move on and on behind it: the first's outputs and all weights are NaN, the second's outputs what they are without that position."""
+    c = attention_case(29, 2, 1, 64, [n], [new])
+    for p in range(n):
+        slot = int(c["table"][0, p // PAGE]) * PAGE + p % PAGE
+        k, v = ref.load(c["pages"], slot)
+        ref.store(c["pages"], slot, np.sign(c["q"][0, 1].astype(np.float64)) * p * 13 / n + 0 * k, v)
+    c["q"][:, 0, 7], c["q"][:, 1, 7] = 1, -1
+    place = (int(c["table"][0, 0]), 0, ref.places(5, 64)[0][7])
+    c["pages"][place] = 60000                                     # (a weight of zero; and what a tolerance can count with)
+    y, tol, _, _ = ref.attention(c, 0.125, 0, 0, one_or_two(c))
+    c["pages"][place] = np.inf
+    got, w = run_attention(thi, c, 0.125, weights=True)
+    assert np.isnan(got[:, 0]).all() and np.isnan(w[0, 0, : n]).all()
+    assert (np.abs(got - y)[:, 1] <= tol[:, 1]).all()
+
+
 @pytest.mark.parametrize("new", [1, 30])
 def test_peaked_and_large_scores(thi, new):
     """Scores far apart, growing along the positions (the maximum moves on and on), and a scale of zero and below."""
