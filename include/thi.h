@@ -335,7 +335,8 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
  *
  * for row t = q_offsets[b] + i, i < n_b = q_offsets[b+1] - q_offsets[b]: the new tokens are the request's last n_b positions, already in the cache.  window 0: everything in
  * front of a token (sinks mean nothing then); positions are places in the page table, so that behind an eviction the window counts what was kept.  Negative ones:
- * THI_ERR_SHAPE.  A row that sees no position is zero.  What a row does not see does not matter to it, NaN and infinities among it; pages outside every window are not read.
+ * THI_ERR_SHAPE.  A row that sees no position is zero, and so is one whose scores are all minus infinity (neither gives any weight).  What a row does not see does not matter to it, NaN
+ * and infinities among it; pages outside every window are not read.
  * q, out [T,Hq,D] fp16; q_offsets [B+1] int32 device memory, not decreasing, or NULL: one token per request, T = B.  max_q <= 65535 is the largest n_b (from the
  * host, it sizes the launch; rows of a request past it are not written, and it is as if their positions were not there).
  *

@@ -460,6 +460,31 @@ def test_weights_of_rows_that_are_not_numbers(thi, what, new, window):
     assert (np.abs(w - u)[fine] <= utol[fine]).all(), (np.abs(w - u)[fine] / utol[fine]).max()
 
 
+@pytest.mark.parametrize("window", [0, 100])
+@pytest.mark.parametrize("new", [1, 4, 40])
+def test_rows_whose_scores_are_all_minus_infinity(thi, new, window):
+    """Such a row's results are zero, also where values are not finite, and it adds no weight; a row next to it whose scores are finite is what it is."""
+    lens = [90, 2600]
+    c = attention_case(30, 2, 1, 64, lens, [new, new])
+    c["q"][:, 0, 7], c["q"][:, 1, 7] = -1, 0.5
+    before = np.random.default_rng(12).standard_normal((2, 1, c["table"].shape[1] * PAGE)).astype(np.float32)
+    for p in range(lens[1]):
+        c["pages"][int(c["table"][1, p // PAGE]), 0, ref.places(p % PAGE, 64)[0][7]] = 0
+    y, tol, u, utol = ref.attention(c, 0.125, window, 4, one_or_two(c), before)
+    for p in range(lens[0]):                                      # the first request: minus infinity for one head, infinity for the other
+        c["pages"][int(c["table"][0, p // PAGE]), 0, ref.places(p % PAGE, 64)[0][7]] = np.inf
+    for p in range(2, lens[0], 9):
+        c["pages"][int(c["table"][0, p // PAGE]), 0, ref.places(p % PAGE, 64)[1][3]] = np.nan if p % 2 else -np.inf
+    got, w = run_attention(thi, c, 0.125, window, 4, weights=True, weights_in=before)
+    assert (got[:new, 0] == 0).all() and np.isnan(got[:new, 1]).all()
+    assert (np.abs(got - y)[new:] <= tol[new:]).all() and (np.abs(w - u)[1][~np.isnan(u[1])] <= utol[1][~np.isnan(u[1])]).all()
+    c["q"][:, 1, 7] = -2                                          # now both heads
+    got, w = run_attention(thi, c, 0.125, window, 4, weights=True, weights_in=before)
+    assert (got[:new] == 0).all()
+    front = lens[0] - new
+    assert np.array_equal(w[0, 0, :front], before[0, 0, :front]) and (w[0, 0, front: lens[0]] == 0).all()
+
+
 @pytest.mark.parametrize("n", [600, 1500, 5000])
 @pytest.mark.parametrize("new", [1, 4, 30])
 def test_infinite_score_next_to_growing_ones(thi, new, n):
