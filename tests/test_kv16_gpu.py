@@ -543,6 +543,59 @@ def test_pages_past_32_bits(thi, new):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("new,weights,MP", [(1, True, 1 << 23), (3, False, 1 << 24), (40, False, 1 << 24), (40, True, 1 << 20)])
+def test_longest_tables(thi, new, weights, MP):
+    """Tables of as many pages as are not refused, of which a few are there: what a request of these pages alone has."""
+    import torch
+    c = attention_case(33, 2, 1, 64, [384], [new])
+    at = np.array([0, 5, 63, 64, MP // 2 + 77, MP - 1])
+    table = torch.full((1, MP), -1, dtype=torch.int32, device="cuda")
+    table[0, dev(at)] = dev(c["table"][0, :6])
+    say(f"[case] attention new={new} MP={MP} weights={weights}")
+    out = torch.full((new, 2, 64), float("nan"), dtype=torch.float16, device="cuda")
+    w = torch.full((1, 1, MP * PAGE), 7.0, device="cuda") if weights else None
+    ws = thi.Workspace(thi.thi_kv16_attention_workspace_bytes(1, new, 2, 1, 64, new, MP, weights), init=False)
+    thi.thi_kv16_attention(dev(c["q"]), dev(c["pages"]), table, dev(np.array([MP * PAGE], np.int32)), dev(c["offsets"]), 0.125, 0, 0, out, new, ws, None, w)
+    y, tol, u, utol = ref.attention(c, 0.125, weight=one_or_two(c))
+    assert (np.abs(host(out.double()) - y) <= tol).all()
+    if weights:
+        got = w.view(MP, PAGE)
+        mine = dev(at)
+        assert (np.abs(host(got[mine].double()).ravel() - u[0, 0, :384]) <= utol[0, 0, :384]).all()
+        got[mine] = 0
+        assert bool((w == 0).all())
+    del w, ws, table
+    torch.cuda.empty_cache()
+
+
+def test_most_requests(thi):
+    """As many requests as are not refused, of up to one page each, some empty, with weights."""
+    import torch
+    from perf import more_operators as plain
+    B = 65535
+    g = torch.Generator(device="cuda").manual_seed(34)
+    pages = torch.randn(B, 1, 128 * 64, device="cuda", generator=g).half()
+    table = torch.randperm(B, device="cuda", generator=g).int()[:, None].contiguous()
+    lens = torch.randint(0, 65, (B,), device="cuda", generator=g).int()
+    q = (2 * torch.randn(B, 1, 64, device="cuda", generator=g)).half()
+    out, w = torch.full_like(q, float("nan")), torch.full((B, 1, PAGE), -1.0, device="cuda")
+    ws = thi.Workspace(thi.thi_kv16_attention_workspace_bytes(B, B, 1, 1, 64, 1, 1, True), init=False)
+    say(f"[case] attention B={B}")
+    thi.thi_kv16_attention(q, pages, table, lens, None, 0.125, 0, 0, out, 1, ws, None, w)
+    held = pages[table[:, 0].long()]
+    k, v = plain._keys(held, 64)[:, 0].double(), plain._values(held, 64)[:, 0].double()
+    seen = torch.arange(PAGE, device="cuda") < lens[:, None]
+    x = q.double()
+    p = torch.where(lens[:, None] > 0, torch.softmax(((k * x).sum(-1) * 0.125).masked_fill(~seen, -float("inf")), -1), 0.0)
+    y = (p[..., None] * v).sum(1)
+    e = 0.125 * (k.abs() * x.abs()).sum(-1) * 72 * 2.0 ** -24 + 2.0 ** -18 + 2.0 ** -20 + ref.TWO_SUMMANDS      # (as tests/kv16_reference.py has it)
+    tol = 2.0 ** -25 + 2.0 ** -11 * y.abs() + ((p * torch.expm1(e))[..., None] * (v - y[:, None]).abs()).sum(1) * torch.exp(e.amax(-1))[:, None] + 256 * 2.0 ** -24 * (p[..., None] * v.abs()).sum(1) \
+        + 2.0 ** -33 * v.abs().sum(1)
+    assert bool(((out[:, 0].double() - y).abs() <= tol).all())
+    off = p * torch.expm1(e + e.amax(-1, keepdim=True) + 128 * 2.0 ** -24) + 1e-30
+    assert bool(((w[:, 0] - p).abs() <= off)[seen].all()) and bool((w[:, 0][~seen] == -1).all())
+
+
 # ---- eviction -----------------------------------------------------------------------------------------------------
 
 
