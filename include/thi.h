@@ -350,7 +350,8 @@ int thi_qk_norm_rope_kv16(const void* qkv, int ld, const void* q_gamma, const vo
  * Scores, statistics and sums are fp32.  Weights reach the matrix cores as fp16: up to 16 rows of a request and cache head (max_q Hq / Hkv) as two summands, beyond as one,
  * cut to its bits, as is the sum that divides the result.  Workspace:
  * thi_kv16_attention_workspace_bytes(), 256-byte aligned; what that says for the largest B, T, max_q and max_pages does for every smaller call with these heads
- * (weights != 0: with weights_out).  Reproducible bit for bit.
+ * (weights != 0: with weights_out).  Without weights it grows no further than what the chip works on at once; with them it has the scores of up to 16 rows of each request and cache head,
+ * 4 bytes for each position of the tables, and past 16 rows 2 D + 8 bytes for each of B max_q Hq rows.  Reproducible bit for bit.
  */
 size_t thi_kv16_attention_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int max_q, int max_pages, int weights);
 int thi_kv16_attention(const void* q, const void* pages, const int* page_table, const int* seq_lens, const int* q_offsets, float scale, int window, int sinks,

@@ -93,7 +93,8 @@ int chunks_worth(long items, long pages, long bytes, int most, int num_cus)
 //   few rows, four, eight waves a workgroup, where there are more of them than the compute units hold: 32 x 2048 of 32/32: 110.5 107.0; 64 x 2000 of these 204 196; 96 x 3000 of 64/8: 117 105; 20 x 2000
 //     of 40/40: 82.6 75.1; where there are not: 24 x 4000 of 32/32: 150 155; 16 x 4000 112 116; 24 x 5000 of 64/8: 50.0 53.3; and of short tables (not past FEW_UNCUT), 32 x 500 of 32/32: 32.0 34.9
 //   in the order of the batch, by length: 24 x 5000 of 64/8: 50.1 45.7; 64 x 6000: 160 146; 30 x 8000: 104 102; 16 x 32000, 4096 seen: 47.6 48.4; 32 x 2048 of 32/32: 106.8 108.0; of fewer or shorter
-//     ones, 3 x 131000: 86.0 86.1; 8 x 1000: 12.6 13.2
+//     ones, 3 x 131000: 86.0 86.1; 8 x 1000: 12.6 13.2.  (The rule looks at neither windows, behind which all see as many pages, nor how many workgroups share a compute unit: 1 to 2 percent lost in the two
+//     cases above that it takes along.  Up to 64 requests, whose lengths one wave holds.)
 void plan(Kv16AttnArgs& a, bool few, int num_cus)
 {
     a.group = a.Hq / a.Hkv;

@@ -59,8 +59,8 @@ __device__ __forceinline__ Sight sight_of(const Kv16AttnArgs& a, const Request& 
 }
 __device__ __forceinline__ bool sees(const Sight& s, int sinks, int pos) { return pos < s.end && (pos >= s.from || pos < sinks); }
 
-// Pages per chunk of a request that looks at `pages` of them: a function of its own length and of how many workgroups the call has, so that a
-// request's chunk borders, and with them the bits of its result, do not depend on its neighbours.
+// Pages per chunk of a request that looks at `pages` of them: a function of its own length and of how many workgroups the call has (by its B, max_q and max_pages), so that in
+// calls of the same extents a request's chunk borders, and with them the bits of its result, do not depend on the other requests.
 __device__ __forceinline__ int chunk_pages(const Kv16AttnArgs& a, int pages)
 {
     const int size = a.nsplit == 1 ? pages : (pages + a.nsplit - 1) / a.nsplit;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv16_attn_decode(Kv16AttnArgs a
             if (d == 0) { po[D] = mn; po[D + 1] = po[D + 2] = lf; }
         }
     };
-    auto merge = [&](int c, float (&cw)[WAVES], float& lf) {      // fixed order: waves 0..3
+    auto merge = [&](int c, float (&cw)[WAVES], float& lf) {      // fixed order: waves 0 .. WAVES - 1
         // (a maximum that is not a number stays one: a wave has it from a score of infinity or NaN, and behind one of the others' slow_row would make a sum of infinity of it, one over which is zero)
         float mn = s_m[0][c];
 #pragma unroll
@@ -474,8 +474,8 @@ __global__ __launch_bounds__(KC_THREADS) void kv16_attn_combine(Kv16AttnArgs a)
 // positions, window 2000, 64/8 heads, 126 us, where the 616 tiles of equal work are two or three to a compute unit, 20 percent more than their mean.  256 rows in one workgroup a compute unit:
 // 267 and 197 us.  Exponentials between products, or by themselves: 209 and 129, 211 and 141; products of 16x16x32 instead of 32x32x16, which read half the
 // operands but take more power, so that the clock goes down: 197 and 129 instead of 209 and 129.  The weights' sum as a product with ones instead of 32 instructions a page: 200.6 -> 196.7 on one card; operands of
-// both products asked for in one stream, over what a turn begins with: -> 194, and 129 -> 125.  Cut into chunks where that fills compute units that have one
-// workgroup: 5 chunks of 128 tokens, window 4096, 126 -> 111 us, but one of 800 on 4000 99 -> 126, for partial results are 4 D bytes a row: not done.
+// both products asked for in one stream, over what a turn begins with: -> 194, and 129 -> 125.  Cut into chunks wherever that fills compute units that have one
+// workgroup: 5 chunks of 128 tokens, window 4096, 126 -> 111 us, but one of 800 on 4000 99 -> 126, for partial results are 4 D bytes a row: so only where chunks_worth() says (kv16_api.hip).
 constexpr int KP_WAVES = 4, KP_AHEAD = 4, KP_BUFS = 2;
 template <int D, int WAVES> constexpr int KP_LDS = 2 * KP_BUFS * 64 * D * 2 + WAVES * 2048;
 

@@ -306,8 +306,8 @@ __global__ __launch_bounds__(THREADS) void kv16_evict_select(Kv16EvictArgs a)
 }
 
 // The move: a workgroup takes one fresh page of one cache head of a layer, 64 kept positions from wherever they were.  All that it reads is asked for at once, the pieces of 16 bytes of
-// the keys and the single values, for a workgroup is short and the wait for memory most of it.  A key's pieces lie beside those of seven neighbours in a cache line, a value's beside those of
-// 31, so that where every third position is kept, nearly all lines of the pages come: of the batch above 0.7 GB, with the 0.3 that are written 140 us at a copy's rate.  (180; of
+// the keys and the single values, for a workgroup is short and the wait for memory most of it.  A key's pieces lie beside those of seven neighbours in a cache line, and so does a
+// value, so that where every third position is kept, nearly all lines of the pages come: of the batch above 0.7 GB, with the 0.3 that are written 140 us at a copy's rate.  (180; of
 // neighbouring positions 149; through LDS, to have the values' lines once: 4 us more.)
 template <int D>
 __global__ __launch_bounds__(KE_MOVE) void kv16_evict_move(Kv16EvictArgs a)
