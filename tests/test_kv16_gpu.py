@@ -926,6 +926,37 @@ def test_prompts_and_mixed_calls_in_graphs(thi):
                     assert torch.equal(x, want[j][name]), (i, k, j, name)
 
 
+def test_calls_at_the_same_time(thi):
+    """Calls of different kinds on three streams at once, each with a workspace of its own: what each gives alone, every time."""
+    import torch
+    kinds = [(attention_case(60, 8, 2, 64, [4000, 700, 66], [1, 1, 2]), 0, 0), (attention_case(61, 4, 4, 128, [300, 200], [300, 33]), 90, 4),
+             (attention_case(62, 8, 1, 128, [5000, 4800, 90], [1, 2, 50]), 0, 0)]
+    calls, want, streams = [], [], [torch.cuda.Stream() for _ in kinds]
+    for c, window, sinks in kinds:
+        t = {k: dev(c[k]) for k in ("q", "pages", "table", "lens", "offsets")}
+        (B, MP), (T, Hq, D), Hkv = c["table"].shape, c["q"].shape, c["pages"].shape[1]
+        o = dict(out=torch.zeros_like(t["q"]), w=torch.zeros(B, Hkv, MP * PAGE, device="cuda"))
+        ws = thi.Workspace(thi.thi_kv16_attention_workspace_bytes(B, T, Hq, Hkv, D, c["max_q"], MP, True), init=False)
+        calls.append((lambda t=t, o=o, c=c, ws=ws, window=window, sinks=sinks, D=D: thi.thi_kv16_attention(t["q"], t["pages"], t["table"], t["lens"], t["offsets"], D ** -0.5, window, sinks,
+                                                                                                       o["out"], c["max_q"], ws, None, o["w"]), o))
+    for call, o in calls:
+        call()
+        torch.cuda.synchronize()
+        want.append({k: x.clone() for k, x in o.items()})
+    for _ in range(5):
+        for _, o in calls:
+            o["out"].fill_(7)
+            o["w"].zero_()
+        torch.cuda.synchronize()
+        for _ in range(8):
+            for stream, (call, _) in zip(streams, calls):
+                with torch.cuda.stream(stream):
+                    call()
+        torch.cuda.synchronize()
+        for (_, o), w in zip(calls, want):
+            assert all(torch.equal(o[k], w[k]) for k in o)
+
+
 @pytest.mark.parametrize("new", [[1, 1, 2], [40, 1, 17]])
 def test_rows_behind_the_last_request_are_left(thi, new):
     """A batch padded to more rows than its requests have: those rows are not written, and the others are what they are without them."""
